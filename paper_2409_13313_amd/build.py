@@ -13,7 +13,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libozimmu.so")
-SOURCES = ["ozimmu_api.hip", "ozimmu_split.hip", "ozimmu_gemm.hip"]
+SOURCES = ["ozimmu_api.hip", "ozimmu_split.hip", "ozimmu_gemm.hip", "ozimmu_mx_api.hip", "ozimmu_mx_quantize.hip", "ozimmu_mx_gemm.hip"]
 # ozimmu_resident.hip holds kernels specialised for a slice count: one compilation per count, all of them linked into
 # the object of the chunk GEMM (whoever links that object gets every way to run the schedule)
 RESIDENT_KS = range(3, 17)

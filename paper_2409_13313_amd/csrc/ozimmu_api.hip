@@ -685,6 +685,7 @@ const char* ozimmu_status_string(int status)
         case OZIMMU_ERR_SLICES: return "invalid slice count or slice range";
         case OZIMMU_ERR_WORKSPACE: return "workspace too small or misaligned";
         case OZIMMU_ERR_HIP: return "HIP launch error";
+        case OZIMMU_ERR_TYPE: return "unknown element type or misaligned elements";
         default: return "unknown status";
     }
 }

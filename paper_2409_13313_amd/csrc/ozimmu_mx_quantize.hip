@@ -1,0 +1,214 @@
+// Quantisation to the microscaled 4-bit form, reading back, and the plain layout of checkpoints (include/ozimmu_mx.h).
+//
+// All of it moves memory: an element is read in 2 or 4 bytes and written in 17/32 of one (or the other way round), with two
+// dozen operations for eight elements between.
+#include "ozimmu_mx_convert.h"
+
+namespace {
+
+using namespace mxk;
+using namespace mxl;
+
+// Blocks along the rows.  A workgroup takes 64 rows x 128 columns (a quarter of a tile): thread t the eight elements t % 16 of
+// rows t / 16 + 16 i, so that 16 lanes read 128 columns of a row side by side; four lanes hold a block and share its maximum.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_mx_quantize_rows(int64_t rows, int64_t n, const typename Elem<TYPE>::Bits* X, int64_t ldx,
+                                                          uint8_t* out, int64_t KT)
+{
+    typedef typename Elem<TYPE>::Bits Bits;
+    const int t = threadIdx.x, chunk = t & 15, c = chunk >> 2, sub = chunk & 3;
+    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + (t >> 4);
+    const int64_t col = kt * TILE_K + chunk * 8;
+    Bits x[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + 16 * i;
+        load_row<TYPE, 8>(X + row * ldx + col, row < rows ? n - col : 0, x[i]);
+    }
+    uint8_t* const tile = out + ((row0 / TILE_R) * KT + kt) * TILE_BYTES;
+    uint32_t scales = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t amax = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t m = magnitude<TYPE>(x[i][e]);
+            amax = m > amax ? m : amax;
+        }
+#pragma unroll
+        for (int d = 1; d < 4; d *= 2) {
+            const uint32_t o = (uint32_t)__shfl_xor((int)amax, d);
+            amax = o > amax ? o : amax;
+        }
+        const uint32_t b = scale_byte(amax);
+        scales |= b << (8 * i);
+        const int64_t row = row0 + 16 * i;
+        if (row < rows) {
+            const uint32_t codes = codes8<TYPE>(x[i], scale_value(b));
+            *(uint32_t*)(tile + code_offset((int)(row % TILE_R), c) + 4 * sub) = codes;
+        }
+    }
+    // (the scales of rows that are not there are those of zeros)
+    if (sub == 0 && row0 < rows) *(uint32_t*)(tile + scale_offset((int)(row0 % TILE_R), c)) = scales;
+}
+
+// Blocks along the columns: row j of the packed matrix is column j of X.  A wave takes 64 columns x 128 rows: lane l the 4 columns
+// l % 16 of block l / 16, whose 32 rows it reads one after the other (16 lanes side by side), so that a block is one lane's.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_mx_quantize_cols(int64_t rows, int64_t n, const typename Elem<TYPE>::Bits* X, int64_t ldx,
+                                                          uint8_t* out, int64_t KT)
+{
+    typedef typename Elem<TYPE>::Bits Bits;
+    const int t = threadIdx.x, lane = t & 63, c = lane >> 4;
+    const int64_t kt = blockIdx.x, col = (int64_t)blockIdx.y * 256 + (t >> 6) * 64 + (lane & 15) * 4;
+    const int64_t row0 = kt * TILE_K + c * BLOCK;
+    Bits x[BLOCK][4];
+#pragma unroll
+    for (int r = 0; r < BLOCK; ++r)
+        load_row<TYPE, 4>(X + (row0 + r) * ldx + col, row0 + r < rows ? n - col : 0, x[r]);
+    uint8_t* const tile = out + ((int64_t)blockIdx.y * KT + kt) * TILE_BYTES;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t amax = 0;
+#pragma unroll
+        for (int r = 0; r < BLOCK; ++r) {
+            const uint32_t m = magnitude<TYPE>(x[r][j]);
+            amax = m > amax ? m : amax;
+        }
+        const uint32_t b = scale_byte(amax);
+        const float s = scale_value(b);
+        uint32_t codes[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            Bits y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = x[8 * q + e][j];
+            codes[q] = codes8<TYPE>(y, s);
+        }
+        if (col + j < n) {
+            const int r = (int)((col + j) % TILE_R);
+            *(v4i*)(tile + code_offset(r, c)) = v4i{(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3]};
+            tile[scale_offset(r, c)] = (uint8_t)b;
+        }
+    }
+}
+
+// Reading back: the same threads as k_mx_quantize_rows.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t n, const uint8_t* in, typename Elem<TYPE>::Bits* X,
+                                                       int64_t ldx, int64_t KT)
+{
+    typedef typename Elem<TYPE>::Bits Bits;
+    const int t = threadIdx.x, chunk = t & 15, c = chunk >> 2, sub = chunk & 3;
+    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + (t >> 4);
+    const int64_t col = kt * TILE_K + chunk * 8;
+    if (row0 >= rows || col >= n) return;
+    const uint8_t* const tile = in + ((row0 / TILE_R) * KT + kt) * TILE_BYTES;
+    const uint32_t scales = *(const uint32_t*)(tile + scale_offset((int)(row0 % TILE_R), c));
+    uint32_t codes[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) codes[i] = *(const uint32_t*)(tile + code_offset((int)(row0 % TILE_R) + 16 * i, c) + 4 * sub);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + 16 * i;
+        if (row >= rows) break;
+        const float s = scale_of((scales >> (8 * i)) & 255u);
+        Bits x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(code_value((codes[i] >> (4 * e)) & 15u) * s);
+        store_row<TYPE, 8>(X + row * ldx + col, n - col, x);
+    }
+}
+
+// Plain layout -> packed and back: one thread a block.
+__global__ __launch_bounds__(256) void k_mx_pack(int64_t rows, int64_t n, const uint8_t* codes, int64_t ldc, const uint8_t* scales,
+                                                 int64_t lds, uint8_t* out, int64_t KT)
+{
+    const int t = threadIdx.x, c = t & 3;
+    const int64_t kt = blockIdx.x, row = (int64_t)blockIdx.y * 64 + (t >> 2);
+    if (row >= rows) return;
+    const int64_t block = kt * 4 + c, left = n - block * BLOCK;  // elements from the block's first one to the row's end
+    uint32_t w[4] = {0, 0, 0, 0};
+    uint8_t b = 0;
+    if (left > 0) {
+        __builtin_memcpy(w, codes + row * ldc + block * 16, 16);
+        b = scales[row * lds + block];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t keep = left - 8 * q;  // codes of this word
+            w[q] = keep >= 8 ? w[q] : (keep <= 0 ? 0u : w[q] & ((1u << (4 * (int)keep)) - 1u));
+        }
+    }
+    uint8_t* const tile = out + ((row / TILE_R) * KT + kt) * TILE_BYTES;
+    *(v4i*)(tile + code_offset((int)(row % TILE_R), c)) = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+    tile[scale_offset((int)(row % TILE_R), c)] = b;
+}
+
+__global__ __launch_bounds__(256) void k_mx_unpack(int64_t rows, int64_t n, const uint8_t* in, uint8_t* codes, int64_t ldc,
+                                                   uint8_t* scales, int64_t lds, int64_t KT)
+{
+    const int t = threadIdx.x, c = t & 3;
+    const int64_t kt = blockIdx.x, row = (int64_t)blockIdx.y * 64 + (t >> 2);
+    const int64_t block = kt * 4 + c;
+    if (row >= rows || block * BLOCK >= n) return;
+    const uint8_t* const tile = in + ((row / TILE_R) * KT + kt) * TILE_BYTES;
+    const v4i w = *(const v4i*)(tile + code_offset((int)(row % TILE_R), c));
+    __builtin_memcpy(codes + row * ldc + block * 16, &w, 16);
+    scales[row * lds + block] = tile[scale_offset((int)(row % TILE_R), c)];
+}
+
+template <int TYPE>
+void quantize(int64_t rows, int64_t n, const void* X, int64_t ldx, void* by_row, void* by_col, hipStream_t st)
+{
+    typedef typename Elem<TYPE>::Bits Bits;
+    if (by_row)
+        hipLaunchKernelGGL(k_mx_quantize_rows<TYPE>, dim3((unsigned)inner_tiles(n), (unsigned)((rows + 63) / 64)), dim3(256), 0, st,
+                           rows, n, (const Bits*)X, ldx, (uint8_t*)by_row, inner_tiles(n));
+    if (by_col)
+        hipLaunchKernelGGL(k_mx_quantize_cols<TYPE>, dim3((unsigned)inner_tiles(rows), (unsigned)row_tiles(n)), dim3(256), 0, st,
+                           rows, n, (const Bits*)X, ldx, (uint8_t*)by_col, inner_tiles(rows));
+}
+
+template <int TYPE> void dequantize(int64_t rows, int64_t n, const void* packed, void* X, int64_t ldx, hipStream_t st)
+{
+    hipLaunchKernelGGL(k_mx_dequantize<TYPE>, dim3((unsigned)inner_tiles(n), (unsigned)((rows + 63) / 64)), dim3(256), 0, st, rows, n,
+                       (const uint8_t*)packed, (typename Elem<TYPE>::Bits*)X, ldx, inner_tiles(n));
+}
+
+}  // namespace
+
+namespace mxk {
+
+hipError_t launch_quantize(int type, int64_t rows, int64_t n, const void* X, int64_t ldx, void* by_row, void* by_col, hipStream_t st)
+{
+    if (type == F32) quantize<F32>(rows, n, X, ldx, by_row, by_col, st);
+    if (type == BF16) quantize<BF16>(rows, n, X, ldx, by_row, by_col, st);
+    if (type == F16) quantize<F16>(rows, n, X, ldx, by_row, by_col, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_dequantize(int type, int64_t rows, int64_t n, const void* packed, void* X, int64_t ldx, hipStream_t st)
+{
+    if (type == F32) dequantize<F32>(rows, n, packed, X, ldx, st);
+    if (type == BF16) dequantize<BF16>(rows, n, packed, X, ldx, st);
+    if (type == F16) dequantize<F16>(rows, n, packed, X, ldx, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_pack(int64_t rows, int64_t n, const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, void* packed,
+                       hipStream_t st)
+{
+    hipLaunchKernelGGL(k_mx_pack, dim3((unsigned)inner_tiles(n), (unsigned)((rows + 63) / 64)), dim3(256), 0, st, rows, n, codes, ldc,
+                       scales, lds, (uint8_t*)packed, inner_tiles(n));
+    return hipGetLastError();
+}
+
+hipError_t launch_unpack(int64_t rows, int64_t n, const void* packed, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
+                         hipStream_t st)
+{
+    hipLaunchKernelGGL(k_mx_unpack, dim3((unsigned)inner_tiles(n), (unsigned)((rows + 63) / 64)), dim3(256), 0, st, rows, n,
+                       (const uint8_t*)packed, codes, ldc, scales, lds, inner_tiles(n));
+    return hipGetLastError();
+}
+
+}  // namespace mxk

@@ -1,0 +1,238 @@
+"""Thin Python binding of the microscaled 4-bit operators (include/ozimmu_mx.h): quantisation, reading back, product, and a
+linear layer with its gradient.
+
+Argument marshalling only: device pointers of torch tensors and the current HIP stream go to the entry points of the same name.
+There is no CPU fallback.  Matrices are 2-D tensors with unit stride along their rows, in float32, bfloat16 or float16; results that
+are not handed over are allocated, workspaces too.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+import torch
+
+from . import ozimmu
+from .ozimmu import OzimmuError
+
+_lib = ozimmu._lib
+_i64, _int, _vp, _sz, _float = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
+
+_SIGNATURES = {
+    "ozimmu_mx_bytes": (_sz, [_i64, _i64]),
+    "ozimmu_mx_quantize": (_int, [_int, _i64, _i64, _vp, _i64, _vp, _vp, _vp]),
+    "ozimmu_mx_dequantize": (_int, [_int, _i64, _i64, _vp, _vp, _i64, _vp]),
+    "ozimmu_mx_pack": (_int, [_i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "ozimmu_mx_unpack": (_int, [_i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "ozimmu_mx_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "ozimmu_mx_backward_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "ozimmu_mx_gemm": (_int, [_i64, _i64, _i64, _float, _vp, _vp, _float, _int, _vp, _i64, _vp, _sz, _vp]),
+    "ozimmu_mx_linear": (_int, [_i64, _i64, _i64, _float, _int, _vp, _i64, _vp, _float, _int, _vp, _i64, _vp, _sz, _vp]),
+    "ozimmu_mx_linear_backward": (_int, [_i64, _i64, _i64, _float, _int, _vp, _i64, _vp, _i64, _vp, _float, _int, _vp, _i64,
+                                         _float, _int, _vp, _i64, _vp, _sz, _vp]),
+}
+for _name, (_restype, _argtypes) in _SIGNATURES.items():
+    getattr(_lib, _name).restype, getattr(_lib, _name).argtypes = _restype, _argtypes
+EXPORTS = list(_SIGNATURES)
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+BLOCK = 32
+
+
+class Packed:
+    """A matrix of rows x n in the packed form: `data` holds its bytes (on the GPU, private layout; see pack and unpack)."""
+    __slots__ = ("data", "rows", "n")
+
+    def __init__(self, data: torch.Tensor, rows: int, n: int):
+        if not (data.is_cuda and data.dtype is torch.uint8 and data.dim() == 1 and data.is_contiguous()):
+            raise ValueError("packed data is a contiguous 1-D uint8 tensor on the GPU")
+        if data.numel() < packed_bytes(rows, n):
+            raise ValueError(f"{data.numel()} bytes for a packed matrix of {rows} x {n}, which takes {packed_bytes(rows, n)}")
+        self.data, self.rows, self.n = data, rows, n
+
+    @property
+    def shape(self) -> Tuple[int, int]:
+        return self.rows, self.n
+
+
+def _matrix(t: torch.Tensor) -> Tuple[int, int, int, int]:
+    """Rows, columns, leading dimension and type number of a matrix on the GPU."""
+    kind = TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"expected float32, bfloat16 or float16, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError("tensor must live on the GPU")
+    if t.dim() != 2:
+        raise ValueError("expected a 2-D tensor")
+    (rows, cols), (ld, unit) = t.shape, t.stride()
+    if (cols > 1 and unit != 1) or (rows > 1 and ld < cols):
+        raise ValueError("expected a 2-D tensor with unit stride along rows that do not overlap")
+    return rows, cols, ld if rows > 1 else max(cols, ld, 1), kind
+
+
+def _output(D: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, dtype, beta: float) -> torch.Tensor:
+    """The caller's output, or a new one."""
+    if D is None:
+        if beta != 0.0:
+            raise ValueError("beta without the matrix that it multiplies")
+        return torch.empty((rows, cols), dtype=dtype, device=like.device)
+    if tuple(D.shape) != (rows, cols):
+        raise ValueError(f"output of {tuple(D.shape)} for a result of {rows} x {cols}")
+    return D
+
+
+def _packed(P: Packed, what: str) -> Packed:
+    if not isinstance(P, Packed):
+        raise ValueError(f"{what} has to be a packed matrix (see quantize and pack), got {type(P).__name__}")
+    return P
+
+
+def _check(status: int) -> None:
+    if status:
+        raise OzimmuError(status)
+
+
+def packed_bytes(rows: int, n: int) -> int:
+    return int(_lib.ozimmu_mx_bytes(rows, n))
+
+
+def workspace_bytes(m: int, n: int, p: int) -> int:
+    return int(_lib.ozimmu_mx_workspace_bytes(m, n, p))
+
+
+def backward_workspace_bytes(m: int, n: int, p: int) -> int:
+    return int(_lib.ozimmu_mx_backward_workspace_bytes(m, n, p))
+
+
+def alloc_workspace(m: int, n: int, p: int, device="cuda", backward: bool = False) -> torch.Tensor:
+    """Workspace for gemm and linear with these sizes; with `backward` for linear_backward too."""
+    nbytes = max(workspace_bytes(m, n, p), backward_workspace_bytes(m, n, p) if backward else 0)
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+def _empty(rows: int, n: int, device) -> Packed:
+    return Packed(torch.empty(packed_bytes(rows, n), dtype=torch.uint8, device=device), rows, n)
+
+
+def quantize(X: torch.Tensor, rows: bool = True, cols: bool = False) -> Tuple[Optional[Packed], Optional[Packed]]:
+    """X quantised with blocks along its rows, and its transpose with blocks along the columns of X (None for what is not asked for)."""
+    m, n, ldx, kind = _matrix(X)
+    if not rows and not cols:
+        raise ValueError("nothing asked for: rows, cols or both")
+    by_row = _empty(m, n, X.device) if rows else None
+    by_col = _empty(n, m, X.device) if cols else None
+    _check(_lib.ozimmu_mx_quantize(kind, m, n, X.data_ptr(), ldx, by_row.data.data_ptr() if rows else None,
+                                   by_col.data.data_ptr() if cols else None, ozimmu._stream()))
+    return by_row, by_col
+
+
+def dequantize(P: Packed, dtype=torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values of a packed matrix."""
+    P = _packed(P, "the matrix")
+    X = _output(out, P.data, P.rows, P.n, dtype, 0.0)
+    _, _, ldx, kind = _matrix(X)
+    _check(_lib.ozimmu_mx_dequantize(kind, P.rows, P.n, P.data.data_ptr(), X.data_ptr(), ldx, ozimmu._stream()))
+    return X
+
+
+def _bytes_matrix(t: torch.Tensor, rows: int, width: int, what: str) -> int:
+    if not t.is_cuda or t.dtype is not torch.uint8 or t.dim() != 2 or tuple(t.shape) != (rows, width):
+        raise ValueError(f"{what}: expected uint8 of {rows} x {width} on the GPU, got {t.dtype} of {tuple(t.shape)}")
+    if width > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < width:
+        raise ValueError(f"{what}: expected unit stride along rows that do not overlap")
+    return t.stride(0) if rows > 1 else max(width, 1)
+
+
+def pack(codes: torch.Tensor, scales: torch.Tensor, n: Optional[int] = None) -> Packed:
+    """A matrix of n columns (default: as many as there are codes) from the plain layout: per row ceil(n / 32) blocks of 16 bytes with
+    two codes each, the first in the lower half, and as many scale bytes."""
+    if scales.dim() != 2:
+        raise ValueError("scales: expected a 2-D tensor")
+    rows, blocks = scales.shape
+    n = blocks * BLOCK if n is None else n
+    if -(-n // BLOCK) != blocks:
+        raise ValueError(f"{blocks} scales a row for {n} columns")
+    ldc, lds = _bytes_matrix(codes, rows, blocks * BLOCK // 2, "codes"), _bytes_matrix(scales, rows, blocks, "scales")
+    P = _empty(rows, n, codes.device)
+    _check(_lib.ozimmu_mx_pack(rows, n, codes.data_ptr(), ldc, scales.data_ptr(), lds, P.data.data_ptr(), ozimmu._stream()))
+    return P
+
+
+def unpack(P: Packed) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Codes and scales of a packed matrix in the plain layout."""
+    P = _packed(P, "the matrix")
+    blocks = -(-P.n // BLOCK)
+    codes = torch.empty((P.rows, blocks * BLOCK // 2), dtype=torch.uint8, device=P.data.device)
+    scales = torch.empty((P.rows, blocks), dtype=torch.uint8, device=P.data.device)
+    _check(_lib.ozimmu_mx_unpack(P.rows, P.n, P.data.data_ptr(), codes.data_ptr(), max(codes.shape[1], 1), scales.data_ptr(),
+                                 max(blocks, 1), ozimmu._stream()))
+    return codes, scales
+
+
+def gemm(A: Packed, B: Packed, dtype=torch.float32, alpha: float = 1.0, beta: float = 0.0, D: Optional[torch.Tensor] = None,
+         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """D <- alpha A B^T + beta D from packed matrices."""
+    A, B = _packed(A, "A"), _packed(B, "B")
+    if A.n != B.n:
+        raise ValueError("inner dimensions differ")
+    m, n, p = A.rows, A.n, B.rows
+    D = _output(D, A.data, m, p, dtype, beta)
+    _, _, ldd, kind = _matrix(D)
+    if workspace is None:
+        workspace = alloc_workspace(m, n, p, D.device)
+    _check(_lib.ozimmu_mx_gemm(m, n, p, alpha, A.data.data_ptr(), B.data.data_ptr(), beta, kind, D.data_ptr(), ldd,
+                               workspace.data_ptr(), workspace.numel(), ozimmu._stream()))
+    return D
+
+
+def linear(X: torch.Tensor, W: Packed, dtype=None, alpha: float = 1.0, beta: float = 0.0, D: Optional[torch.Tensor] = None,
+           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """D <- alpha Q(X) W^T + beta D for rows X as they come and packed weights W (D in the type of X unless said otherwise)."""
+    m, n, ldx, xkind = _matrix(X)
+    W = _packed(W, "W")
+    if W.n != n:
+        raise ValueError("inner dimensions differ")
+    p = W.rows
+    D = _output(D, X, m, p, dtype or X.dtype, beta)
+    _, _, ldd, dkind = _matrix(D)
+    if workspace is None:
+        workspace = alloc_workspace(m, n, p, X.device)
+    _check(_lib.ozimmu_mx_linear(m, n, p, alpha, xkind, X.data_ptr(), ldx, W.data.data_ptr(), beta, dkind, D.data_ptr(), ldd,
+                                 workspace.data_ptr(), workspace.numel(), ozimmu._stream()))
+    return D
+
+
+def linear_backward(G: torch.Tensor, X: Optional[torch.Tensor], Wt: Optional[Packed], alpha: float = 1.0, beta_x: float = 0.0,
+                    beta_w: float = 0.0, dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Gradients of linear from the gradient G of its output: dX <- alpha Q(G) Wt^T + beta_x dX (Wt: the by-column form of the weights
+    from quantize(W, cols=True); None: no dX) and dW <- alpha Q(G^T) Q(X^T)^T + beta_w dW (X None: no dW).  Unless they are handed over,
+    dX comes in the type of G and dW in float32."""
+    m, p, ldg, kind = _matrix(G)
+    if X is None and Wt is None:
+        raise ValueError("neither X (for dW) nor Wt (for dX) given")
+    if (X is None and dW is not None) or (Wt is None and dX is not None):
+        raise ValueError("dW takes X, dX takes Wt")
+    n = X.shape[1] if X is not None and X.dim() == 2 else (Wt.rows if Wt is not None else 0)
+    ldx = lddx = lddw = dxkind = dwkind = 0
+    if X is not None:
+        if X.dtype is not G.dtype:
+            raise ValueError("X and G have to be of one type")
+        mx_, n, ldx, _ = _matrix(X)
+        if mx_ != m:
+            raise ValueError("X and G have to have as many rows")
+        dW = _output(dW, G, p, n, torch.float32, beta_w)
+        _, _, lddw, dwkind = _matrix(dW)
+    if Wt is not None:
+        if _packed(Wt, "Wt").shape != (n, p):
+            raise ValueError(f"Wt of {Wt.shape} for a layer of {n} to {p}")
+        dX = _output(dX, G, m, n, G.dtype, beta_x)
+        _, _, lddx, dxkind = _matrix(dX)
+    if workspace is None:
+        workspace = torch.empty(max(backward_workspace_bytes(m, n, p), 256), dtype=torch.uint8, device=G.device)
+    _check(_lib.ozimmu_mx_linear_backward(m, n, p, alpha, kind, G.data_ptr(), ldg, X.data_ptr() if X is not None else None, ldx,
+                                          Wt.data.data_ptr() if Wt is not None else None, beta_x, dxkind,
+                                          dX.data_ptr() if dX is not None else None, lddx, beta_w, dwkind,
+                                          dW.data_ptr() if dW is not None else None, lddw, workspace.data_ptr(), workspace.numel(),
+                                          ozimmu._stream()))
+    return dX, dW
