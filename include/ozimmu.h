@@ -48,7 +48,8 @@ enum {
     OZIMMU_ERR_SLICES = -3,     /* k outside 1..OZIMMU_MAX_SLICES, or g / s range invalid */
     OZIMMU_ERR_WORKSPACE = -4,  /* workspace too small or misaligned (needs 256-byte alignment) */
     OZIMMU_ERR_HIP = -5,        /* a kernel launch reported a HIP error */
-    OZIMMU_ERR_TYPE = -6        /* no such element type, or a pointer that its alignment does not fit (ozimmu_mx.h) */
+    OZIMMU_ERR_TYPE = -6,       /* no such element type, or a pointer that its alignment does not fit (ozimmu_mx.h) */
+    OZIMMU_ERR_WAY = -7         /* a call that cannot be run in the way it asks for (ozimmu_mx.h) */
 };
 
 /* Human-readable text for a status code (static storage, host). */

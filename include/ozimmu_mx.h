@@ -63,6 +63,15 @@ size_t ozimmu_mx_backward_workspace_bytes(int64_t m, int64_t n, int64_t p);
 int ozimmu_mx_gemm(int64_t m, int64_t n, int64_t p, float alpha, const void *A, const void *B, float beta, int type, void *D,
                    int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);
 
+/* The same, run in a given way instead of the library's choice (OZIMMU_ERR_WAY where it cannot run so); and that choice.  Debug / test
+ * helpers; the second one is host, pure. */
+enum { OZIMMU_MX_WAY_AUTO = -1,
+       OZIMMU_MX_WAY_DIRECT = 0,    /* 64 x 64 outputs a workgroup, operands from memory into registers */
+       OZIMMU_MX_WAY_TILE = 1 };    /* 256 x 256 outputs a workgroup at a time, operands through LDS */
+int ozimmu_mx_gemm_way(int way, int64_t m, int64_t n, int64_t p, float alpha, const void *A, const void *B, float beta, int type,
+                       void *D, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);
+int ozimmu_mx_choose(int64_t m, int64_t n, int64_t p, int64_t ldd);
+
 /* The forward pass of a linear layer: D <- alpha Q(X) W^T + beta D, X (device, m x n, ldx >= n) of type `xtype`, W packed
  * p x n, D of type `dtype`.  The same as ozimmu_mx_quantize(X) and ozimmu_mx_gemm; for few rows in one launch. */
 int ozimmu_mx_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void *X, int64_t ldx, const void *W, float beta,

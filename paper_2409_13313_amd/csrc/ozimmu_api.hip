@@ -686,6 +686,7 @@ const char* ozimmu_status_string(int status)
         case OZIMMU_ERR_WORKSPACE: return "workspace too small or misaligned";
         case OZIMMU_ERR_HIP: return "HIP launch error";
         case OZIMMU_ERR_TYPE: return "unknown element type or misaligned elements";
+        case OZIMMU_ERR_WAY: return "the call cannot be run in this way";
         default: return "unknown status";
     }
 }

@@ -117,15 +117,24 @@ size_t ozimmu_mx_backward_workspace_bytes(int64_t m, int64_t n, int64_t p)
 int ozimmu_mx_gemm(int64_t m, int64_t n, int64_t p, float alpha, const void* A, const void* B, float beta, int type, void* D,
                    int64_t ldd, void* workspace, size_t workspace_bytes, void* stream)
 {
+    return ozimmu_mx_gemm_way(OZIMMU_MX_WAY_AUTO, m, n, p, alpha, A, B, beta, type, D, ldd, workspace, workspace_bytes, stream);
+}
+
+int ozimmu_mx_gemm_way(int way, int64_t m, int64_t n, int64_t p, float alpha, const void* A, const void* B, float beta, int type, void* D,
+                       int64_t ldd, void* workspace, size_t workspace_bytes, void* stream)
+{
     if (!sizes_ok(m, n) || !sizes_ok(p, n)) return OZIMMU_ERR_DIM;
     CHECK(matrix_status(type, D, m, p, ldd));
+    if (way != OZIMMU_MX_WAY_AUTO && !mxk::way_fits(way, m, n, p, ldd)) return OZIMMU_ERR_WAY;
     if (m == 0 || p == 0) return OZIMMU_OK;
     CHECK(packed_status(A, m, n));
     CHECK(packed_status(B, p, n));
     CHECK(workspace_status(workspace, workspace_bytes, ozimmu_mx_workspace_bytes(m, n, p)));
     const mxk::Gemm g = {m, n, p, (const uint8_t*)A, (const uint8_t*)B, D, ldd, type, alpha, beta};
-    return launched(mxk::launch_gemm(g, (hipStream_t)stream));
+    return launched(mxk::launch_gemm(g, way, (hipStream_t)stream));
 }
+
+int ozimmu_mx_choose(int64_t m, int64_t n, int64_t p, int64_t ldd) { return mxk::choose(m, n, p, ldd); }
 
 int ozimmu_mx_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void* X, int64_t ldx, const void* W, float beta,
                      int dtype, void* D, int64_t ldd, void* workspace, size_t workspace_bytes, void* stream)
@@ -139,7 +148,7 @@ int ozimmu_mx_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, co
     const hipStream_t st = (hipStream_t)stream;
     if (n > 0) CHECK(launched(mxk::launch_quantize(xtype, m, n, X, ldx, workspace, nullptr, st)));
     const mxk::Gemm g = {m, n, p, (const uint8_t*)workspace, (const uint8_t*)W, D, ldd, dtype, alpha, beta};
-    return launched(mxk::launch_gemm(g, st));
+    return launched(mxk::launch_gemm(g, mxk::WAY_AUTO, st));
 }
 
 int ozimmu_mx_linear_backward(int64_t m, int64_t n, int64_t p, float alpha, int type, const void* G, int64_t ldg, const void* X,
@@ -166,12 +175,12 @@ int ozimmu_mx_linear_backward(int64_t m, int64_t n, int64_t p, float alpha, int 
         CHECK(launched(mxk::launch_quantize(type, m, p, G, ldg, want_x ? g_rows : nullptr, want_w ? g_cols : nullptr, st)));
     if (want_x) {
         const mxk::Gemm g = {m, p, n, g_rows, (const uint8_t*)Wt, dX, lddx, dx_type, alpha, beta_x};
-        CHECK(launched(mxk::launch_gemm(g, st)));
+        CHECK(launched(mxk::launch_gemm(g, mxk::WAY_AUTO, st)));
     }
     if (want_w) {
         if (m > 0) CHECK(launched(mxk::launch_quantize(type, m, n, X, ldx, nullptr, x_cols, st)));
         const mxk::Gemm g = {p, m, n, g_cols, x_cols, dW, lddw, dw_type, alpha, beta_w};
-        CHECK(launched(mxk::launch_gemm(g, st)));
+        CHECK(launched(mxk::launch_gemm(g, mxk::WAY_AUTO, st)));
     }
     return OZIMMU_OK;
 }

@@ -4,6 +4,7 @@
 // to 16 x 16 FP32 sums: 16 cycles of a SIMD, 4096 operations a cycle.  The fragments of B are its first operand, so that a lane's four
 // sums are four neighbouring columns of one row of D.
 #include "ozimmu_mx_convert.h"
+#include <type_traits>
 
 namespace {
 
@@ -36,16 +37,23 @@ template <int TYPE, int N> __device__ inline void finish(const Gemm& g, int64_t 
     store_row<TYPE, N>(out, left, x);
 }
 
+template <int I, int N, class F> __device__ inline void static_for(F&& f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<I + 1, N>(f);
+    }
+}
+
 // 64 x 64 outputs by four waves, each a quarter of the inner tiles straight from memory into registers; their sums meet in LDS.
 template <int TYPE> __global__ __launch_bounds__(256) void k_mx_direct(Gemm g, int64_t KT)
 {
-    constexpr int PITCH = 64 + 4;  // floats between the rows of a wave's sums: 16 rows fall on different banks
+    constexpr int PITCH = 64 + 4;  // floats between the rows of a wave's sums: rows fall on different banks
     __shared__ __align__(16) float sums[4 * 64 * PITCH];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int64_t row0 = (int64_t)blockIdx.y * 64, col0 = (int64_t)blockIdx.x * 64;
-    const uint8_t* const A = g.A + row0 / TILE_R * KT * TILE_BYTES;
-    const uint8_t* const B = g.B + col0 / TILE_R * KT * TILE_BYTES;
-    const int qa = (int)(row0 % TILE_R) / 64, qb = (int)(col0 % TILE_R) / 64;
+    const uint8_t* const A = g.A + row0 / TILE_R * KT * TILE_BYTES + row0 % TILE_R / 64 * QUARTER_BYTES;
+    const uint8_t* const B = g.B + col0 / TILE_R * KT * TILE_BYTES + col0 % TILE_R / 64 * QUARTER_BYTES;
     v4f acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -57,25 +65,23 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_direct(Gemm g, i
         v4i fa[4], fb[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            fa[i] = *(const v4i*)(ta + (4 * qa + i) * FRAGMENT_BYTES + lane * 16);
-            fb[i] = *(const v4i*)(tb + (4 * qb + i) * FRAGMENT_BYTES + lane * 16);
+            fa[i] = *(const v4i*)(ta + SCALE_BYTES + i * FRAGMENT_BYTES + lane * 16);
+            fb[i] = *(const v4i*)(tb + SCALE_BYTES + i * FRAGMENT_BYTES + lane * 16);
         }
-        const int sa = *(const int*)(ta + CODE_BYTES + qa * 256 + lane * 4);
-        const int sb = *(const int*)(tb + CODE_BYTES + qb * 256 + lane * 4);
-#define ROW(I)                                                \
-    acc[I][0] = mfma<0, I>(fb[0], sb, fa[I], sa, acc[I][0]); \
-    acc[I][1] = mfma<1, I>(fb[1], sb, fa[I], sa, acc[I][1]); \
-    acc[I][2] = mfma<2, I>(fb[2], sb, fa[I], sa, acc[I][2]); \
-    acc[I][3] = mfma<3, I>(fb[3], sb, fa[I], sa, acc[I][3]);
-        ROW(0) ROW(1) ROW(2) ROW(3)
-#undef ROW
+        const int sa = *(const int*)(ta + lane * 4), sb = *(const int*)(tb + lane * 4);
+        static_for<0, 4>([&](auto I) {
+            static_for<0, 4>([&](auto J) {
+                constexpr int i = decltype(I)::value, j = decltype(J)::value;
+                acc[i][j] = mfma<j, i>(fb[j], sb, fa[i], sa, acc[i][j]);
+            });
+        });
     }
-    // lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of every 16 x 16 tile
+    // of the row at place l % 16 of fragment i, lane l holds the columns at places 4 (l / 16) .. + 3 of fragment j
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            *(v4f*)(sums + (wave * 64 + i * 16 + (lane & 15)) * PITCH + j * 16 + 4 * (lane >> 4)) = acc[i][j];
+            *(v4f*)(sums + (wave * 64 + row_of(i, lane & 15)) * PITCH + row_of(j, lane >> 4 << 2)) = acc[i][j];
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -94,15 +100,325 @@ template <int TYPE> void direct(const Gemm& g, hipStream_t st)
     hipLaunchKernelGGL(k_mx_direct<TYPE>, grid, dim3(256), 0, st, g, inner_tiles(g.n));
 }
 
+// ---- 256 x 256 outputs by a workgroup of four waves, 128 x 128 each: 256 FP32 sums a lane, one wave a SIMD ----
+//
+// A workgroup per compute unit takes one tile of the output after the other.  A stage is one tile of A and one of B (128 inner
+// elements, 34 KiB).  The stages of all its output tiles are one stream from memory straight into a ring of four in LDS, four stages ahead
+// of the products: while a tile's sums are written out, the first stages of the next one arrive.  A stage is one step of 64
+// matrix instructions a wave, run as four quarters of 4 x 4 fragments on four sets of four fragments (16 bytes a lane each) and one
+// register of scales: (A lo, B lo), (A lo, B hi), (A hi, B lo), (A hi, B hi).  Quarter 0 fetches B hi and A hi, quarters 2 and 3 A lo and
+// B lo of the next stage, so that a fragment is there 16 matrix instructions ahead of its first use.
+// One barrier a stage, in its middle, where every wave has fetched all of the stage and its own copies of the next one have landed: behind
+// it the stage's place in the ring takes the copies of the fourth stage from here.  Ten copies a wave and stage; those behind the last
+// stage are out of the buffer's range: they read nothing, but count, so that every stage waits alike.
+constexpr int RING = 4, STAGE_BYTES = 2 * TILE_BYTES, COPIES = 10;
+constexpr int NXCD = 8, BAND = 8;
+
+template <int N> __device__ inline void wait_vmcnt() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Workgroup b runs on XCD b % 8.  The tiles are cut into eight contiguous ranges, one an XCD, in bands of 8 tile rows walked column by
+// column: the 32 tiles that an XCD works on at a time share 8 panels of A and 4 of B in its L2.
+struct Order {
+    int TM, TP, next, last, step;
+    __device__ inline Order(int TM_, int TP_) : TM(TM_), TP(TP_)
+    {
+        const int T = TM * TP, xcd = blockIdx.x % NXCD, begin = xcd * (T / NXCD) + (xcd < T % NXCD ? xcd : T % NXCD);
+        next = begin + blockIdx.x / NXCD;
+        last = begin + T / NXCD + (xcd < T % NXCD ? 1 : 0);
+        step = gridDim.x / NXCD + (xcd < (int)(gridDim.x % NXCD) ? 1 : 0);
+    }
+    // the next tile of this workgroup; false behind its last one
+    __device__ inline bool take(int& tm, int& tp)
+    {
+        if (next >= last) return false;
+        const int band = next / (BAND * TP), in_band = next % (BAND * TP);
+        const int height = TM - band * BAND < BAND ? TM - band * BAND : BAND;
+        tm = __builtin_amdgcn_readfirstlane(band * BAND + in_band % height);
+        tp = __builtin_amdgcn_readfirstlane(in_band / height);
+        next += step;
+        return true;
+    }
+};
+
+// A tile of one operand as a buffer
+__device__ inline v4i tile_resource(uint64_t address, bool any)
+{
+    return v4i{(int)(uint32_t)address, (int)(uint32_t)(address >> 32), any ? TILE_BYTES : 0, 0x00020000};
+}
+
+// Copy Q of a quarter of a tile: 256 bytes of scales (Q = 0, which sets M0 to the quarter's place in LDS for the others too) or a fragment.
+// Lane i writes LDS bytes [M0 + offset + its 4 or 16 bytes); the instruction's offset moves both addresses alike; one wait state
+// separates the write of M0 from the copy.
+template <int Q> __device__ inline void copy_quarter(uint32_t m0, uint32_t voff4, uint32_t voff16, v4i source)
+{
+    if constexpr (Q == 0)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(m0), "v"(voff4), "s"(source) : "memory");
+    else
+        asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" ::"v"(voff16), "s"(source), "n"(SCALE_BYTES + (Q - 1) * FRAGMENT_BYTES)
+                     : "memory");
+}
+
+// Eight neighbouring sums of a row into D; `left`: columns of D from the first of them on (WHOLE: eight at least).
+template <int TYPE, bool WHOLE, bool BETA>
+__device__ inline void put8(__attribute__((address_space(1))) typename Elem<TYPE>::Bits* out, int left, float alpha, float beta, const float* v)
+{
+    typename Elem<TYPE>::Bits x[8];
+    if (WHOLE || left >= 8) {
+        if constexpr (BETA) {
+            __builtin_memcpy(x, out, sizeof(x));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(alpha * v[e] + beta * to_float<TYPE>(x[e]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(alpha * v[e]);
+        }
+        __builtin_memcpy(out, x, sizeof(x));
+    } else if (left > 0) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < left) out[e] = from_float<TYPE>(BETA ? alpha * v[e] + beta * to_float<TYPE>(out[e]) : alpha * v[e]);
+    }
+}
+
+template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int KT, int TM, int TP)
+{
+    __shared__ __align__(16) uint8_t ring[RING * STAGE_BYTES];
+    const int t = threadIdx.x, lane = t & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
+    const uint32_t voff4 = wave * QUARTER_BYTES + lane * 4, voff16 = wave * QUARTER_BYTES + lane * 16;
+    const uint32_t m0_wave = lds + wave * QUARTER_BYTES;
+    typedef __attribute__((address_space(3))) const v4i* lds_v4i;
+    typedef __attribute__((address_space(3))) const int* lds_int;
+    // this lane's bytes of fragment 0 and of the scales in the wave's first quarter of A and of B, in ring place 0
+    const uint32_t fragA = lds + 2 * wm * QUARTER_BYTES + SCALE_BYTES + lane * 16;
+    const uint32_t fragB = lds + TILE_BYTES + 2 * wn * QUARTER_BYTES + SCALE_BYTES + lane * 16;
+    const uint32_t scaleA = lds + 2 * wm * QUARTER_BYTES + lane * 4;
+    const uint32_t scaleB = lds + TILE_BYTES + 2 * wn * QUARTER_BYTES + lane * 4;
+
+    // the stage that is copied next: its tiles, how many stages of its output tile are left, and the ring offset it goes to
+    Order copy_order(TM, TP);
+    uint64_t pa = 0, pb = 0;
+    int copy_left = 0;
+    bool any = true;
+    uint32_t to = 0;
+    auto advance = [](uint32_t& place) { place = place == (RING - 1) * STAGE_BYTES ? 0 : place + STAGE_BYTES; };
+    auto find_stage = [&]() {
+        if (copy_left == 0) {
+            int tm, tp;
+            any = copy_order.take(tm, tp);
+            if (any) {
+                pa = (uint64_t)(uintptr_t)g.A + (uint64_t)tm * KT * TILE_BYTES;
+                pb = (uint64_t)(uintptr_t)g.B + (uint64_t)tp * KT * TILE_BYTES;
+            }
+            copy_left = KT;
+        }
+    };
+    auto stage_copied = [&]() {
+        pa += TILE_BYTES;
+        pb += TILE_BYTES;
+        --copy_left;
+        advance(to);
+    };
+    static_for<0, RING>([&](auto) {
+        find_stage();
+        static_for<0, COPIES / 2>([&](auto Q) { copy_quarter<decltype(Q)::value>(m0_wave + to, voff4, voff16, tile_resource(pa, any)); });
+        static_for<0, COPIES / 2>([&](auto Q) { copy_quarter<decltype(Q)::value>(m0_wave + to + TILE_BYTES, voff4, voff16, tile_resource(pb, any)); });
+        stage_copied();
+    });
+
+    v4f acc[8][8];
+    v4i faL[4], faH[4], fbL[4], fbH[4];
+    int saL, saH, sbL, sbH;
+    uint32_t here = 0;  // ring offset of the current stage
+    // half of sub-step S of a quarter: two matrix instructions on fragment S of the set that was fetched last (B's with BY_B) and the other set
+    auto math = [&](const v4i* fa, int sa, const v4i* fb, int sb, auto I0, auto J0, auto S, auto BY_B, auto X0) {
+        static_for<0, 2>([&](auto X) {
+            constexpr int s = decltype(S)::value, x = decltype(X0)::value + decltype(X)::value, y = (s & 1) ? 3 - x : x;
+            constexpr int i = decltype(BY_B)::value ? y : s, j = decltype(BY_B)::value ? s : y;
+            v4f& c = acc[decltype(I0)::value + i][decltype(J0)::value + j];
+            c = mfma<j, i>(fb[j], sb, fa[i], sa, c);
+        });
+    };
+    typedef std::integral_constant<int, 0> N0;
+    typedef std::integral_constant<int, 2> N2;
+    typedef std::integral_constant<int, 4> N4;
+    typedef std::true_type ByB;
+    typedef std::false_type ByA;
+
+    wait_vmcnt<(RING - 1) * COPIES>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        faL[q] = *(lds_v4i)(uintptr_t)(fragA + q * FRAGMENT_BYTES);
+        fbL[q] = *(lds_v4i)(uintptr_t)(fragB + q * FRAGMENT_BYTES);
+    }
+    saL = *(lds_int)(uintptr_t)scaleA;
+    sbL = *(lds_int)(uintptr_t)scaleB;
+
+    // Stores count as copies do.  In the two stages behind the end of a tile, all of whose STORES stores were made, they are newer than
+    // the copies that are waited for and need not be over.
+    constexpr int STORES = TYPE == F32 ? 64 : 32, NEWER = (RING - 2) * COPIES;
+    constexpr int NEWER_STORES = NEWER + STORES < 63 ? NEWER + STORES : 63;
+    int fresh = 0;  // stages for which that holds
+    Order order(TM, TP);
+    int tm, tp;
+    while (order.take(tm, tp)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                acc[i][j] = v4f{0, 0, 0, 0};
+                asm volatile("" : "+a"(acc[i][j]));  // (in its accumulation registers from here on)
+            }
+        for (int it = 0; it < KT; ++it) {
+            const uint32_t fa_here = fragA + here, fb_here = fragB + here, sa_here = scaleA + here, sb_here = scaleB + here;
+            advance(here);
+            const uint32_t fa_next = fragA + here, fb_next = fragB + here, sa_next = scaleA + here, sb_next = scaleB + here;
+            // quarter 0: the upper halves of A and B come in
+            static_for<0, 4>([&](auto Q) {
+                constexpr int q = decltype(Q)::value;
+                fbH[q] = *(lds_v4i)(uintptr_t)(fb_here + QUARTER_BYTES + q * FRAGMENT_BYTES);
+                if constexpr (q == 0) sbH = *(lds_int)(uintptr_t)(sb_here + QUARTER_BYTES);
+                math(faL, saL, fbL, sbL, N0{}, N0{}, Q, ByB{}, N0{});
+                __builtin_amdgcn_sched_barrier(0);
+                faH[q] = *(lds_v4i)(uintptr_t)(fa_here + QUARTER_BYTES + q * FRAGMENT_BYTES);
+                if constexpr (q == 0) saH = *(lds_int)(uintptr_t)(sa_here + QUARTER_BYTES);
+                math(faL, saL, fbL, sbL, N0{}, N0{}, Q, ByB{}, N2{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            // quarter 1
+            static_for<0, 4>([&](auto Q) {
+                math(faL, saL, fbH, sbH, N0{}, N4{}, Q, ByB{}, N0{});
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (decltype(Q)::value == 1) find_stage();
+                math(faL, saL, fbH, sbH, N0{}, N4{}, Q, ByB{}, N2{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            if (fresh > 0) {
+                --fresh;
+                wait_vmcnt<NEWER_STORES>();
+            } else {
+                wait_vmcnt<NEWER>();
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            const v4i source_a = tile_resource(pa, any), source_b = tile_resource(pb, any);
+            // quarter 2: the lower half of A of the next stage (behind the last one: what the ring holds, unused)
+            static_for<0, 4>([&](auto Q) {
+                constexpr int q = decltype(Q)::value;
+                faL[q] = *(lds_v4i)(uintptr_t)(fa_next + q * FRAGMENT_BYTES);
+                if constexpr (q == 0) saL = *(lds_int)(uintptr_t)sa_next;
+                math(faH, saH, fbL, sbL, N4{}, N0{}, Q, ByA{}, N0{});
+                __builtin_amdgcn_sched_barrier(0);
+                copy_quarter<q>(m0_wave + to, voff4, voff16, source_a);
+                math(faH, saH, fbL, sbL, N4{}, N0{}, Q, ByA{}, N2{});
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (q == 3) copy_quarter<4>(m0_wave + to, voff4, voff16, source_a);
+            });
+            // quarter 3: its lower half of B
+            static_for<0, 4>([&](auto Q) {
+                constexpr int q = decltype(Q)::value;
+                fbL[q] = *(lds_v4i)(uintptr_t)(fb_next + q * FRAGMENT_BYTES);
+                if constexpr (q == 0) sbL = *(lds_int)(uintptr_t)sb_next;
+                math(faH, saH, fbH, sbH, N4{}, N4{}, Q, ByA{}, N0{});
+                __builtin_amdgcn_sched_barrier(0);
+                copy_quarter<q>(m0_wave + to + TILE_BYTES, voff4, voff16, source_b);
+                math(faH, saH, fbH, sbH, N4{}, N4{}, Q, ByA{}, N2{});
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (q == 3) copy_quarter<4>(m0_wave + to + TILE_BYTES, voff4, voff16, source_b);
+            });
+            stage_copied();
+        }
+        // (left alone, the register allocator parks accumulators in scratch memory and copies all of them at once; so they are read by
+        // asm statements below, and the wait states behind the last matrix instruction are written out)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+        asm volatile("s_nop 15\n\ts_nop 15");
+        // fragment (i, j), register r: row at place l % 16 of fragment i % 4 of A's quarter i / 4, column at place 4 (l / 16) + r of
+        // fragment j % 4 of B's quarter j / 4: fragments j and j + 1 (j even) are 8 neighbouring columns
+        // (lane parts made opaque here, or they are formed at kernel entry and live through everything; addresses are a uniform base
+        // and a 32-bit lane offset)
+        typedef typename Elem<TYPE>::Bits Bits;
+        typedef __attribute__((address_space(1))) Bits Global;
+        int lr = lane & 15, lc = lane >> 4;
+        asm volatile("" : "+v"(lr), "+v"(lc));
+        const int row_lane = row_of(0, lr), col_lane = row_of(0, lc << 2);
+        const uint32_t off = ((uint32_t)row_lane * (uint32_t)g.ldd + (uint32_t)col_lane) * (uint32_t)sizeof(Bits);
+        const int64_t row0 = (int64_t)tm * TILE_R + wm * 128, col0 = (int64_t)tp * TILE_R + wn * 128;
+        const int rows_left = (int)(g.m - row0 < 128 ? g.m - row0 : 128) - row_lane, cols_left = (int)(g.p - col0 < 128 ? g.p - col0 : 128) - col_lane;
+        auto put = [&](auto WHOLE, auto BETA) {
+            constexpr bool whole = decltype(WHOLE)::value;
+            static_for<0, 8>([&](auto I) {
+                constexpr int i = decltype(I)::value, ri = i / 4 * 64 + row_of(i % 4, 0);
+                uint64_t base = (uint64_t)(uintptr_t)((Bits*)g.D + (row0 + ri) * g.ldd + col0);
+                asm volatile("" : "+s"(base));
+                if (whole || ri < rows_left) {
+                    static_for<0, 4>([&](auto J) {
+                        constexpr int j = 2 * decltype(J)::value, cj = j / 4 * 64 + row_of(j % 4, 0);
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][j + e / 4][e % 4]));
+                        put8<TYPE, whole, decltype(BETA)::value>((Global*)(base + off) + cj, cols_left - cj, g.alpha, g.beta, v);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                }
+            });
+        };
+        fresh = 0;
+        if (g.beta != 0.0f) {
+            put(std::false_type{}, std::true_type{});
+        } else if ((int64_t)(tm + 1) * TILE_R <= g.m && (int64_t)(tp + 1) * TILE_R <= g.p) {
+            put(std::true_type{}, std::false_type{});
+            fresh = 2;
+        } else {
+            put(std::false_type{}, std::false_type{});
+        }
+    }
+    wait_vmcnt<0>();  // no copy may still be writing LDS when the workgroup retires
+}
+
+template <int TYPE> void tile(const Gemm& g, hipStream_t st)
+{
+    const int TM = (int)row_tiles(g.m), TP = (int)row_tiles(g.p);
+    hipLaunchKernelGGL(k_mx_tile<TYPE>, dim3((unsigned)(TM * TP < 256 ? TM * TP : 256)), dim3(256), 0, st, g, (int)inner_tiles(g.n), TM, TP);
+}
+
+template <int TYPE> void product(const Gemm& g, int way, hipStream_t st)
+{
+    if (way == WAY_TILE)
+        tile<TYPE>(g, st);
+    else
+        direct<TYPE>(g, st);
+}
+
 }  // namespace
 
 namespace mxk {
 
-hipError_t launch_gemm(const Gemm& g, hipStream_t st)
+// (32-bit offsets of a lane inside 28 rows of D, and 32-bit numbers of tiles)
+bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd)
 {
-    if (g.dtype == F32) direct<F32>(g, st);
-    if (g.dtype == BF16) direct<BF16>(g, st);
-    if (g.dtype == F16) direct<F16>(g, st);
+    if (way == WAY_TILE) return n > 0 && ldd < (1 << 24) && row_tiles(m) * row_tiles(p) < ((int64_t)1 << 30);
+    return way == WAY_DIRECT;
+}
+
+int choose(int64_t m, int64_t n, int64_t p, int64_t ldd)
+{
+    return way_fits(WAY_TILE, m, n, p, ldd) && row_tiles(m) * row_tiles(p) >= 128 ? WAY_TILE : WAY_DIRECT;
+}
+
+hipError_t launch_gemm(const Gemm& g, int way, hipStream_t st)
+{
+    if (way == WAY_AUTO) way = choose(g.m, g.n, g.p, g.ldd);
+    if (g.dtype == F32) product<F32>(g, way, st);
+    if (g.dtype == BF16) product<BF16>(g, way, st);
+    if (g.dtype == F16) product<F16>(g, way, st);
     return hipGetLastError();
 }
 

@@ -10,19 +10,20 @@ using namespace mxk;
 using namespace mxl;
 
 // Blocks along the rows.  A workgroup takes 64 rows x 128 columns (a quarter of a tile): thread t the eight elements t % 16 of
-// rows t / 16 + 16 i, so that 16 lanes read 128 columns of a row side by side; four lanes hold a block and share its maximum.
+// the four rows at place t / 16 of the fragments, so that 16 lanes read 128 columns of a row side by side; four lanes hold a block and
+// share its maximum.
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_mx_quantize_rows(int64_t rows, int64_t n, const typename Elem<TYPE>::Bits* X, int64_t ldx,
                                                           uint8_t* out, int64_t KT)
 {
     typedef typename Elem<TYPE>::Bits Bits;
     const int t = threadIdx.x, chunk = t & 15, c = chunk >> 2, sub = chunk & 3;
-    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + (t >> 4);
+    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + row_of(0, t >> 4);
     const int64_t col = kt * TILE_K + chunk * 8;
     Bits x[4][8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + 16 * i;
+        const int64_t row = row0 + row_of(i, 0);
         load_row<TYPE, 8>(X + row * ldx + col, row < rows ? n - col : 0, x[i]);
     }
     uint8_t* const tile = out + ((row0 / TILE_R) * KT + kt) * TILE_BYTES;
@@ -42,7 +43,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize_rows(int64_t rows, int64_t 
         }
         const uint32_t b = scale_byte(amax);
         scales |= b << (8 * i);
-        const int64_t row = row0 + 16 * i;
+        const int64_t row = row0 + row_of(i, 0);
         if (row < rows) {
             const uint32_t codes = codes8<TYPE>(x[i], scale_value(b));
             *(uint32_t*)(tile + code_offset((int)(row % TILE_R), c) + 4 * sub) = codes;
@@ -100,17 +101,17 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t n, 
 {
     typedef typename Elem<TYPE>::Bits Bits;
     const int t = threadIdx.x, chunk = t & 15, c = chunk >> 2, sub = chunk & 3;
-    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + (t >> 4);
+    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + row_of(0, t >> 4);
     const int64_t col = kt * TILE_K + chunk * 8;
     if (row0 >= rows || col >= n) return;
     const uint8_t* const tile = in + ((row0 / TILE_R) * KT + kt) * TILE_BYTES;
     const uint32_t scales = *(const uint32_t*)(tile + scale_offset((int)(row0 % TILE_R), c));
     uint32_t codes[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) codes[i] = *(const uint32_t*)(tile + code_offset((int)(row0 % TILE_R) + 16 * i, c) + 4 * sub);
+    for (int i = 0; i < 4; ++i) codes[i] = *(const uint32_t*)(tile + code_offset((int)(row0 % TILE_R) + row_of(i, 0), c) + 4 * sub);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + 16 * i;
+        const int64_t row = row0 + row_of(i, 0);
         if (row >= rows) break;
         const float s = scale_of((scales >> (8 * i)) & 255u);
         Bits x[8];

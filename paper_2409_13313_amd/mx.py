@@ -27,6 +27,8 @@ _SIGNATURES = {
     "ozimmu_mx_workspace_bytes": (_sz, [_i64, _i64, _i64]),
     "ozimmu_mx_backward_workspace_bytes": (_sz, [_i64, _i64, _i64]),
     "ozimmu_mx_gemm": (_int, [_i64, _i64, _i64, _float, _vp, _vp, _float, _int, _vp, _i64, _vp, _sz, _vp]),
+    "ozimmu_mx_gemm_way": (_int, [_int, _i64, _i64, _i64, _float, _vp, _vp, _float, _int, _vp, _i64, _vp, _sz, _vp]),
+    "ozimmu_mx_choose": (_int, [_i64, _i64, _i64, _i64]),
     "ozimmu_mx_linear": (_int, [_i64, _i64, _i64, _float, _int, _vp, _i64, _vp, _float, _int, _vp, _i64, _vp, _sz, _vp]),
     "ozimmu_mx_linear_backward": (_int, [_i64, _i64, _i64, _float, _int, _vp, _i64, _vp, _i64, _vp, _float, _int, _vp, _i64,
                                          _float, _int, _vp, _i64, _vp, _sz, _vp]),
@@ -37,6 +39,7 @@ EXPORTS = list(_SIGNATURES)
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 BLOCK = 32
+WAYS = {"auto": -1, "direct": 0, "tile": 1}
 
 
 class Packed:
@@ -170,8 +173,8 @@ def unpack(P: Packed) -> Tuple[torch.Tensor, torch.Tensor]:
 
 
 def gemm(A: Packed, B: Packed, dtype=torch.float32, alpha: float = 1.0, beta: float = 0.0, D: Optional[torch.Tensor] = None,
-         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """D <- alpha A B^T + beta D from packed matrices."""
+         workspace: Optional[torch.Tensor] = None, way: str = "auto") -> torch.Tensor:
+    """D <- alpha A B^T + beta D from packed matrices; `way` forces how it is run (see ozimmu_mx_gemm_way in the header)."""
     A, B = _packed(A, "A"), _packed(B, "B")
     if A.n != B.n:
         raise ValueError("inner dimensions differ")
@@ -180,8 +183,8 @@ def gemm(A: Packed, B: Packed, dtype=torch.float32, alpha: float = 1.0, beta: fl
     _, _, ldd, kind = _matrix(D)
     if workspace is None:
         workspace = alloc_workspace(m, n, p, D.device)
-    _check(_lib.ozimmu_mx_gemm(m, n, p, alpha, A.data.data_ptr(), B.data.data_ptr(), beta, kind, D.data_ptr(), ldd,
-                               workspace.data_ptr(), workspace.numel(), ozimmu._stream()))
+    _check(_lib.ozimmu_mx_gemm_way(WAYS[way], m, n, p, alpha, A.data.data_ptr(), B.data.data_ptr(), beta, kind, D.data_ptr(), ldd,
+                                   workspace.data_ptr(), workspace.numel(), ozimmu._stream()))
     return D
 
 

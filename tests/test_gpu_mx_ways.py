@@ -1,0 +1,61 @@
+"""Every way of running a product of microscaled 4-bit matrices, forced where the library would choose another, against the product of
+the same values in 64 bits (bounds as for the library's choice)."""
+import numpy as np
+import pytest
+
+from oracle import mx as ref
+from test_gpu_mx_product import EPS, TINY, TYPES, check, f64, matrix
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+# (rows, inner dimension, columns): one tile, several, edges in both directions, one to nine inner tiles and more, whole tiles only
+SHAPES = [(1, 1, 1), (5, 129, 300), (256, 128, 256), (256, 512, 512), (257, 640, 255), (513, 300, 260), (300, 1100, 1037), (512, 1280, 768),
+          (700, 2049, 515), (1024, 384, 1280), (2100, 257, 2300), (4352, 640, 4400)]
+
+
+@pytest.fixture(scope="module")
+def mx():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: the HIP path has no CPU fallback")
+    from paper_2409_13313_amd import mx
+    return mx
+
+
+def product(A, B):
+    """A B^T in 64 bits (on the GPU where it is large), and the sum of magnitudes."""
+    a, b = torch.from_numpy(A).cuda(), torch.from_numpy(B).cuda()
+    return (a @ b.t()).cpu().numpy(), (a.abs() @ b.abs().t()).cpu().numpy()
+
+
+@pytest.mark.parametrize("m,n,p", SHAPES)
+@pytest.mark.parametrize("way", ["direct", "tile"])
+def test_way(mx, way, m, n, p):
+    print(f"{way} {m} x {n} x {p}", flush=True)
+    A, B = matrix(m, n, "bf16", m + n), matrix(p, n, "bf16", p + n + 1)
+    qa, qb = ref.read_back(f64(A)), ref.read_back(f64(B))
+    want, size = product(qa, qb)
+    bound = max(n, 1) * 2.0 ** -23 * size
+    (PA, _), (PB, _) = mx.quantize(A), mx.quantize(B)
+    for kind, t in TYPES.items():
+        check(mx.gemm(PA, PB, t, way=way), want, bound, kind, n, kind)
+        big = torch.full((m + 1, p + 3), 5.0, dtype=t, device="cuda")
+        mx.gemm(PA, PB, D=big[:m, 1:p + 1], way=way)
+        check(big[:m, 1:p + 1], want, bound, kind, n, kind)
+        assert (big[:, 0] == 5).all() and (big[:, p + 1:] == 5).all() and (big[m] == 5).all()
+        old = matrix(m, p, kind, 3)
+        got = mx.gemm(PA, PB, alpha=-0.5, beta=2.0, D=old.clone(), way=way)
+        limit = 0.5 * bound + 3 * 2.0 ** -24 * (0.5 * (np.abs(want) + bound) + 2 * np.abs(f64(old)))
+        check(got, -0.5 * want + 2.0 * f64(old), limit, kind, n, kind)
+
+
+@pytest.mark.parametrize("way", ["direct", "tile"])
+def test_again_and_again(mx, way):
+    """The same bits from call to call, with other work between."""
+    m, n, p = 1800, 900, 2000
+    (PA, _), (PB, _) = mx.quantize(matrix(m, n, "bf16", 1)), mx.quantize(matrix(p, n, "bf16", 2))
+    first = mx.gemm(PA, PB, torch.bfloat16, way=way)
+    for k in range(20):
+        D = torch.full((m, p), float("nan"), dtype=torch.bfloat16, device="cuda")
+        mx.gemm(PA, PB, D=D, way=way)
+        assert torch.equal(D, first), k
