@@ -106,13 +106,16 @@ template <int TYPE> void direct(const Gemm& g, hipStream_t st)
 // elements, 34 KiB).  The stages of all its output tiles are one stream from memory straight into a ring of four in LDS, four stages ahead
 // of the products: while a tile's sums are written out, the first stages of the next one arrive.  A stage is one step of 64
 // matrix instructions a wave, run as four quarters of 4 x 4 fragments on four sets of four fragments (16 bytes a lane each) and one
-// register of scales: (A lo, B lo), (A lo, B hi), (A hi, B lo), (A hi, B hi).  Quarter 0 fetches B hi and A hi, quarters 2 and 3 A lo and
-// B lo of the next stage, so that a fragment is there 16 matrix instructions ahead of its first use.
+// register of scales: (A lo, B lo), (A lo, B hi), (A hi, B lo), (A hi, B hi).  Quarter 0 fetches B hi, quarter 1 A hi, quarters 2 and 3
+// A lo and B lo of the next stage, so that a fragment is on its way 8 to 16 matrix instructions ahead of its first use.
+// A scaled matrix instruction takes three of its four issue slots itself (a second vector instruction beside it costs 4 cycles), so
+// everything else is spread: one fetch every four of them, a copy every six.
 // One barrier a stage, in its middle, where every wave has fetched all of the stage and its own copies of the next one have landed: behind
 // it the stage's place in the ring takes the copies of the fourth stage from here.  Ten copies a wave and stage; those behind the last
 // stage are out of the buffer's range: they read nothing, but count, so that every stage waits alike.
 constexpr int RING = 4, STAGE_BYTES = 2 * TILE_BYTES, COPIES = 10;
 constexpr int NXCD = 8, BAND = 8;
+constexpr int64_t MEMORY_SIDE_CACHE = (int64_t)256 << 20;
 
 template <int N> __device__ inline void wait_vmcnt() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -158,20 +161,15 @@ template <int Q> __device__ inline void copy_quarter(uint32_t m0, uint32_t voff4
                      : "memory");
 }
 
-// Eight neighbouring sums of a row into D; `left`: columns of D from the first of them on (WHOLE: eight at least).
-template <int TYPE, bool WHOLE, bool BETA>
+// Eight neighbouring sums of a row into D; `left`: columns of D from the first of them on.
+template <int TYPE, bool BETA>
 __device__ inline void put8(__attribute__((address_space(1))) typename Elem<TYPE>::Bits* out, int left, float alpha, float beta, const float* v)
 {
     typename Elem<TYPE>::Bits x[8];
-    if (WHOLE || left >= 8) {
-        if constexpr (BETA) {
-            __builtin_memcpy(x, out, sizeof(x));
+    if (left >= 8) {
+        if constexpr (BETA) __builtin_memcpy(x, out, sizeof(x));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(alpha * v[e] + beta * to_float<TYPE>(x[e]));
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(alpha * v[e]);
-        }
+        for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(BETA ? alpha * v[e] + beta * to_float<TYPE>(x[e]) : alpha * v[e]);
         __builtin_memcpy(out, x, sizeof(x));
     } else if (left > 0) {
 #pragma unroll
@@ -180,7 +178,33 @@ __device__ inline void put8(__attribute__((address_space(1))) typename Elem<TYPE
     }
 }
 
-template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int KT, int TM, int TP)
+// The same where all eight lie inside D and its old values do not matter: written through the L2, so that the kernel's end has nothing
+// left to write back (4096 x 2048 x 4096: 21.1 us, 22.5 with plain stores; 8192 x 2048 x 8192: 70 and 73.5).  STREAM: past the caches, for
+// outputs that with the operands exceed the memory-side cache (8192 x 8192 x 16384, 268 MB of D: 434 us, written through 471, plain 477;
+// 134 MB of D, inner dimension 4096: 128, 119, 117).  Two wait states keep what follows off the registers of a 16-byte store.
+template <bool STREAM, int OFFSET> __device__ inline void store16(uint64_t base, uint32_t off, v4i y)
+{
+    if constexpr (STREAM)
+        asm volatile("global_store_dwordx4 %0, %1, %2 offset:%3 sc1 nt\n\ts_nop 1" ::"v"(off), "v"(y), "s"(base), "n"(OFFSET) : "memory");
+    else
+        asm volatile("global_store_dwordx4 %0, %1, %2 offset:%3 sc0 sc1\n\ts_nop 1" ::"v"(off), "v"(y), "s"(base), "n"(OFFSET) : "memory");
+}
+template <int TYPE, bool STREAM, int COLUMN>
+__device__ inline void put8_whole(uint64_t base, uint32_t off, float alpha, const float* v)
+{
+    constexpr int size = sizeof(typename Elem<TYPE>::Bits);
+    typename Elem<TYPE>::Bits x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(alpha * v[e]);
+    static_for<0, size / 2>([&](auto H) {
+        constexpr int h = decltype(H)::value;
+        v4i y;
+        __builtin_memcpy(&y, (const char*)x + 16 * h, 16);
+        store16<STREAM, COLUMN * size + 16 * h>(base, off, y);
+    });
+}
+
+template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int KT, int TM, int TP, int stream)
 {
     __shared__ __align__(16) uint8_t ring[RING * STAGE_BYTES];
     const int t = threadIdx.x, lane = t & 63;
@@ -197,41 +221,54 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
     const uint32_t scaleA = lds + 2 * wm * QUARTER_BYTES + lane * 4;
     const uint32_t scaleB = lds + TILE_BYTES + 2 * wn * QUARTER_BYTES + lane * 4;
 
-    // the stage that is copied next: its tiles, how many stages of its output tile are left, and the ring offset it goes to
-    Order copy_order(TM, TP);
-    uint64_t pa = 0, pb = 0;
-    int copy_left = 0;
-    bool any = true;
-    uint32_t to = 0;
-    auto advance = [](uint32_t& place) { place = place == (RING - 1) * STAGE_BYTES ? 0 : place + STAGE_BYTES; };
-    auto find_stage = [&]() {
-        if (copy_left == 0) {
-            int tm, tp;
-            any = copy_order.take(tm, tp);
-            if (any) {
-                pa = (uint64_t)(uintptr_t)g.A + (uint64_t)tm * KT * TILE_BYTES;
-                pb = (uint64_t)(uintptr_t)g.B + (uint64_t)tp * KT * TILE_BYTES;
-            }
-            copy_left = KT;
+    // What is copied next of A and of B: the address of the tile, its bytes (0 behind the last one), how many stages of its output tile are
+    // left.  Copies are four stages ahead at most and an output tile has at least as many, so that the operand tiles behind it (`after`)
+    // are looked up once an output tile, outside the loop over its stages: there is no branch in there.
+    struct Source {
+        uint64_t at, after;
+        int bytes, bytes_after, left;
+        __device__ inline v4i resource() const { return v4i{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), bytes, 0x00020000}; }
+        __device__ inline void next(int KT)
+        {
+            --left;
+            const bool over = left == 0;
+            at = over ? after : at + TILE_BYTES;
+            bytes = over ? bytes_after : bytes;
+            left = over ? KT : left;
         }
     };
-    auto stage_copied = [&]() {
-        pa += TILE_BYTES;
-        pb += TILE_BYTES;
-        --copy_left;
-        advance(to);
+    Source a = {0, 0, 0, 0, KT}, b = {0, 0, 0, 0, KT};
+    Order copy_order(TM, TP);
+    auto look_up = [&]() {
+        int tm, tp;
+        const bool any = copy_order.take(tm, tp);
+        a.bytes_after = b.bytes_after = any ? TILE_BYTES : 0;
+        if (any) {
+            a.after = (uint64_t)(uintptr_t)g.A + (uint64_t)tm * KT * TILE_BYTES;
+            b.after = (uint64_t)(uintptr_t)g.B + (uint64_t)tp * KT * TILE_BYTES;
+        }
     };
-    static_for<0, RING>([&](auto) {
-        find_stage();
-        static_for<0, COPIES / 2>([&](auto Q) { copy_quarter<decltype(Q)::value>(m0_wave + to, voff4, voff16, tile_resource(pa, any)); });
-        static_for<0, COPIES / 2>([&](auto Q) { copy_quarter<decltype(Q)::value>(m0_wave + to + TILE_BYTES, voff4, voff16, tile_resource(pb, any)); });
-        stage_copied();
+    look_up();
+    a.at = a.after;
+    b.at = b.after;
+    a.bytes = b.bytes = a.bytes_after;
+    uint32_t here = 0, to = 0;  // ring offsets: the current stage, the stage that is copied
+    auto advance = [](uint32_t& place) { place = place == (RING - 1) * STAGE_BYTES ? 0 : place + STAGE_BYTES; };
+    auto copy_a = [&](auto Q) { copy_quarter<decltype(Q)::value>(m0_wave + to, voff4, voff16, a.resource()); };
+    auto copy_b = [&](auto Q) { copy_quarter<decltype(Q)::value>(m0_wave + to + TILE_BYTES, voff4, voff16, b.resource()); };
+    static_for<0, RING>([&](auto S) {
+        static_for<0, COPIES / 2>(copy_a);
+        if constexpr (decltype(S)::value < RING - 1) {  // (the main loop begins with the last one's B)
+            a.next(KT);
+            static_for<0, COPIES / 2>(copy_b);
+            b.next(KT);
+            advance(to);
+        }
     });
 
     v4f acc[8][8];
     v4i faL[4], faH[4], fbL[4], fbH[4];
     int saL, saH, sbL, sbH;
-    uint32_t here = 0;  // ring offset of the current stage
     // half of sub-step S of a quarter: two matrix instructions on fragment S of the set that was fetched last (B's with BY_B) and the other set
     auto math = [&](const v4i* fa, int sa, const v4i* fb, int sb, auto I0, auto J0, auto S, auto BY_B, auto X0) {
         static_for<0, 2>([&](auto X) {
@@ -247,16 +284,20 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
     typedef std::true_type ByB;
     typedef std::false_type ByA;
 
-    wait_vmcnt<(RING - 1) * COPIES>();
+    wait_vmcnt<(RING - 1) * COPIES - COPIES / 2>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    // addresses of the current stage and, from the middle of a stage on, of the next one
+    uint32_t fa_at = fragA, fb_at = fragB, sa_at = scaleA, sb_at = scaleB;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        faL[q] = *(lds_v4i)(uintptr_t)(fragA + q * FRAGMENT_BYTES);
-        fbL[q] = *(lds_v4i)(uintptr_t)(fragB + q * FRAGMENT_BYTES);
+        faL[q] = *(lds_v4i)(uintptr_t)(fa_at + q * FRAGMENT_BYTES);
+        fbL[q] = *(lds_v4i)(uintptr_t)(fb_at + q * FRAGMENT_BYTES);
     }
-    saL = *(lds_int)(uintptr_t)scaleA;
-    sbL = *(lds_int)(uintptr_t)scaleB;
+    saL = *(lds_int)(uintptr_t)sa_at;
+    saH = *(lds_int)(uintptr_t)(sa_at + QUARTER_BYTES);
+    sbL = *(lds_int)(uintptr_t)sb_at;
+    sbH = *(lds_int)(uintptr_t)(sb_at + QUARTER_BYTES);
 
     // Stores count as copies do.  In the two stages behind the end of a tile, all of whose STORES stores were made, they are newer than
     // the copies that are waited for and need not be over.
@@ -266,6 +307,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
     Order order(TM, TP);
     int tm, tp;
     while (order.take(tm, tp)) {
+        look_up();
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -274,64 +316,78 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
                 asm volatile("" : "+a"(acc[i][j]));  // (in its accumulation registers from here on)
             }
         for (int it = 0; it < KT; ++it) {
-            const uint32_t fa_here = fragA + here, fb_here = fragB + here, sa_here = scaleA + here, sb_here = scaleB + here;
-            advance(here);
-            const uint32_t fa_next = fragA + here, fb_next = fragB + here, sa_next = scaleA + here, sb_next = scaleB + here;
-            // quarter 0: the upper halves of A and B come in
+            // quarter 0: the upper half of B comes in, the first copies of B go out
             static_for<0, 4>([&](auto Q) {
                 constexpr int q = decltype(Q)::value;
-                fbH[q] = *(lds_v4i)(uintptr_t)(fb_here + QUARTER_BYTES + q * FRAGMENT_BYTES);
-                if constexpr (q == 0) sbH = *(lds_int)(uintptr_t)(sb_here + QUARTER_BYTES);
+                fbH[q] = *(lds_v4i)(uintptr_t)(fb_at + QUARTER_BYTES + q * FRAGMENT_BYTES);
                 math(faL, saL, fbL, sbL, N0{}, N0{}, Q, ByB{}, N0{});
                 __builtin_amdgcn_sched_barrier(0);
-                faH[q] = *(lds_v4i)(uintptr_t)(fa_here + QUARTER_BYTES + q * FRAGMENT_BYTES);
-                if constexpr (q == 0) saH = *(lds_int)(uintptr_t)(sa_here + QUARTER_BYTES);
+                if constexpr (q == 0 || q == 2) copy_b(std::integral_constant<int, q / 2>{});
+                if constexpr (q == 1) a.next(KT);
                 math(faL, saL, fbL, sbL, N0{}, N0{}, Q, ByB{}, N2{});
                 __builtin_amdgcn_sched_barrier(0);
             });
-            // quarter 1
+            // quarter 1: the upper half of A, early, so that it is there at the barrier
             static_for<0, 4>([&](auto Q) {
+                constexpr int q = decltype(Q)::value;
+                if constexpr (q < 2) faH[2 * q] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + 2 * q * FRAGMENT_BYTES);
+                if constexpr (q == 2) copy_b(std::integral_constant<int, 3>{});
                 math(faL, saL, fbH, sbH, N0{}, N4{}, Q, ByB{}, N0{});
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (decltype(Q)::value == 1) find_stage();
+                if constexpr (q < 2) faH[2 * q + 1] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + (2 * q + 1) * FRAGMENT_BYTES);
+                if constexpr (q == 1) copy_b(std::integral_constant<int, 2>{});
+                if constexpr (q == 3) copy_b(std::integral_constant<int, 4>{});
                 math(faL, saL, fbH, sbH, N0{}, N4{}, Q, ByB{}, N2{});
                 __builtin_amdgcn_sched_barrier(0);
             });
-            if (fresh > 0) {
-                --fresh;
-                wait_vmcnt<NEWER_STORES>();
-            } else {
-                wait_vmcnt<NEWER>();
-            }
+            // (a branch that the compiler does not see: at one that it sees it gathers the matrix instructions behind it)
+            asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(%1)\n1:\n\ts_waitcnt vmcnt(%2)" ::"s"(fresh), "n"(NEWER),
+                         "n"(NEWER_STORES)
+                         : "memory", "scc");
+            --fresh;
+            to = here;
+            advance(here);
+            fa_at = fragA + here;
+            fb_at = fragB + here;
+            sa_at = scaleA + here;
+            sb_at = scaleB + here;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            const v4i source_a = tile_resource(pa, any), source_b = tile_resource(pb, any);
-            // quarter 2: the lower half of A of the next stage (behind the last one: what the ring holds, unused)
+            // quarter 2: the lower half of A of the next stage (behind the last one: what the ring holds, unused); copies of A
+            int sa_next[2], sb_next[2];
             static_for<0, 4>([&](auto Q) {
                 constexpr int q = decltype(Q)::value;
-                faL[q] = *(lds_v4i)(uintptr_t)(fa_next + q * FRAGMENT_BYTES);
-                if constexpr (q == 0) saL = *(lds_int)(uintptr_t)sa_next;
+                faL[q] = *(lds_v4i)(uintptr_t)(fa_at + q * FRAGMENT_BYTES);
                 math(faH, saH, fbL, sbL, N4{}, N0{}, Q, ByA{}, N0{});
                 __builtin_amdgcn_sched_barrier(0);
-                copy_quarter<q>(m0_wave + to, voff4, voff16, source_a);
+                if constexpr (q == 0 || q == 2) copy_a(std::integral_constant<int, q / 2>{});
+                if constexpr (q == 1) {
+                    sa_next[0] = *(lds_int)(uintptr_t)sa_at;
+                    sa_next[1] = *(lds_int)(uintptr_t)(sa_at + QUARTER_BYTES);
+                }
+                if constexpr (q == 3) {
+                    sb_next[0] = *(lds_int)(uintptr_t)sb_at;
+                    sb_next[1] = *(lds_int)(uintptr_t)(sb_at + QUARTER_BYTES);
+                }
                 math(faH, saH, fbL, sbL, N4{}, N0{}, Q, ByA{}, N2{});
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (q == 3) copy_quarter<4>(m0_wave + to, voff4, voff16, source_a);
             });
             // quarter 3: its lower half of B
             static_for<0, 4>([&](auto Q) {
                 constexpr int q = decltype(Q)::value;
-                fbL[q] = *(lds_v4i)(uintptr_t)(fb_next + q * FRAGMENT_BYTES);
-                if constexpr (q == 0) sbL = *(lds_int)(uintptr_t)sb_next;
+                fbL[q] = *(lds_v4i)(uintptr_t)(fb_at + q * FRAGMENT_BYTES);
                 math(faH, saH, fbH, sbH, N4{}, N4{}, Q, ByA{}, N0{});
                 __builtin_amdgcn_sched_barrier(0);
-                copy_quarter<q>(m0_wave + to + TILE_BYTES, voff4, voff16, source_b);
+                if constexpr (q == 0) b.next(KT);
+                if constexpr (q > 0) copy_a(std::integral_constant<int, 1 + q>{});
                 math(faH, saH, fbH, sbH, N4{}, N4{}, Q, ByA{}, N2{});
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (q == 3) copy_quarter<4>(m0_wave + to + TILE_BYTES, voff4, voff16, source_b);
             });
-            stage_copied();
+            saL = sa_next[0];
+            saH = sa_next[1];
+            sbL = sb_next[0];
+            sbH = sb_next[1];
         }
         // (left alone, the register allocator parks accumulators in scratch memory and copies all of them at once; so they are read by
         // asm statements below, and the wait states behind the last matrix instruction are written out)
@@ -352,32 +408,42 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
         const uint32_t off = ((uint32_t)row_lane * (uint32_t)g.ldd + (uint32_t)col_lane) * (uint32_t)sizeof(Bits);
         const int64_t row0 = (int64_t)tm * TILE_R + wm * 128, col0 = (int64_t)tp * TILE_R + wn * 128;
         const int rows_left = (int)(g.m - row0 < 128 ? g.m - row0 : 128) - row_lane, cols_left = (int)(g.p - col0 < 128 ? g.p - col0 : 128) - col_lane;
-        auto put = [&](auto WHOLE, auto BETA) {
-            constexpr bool whole = decltype(WHOLE)::value;
+        // eight sums at a time: v, the row (of the wave's 128, but for the lane's part) and the column
+        auto each = [&](auto&& f) {
             static_for<0, 8>([&](auto I) {
                 constexpr int i = decltype(I)::value, ri = i / 4 * 64 + row_of(i % 4, 0);
                 uint64_t base = (uint64_t)(uintptr_t)((Bits*)g.D + (row0 + ri) * g.ldd + col0);
                 asm volatile("" : "+s"(base));
-                if (whole || ri < rows_left) {
-                    static_for<0, 4>([&](auto J) {
-                        constexpr int j = 2 * decltype(J)::value, cj = j / 4 * 64 + row_of(j % 4, 0);
-                        float v[8];
+                static_for<0, 4>([&](auto J) {
+                    constexpr int j = 2 * decltype(J)::value, cj = j / 4 * 64 + row_of(j % 4, 0);
+                    float v[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][j + e / 4][e % 4]));
-                        put8<TYPE, whole, decltype(BETA)::value>((Global*)(base + off) + cj, cols_left - cj, g.alpha, g.beta, v);
-                        __builtin_amdgcn_sched_barrier(0);
-                    });
-                }
+                    for (int e = 0; e < 8; ++e) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][j + e / 4][e % 4]));
+                    f(base, std::integral_constant<int, ri>{}, std::integral_constant<int, cj>{}, v);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+        };
+        auto whole = [&](auto STREAM) {
+            each([&](uint64_t base, auto, auto CJ, const float* v) { put8_whole<TYPE, decltype(STREAM)::value, decltype(CJ)::value>(base, off, g.alpha, v); });
+        };
+        auto edge = [&](auto BETA) {
+            each([&](uint64_t base, auto RI, auto CJ, const float* v) {
+                constexpr int ri = decltype(RI)::value, cj = decltype(CJ)::value;
+                put8<TYPE, decltype(BETA)::value>((Global*)(base + off) + cj, ri < rows_left ? cols_left - cj : 0, g.alpha, g.beta, v);
             });
         };
         fresh = 0;
         if (g.beta != 0.0f) {
-            put(std::false_type{}, std::true_type{});
-        } else if ((int64_t)(tm + 1) * TILE_R <= g.m && (int64_t)(tp + 1) * TILE_R <= g.p) {
-            put(std::true_type{}, std::false_type{});
-            fresh = 2;
+            edge(std::true_type{});
+        } else if ((int64_t)(tm + 1) * TILE_R > g.m || (int64_t)(tp + 1) * TILE_R > g.p) {
+            edge(std::false_type{});
         } else {
-            put(std::false_type{}, std::false_type{});
+            if (stream)
+                whole(std::true_type{});
+            else
+                whole(std::false_type{});
+            fresh = 2;
         }
     }
     wait_vmcnt<0>();  // no copy may still be writing LDS when the workgroup retires
@@ -386,7 +452,9 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
 template <int TYPE> void tile(const Gemm& g, hipStream_t st)
 {
     const int TM = (int)row_tiles(g.m), TP = (int)row_tiles(g.p);
-    hipLaunchKernelGGL(k_mx_tile<TYPE>, dim3((unsigned)(TM * TP < 256 ? TM * TP : 256)), dim3(256), 0, st, g, (int)inner_tiles(g.n), TM, TP);
+    const int64_t moved = packed_bytes(g.m, g.n) + packed_bytes(g.p, g.n) + g.m * g.p * (int64_t)sizeof(typename Elem<TYPE>::Bits);
+    hipLaunchKernelGGL(k_mx_tile<TYPE>, dim3((unsigned)(TM * TP < 256 ? TM * TP : 256)), dim3(256), 0, st, g, (int)inner_tiles(g.n), TM, TP,
+                       moved > MEMORY_SIDE_CACHE);
 }
 
 template <int TYPE> void product(const Gemm& g, int way, hipStream_t st)
@@ -404,7 +472,7 @@ namespace mxk {
 // (32-bit offsets of a lane inside 28 rows of D, and 32-bit numbers of tiles)
 bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd)
 {
-    if (way == WAY_TILE) return n > 0 && ldd < (1 << 24) && row_tiles(m) * row_tiles(p) < ((int64_t)1 << 30);
+    if (way == WAY_TILE) return inner_tiles(n) >= RING && ldd < (1 << 24) && row_tiles(m) * row_tiles(p) < ((int64_t)1 << 30);
     return way == WAY_DIRECT;
 }
 

@@ -37,6 +37,10 @@ def test_way(mx, way, m, n, p):
     want, size = product(qa, qb)
     bound = max(n, 1) * 2.0 ** -23 * size
     (PA, _), (PB, _) = mx.quantize(A), mx.quantize(B)
+    if way == "tile" and n <= 384:     # (its ring has four places: it is for inner dimensions that fill them)
+        with pytest.raises(Exception, match="this way"):
+            mx.gemm(PA, PB, way=way)
+        return
     for kind, t in TYPES.items():
         check(mx.gemm(PA, PB, t, way=way), want, bound, kind, n, kind)
         big = torch.full((m + 1, p + 3), 5.0, dtype=t, device="cuda")
