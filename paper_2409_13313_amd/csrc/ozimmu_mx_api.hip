@@ -8,6 +8,7 @@ namespace {
 
 // rows <= 2^22 - 256: every grid dimension stays within the HIP limits (64 rows a workgroup along y)
 constexpr int64_t MAX_ROWS = ((int64_t)1 << 22) - 256;
+constexpr int64_t MAX_BLOCKS = (int64_t)1 << 24;  // workgroups of 256 threads in one dimension (128 x 128 elements each: more than fit memory)
 constexpr int64_t MAX_INNER = (int64_t)1 << 29;
 constexpr int64_t MAX_LD = ((int64_t)1 << 40) - 1;  // products of a row number and a leading dimension stay within 64 bits
 
@@ -57,7 +58,7 @@ size_t ozimmu_mx_bytes(int64_t rows, int64_t n) { return sizes_ok(rows, n) ? (si
 int ozimmu_mx_quantize(int type, int64_t rows, int64_t n, const void* X, int64_t ldx, void* by_row, void* by_col, void* stream)
 {
     if (by_row && !sizes_ok(rows, n)) return OZIMMU_ERR_DIM;
-    if (by_col && !sizes_ok(n, rows)) return OZIMMU_ERR_DIM;
+    if (by_col && (!sizes_ok(n, rows) || mxl::inner_tiles(rows) * mxl::inner_tiles(n) >= MAX_BLOCKS)) return OZIMMU_ERR_DIM;
     if (rows < 0 || n < 0) return OZIMMU_ERR_DIM;
     CHECK(matrix_status(type, X, rows, n, ldx));
     if (rows == 0 || n == 0) return OZIMMU_OK;

@@ -15,12 +15,32 @@ template <> struct Elem<F32> { typedef uint32_t Bits; };
 template <> struct Elem<BF16> { typedef uint16_t Bits; };
 template <> struct Elem<F16> { typedef uint16_t Bits; };
 
-// magnitude of an element as the bits of its FP32 value (order of magnitudes = order of these integers; NaN above infinity)
-template <int TYPE> __device__ inline uint32_t magnitude(typename Elem<TYPE>::Bits x)
+// Largest magnitude of N elements (N even) as an integer: magnitudes are ordered as their bits are, NaN above infinity.
+// (16-bit types: two at a time.)  f32_bits() makes such an integer the bits of the FP32 value.
+typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
+template <int TYPE, int N> __device__ inline uint32_t max_magnitude(const typename Elem<TYPE>::Bits* x)
 {
-    if constexpr (TYPE == F32) return x & 0x7fffffffu;
-    if constexpr (TYPE == BF16) return (uint32_t)(x & 0x7fffu) << 16;
-    if constexpr (TYPE == F16) return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)(x & 0x7fffu)));
+    if constexpr (TYPE == F32) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t a = x[i] & 0x7fffffffu;
+            m = a > m ? a : m;
+        }
+        return m;
+    } else {
+        v2u16 m = {0, 0};
+#pragma unroll
+        for (int i = 0; i < N; i += 2)
+            m = __builtin_elementwise_max(m, __builtin_bit_cast(v2u16, ((uint32_t)x[i] | (uint32_t)x[i + 1] << 16) & 0x7fff7fffu));
+        return m[0] > m[1] ? m[0] : m[1];
+    }
+}
+template <int TYPE> __device__ inline uint32_t f32_bits(uint32_t magnitude)
+{
+    if constexpr (TYPE == F32) return magnitude;
+    if constexpr (TYPE == BF16) return magnitude << 16;
+    if constexpr (TYPE == F16) return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)magnitude));
 }
 
 // scale byte of a block whose largest magnitude has these bits: floor(log2) - 2, biased, at least 0; 255 for infinities and NaN
@@ -60,14 +80,38 @@ template <int TYPE> __device__ inline uint32_t codes8(const typename Elem<TYPE>:
     return r;
 }
 
-// FP32 value of a code: exact; the product with a scale is exact too, or the infinity or NaN that it stands for
-__device__ inline float code_value(uint32_t code)
+// 8 codes -> 8 elements, rounded where the type cannot hold code times scale.  The conversion instruction multiplies by the power of two
+// whose exponent bits the scale has; a NaN is put in here.
+template <int TYPE> __device__ inline void values8(uint32_t codes, uint32_t b, typename Elem<TYPE>::Bits* x)
 {
-    const uint32_t m = code & 7u;  // 0, 0.5, 1, 1.5, 2, 3, 4, 6: exponent and mantissa as in FP32 but for 0.5
-    const uint32_t bits = m < 2u ? m * 0x3f000000u : ((m + 252u) << 22);
-    return __uint_as_float(bits | (code & 8u) << 28);
+    const float s = scale_value(b);
+    if constexpr (TYPE == F32) {
+        typedef float v2f __attribute__((ext_vector_type(2)));
+        const v2f v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1),
+                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 3)};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = b == 255u ? 0x7fc00000u : __float_as_uint(v[e / 2][e % 2]);
+    } else {
+        uint32_t w[4];
+        if constexpr (TYPE == BF16) {
+            w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0));
+            w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1));
+            w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2));
+            w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3));
+        } else {
+            w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 0));
+            w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 1));
+            w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 2));
+            w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, 3));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = b == 255u ? (TYPE == BF16 ? 0x7fc07fc0u : 0x7e007e00u) : w[i];
+            x[2 * i] = (uint16_t)w[i];
+            x[2 * i + 1] = (uint16_t)(w[i] >> 16);
+        }
+    }
 }
-__device__ inline float scale_of(uint32_t b) { return b == 255u ? __uint_as_float(0x7fc00000u) : scale_value(b); }
 
 // FP32 -> element, one rounding (nearest even)
 template <int TYPE> __device__ inline typename Elem<TYPE>::Bits from_float(float v)

@@ -12,84 +12,92 @@ using namespace mxl;
 // Blocks along the rows.  A workgroup takes 64 rows x 128 columns (a quarter of a tile): thread t the eight elements t % 16 of
 // the four rows at place t / 16 of the fragments, so that 16 lanes read 128 columns of a row side by side; four lanes hold a block and
 // share its maximum.
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_mx_quantize_rows(int64_t rows, int64_t n, const typename Elem<TYPE>::Bits* X, int64_t ldx,
-                                                          uint8_t* out, int64_t KT)
+template <int TYPE> __device__ inline void quantize_rows(const typename Elem<TYPE>::Bits (&x)[4][8], int64_t row0, int64_t rows, uint8_t* tile, int chunk)
 {
-    typedef typename Elem<TYPE>::Bits Bits;
-    const int t = threadIdx.x, chunk = t & 15, c = chunk >> 2, sub = chunk & 3;
-    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + row_of(0, t >> 4);
-    const int64_t col = kt * TILE_K + chunk * 8;
-    Bits x[4][8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + row_of(i, 0);
-        load_row<TYPE, 8>(X + row * ldx + col, row < rows ? n - col : 0, x[i]);
-    }
-    uint8_t* const tile = out + ((row0 / TILE_R) * KT + kt) * TILE_BYTES;
+    const int c = chunk >> 2, sub = chunk & 3;
     uint32_t scales = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t amax = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t m = magnitude<TYPE>(x[i][e]);
-            amax = m > amax ? m : amax;
-        }
+        uint32_t amax = max_magnitude<TYPE, 8>(x[i]);
 #pragma unroll
         for (int d = 1; d < 4; d *= 2) {
             const uint32_t o = (uint32_t)__shfl_xor((int)amax, d);
             amax = o > amax ? o : amax;
         }
-        const uint32_t b = scale_byte(amax);
+        const uint32_t b = scale_byte(f32_bits<TYPE>(amax));
         scales |= b << (8 * i);
         const int64_t row = row0 + row_of(i, 0);
-        if (row < rows) {
-            const uint32_t codes = codes8<TYPE>(x[i], scale_value(b));
-            *(uint32_t*)(tile + code_offset((int)(row % TILE_R), c) + 4 * sub) = codes;
-        }
+        if (row < rows) *(uint32_t*)(tile + code_offset((int)(row % TILE_R), c) + 4 * sub) = codes8<TYPE>(x[i], scale_value(b));
     }
     // (the scales of rows that are not there are those of zeros)
     if (sub == 0 && row0 < rows) *(uint32_t*)(tile + scale_offset((int)(row0 % TILE_R), c)) = scales;
 }
 
-// Blocks along the columns: row j of the packed matrix is column j of X.  A wave takes 64 columns x 128 rows: lane l the 4 columns
-// l % 16 of block l / 16, whose 32 rows it reads one after the other (16 lanes side by side), so that a block is one lane's.
 template <int TYPE>
-__global__ __launch_bounds__(256) void k_mx_quantize_cols(int64_t rows, int64_t n, const typename Elem<TYPE>::Bits* X, int64_t ldx,
+__global__ __launch_bounds__(256) void k_mx_quantize_rows(int64_t rows, int64_t n, const typename Elem<TYPE>::Bits* X, int64_t ldx,
                                                           uint8_t* out, int64_t KT)
 {
+    typename Elem<TYPE>::Bits x[4][8];
+    const int t = threadIdx.x, chunk = t & 15;
+    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + row_of(0, t >> 4), col = kt * TILE_K + chunk * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + row_of(i, 0);
+        load_row<TYPE, 8>(X + row * ldx + col, row < rows ? n - col : 0, x[i]);
+    }
+    quantize_rows<TYPE>(x, row0, rows, out + ((row0 / TILE_R) * KT + kt) * TILE_BYTES, chunk);
+}
+
+// Blocks along the columns, and along the rows too where by_row is given.  A workgroup takes 128 rows x 128 columns, read as above (rows
+// quantised on the way) and left in LDS as they are; then wave w takes block w of all columns, lane l columns 2 l and 2 l + 1: it reads
+// their 32 rows one after the other, 64 lanes a row side by side, so that a block is one lane's.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_mx_quantize_cols(int64_t rows, int64_t n, const typename Elem<TYPE>::Bits* X, int64_t ldx,
+                                                          uint8_t* by_row, uint8_t* by_col, int64_t KT_row, int64_t KT_col)
+{
     typedef typename Elem<TYPE>::Bits Bits;
-    const int t = threadIdx.x, lane = t & 63, c = lane >> 4;
-    const int64_t kt = blockIdx.x, col = (int64_t)blockIdx.y * 256 + (t >> 6) * 64 + (lane & 15) * 4;
-    const int64_t row0 = kt * TILE_K + c * BLOCK;
-    Bits x[BLOCK][4];
+    __shared__ __align__(16) Bits held[128 * 128];
+    const int t = threadIdx.x, chunk = t & 15;
+    // (one number for both: there may be more row tiles than a grid has in its second dimension)
+    const uint32_t tiles = (uint32_t)((n + 127) / 128), tile_col = blockIdx.x % tiles, tile_row = blockIdx.x / tiles;
+    const int64_t col0 = (int64_t)tile_col * 128, first = (int64_t)tile_row * 128;
+    Bits x[2][4][8];
 #pragma unroll
-    for (int r = 0; r < BLOCK; ++r)
-        load_row<TYPE, 4>(X + (row0 + r) * ldx + col, row0 + r < rows ? n - col : 0, x[r]);
-    uint8_t* const tile = out + ((int64_t)blockIdx.y * KT + kt) * TILE_BYTES;
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t amax = 0;
-#pragma unroll
-        for (int r = 0; r < BLOCK; ++r) {
-            const uint32_t m = magnitude<TYPE>(x[r][j]);
-            amax = m > amax ? m : amax;
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = first + h * 64 + row_of(i, t >> 4);
+            load_row<TYPE, 8>(X + row * ldx + col0 + chunk * 8, row < rows ? n - col0 - chunk * 8 : 0, x[h][i]);
         }
-        const uint32_t b = scale_byte(amax);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) __builtin_memcpy(held + (h * 64 + row_of(i, t >> 4)) * 128 + chunk * 8, x[h][i], 8 * sizeof(Bits));
+        const int64_t row0 = first + h * 64 + row_of(0, t >> 4);
+        if (by_row) quantize_rows<TYPE>(x[h], row0, rows, by_row + ((row0 / TILE_R) * KT_row + tile_col) * TILE_BYTES, chunk);
+    }
+    __syncthreads();
+    const int c = t >> 6, lane = t & 63;
+    Bits y[2][BLOCK];
+#pragma unroll
+    for (int r = 0; r < BLOCK; ++r) {
+        Bits pair[2];
+        __builtin_memcpy(pair, held + (c * BLOCK + r) * 128 + 2 * lane, sizeof(pair));
+        y[0][r] = pair[0];
+        y[1][r] = pair[1];
+    }
+    uint8_t* const tile = by_col + ((col0 / TILE_R) * KT_col + tile_row) * TILE_BYTES;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t b = scale_byte(f32_bits<TYPE>(max_magnitude<TYPE, BLOCK>(y[j])));
         const float s = scale_value(b);
-        uint32_t codes[4];
+        v4i codes;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            Bits y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = x[8 * q + e][j];
-            codes[q] = codes8<TYPE>(y, s);
-        }
-        if (col + j < n) {
-            const int r = (int)((col + j) % TILE_R);
-            *(v4i*)(tile + code_offset(r, c)) = v4i{(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3]};
-            tile[scale_offset(r, c)] = (uint8_t)b;
+        for (int q = 0; q < 4; ++q) codes[q] = (int)codes8<TYPE>(y[j] + 8 * q, s);
+        const int64_t col = col0 + 2 * lane + j;
+        if (col < n) {
+            *(v4i*)(tile + code_offset((int)(col % TILE_R), c)) = codes;
+            tile[scale_offset((int)(col % TILE_R), c)] = (uint8_t)b;
         }
     }
 }
@@ -113,10 +121,8 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t n, 
     for (int i = 0; i < 4; ++i) {
         const int64_t row = row0 + row_of(i, 0);
         if (row >= rows) break;
-        const float s = scale_of((scales >> (8 * i)) & 255u);
         Bits x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(code_value((codes[i] >> (4 * e)) & 15u) * s);
+        values8<TYPE>(codes[i], (scales >> (8 * i)) & 255u, x);
         store_row<TYPE, 8>(X + row * ldx + col, n - col, x);
     }
 }
@@ -162,12 +168,12 @@ template <int TYPE>
 void quantize(int64_t rows, int64_t n, const void* X, int64_t ldx, void* by_row, void* by_col, hipStream_t st)
 {
     typedef typename Elem<TYPE>::Bits Bits;
-    if (by_row)
+    if (by_col)
+        hipLaunchKernelGGL(k_mx_quantize_cols<TYPE>, dim3((unsigned)(inner_tiles(n) * inner_tiles(rows))), dim3(256), 0, st, rows, n,
+                           (const Bits*)X, ldx, (uint8_t*)by_row, (uint8_t*)by_col, inner_tiles(n), inner_tiles(rows));
+    else
         hipLaunchKernelGGL(k_mx_quantize_rows<TYPE>, dim3((unsigned)inner_tiles(n), (unsigned)((rows + 63) / 64)), dim3(256), 0, st,
                            rows, n, (const Bits*)X, ldx, (uint8_t*)by_row, inner_tiles(n));
-    if (by_col)
-        hipLaunchKernelGGL(k_mx_quantize_cols<TYPE>, dim3((unsigned)inner_tiles(rows), (unsigned)row_tiles(n)), dim3(256), 0, st,
-                           rows, n, (const Bits*)X, ldx, (uint8_t*)by_col, inner_tiles(rows));
 }
 
 template <int TYPE> void dequantize(int64_t rows, int64_t n, const void* packed, void* X, int64_t ldx, hipStream_t st)

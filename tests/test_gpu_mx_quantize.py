@@ -140,6 +140,18 @@ def test_plain_layout(mx):
         assert np.array_equal(mx.dequantize(P).cpu().numpy(), values, equal_nan=True)
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_every_code_with_every_scale(mx, kind):
+    """Values that the type cannot hold are rounded once, to infinity and to subnormal numbers too."""
+    codes = np.tile(np.arange(32, dtype=np.uint8) % 16, (256, 1))
+    scales = np.arange(256, dtype=np.uint8).reshape(256, 1)
+    P = mx.pack(torch.from_numpy(ref.bytes_of(codes)).cuda(), torch.from_numpy(scales).cuda())
+    want = torch.from_numpy(ref.values(codes, scales, 32)).to(TYPES[kind])
+    got = mx.dequantize(P, TYPES[kind]).cpu()
+    fine = ~torch.isnan(want)
+    assert torch.equal(torch.isnan(got), ~fine) and torch.equal(got[fine], want[fine])
+
+
 def test_rows_far_behind_2_32_bytes(mx):
     """A view whose last row begins behind 4 GiB."""
     ld = (1 << 31) + 8
