@@ -54,7 +54,7 @@ hipError_t launch_pack(int64_t rows, int64_t n, const uint8_t* codes, int64_t ld
 hipError_t launch_unpack(int64_t rows, int64_t n, const void* packed, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
                          hipStream_t st);
 
-// D <- alpha A B^T + beta D; with X (of xtype, m x n, ldx) in the place of A: quantised on the way
+// D <- alpha A B^T + beta D
 struct Gemm {
     int64_t m, n, p;
     const uint8_t* A;
@@ -69,5 +69,8 @@ enum { WAY_AUTO = -1, WAY_DIRECT = 0, WAY_TILE = 1, WAYS = 2 };
 int choose(int64_t m, int64_t n, int64_t p, int64_t ldd);
 bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd);
 hipError_t launch_gemm(const Gemm& g, int way, hipStream_t st);
+// D <- alpha Q(X) B^T + beta D in one launch (g.A is not looked at); few_rows(m): the rows that this is for
+bool few_rows(int64_t m);
+hipError_t launch_few(const Gemm& g, int xtype, const void* X, int64_t ldx, hipStream_t st);
 
 }  // namespace mxk

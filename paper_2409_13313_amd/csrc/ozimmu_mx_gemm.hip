@@ -470,6 +470,116 @@ template <int TYPE> void tile(const Gemm& g, hipStream_t st)
                        moved > MEMORY_SIDE_CACHE);
 }
 
+// ---- few rows of X, quantised on the way: 16 rows and FB fragments of W's (16 columns each) by a workgroup ----
+//
+// The time of such a call is that of reading W once and of its launches, so this is one launch: eight waves share the inner tiles, each
+// takes its fragments of W straight from memory into registers, four tiles at a time, and quantises the blocks of X that meet them - a lane
+// holds a block as the matrix instruction wants it, so that its scale takes no exchange between lanes.  The waves' sums meet in LDS.
+// Every workgroup quantises all of X: FB is as large as leaves a workgroup for every compute unit.
+constexpr int FEW_ROWS = 16, FEW_WAVES = 8, FEW_TILES = 4;
+
+template <int XTYPE, int FB> __global__ __launch_bounds__(64 * FEW_WAVES) void k_mx_few(Gemm g, const typename Elem<XTYPE>::Bits* X, int64_t ldx, int64_t KT)
+{
+    typedef typename Elem<XTYPE>::Bits Bits;
+    __shared__ __align__(16) v4f sums[FEW_WAVES][FB][64];
+    const int t = threadIdx.x, lane = t & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int64_t row0 = (int64_t)blockIdx.y * FEW_ROWS, col0 = (int64_t)blockIdx.x / (4 / FB) * QUARTER_R;
+    const int f0 = (int)(blockIdx.x % (4 / FB)) * FB;  // first of the workgroup's fragments of the quarter
+    const uint8_t* const W = g.B + col0 / TILE_R * KT * TILE_BYTES + col0 % TILE_R / QUARTER_R * QUARTER_BYTES;
+    const int64_t row = row0 + (lane & 15);
+    const Bits* const x_lane = X + row * ldx + (lane >> 4) * BLOCK;
+    // elements of the row from the lane's block of tile 0 on
+    const int64_t here = row < g.m ? g.n - (lane >> 4) * BLOCK : 0;
+
+    v4f acc[FB];
+#pragma unroll
+    for (int f = 0; f < FB; ++f) acc[f] = v4f{0, 0, 0, 0};
+    auto block = [&](const Bits* x, v4i& codes) -> int {
+        const uint32_t b = scale_byte(f32_bits<XTYPE>(max_magnitude<XTYPE, BLOCK>(x)));
+        const float s = scale_value(b);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) codes[q] = (int)codes8<XTYPE>(x + 8 * q, s);
+        return (int)b;
+    };
+    auto multiply = [&](const v4i* w, int sw, v4i x, int sx) {
+        sw >>= 8 * f0;
+        static_for<0, FB>([&](auto F) { acc[decltype(F)::value] = mfma<decltype(F)::value, 0>(w[decltype(F)::value], sw, x, sx, acc[decltype(F)::value]); });
+    };
+    for (int64_t kt0 = wave; kt0 < KT; kt0 += FEW_WAVES * FEW_TILES) {
+        v4i w[FEW_TILES][FB];
+        int sw[FEW_TILES];
+        Bits x[FEW_TILES][BLOCK];
+#pragma unroll
+        for (int u = 0; u < FEW_TILES; ++u) {
+            // (a tile behind the last one: the last one again, with zeros for X)
+            const int64_t kt = kt0 + u * FEW_WAVES, at = kt < KT ? kt : KT - 1;
+            const uint8_t* const tile = W + at * TILE_BYTES;
+#pragma unroll
+            for (int f = 0; f < FB; ++f) w[u][f] = *(const v4i*)(tile + SCALE_BYTES + (f0 + f) * FRAGMENT_BYTES + lane * 16);
+            sw[u] = *(const int*)(tile + lane * 4);
+            if (kt < KT && here - kt * TILE_K >= BLOCK) {
+                __builtin_memcpy(x[u], x_lane + kt * TILE_K, sizeof(x[u]));
+            } else {
+#pragma unroll
+                for (int e = 0; e < BLOCK; ++e) x[u][e] = 0;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < FEW_TILES; ++u) {
+            v4i codes;
+            const int sx = block(x[u], codes);
+            multiply(w[u], sw[u], codes, sx);
+        }
+    }
+    // the block that a row ends in, where it is not a whole one: zeros for the others
+    if (g.n % BLOCK != 0 && wave == (int)((KT - 1) % FEW_WAVES)) {
+        const uint8_t* const tile = W + (KT - 1) * TILE_BYTES;
+        const int64_t left = here - (KT - 1) * TILE_K;
+        v4i w[FB], codes;
+        Bits x[BLOCK];
+#pragma unroll
+        for (int f = 0; f < FB; ++f) w[f] = *(const v4i*)(tile + SCALE_BYTES + (f0 + f) * FRAGMENT_BYTES + lane * 16);
+        const int sw = *(const int*)(tile + lane * 4);
+#pragma unroll
+        for (int e = 0; e < BLOCK; ++e) x[e] = left < BLOCK && e < left ? x_lane[(KT - 1) * TILE_K + e] : 0;
+        const int sx = block(x, codes);
+        multiply(w, sw, codes, sx);
+    }
+#pragma unroll
+    for (int f = 0; f < FB; ++f) sums[wave][f][lane] = acc[f];
+    __syncthreads();
+    // lane l of fragment f: columns at places 4 (l / 16) .. + 3 for row l % 16
+    if (t < FB * 64) {
+        const int f = t >> 6;
+        v4f s = sums[0][f][lane];
+#pragma unroll
+        for (int w = 1; w < FEW_WAVES; ++w) s += sums[w][f][lane];
+        const float v[4] = {s[0], s[1], s[2], s[3]};
+        const int64_t col = col0 + row_of(f0 + f, lane >> 4 << 2);
+        if (g.dtype == F32) finish<F32, 4>(g, row, col, v);
+        if (g.dtype == BF16) finish<BF16, 4>(g, row, col, v);
+        if (g.dtype == F16) finish<F16, 4>(g, row, col, v);
+    }
+}
+
+template <int XTYPE, int FB> void few(const Gemm& g, const void* X, int64_t ldx, hipStream_t st)
+{
+    const dim3 grid((unsigned)((g.p + QUARTER_R - 1) / QUARTER_R * (4 / FB)), (unsigned)((g.m + FEW_ROWS - 1) / FEW_ROWS));
+    k_mx_few<XTYPE, FB><<<grid, dim3(64 * FEW_WAVES), 0, st>>>(g, (const typename Elem<XTYPE>::Bits*)X, ldx, inner_tiles(g.n));
+}
+
+template <int XTYPE> void few(const Gemm& g, const void* X, int64_t ldx, hipStream_t st)
+{
+    const int64_t quarters = (g.p + QUARTER_R - 1) / QUARTER_R * ((g.m + FEW_ROWS - 1) / FEW_ROWS);
+    if (quarters >= 256)
+        few<XTYPE, 4>(g, X, ldx, st);
+    else if (quarters >= 128)
+        few<XTYPE, 2>(g, X, ldx, st);
+    else
+        few<XTYPE, 1>(g, X, ldx, st);
+}
+
 template <int TYPE> void product(const Gemm& g, int way, hipStream_t st)
 {
     if (way == WAY_TILE)
@@ -492,6 +602,16 @@ bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd)
 int choose(int64_t m, int64_t n, int64_t p, int64_t ldd)
 {
     return way_fits(WAY_TILE, m, n, p, ldd) && row_tiles(m) * row_tiles(p) >= 128 ? WAY_TILE : WAY_DIRECT;
+}
+
+bool few_rows(int64_t m) { return m <= FEW_ROWS; }
+
+hipError_t launch_few(const Gemm& g, int xtype, const void* X, int64_t ldx, hipStream_t st)
+{
+    if (xtype == F32) few<F32>(g, X, ldx, st);
+    if (xtype == BF16) few<BF16>(g, X, ldx, st);
+    if (xtype == F16) few<F16>(g, X, ldx, st);
+    return hipGetLastError();
 }
 
 hipError_t launch_gemm(const Gemm& g, int way, hipStream_t st)

@@ -113,6 +113,10 @@ def alloc_workspace(m: int, n: int, p: int, device="cuda", backward: bool = Fals
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
+def _room(workspace: Optional[torch.Tensor]):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+
+
 def _empty(rows: int, n: int, device) -> Packed:
     return Packed(torch.empty(packed_bytes(rows, n), dtype=torch.uint8, device=device), rows, n)
 
@@ -181,10 +185,8 @@ def gemm(A: Packed, B: Packed, dtype=torch.float32, alpha: float = 1.0, beta: fl
     m, n, p = A.rows, A.n, B.rows
     D = _output(D, A.data, m, p, dtype, beta)
     _, _, ldd, kind = _matrix(D)
-    if workspace is None:
-        workspace = alloc_workspace(m, n, p, D.device)
     _check(_lib.ozimmu_mx_gemm_way(WAYS[way], m, n, p, alpha, A.data.data_ptr(), B.data.data_ptr(), beta, kind, D.data_ptr(), ldd,
-                                   workspace.data_ptr(), workspace.numel(), ozimmu._stream()))
+                                   None, 0, ozimmu._stream()))
     return D
 
 
@@ -198,10 +200,10 @@ def linear(X: torch.Tensor, W: Packed, dtype=None, alpha: float = 1.0, beta: flo
     p = W.rows
     D = _output(D, X, m, p, dtype or X.dtype, beta)
     _, _, ldd, dkind = _matrix(D)
-    if workspace is None:
+    if workspace is None and workspace_bytes(m, n, p):
         workspace = alloc_workspace(m, n, p, X.device)
     _check(_lib.ozimmu_mx_linear(m, n, p, alpha, xkind, X.data_ptr(), ldx, W.data.data_ptr(), beta, dkind, D.data_ptr(), ldd,
-                                 workspace.data_ptr(), workspace.numel(), ozimmu._stream()))
+                                 *_room(workspace), ozimmu._stream()))
     return D
 
 
