@@ -66,8 +66,9 @@ int ozimmu_mx_gemm(int64_t m, int64_t n, int64_t p, float alpha, const void *A, 
 /* The same, run in a given way instead of the library's choice (OZIMMU_ERR_WAY where it cannot run so); and that choice.  Debug / test
  * helpers; the second one is host, pure. */
 enum { OZIMMU_MX_WAY_AUTO = -1,
-       OZIMMU_MX_WAY_DIRECT = 0,    /* 64 x 64 outputs a workgroup, operands from memory into registers */
-       OZIMMU_MX_WAY_TILE = 1 };    /* 256 x 256 outputs a workgroup at a time, operands through LDS */
+       OZIMMU_MX_WAY_DIRECT = 0,    /* 64 rows and 16 to 64 columns a workgroup, operands from memory into registers */
+       OZIMMU_MX_WAY_TILE = 1,      /* 256 x 256 outputs a workgroup at a time, operands through LDS; inner dimensions above 384 */
+       OZIMMU_MX_WAY_HALF = 2 };    /* 256 x 128; inner dimensions above 640 */
 int ozimmu_mx_gemm_way(int way, int64_t m, int64_t n, int64_t p, float alpha, const void *A, const void *B, float beta, int type,
                        void *D, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);
 int ozimmu_mx_choose(int64_t m, int64_t n, int64_t p, int64_t ldd);

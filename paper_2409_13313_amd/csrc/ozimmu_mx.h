@@ -65,12 +65,12 @@ struct Gemm {
     float alpha, beta;
 };
 // How a product is run (OZIMMU_MX_WAY_*); WAY_AUTO: choose() says
-enum { WAY_AUTO = -1, WAY_DIRECT = 0, WAY_TILE = 1, WAYS = 2 };
+enum { WAY_AUTO = -1, WAY_DIRECT = 0, WAY_TILE = 1, WAY_HALF = 2 };
 int choose(int64_t m, int64_t n, int64_t p, int64_t ldd);
 bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd);
 hipError_t launch_gemm(const Gemm& g, int way, hipStream_t st);
-// D <- alpha Q(X) B^T + beta D in one launch (g.A is not looked at); few_rows(m): the rows that this is for
-bool few_rows(int64_t m);
+// D <- alpha Q(X) B^T + beta D in one launch (g.A is not looked at); few_rows(m, p): what this is for
+bool few_rows(int64_t m, int64_t p);
 hipError_t launch_few(const Gemm& g, int xtype, const void* X, int64_t ldx, hipStream_t st);
 
 }  // namespace mxk

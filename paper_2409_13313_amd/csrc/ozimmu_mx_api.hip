@@ -104,7 +104,7 @@ int ozimmu_mx_unpack(int64_t rows, int64_t n, const void* packed, uint8_t* codes
 // workspace of a product whose A is quantised in the call: A packed, then what the product itself needs
 size_t ozimmu_mx_workspace_bytes(int64_t m, int64_t n, int64_t p)
 {
-    if (!sizes_ok(m, n) || !sizes_ok(p, n) || mxk::few_rows(m)) return 0;
+    if (!sizes_ok(m, n) || !sizes_ok(p, n) || mxk::few_rows(m, p)) return 0;
     return round256((size_t)mxl::packed_bytes(m, n));
 }
 
@@ -149,7 +149,7 @@ int ozimmu_mx_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, co
     CHECK(workspace_status(workspace, workspace_bytes, ozimmu_mx_workspace_bytes(m, n, p)));
     const hipStream_t st = (hipStream_t)stream;
     const mxk::Gemm g = {m, n, p, (const uint8_t*)workspace, (const uint8_t*)W, D, ldd, dtype, alpha, beta};
-    if (mxk::few_rows(m)) return launched(mxk::launch_few(g, xtype, X, ldx, st));
+    if (mxk::few_rows(m, p)) return launched(mxk::launch_few(g, xtype, X, ldx, st));
     if (n > 0) CHECK(launched(mxk::launch_quantize(xtype, m, n, X, ldx, workspace, nullptr, st)));
     return launched(mxk::launch_gemm(g, mxk::WAY_AUTO, st));
 }

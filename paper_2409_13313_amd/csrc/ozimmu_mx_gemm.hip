@@ -18,6 +18,8 @@ template <int SEL_B, int SEL_A> __device__ inline v4f mfma(v4i b, int sb, v4i a,
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(b), operand(a), acc, 4, 4, SEL_B, sb, SEL_A, sa);
 }
 
+constexpr int64_t COMPUTE_UNITS = 256;
+
 // v: N sums of one row, from column col on, into D
 template <int TYPE, int N> __device__ inline void finish(const Gemm& g, int64_t row, int64_t col, const float* v)
 {
@@ -45,59 +47,118 @@ template <int I, int N, class F> __device__ inline void static_for(F&& f)
     }
 }
 
-// 64 x 64 outputs by four waves, each a quarter of the inner tiles straight from memory into registers; their sums meet in LDS.
-template <int TYPE> __global__ __launch_bounds__(256) void k_mx_direct(Gemm g, int64_t KT)
+// v: N sums of one row in FP32, into D of whatever type
+template <int N> __device__ inline void finish_any(const Gemm& g, int64_t row, int64_t col, const float* v)
 {
-    constexpr int PITCH = 64 + 4;  // floats between the rows of a wave's sums: rows fall on different banks
-    __shared__ __align__(16) float sums[4 * 64 * PITCH];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int64_t row0 = (int64_t)blockIdx.y * 64, col0 = (int64_t)blockIdx.x * 64;
-    const uint8_t* const A = g.A + row0 / TILE_R * KT * TILE_BYTES + row0 % TILE_R / 64 * QUARTER_BYTES;
-    const uint8_t* const B = g.B + col0 / TILE_R * KT * TILE_BYTES + col0 % TILE_R / 64 * QUARTER_BYTES;
-    v4f acc[4][4];
+    if (g.dtype == F32) finish<F32, N>(g, row, col, v);
+    if (g.dtype == BF16) finish<BF16, N>(g, row, col, v);
+    if (g.dtype == F16) finish<F16, N>(g, row, col, v);
+}
+
+// ---- 64 rows x FB fragments of B (16 columns each) by a workgroup, operands straight from memory into registers ----
+//
+// For outputs too small for the tiles below: the waves share the inner tiles, TILES of them on their way at a time, and their sums meet in
+// LDS.
+template <int FB, int WAVES, int TILES> __global__ __launch_bounds__(64 * WAVES) void k_mx_direct(Gemm g, int64_t KT)
+{
+    constexpr int PITCH = 16 * FB + 4;  // floats between the rows of a wave's sums: rows fall on different banks
+    constexpr int SLOTS = 4;
+    __shared__ __align__(16) float sums[SLOTS * 64 * PITCH];
+    const int t = threadIdx.x, lane = t & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int64_t row0 = (int64_t)blockIdx.y * 64, col0 = (int64_t)blockIdx.x / (4 / FB) * QUARTER_R;
+    const int f0 = (int)(blockIdx.x % (4 / FB)) * FB;  // first of the workgroup's fragments of the quarter
+    const uint8_t* const A = g.A + row0 / TILE_R * KT * TILE_BYTES + row0 % TILE_R / QUARTER_R * QUARTER_BYTES;
+    const uint8_t* const B = g.B + col0 / TILE_R * KT * TILE_BYTES + col0 % TILE_R / QUARTER_R * QUARTER_BYTES;
+    v4f acc[4][FB];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = v4f{0, 0, 0, 0};
-    for (int64_t kt = wave; kt < KT; kt += 4) {
-        const uint8_t* const ta = A + kt * TILE_BYTES;
-        const uint8_t* const tb = B + kt * TILE_BYTES;
-        v4i fa[4], fb[4];
+        for (int j = 0; j < FB; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+    for (int64_t kt0 = wave; kt0 < KT; kt0 += WAVES * TILES) {
+        v4i fa[TILES][4], fb[TILES][FB];
+        int sa[TILES], sb[TILES];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            fa[i] = *(const v4i*)(ta + SCALE_BYTES + i * FRAGMENT_BYTES + lane * 16);
-            fb[i] = *(const v4i*)(tb + SCALE_BYTES + i * FRAGMENT_BYTES + lane * 16);
+        for (int u = 0; u < TILES; ++u) {
+            const int64_t kt = kt0 + u * WAVES < KT ? kt0 + u * WAVES : KT - 1;
+            const uint8_t* const ta = A + kt * TILE_BYTES;
+            const uint8_t* const tb = B + kt * TILE_BYTES;
+#pragma unroll
+            for (int j = 0; j < FB; ++j) fb[u][j] = *(const v4i*)(tb + SCALE_BYTES + (f0 + j) * FRAGMENT_BYTES + lane * 16);
+            sb[u] = *(const int*)(tb + lane * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fa[u][i] = *(const v4i*)(ta + SCALE_BYTES + i * FRAGMENT_BYTES + lane * 16);
+            sa[u] = *(const int*)(ta + lane * 4);
         }
-        const int sa = *(const int*)(ta + lane * 4), sb = *(const int*)(tb + lane * 4);
-        static_for<0, 4>([&](auto I) {
-            static_for<0, 4>([&](auto J) {
-                constexpr int i = decltype(I)::value, j = decltype(J)::value;
-                acc[i][j] = mfma<j, i>(fb[j], sb, fa[i], sa, acc[i][j]);
+#pragma unroll
+        for (int u = 0; u < TILES; ++u) {
+            if (kt0 + u * WAVES >= KT) break;
+            const int s = sb[u] >> (8 * f0);
+            static_for<0, 4>([&](auto I) {
+                static_for<0, FB>([&](auto J) {
+                    constexpr int i = decltype(I)::value, j = decltype(J)::value;
+                    acc[i][j] = mfma<j, i>(fb[u][j], s, fa[u][i], sa[u], acc[i][j]);
+                });
             });
-        });
+        }
     }
     // of the row at place l % 16 of fragment i, lane l holds the columns at places 4 (l / 16) .. + 3 of fragment j
+    auto slot = [&](int w, int i, int j) { return (v4f*)(sums + (w * 64 + row_of(i, lane & 15)) * PITCH + j * 16 + (lane >> 4 << 2)); };
+    if constexpr (WAVES > SLOTS) {
+        // (as many waves again: theirs are added first)
+        static_assert(WAVES == 2 * SLOTS, "two waves to a slot");
+        if (wave >= SLOTS)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            *(v4f*)(sums + (wave * 64 + row_of(i, lane & 15)) * PITCH + row_of(j, lane >> 4 << 2)) = acc[i][j];
+                for (int j = 0; j < FB; ++j) *slot(wave - SLOTS, i, j) = acc[i][j];
+        __syncthreads();
+        if (wave < SLOTS)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < FB; ++j) *slot(wave, i, j) += acc[i][j];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j) *slot(wave, i, j) = acc[i][j];
+    }
     __syncthreads();
+    constexpr int GROUPS = 64 * 4 * FB;  // of four columns
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int r = u * 16 + t / 16, c = (t % 16) * 4;
-        v4f s = *(const v4f*)(sums + r * PITCH + c);
+    for (int u = 0; u < (GROUPS + 64 * WAVES - 1) / (64 * WAVES); ++u) {
+        const int at = u * 64 * WAVES + t;
+        if (GROUPS % (64 * WAVES) != 0 && at >= GROUPS) break;
+        // neighbouring threads, neighbouring columns: place 4 a + .. of fragment j is column 8 a + 4 j + .. (of 32)
+        const int r = at / (4 * FB), q = at % (4 * FB), j = FB == 1 ? 0 : (q & 1) + q / 8 * 2, a = FB == 1 ? q : q / 2 % 4;
+        v4f s = *(const v4f*)(sums + r * PITCH + j * 16 + 4 * a);
 #pragma unroll
-        for (int w = 1; w < 4; ++w) s += *(const v4f*)(sums + (w * 64 + r) * PITCH + c);
+        for (int w = 1; w < SLOTS; ++w) s += *(const v4f*)(sums + (w * 64 + r) * PITCH + j * 16 + 4 * a);
         const float v[4] = {s[0], s[1], s[2], s[3]};
-        finish<TYPE, 4>(g, row0 + r, col0 + c, v);
+        finish_any<4>(g, row0 + r, col0 + row_of(f0 + j, 4 * a), v);
     }
 }
 
-template <int TYPE> void direct(const Gemm& g, hipStream_t st)
+template <int FB, int WAVES, int TILES> void direct(const Gemm& g, hipStream_t st)
 {
-    const dim3 grid((unsigned)((g.p + 63) / 64), (unsigned)((g.m + 63) / 64));
-    hipLaunchKernelGGL(k_mx_direct<TYPE>, grid, dim3(256), 0, st, g, inner_tiles(g.n));
+    const dim3 grid((unsigned)((g.p + QUARTER_R - 1) / QUARTER_R * (4 / FB)), (unsigned)((g.m + 63) / 64));
+    k_mx_direct<FB, WAVES, TILES><<<grid, dim3(64 * WAVES), 0, st>>>(g, inner_tiles(g.n));
+}
+
+// Fewer fragments of B a workgroup where there are few workgroups (64 x 4096 x 4096, 1, 2, 4 fragments: 5.5, 5.9, 7.4 us; 256 rows: 8.0,
+// 7.2, 7.7; 1024 rows: 24, 18.9, 16.7); eight waves where they all run at once and have four tiles each (64 x 8192 x 1024, 8 and 4 waves: 7.5 and
+// 8.2 us; 64 x 2048 x 2048: 3.7 and 3.6).
+void direct(const Gemm& g, hipStream_t st)
+{
+    const int64_t units = (g.p + QUARTER_R - 1) / QUARTER_R * ((g.m + 63) / 64);
+    const bool deep = inner_tiles(g.n) >= 32;
+    if (units * 4 <= COMPUTE_UNITS)
+        deep ? direct<1, 8, 1>(g, st) : direct<1, 4, 1>(g, st);
+    else if (units <= COMPUTE_UNITS * 5 / 4)
+        deep && units * 2 <= COMPUTE_UNITS ? direct<2, 8, 1>(g, st) : direct<2, 4, 1>(g, st);
+    else
+        direct<4, 4, 1>(g, st);
 }
 
 // ---- 256 x 256 outputs by a workgroup of four waves, 128 x 128 each: 256 FP32 sums a lane, one wave a SIMD ----
@@ -143,11 +204,24 @@ struct Order {
     }
 };
 
-// A tile of one operand as a buffer
-__device__ inline v4i tile_resource(uint64_t address, bool any)
-{
-    return v4i{(int)(uint32_t)address, (int)(uint32_t)(address >> 32), any ? TILE_BYTES : 0, 0x00020000};
-}
+// What is copied next of an operand: the address of the tile (or half of it), its bytes (0: nothing is read), how many stages of the output
+// tile are left.  Copies are a ring ahead at most and an output tile has at least as many stages, so that the operand tiles behind it
+// (`after`) are looked up once an output tile, outside the loop over its stages: there is no branch in there.  (All of it stays in scalar
+// registers that scalar instructions write: the copies below are asm statements, and the compiler would not put the wait states between a
+// vector instruction that writes their operands and them.)
+struct Source {
+    uint64_t at, after;
+    int bytes, bytes_after, left;
+    __device__ inline v4i resource() const { return v4i{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), bytes, 0x00020000}; }
+    __device__ inline void next(int stages)
+    {
+        --left;
+        const bool over = left == 0;
+        at = over ? after : at + TILE_BYTES;
+        bytes = over ? bytes_after : bytes;
+        left = over ? stages : left;
+    }
+};
 
 // Copy Q of a quarter of a tile: 256 bytes of scales (Q = 0, which sets M0 to the quarter's place in LDS for the others too) or a fragment.
 // Lane i writes LDS bytes [M0 + offset + its 4 or 16 bytes); the instruction's offset moves both addresses alike; one wait state
@@ -216,6 +290,70 @@ __device__ inline void put8_whole(uint64_t base, uint32_t off, float alpha, cons
     }
 }
 
+// A wave's sums into D: 8 x NJ fragments from row row0, column col0 on.  Fragment (i, j), register r: row at place l % 16 of fragment i % 4 of
+// A's quarter i / 4, column at place 4 (l / 16) + r of fragment j % 4 of B's quarter j / 4; fragments j and j + 1 (j even) are 8 neighbouring
+// columns.  whole: all of the workgroup's tile lies inside D; true is returned where that many stores were made, one for every two fragments (in
+// FP32: each).
+template <int TYPE, int NJ>
+__device__ inline bool put_tile(const Gemm& g, v4f (&acc)[8][NJ], int64_t row0, int64_t col0, bool whole_tile, bool stream, int lane)
+{
+    typedef typename Elem<TYPE>::Bits Bits;
+    typedef __attribute__((address_space(1))) Bits Global;
+    // (left alone, the register allocator parks accumulators in scratch memory and copies all of them at once; so they are read by asm
+    // statements below, and the wait states behind the last matrix instruction are written out)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+    asm volatile("s_nop 15\n\ts_nop 15");
+    // (lane parts made opaque here, or they are formed at kernel entry and live through everything; addresses are a uniform base and a
+    // 32-bit lane offset)
+    int lr = lane & 15, lc = lane >> 4;
+    asm volatile("" : "+v"(lr), "+v"(lc));
+    const int row_lane = row_of(0, lr), col_lane = row_of(0, lc << 2);
+    const uint32_t off = ((uint32_t)row_lane * (uint32_t)g.ldd + (uint32_t)col_lane) * (uint32_t)sizeof(Bits);
+    // eight sums at a time: v, the row (but for the lane's part) and the column
+    auto each = [&](auto&& f) {
+        static_for<0, 8>([&](auto I) {
+            constexpr int i = decltype(I)::value, ri = i / 4 * 64 + row_of(i % 4, 0);
+            uint64_t base = (uint64_t)(uintptr_t)((Bits*)g.D + (row0 + ri) * g.ldd + col0);
+            asm volatile("" : "+s"(base));
+            static_for<0, NJ / 2>([&](auto J) {
+                constexpr int j = 2 * decltype(J)::value, cj = j / 4 * 64 + row_of(j % 4, 0);
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][j + e / 4][e % 4]));
+                f(base, std::integral_constant<int, ri>{}, std::integral_constant<int, cj>{}, v);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+    };
+    auto whole = [&](auto STREAM) {
+        const uint32_t off16 = TYPE == F32 ? ((uint32_t)row_lane * (uint32_t)g.ldd + (uint32_t)lc * 4u) * 4u : off;
+        each([&](uint64_t base, auto, auto CJ, const float* v) { put8_whole<TYPE, decltype(STREAM)::value, decltype(CJ)::value>(base, off16, g.alpha, v); });
+    };
+    auto edge = [&](auto BETA) {
+        const int rows_left = (int)(g.m - row0 < 128 ? g.m - row0 : 128) - row_lane;
+        const int cols_left = (int)(g.p - col0 < 128 ? g.p - col0 : 128) - col_lane;
+        each([&](uint64_t base, auto RI, auto CJ, const float* v) {
+            constexpr int ri = decltype(RI)::value, cj = decltype(CJ)::value;
+            put8<TYPE, decltype(BETA)::value>((Global*)(base + off) + cj, ri < rows_left ? cols_left - cj : 0, g.alpha, g.beta, v);
+        });
+    };
+    if (g.beta != 0.0f) {
+        edge(std::true_type{});
+    } else if (!whole_tile) {
+        edge(std::false_type{});
+    } else {
+        if (stream)
+            whole(std::true_type{});
+        else
+            whole(std::false_type{});
+        return true;
+    }
+    return false;
+}
+
 template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int KT, int TM, int TP, int stream)
 {
     __shared__ __align__(16) uint8_t ring[RING * STAGE_BYTES];
@@ -233,22 +371,6 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
     const uint32_t scaleA = lds + 2 * wm * QUARTER_BYTES + lane * 4;
     const uint32_t scaleB = lds + TILE_BYTES + 2 * wn * QUARTER_BYTES + lane * 4;
 
-    // What is copied next of A and of B: the address of the tile, its bytes (0 behind the last one), how many stages of its output tile are
-    // left.  Copies are four stages ahead at most and an output tile has at least as many, so that the operand tiles behind it (`after`)
-    // are looked up once an output tile, outside the loop over its stages: there is no branch in there.
-    struct Source {
-        uint64_t at, after;
-        int bytes, bytes_after, left;
-        __device__ inline v4i resource() const { return v4i{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), bytes, 0x00020000}; }
-        __device__ inline void next(int KT)
-        {
-            --left;
-            const bool over = left == 0;
-            at = over ? after : at + TILE_BYTES;
-            bytes = over ? bytes_after : bytes;
-            left = over ? KT : left;
-        }
-    };
     Source a = {0, 0, 0, 0, KT}, b = {0, 0, 0, 0, KT};
     Order copy_order(TM, TP);
     auto look_up = [&]() {
@@ -401,73 +523,24 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
             sbL = sb_next[0];
             sbH = sb_next[1];
         }
-        // (left alone, the register allocator parks accumulators in scratch memory and copies all of them at once; so they are read by
-        // asm statements below, and the wait states behind the last matrix instruction are written out)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
-        asm volatile("s_nop 15\n\ts_nop 15");
-        // fragment (i, j), register r: row at place l % 16 of fragment i % 4 of A's quarter i / 4, column at place 4 (l / 16) + r of
-        // fragment j % 4 of B's quarter j / 4: fragments j and j + 1 (j even) are 8 neighbouring columns
-        // (lane parts made opaque here, or they are formed at kernel entry and live through everything; addresses are a uniform base
-        // and a 32-bit lane offset)
-        typedef typename Elem<TYPE>::Bits Bits;
-        typedef __attribute__((address_space(1))) Bits Global;
-        int lr = lane & 15, lc = lane >> 4;
-        asm volatile("" : "+v"(lr), "+v"(lc));
-        const int row_lane = row_of(0, lr), col_lane = row_of(0, lc << 2);
-        const uint32_t off = ((uint32_t)row_lane * (uint32_t)g.ldd + (uint32_t)col_lane) * (uint32_t)sizeof(Bits);
-        const int64_t row0 = (int64_t)tm * TILE_R + wm * 128, col0 = (int64_t)tp * TILE_R + wn * 128;
-        const int rows_left = (int)(g.m - row0 < 128 ? g.m - row0 : 128) - row_lane, cols_left = (int)(g.p - col0 < 128 ? g.p - col0 : 128) - col_lane;
-        // eight sums at a time: v, the row (of the wave's 128, but for the lane's part) and the column
-        auto each = [&](auto&& f) {
-            static_for<0, 8>([&](auto I) {
-                constexpr int i = decltype(I)::value, ri = i / 4 * 64 + row_of(i % 4, 0);
-                uint64_t base = (uint64_t)(uintptr_t)((Bits*)g.D + (row0 + ri) * g.ldd + col0);
-                asm volatile("" : "+s"(base));
-                static_for<0, 4>([&](auto J) {
-                    constexpr int j = 2 * decltype(J)::value, cj = j / 4 * 64 + row_of(j % 4, 0);
-                    float v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][j + e / 4][e % 4]));
-                    f(base, std::integral_constant<int, ri>{}, std::integral_constant<int, cj>{}, v);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-            });
-        };
-        auto whole = [&](auto STREAM) {
-            const uint32_t off16 = TYPE == F32 ? ((uint32_t)row_lane * (uint32_t)g.ldd + (uint32_t)lc * 4u) * 4u : off;
-            each([&](uint64_t base, auto, auto CJ, const float* v) { put8_whole<TYPE, decltype(STREAM)::value, decltype(CJ)::value>(base, off16, g.alpha, v); });
-        };
-        auto edge = [&](auto BETA) {
-            each([&](uint64_t base, auto RI, auto CJ, const float* v) {
-                constexpr int ri = decltype(RI)::value, cj = decltype(CJ)::value;
-                put8<TYPE, decltype(BETA)::value>((Global*)(base + off) + cj, ri < rows_left ? cols_left - cj : 0, g.alpha, g.beta, v);
-            });
-        };
-        fresh = 0;
-        if (g.beta != 0.0f) {
-            edge(std::true_type{});
-        } else if ((int64_t)(tm + 1) * TILE_R > g.m || (int64_t)(tp + 1) * TILE_R > g.p) {
-            edge(std::false_type{});
-        } else {
-            if (stream)
-                whole(std::true_type{});
-            else
-                whole(std::false_type{});
-            fresh = 2;
-        }
+        fresh = put_tile<TYPE, 8>(g, acc, (int64_t)tm * TILE_R + wm * 128, (int64_t)tp * TILE_R + wn * 128,
+                                  (int64_t)(tm + 1) * TILE_R <= g.m && (int64_t)(tp + 1) * TILE_R <= g.p, stream, lane)
+                    ? RING - 2
+                    : 0;
     }
     wait_vmcnt<0>();  // no copy may still be writing LDS when the workgroup retires
 }
 
+template <int TYPE> int streams(const Gemm& g)
+{
+    return packed_bytes(g.m, g.n) + packed_bytes(g.p, g.n) + g.m * g.p * (int64_t)sizeof(typename Elem<TYPE>::Bits) > MEMORY_SIDE_CACHE;
+}
+inline unsigned one_each(int64_t tiles) { return (unsigned)(tiles < COMPUTE_UNITS ? tiles : COMPUTE_UNITS); }
+
 template <int TYPE> void tile(const Gemm& g, hipStream_t st)
 {
     const int TM = (int)row_tiles(g.m), TP = (int)row_tiles(g.p);
-    const int64_t moved = packed_bytes(g.m, g.n) + packed_bytes(g.p, g.n) + g.m * g.p * (int64_t)sizeof(typename Elem<TYPE>::Bits);
-    hipLaunchKernelGGL(k_mx_tile<TYPE>, dim3((unsigned)(TM * TP < 256 ? TM * TP : 256)), dim3(256), 0, st, g, (int)inner_tiles(g.n), TM, TP,
-                       moved > MEMORY_SIDE_CACHE);
+    k_mx_tile<TYPE><<<dim3(one_each((int64_t)TM * TP)), dim3(256), 0, st>>>(g, (int)inner_tiles(g.n), TM, TP, streams<TYPE>(g));
 }
 
 // ---- few rows of X, quantised on the way: 16 rows and FB fragments of W's (16 columns each) by a workgroup ----
@@ -476,12 +549,13 @@ template <int TYPE> void tile(const Gemm& g, hipStream_t st)
 // takes its fragments of W straight from memory into registers, four tiles at a time, and quantises the blocks of X that meet them - a lane
 // holds a block as the matrix instruction wants it, so that its scale takes no exchange between lanes.  The waves' sums meet in LDS.
 // Every workgroup quantises all of X: FB is as large as leaves a workgroup for every compute unit.
-constexpr int FEW_ROWS = 16, FEW_WAVES = 8, FEW_TILES = 4;
+constexpr int FEW_ROWS = 16;
 
-template <int XTYPE, int FB> __global__ __launch_bounds__(64 * FEW_WAVES) void k_mx_few(Gemm g, const typename Elem<XTYPE>::Bits* X, int64_t ldx, int64_t KT)
+template <int XTYPE, int FB, int WAVES, int TILES>
+__global__ __launch_bounds__(64 * WAVES) void k_mx_few(Gemm g, const typename Elem<XTYPE>::Bits* X, int64_t ldx, int64_t KT)
 {
     typedef typename Elem<XTYPE>::Bits Bits;
-    __shared__ __align__(16) v4f sums[FEW_WAVES][FB][64];
+    __shared__ __align__(16) v4f sums[WAVES][FB][64];
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t row0 = (int64_t)blockIdx.y * FEW_ROWS, col0 = (int64_t)blockIdx.x / (4 / FB) * QUARTER_R;
@@ -506,14 +580,14 @@ template <int XTYPE, int FB> __global__ __launch_bounds__(64 * FEW_WAVES) void k
         sw >>= 8 * f0;
         static_for<0, FB>([&](auto F) { acc[decltype(F)::value] = mfma<decltype(F)::value, 0>(w[decltype(F)::value], sw, x, sx, acc[decltype(F)::value]); });
     };
-    for (int64_t kt0 = wave; kt0 < KT; kt0 += FEW_WAVES * FEW_TILES) {
-        v4i w[FEW_TILES][FB];
-        int sw[FEW_TILES];
-        Bits x[FEW_TILES][BLOCK];
+    for (int64_t kt0 = wave; kt0 < KT; kt0 += WAVES * TILES) {
+        v4i w[TILES][FB];
+        int sw[TILES];
+        Bits x[TILES][BLOCK];
 #pragma unroll
-        for (int u = 0; u < FEW_TILES; ++u) {
+        for (int u = 0; u < TILES; ++u) {
             // (a tile behind the last one: the last one again, with zeros for X)
-            const int64_t kt = kt0 + u * FEW_WAVES, at = kt < KT ? kt : KT - 1;
+            const int64_t kt = kt0 + u * WAVES, at = kt < KT ? kt : KT - 1;
             const uint8_t* const tile = W + at * TILE_BYTES;
 #pragma unroll
             for (int f = 0; f < FB; ++f) w[u][f] = *(const v4i*)(tile + SCALE_BYTES + (f0 + f) * FRAGMENT_BYTES + lane * 16);
@@ -526,14 +600,14 @@ template <int XTYPE, int FB> __global__ __launch_bounds__(64 * FEW_WAVES) void k
             }
         }
 #pragma unroll
-        for (int u = 0; u < FEW_TILES; ++u) {
+        for (int u = 0; u < TILES; ++u) {
             v4i codes;
             const int sx = block(x[u], codes);
             multiply(w[u], sw[u], codes, sx);
         }
     }
     // the block that a row ends in, where it is not a whole one: zeros for the others
-    if (g.n % BLOCK != 0 && wave == (int)((KT - 1) % FEW_WAVES)) {
+    if (g.n % BLOCK != 0 && wave == (int)((KT - 1) % WAVES)) {
         const uint8_t* const tile = W + (KT - 1) * TILE_BYTES;
         const int64_t left = here - (KT - 1) * TILE_K;
         v4i w[FB], codes;
@@ -554,38 +628,204 @@ template <int XTYPE, int FB> __global__ __launch_bounds__(64 * FEW_WAVES) void k
         const int f = t >> 6;
         v4f s = sums[0][f][lane];
 #pragma unroll
-        for (int w = 1; w < FEW_WAVES; ++w) s += sums[w][f][lane];
+        for (int w = 1; w < WAVES; ++w) s += sums[w][f][lane];
         const float v[4] = {s[0], s[1], s[2], s[3]};
-        const int64_t col = col0 + row_of(f0 + f, lane >> 4 << 2);
-        if (g.dtype == F32) finish<F32, 4>(g, row, col, v);
-        if (g.dtype == BF16) finish<BF16, 4>(g, row, col, v);
-        if (g.dtype == F16) finish<F16, 4>(g, row, col, v);
+        finish_any<4>(g, row, col0 + row_of(f0 + f, lane >> 4 << 2), v);
     }
 }
 
-template <int XTYPE, int FB> void few(const Gemm& g, const void* X, int64_t ldx, hipStream_t st)
+template <int XTYPE, int FB, int WAVES, int TILES> void few(const Gemm& g, const void* X, int64_t ldx, hipStream_t st)
 {
     const dim3 grid((unsigned)((g.p + QUARTER_R - 1) / QUARTER_R * (4 / FB)), (unsigned)((g.m + FEW_ROWS - 1) / FEW_ROWS));
-    k_mx_few<XTYPE, FB><<<grid, dim3(64 * FEW_WAVES), 0, st>>>(g, (const typename Elem<XTYPE>::Bits*)X, ldx, inner_tiles(g.n));
+    k_mx_few<XTYPE, FB, WAVES, TILES><<<grid, dim3(64 * WAVES), 0, st>>>(g, (const typename Elem<XTYPE>::Bits*)X, ldx, inner_tiles(g.n));
 }
 
+// One round of workgroups on the 256 compute units (beyond that two launches are faster: 48 rows through 8192 x 8192 19.3 us in two, 22.1 in
+// one; 32 rows 18.8 and 13.6), up to 64 rows (64 rows through 4096 x 4096 7.8 us, in two 8.7; 96 rows 12.1 and 9.2), of as few fragments each as that allows: the more workgroups, the more of W on its way at a time (16 rows
+// through 4096 x 4096: 1, 2, 4 fragments 6.9, 7.0, 7.5 us; 4096 x 14336: 18.4, 11.4, 8.8).  Up to 16 rows any number of rounds.
+inline int64_t few_units(int64_t m, int64_t p) { return (p + QUARTER_R - 1) / QUARTER_R * ((m + FEW_ROWS - 1) / FEW_ROWS); }
+
+// Four rows and fewer: little of the time goes into X, and sixteen waves with one tile each bring W in sooner than eight with two (one row
+// through 16384 x 4096: 11.4 and 15.3 us; twelve rows: 20.2 and 17.2).
 template <int XTYPE> void few(const Gemm& g, const void* X, int64_t ldx, hipStream_t st)
 {
-    const int64_t quarters = (g.p + QUARTER_R - 1) / QUARTER_R * ((g.m + FEW_ROWS - 1) / FEW_ROWS);
-    if (quarters >= 256)
-        few<XTYPE, 4>(g, X, ldx, st);
-    else if (quarters >= 128)
-        few<XTYPE, 2>(g, X, ldx, st);
+    const int64_t units = few_units(g.m, g.p);
+    if (units * 4 <= COMPUTE_UNITS)
+        g.m <= 4 ? few<XTYPE, 1, 16, 1>(g, X, ldx, st) : few<XTYPE, 1, 8, 2>(g, X, ldx, st);
+    else if (units * 2 <= COMPUTE_UNITS)
+        g.m <= 4 ? few<XTYPE, 2, 16, 1>(g, X, ldx, st) : few<XTYPE, 2, 8, 2>(g, X, ldx, st);
     else
-        few<XTYPE, 1>(g, X, ldx, st);
+        // (one tile each: also where there are no more, 12 rows through 1024 x 65536 9.2 and 11.2 us)
+        g.m <= 8 || inner_tiles(g.n) <= 8 ? few<XTYPE, 4, 8, 1>(g, X, ldx, st) : few<XTYPE, 4, 8, 2>(g, X, ldx, st);
+}
+
+// ---- 256 x 128 outputs by a workgroup: the same with half a tile of B, for outputs of too few tiles ----
+//
+// A wave has 128 x 64 outputs; a stage (26 KiB) is 32 matrix instructions of it, (A lo, B) and (A hi, B), and the ring has six places.  A fragment
+// of B gives way to the next stage's as soon as its last four products are done.  In LDS B is four pieces of two fragments, each behind the
+// scales of its quarter, one from each wave.
+constexpr int HALF_RING = 6, PIECE_BYTES = SCALE_BYTES + 2 * FRAGMENT_BYTES, HALF_STAGE_BYTES = TILE_BYTES + 4 * PIECE_BYTES, HALF_COPIES = 8;
+
+template <int TYPE> __global__ __launch_bounds__(256) void k_mx_half(Gemm g, int KT, int TM, int TP, int stream)
+{
+    __shared__ __align__(16) uint8_t ring[HALF_RING * HALF_STAGE_BYTES];
+    const int t = threadIdx.x, lane = t & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
+    const uint32_t voffA4 = wave * QUARTER_BYTES + lane * 4, voffA16 = wave * QUARTER_BYTES + lane * 16;
+    const uint32_t voffB4 = (wave >> 1) * QUARTER_BYTES + lane * 4, voffB16 = (wave >> 1) * QUARTER_BYTES + (wave & 1) * 2 * FRAGMENT_BYTES + lane * 16;
+    const uint32_t m0_a = lds + wave * QUARTER_BYTES, m0_b = lds + TILE_BYTES + wave * PIECE_BYTES;
+    typedef __attribute__((address_space(3))) const v4i* lds_v4i;
+    typedef __attribute__((address_space(3))) const int* lds_int;
+    const uint32_t fragA = lds + 2 * wm * QUARTER_BYTES + SCALE_BYTES + lane * 16, scaleA = lds + 2 * wm * QUARTER_BYTES + lane * 4;
+    const uint32_t fragB = lds + TILE_BYTES + 2 * wn * PIECE_BYTES + SCALE_BYTES + lane * 16, scaleB = lds + TILE_BYTES + 2 * wn * PIECE_BYTES + lane * 4;
+
+    Source a = {0, 0, 0, 0, KT}, b = {0, 0, 0, 0, KT};
+    Order copy_order(TM, TP);
+    auto look_up = [&]() {
+        int tm, tp;
+        const bool any = copy_order.take(tm, tp);
+        a.bytes_after = any ? TILE_BYTES : 0;
+        b.bytes_after = any ? 2 * QUARTER_BYTES : 0;
+        if (any) {
+            a.after = (uint64_t)(uintptr_t)g.A + (uint64_t)tm * KT * TILE_BYTES;
+            b.after = (uint64_t)(uintptr_t)g.B + (uint64_t)(tp >> 1) * KT * TILE_BYTES + (uint64_t)(tp & 1) * 2 * QUARTER_BYTES;
+        }
+    };
+    look_up();
+    a.at = a.after;
+    b.at = b.after;
+    a.bytes = a.bytes_after;
+    b.bytes = b.bytes_after;
+    uint32_t here = 0, to = 0;  // ring offsets: the current stage, the stage that is copied
+    auto advance = [](uint32_t& place) { place = place == (HALF_RING - 1) * HALF_STAGE_BYTES ? 0 : place + HALF_STAGE_BYTES; };
+    auto copy_a = [&](auto Q) { copy_quarter<decltype(Q)::value>(m0_a + to, voffA4, voffA16, a.resource()); };
+    auto copy_b = [&](auto Q) { copy_quarter<decltype(Q)::value>(m0_b + to, voffB4, voffB16, b.resource()); };
+    // copies 0 .. 2 of A in the second half of a stage, the other two and B's in the first half of the next one
+    constexpr int EARLY = 3;
+    static_for<0, HALF_RING>([&](auto S) {
+        constexpr bool last = decltype(S)::value == HALF_RING - 1;
+        static_for<0, last ? EARLY : 5>(copy_a);
+        if constexpr (!last) {
+            a.next(KT);
+            static_for<0, 3>(copy_b);
+            b.next(KT);
+            advance(to);
+        }
+    });
+
+    v4f acc[8][4];
+    v4i faL[4], faH[4], fb[4];
+    int saL, saH, sb;
+    // half of sub-step S: two matrix instructions on fragment S of B and two of A
+    auto math = [&](const v4i* fa, int sa, auto I0, auto S, auto X0) {
+        static_for<0, 2>([&](auto X) {
+            constexpr int j = decltype(S)::value, x = decltype(X0)::value + decltype(X)::value, i = (j & 1) ? 3 - x : x;
+            v4f& c = acc[decltype(I0)::value + i][j];
+            c = mfma<j, i>(fb[j], sb, fa[i], sa, c);
+        });
+    };
+    typedef std::integral_constant<int, 0> N0;
+    typedef std::integral_constant<int, 2> N2;
+    typedef std::integral_constant<int, 4> N4;
+
+    wait_vmcnt<(HALF_RING - 2) * HALF_COPIES + EARLY>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    uint32_t fa_at = fragA, fb_at = fragB, sa_at = scaleA, sb_at = scaleB;
+    auto piece = [](int f) { return f / 2 * PIECE_BYTES + f % 2 * FRAGMENT_BYTES; };
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        faL[q] = *(lds_v4i)(uintptr_t)(fa_at + q * FRAGMENT_BYTES);
+        fb[q] = *(lds_v4i)(uintptr_t)(fb_at + piece(q));
+    }
+    saL = *(lds_int)(uintptr_t)sa_at;
+    sb = *(lds_int)(uintptr_t)sb_at;
+
+    // (as above: stores newer than the copies that are waited for need not be over; here in the four stages behind a tile)
+    constexpr int STORES = TYPE == F32 ? 32 : 16, NEWER = (HALF_RING - 2) * HALF_COPIES;
+    constexpr int NEWER_STORES = NEWER + STORES < 63 ? NEWER + STORES : 63;
+    int fresh = 0;
+    Order order(TM, TP);
+    int tm, tp;
+    while (order.take(tm, tp)) {
+        look_up();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                acc[i][j] = v4f{0, 0, 0, 0};
+                asm volatile("" : "+a"(acc[i][j]));
+            }
+        for (int it = 0; it < KT; ++it) {
+            // (A lo, B): the upper half of A comes in, early, so that it is there at the barrier; the rest of the copies
+            static_for<0, 4>([&](auto Q) {
+                constexpr int q = decltype(Q)::value;
+                if constexpr (q < 2) faH[2 * q] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + 2 * q * FRAGMENT_BYTES);
+                if constexpr (q == 0) saH = *(lds_int)(uintptr_t)(sa_at + QUARTER_BYTES);
+                if constexpr (q >= 2) copy_b(std::integral_constant<int, q - 2>{});
+                math(faL, saL, N0{}, Q, N0{});
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (q < 2) faH[2 * q + 1] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + (2 * q + 1) * FRAGMENT_BYTES);
+                if constexpr (q < 2) copy_a(std::integral_constant<int, EARLY + q>{});
+                if constexpr (q == 2) a.next(KT);
+                if constexpr (q == 3) copy_b(std::integral_constant<int, 2>{});
+                math(faL, saL, N0{}, Q, N2{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(%1)\n1:\n\ts_waitcnt vmcnt(%2)" ::"s"(fresh), "n"(NEWER),
+                         "n"(NEWER_STORES)
+                         : "memory", "scc");
+            --fresh;
+            to = here;
+            advance(here);
+            fa_at = fragA + here;
+            fb_at = fragB + here;
+            sa_at = scaleA + here;
+            sb_at = scaleB + here;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            // (A hi, B): the lower half of A and B of the next stage (behind the last one: what the ring holds, unused)
+            int sb_next;
+            static_for<0, 4>([&](auto Q) {
+                constexpr int q = decltype(Q)::value;
+                faL[q] = *(lds_v4i)(uintptr_t)(fa_at + q * FRAGMENT_BYTES);
+                if constexpr (q == 1) saL = *(lds_int)(uintptr_t)sa_at;
+                math(faH, saH, N4{}, Q, N0{});
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (q == 2) sb_next = *(lds_int)(uintptr_t)sb_at;
+                if constexpr (q == 0) b.next(KT);
+                if constexpr (q >= 1) copy_a(std::integral_constant<int, q - 1>{});
+                math(faH, saH, N4{}, Q, N2{});
+                __builtin_amdgcn_sched_barrier(0);
+                fb[q] = *(lds_v4i)(uintptr_t)(fb_at + piece(q));
+            });
+            sb = sb_next;
+        }
+        fresh = put_tile<TYPE, 4>(g, acc, (int64_t)tm * TILE_R + wm * 128, (int64_t)tp * 128 + wn * 64,
+                                  (int64_t)(tm + 1) * TILE_R <= g.m && (int64_t)(tp + 1) * 128 <= g.p, stream, lane)
+                    ? HALF_RING - 2
+                    : 0;
+    }
+    wait_vmcnt<0>();
+}
+
+template <int TYPE> void half(const Gemm& g, hipStream_t st)
+{
+    const int TM = (int)row_tiles(g.m), TP = (int)((g.p + 127) / 128);
+    k_mx_half<TYPE><<<dim3(one_each((int64_t)TM * TP)), dim3(256), 0, st>>>(g, (int)inner_tiles(g.n), TM, TP, streams<TYPE>(g));
 }
 
 template <int TYPE> void product(const Gemm& g, int way, hipStream_t st)
 {
     if (way == WAY_TILE)
         tile<TYPE>(g, st);
+    else if (way == WAY_HALF)
+        half<TYPE>(g, st);
     else
-        direct<TYPE>(g, st);
+        direct(g, st);
 }
 
 }  // namespace
@@ -595,16 +835,33 @@ namespace mxk {
 // (32-bit offsets of a lane inside 28 rows of D, and 32-bit numbers of tiles)
 bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd)
 {
-    if (way == WAY_TILE) return inner_tiles(n) >= RING && ldd < (1 << 24) && row_tiles(m) * row_tiles(p) < ((int64_t)1 << 30);
+    if (way == WAY_TILE || way == WAY_HALF)
+        return inner_tiles(n) >= (way == WAY_TILE ? RING : HALF_RING) && ldd < (1 << 24) && row_tiles(m) * row_tiles(p) < ((int64_t)1 << 28);
     return way == WAY_DIRECT;
+}
+
+// Microseconds that each way takes, roughly: the tiles by rounds of one for every compute unit, k_mx_direct by its workgroups.  Fitted to
+// (m x n x p: direct, half, tile)  256 x 4096 x 4096: 6.8, 16.8, 24.9;  1024 x 4096 x 4096: 17.3, 17.8, 25.5;  2048 x 4096 x 4096: 32.7, 21.5, 27.0;
+// 4096 x 4096 x 4096: 66, 39.0, 36.2;  512 x 8192 x 8192: 29.2, 29.1, 43.3;  1024 x 8192 x 8192: 60, 35.0, 44.3;  2048 x 8192 x 8192: 117, 68, 59;
+// 512 x 1024 x 8192: 9.8, 8.6, 11.7;  512 x 4096 x 14336: 33.6, 19.5, 27.6;  1024 x 4096 x 14336: 61, 36.0, 31.2;  4096 x 2051 x 1283: 19.5, 15.9, 24.8.
+double estimate_us(int way, int64_t m, int64_t n, int64_t p)
+{
+    const double KT = (double)inner_tiles(n);
+    const auto rounds = [](int64_t tiles) { return (double)((tiles + COMPUTE_UNITS - 1) / COMPUTE_UNITS); };
+    if (way == WAY_TILE) return rounds(row_tiles(m) * row_tiles(p)) * (7.5 + 0.62 * KT);
+    if (way == WAY_HALF) return rounds(row_tiles(m) * ((p + 127) / 128)) * (5.5 + 0.42 * KT);
+    return 3.0 + (double)(((m + 63) / 64) * ((p + 63) / 64)) * (0.0035 + 0.0004 * KT);
 }
 
 int choose(int64_t m, int64_t n, int64_t p, int64_t ldd)
 {
-    return way_fits(WAY_TILE, m, n, p, ldd) && row_tiles(m) * row_tiles(p) >= 128 ? WAY_TILE : WAY_DIRECT;
+    int best = WAY_DIRECT;
+    for (int way : {WAY_TILE, WAY_HALF})
+        if (way_fits(way, m, n, p, ldd) && estimate_us(way, m, n, p) < estimate_us(best, m, n, p)) best = way;
+    return best;
 }
 
-bool few_rows(int64_t m) { return m <= FEW_ROWS; }
+bool few_rows(int64_t m, int64_t p) { return m <= FEW_ROWS || (m <= 4 * FEW_ROWS && few_units(m, p) <= COMPUTE_UNITS); }
 
 hipError_t launch_few(const Gemm& g, int xtype, const void* X, int64_t ldx, hipStream_t st)
 {

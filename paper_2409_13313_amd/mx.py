@@ -39,7 +39,7 @@ EXPORTS = list(_SIGNATURES)
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 BLOCK = 32
-WAYS = {"auto": -1, "direct": 0, "tile": 1}
+WAYS = {"auto": -1, "direct": 0, "tile": 1, "half": 2}
 
 
 class Packed:

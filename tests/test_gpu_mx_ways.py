@@ -29,7 +29,7 @@ def product(A, B):
 
 
 @pytest.mark.parametrize("m,n,p", SHAPES)
-@pytest.mark.parametrize("way", ["direct", "tile"])
+@pytest.mark.parametrize("way", ["direct", "tile", "half"])
 def test_way(mx, way, m, n, p):
     print(f"{way} {m} x {n} x {p}", flush=True)
     A, B = matrix(m, n, "bf16", m + n), matrix(p, n, "bf16", p + n + 1)
@@ -37,7 +37,7 @@ def test_way(mx, way, m, n, p):
     want, size = product(qa, qb)
     bound = max(n, 1) * 2.0 ** -23 * size
     (PA, _), (PB, _) = mx.quantize(A), mx.quantize(B)
-    if way == "tile" and n <= 384:     # (its ring has four places: it is for inner dimensions that fill them)
+    if n <= {"direct": 0, "tile": 384, "half": 640}[way]:     # (their rings have four and six places: inner dimensions that fill them)
         with pytest.raises(Exception, match="this way"):
             mx.gemm(PA, PB, way=way)
         return
@@ -53,7 +53,7 @@ def test_way(mx, way, m, n, p):
         check(got, -0.5 * want + 2.0 * f64(old), limit, kind, n, kind)
 
 
-@pytest.mark.parametrize("way", ["direct", "tile"])
+@pytest.mark.parametrize("way", ["direct", "tile", "half"])
 def test_again_and_again(mx, way):
     """The same bits from call to call, with other work between."""
     m, n, p = 1800, 900, 2000
