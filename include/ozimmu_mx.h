@@ -52,8 +52,9 @@ int ozimmu_mx_pack(int64_t rows, int64_t n, const uint8_t *codes, int64_t ldc, c
 int ozimmu_mx_unpack(int64_t rows, int64_t n, const void *packed, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds,
                      void *stream);
 
-/* Bytes of device workspace (256-byte aligned) that ozimmu_mx_gemm and ozimmu_mx_linear need for D of m x p and an inner dimension of n;
- * and ozimmu_mx_linear_backward for X of m x n and G of m x p.  0 for sizes out of range.  Host, pure. */
+/* Bytes of device workspace (256-byte aligned, contents irrelevant) that ozimmu_mx_linear needs for X of m x n and D of m x p, 0 where it
+ * takes one launch and needs none (workspace may be NULL then), and ozimmu_mx_linear_backward for X of m x n and G of m x p.  Calls that may
+ * run at the same time must not share one.  0 for sizes out of range.  Host, pure. */
 size_t ozimmu_mx_workspace_bytes(int64_t m, int64_t n, int64_t p);
 size_t ozimmu_mx_backward_workspace_bytes(int64_t m, int64_t n, int64_t p);
 
@@ -61,7 +62,7 @@ size_t ozimmu_mx_backward_workspace_bytes(int64_t m, int64_t n, int64_t p);
  * Sums are formed in FP32 on the matrix cores; alpha and beta are applied in FP32 and D is rounded once.  beta == 0: the old D is
  * not read.  n == 0: the product is zero. */
 int ozimmu_mx_gemm(int64_t m, int64_t n, int64_t p, float alpha, const void *A, const void *B, float beta, int type, void *D,
-                   int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);
+                   int64_t ldd, void *stream);
 
 /* The same, run in a given way instead of the library's choice (OZIMMU_ERR_WAY where it cannot run so); and that choice.  Debug / test
  * helpers; the second one is host, pure. */
@@ -70,7 +71,7 @@ enum { OZIMMU_MX_WAY_AUTO = -1,
        OZIMMU_MX_WAY_TILE = 1,      /* 256 x 256 outputs a workgroup at a time, operands through LDS; inner dimensions above 384 */
        OZIMMU_MX_WAY_HALF = 2 };    /* 256 x 128; inner dimensions above 640 */
 int ozimmu_mx_gemm_way(int way, int64_t m, int64_t n, int64_t p, float alpha, const void *A, const void *B, float beta, int type,
-                       void *D, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);
+                       void *D, int64_t ldd, void *stream);
 int ozimmu_mx_choose(int64_t m, int64_t n, int64_t p, int64_t ldd);
 
 /* The forward pass of a linear layer: D <- alpha Q(X) W^T + beta D, X (device, m x n, ldx >= n) of type `xtype`, W packed

@@ -47,7 +47,15 @@ namespace mxk {
 
 enum Type { F32 = 0, BF16 = 1, F16 = 2 };
 
-hipError_t launch_quantize(int type, int64_t rows, int64_t n, const void* X, int64_t ldx, void* by_row, void* by_col, hipStream_t st);
+// X of rows x n, and where it goes (nullptr: not wanted; at least one of them)
+struct Quantize {
+    int64_t rows, n;
+    const void* X;
+    int64_t ldx;
+    void *by_row, *by_col;
+};
+hipError_t launch_quantize(int type, const Quantize& q, hipStream_t st);
+hipError_t launch_quantize2(int type, const Quantize& a, const Quantize& b, hipStream_t st);  // in one launch; both with by_col
 hipError_t launch_dequantize(int type, int64_t rows, int64_t n, const void* packed, void* X, int64_t ldx, hipStream_t st);
 hipError_t launch_pack(int64_t rows, int64_t n, const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, void* packed,
                        hipStream_t st);
@@ -69,6 +77,7 @@ enum { WAY_AUTO = -1, WAY_DIRECT = 0, WAY_TILE = 1, WAY_HALF = 2 };
 int choose(int64_t m, int64_t n, int64_t p, int64_t ldd);
 bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd);
 hipError_t launch_gemm(const Gemm& g, int way, hipStream_t st);
+hipError_t launch_gemm2(const Gemm& a, const Gemm& b, hipStream_t st);  // both; neither waits for the other
 // D <- alpha Q(X) B^T + beta D in one launch (g.A is not looked at); few_rows(m, p): what this is for
 bool few_rows(int64_t m, int64_t p);
 hipError_t launch_few(const Gemm& g, int xtype, const void* X, int64_t ldx, hipStream_t st);

@@ -8,7 +8,6 @@ namespace {
 
 // rows <= 2^22 - 256: every grid dimension stays within the HIP limits (64 rows a workgroup along y)
 constexpr int64_t MAX_ROWS = ((int64_t)1 << 22) - 256;
-constexpr int64_t MAX_BLOCKS = (int64_t)1 << 24;  // workgroups of 256 threads in one dimension (128 x 128 elements each: more than fit memory)
 constexpr int64_t MAX_INNER = (int64_t)1 << 29;
 constexpr int64_t MAX_LD = ((int64_t)1 << 40) - 1;  // products of a row number and a leading dimension stay within 64 bits
 
@@ -58,13 +57,13 @@ size_t ozimmu_mx_bytes(int64_t rows, int64_t n) { return sizes_ok(rows, n) ? (si
 int ozimmu_mx_quantize(int type, int64_t rows, int64_t n, const void* X, int64_t ldx, void* by_row, void* by_col, void* stream)
 {
     if (by_row && !sizes_ok(rows, n)) return OZIMMU_ERR_DIM;
-    if (by_col && (!sizes_ok(n, rows) || mxl::inner_tiles(rows) * mxl::inner_tiles(n) >= MAX_BLOCKS)) return OZIMMU_ERR_DIM;
+    if (by_col && !sizes_ok(n, rows)) return OZIMMU_ERR_DIM;
     if (rows < 0 || n < 0) return OZIMMU_ERR_DIM;
     CHECK(matrix_status(type, X, rows, n, ldx));
     if (rows == 0 || n == 0) return OZIMMU_OK;
     if (!by_row && !by_col) return OZIMMU_ERR_NULL;
     if (!aligned(by_row) || !aligned(by_col)) return OZIMMU_ERR_WORKSPACE;
-    return launched(mxk::launch_quantize(type, rows, n, X, ldx, by_row, by_col, (hipStream_t)stream));
+    return launched(mxk::launch_quantize(type, {rows, n, X, ldx, by_row, by_col}, (hipStream_t)stream));
 }
 
 int ozimmu_mx_dequantize(int type, int64_t rows, int64_t n, const void* packed, void* X, int64_t ldx, void* stream)
@@ -116,13 +115,13 @@ size_t ozimmu_mx_backward_workspace_bytes(int64_t m, int64_t n, int64_t p)
 }
 
 int ozimmu_mx_gemm(int64_t m, int64_t n, int64_t p, float alpha, const void* A, const void* B, float beta, int type, void* D,
-                   int64_t ldd, void* workspace, size_t workspace_bytes, void* stream)
+                   int64_t ldd, void* stream)
 {
-    return ozimmu_mx_gemm_way(OZIMMU_MX_WAY_AUTO, m, n, p, alpha, A, B, beta, type, D, ldd, workspace, workspace_bytes, stream);
+    return ozimmu_mx_gemm_way(OZIMMU_MX_WAY_AUTO, m, n, p, alpha, A, B, beta, type, D, ldd, stream);
 }
 
 int ozimmu_mx_gemm_way(int way, int64_t m, int64_t n, int64_t p, float alpha, const void* A, const void* B, float beta, int type, void* D,
-                       int64_t ldd, void* workspace, size_t workspace_bytes, void* stream)
+                       int64_t ldd, void* stream)
 {
     if (!sizes_ok(m, n) || !sizes_ok(p, n)) return OZIMMU_ERR_DIM;
     CHECK(matrix_status(type, D, m, p, ldd));
@@ -130,8 +129,6 @@ int ozimmu_mx_gemm_way(int way, int64_t m, int64_t n, int64_t p, float alpha, co
     if (m == 0 || p == 0) return OZIMMU_OK;
     CHECK(packed_status(A, m, n));
     CHECK(packed_status(B, p, n));
-    (void)workspace;
-    (void)workspace_bytes;
     const mxk::Gemm g = {m, n, p, (const uint8_t*)A, (const uint8_t*)B, D, ldd, type, alpha, beta};
     return launched(mxk::launch_gemm(g, way, (hipStream_t)stream));
 }
@@ -150,7 +147,7 @@ int ozimmu_mx_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, co
     const hipStream_t st = (hipStream_t)stream;
     const mxk::Gemm g = {m, n, p, (const uint8_t*)workspace, (const uint8_t*)W, D, ldd, dtype, alpha, beta};
     if (mxk::few_rows(m, p)) return launched(mxk::launch_few(g, xtype, X, ldx, st));
-    if (n > 0) CHECK(launched(mxk::launch_quantize(xtype, m, n, X, ldx, workspace, nullptr, st)));
+    if (n > 0) CHECK(launched(mxk::launch_quantize(xtype, {m, n, X, ldx, workspace, nullptr}, st)));
     return launched(mxk::launch_gemm(g, mxk::WAY_AUTO, st));
 }
 
@@ -174,17 +171,18 @@ int ozimmu_mx_linear_backward(int64_t m, int64_t n, int64_t p, float alpha, int 
     uint8_t* const g_cols = g_rows + mxl::packed_bytes(m, p);
     uint8_t* const x_cols = g_cols + mxl::packed_bytes(p, m);
     const bool want_x = dX && m > 0 && n > 0, want_w = dW && p > 0 && n > 0;
-    if (m > 0 && p > 0 && (want_x || want_w))
-        CHECK(launched(mxk::launch_quantize(type, m, p, G, ldg, want_x ? g_rows : nullptr, want_w ? g_cols : nullptr, st)));
-    if (want_x) {
-        const mxk::Gemm g = {m, p, n, g_rows, (const uint8_t*)Wt, dX, lddx, dx_type, alpha, beta_x};
-        CHECK(launched(mxk::launch_gemm(g, mxk::WAY_AUTO, st)));
+    if (m > 0 && p > 0) {
+        const mxk::Quantize gq = {m, p, G, ldg, want_x ? g_rows : nullptr, want_w ? g_cols : nullptr}, xq = {m, n, X, ldx, nullptr, x_cols};
+        if (want_w)
+            CHECK(launched(mxk::launch_quantize2(type, gq, xq, st)));
+        else if (want_x)
+            CHECK(launched(mxk::launch_quantize(type, gq, st)));
     }
-    if (want_w) {
-        if (m > 0) CHECK(launched(mxk::launch_quantize(type, m, n, X, ldx, nullptr, x_cols, st)));
-        const mxk::Gemm g = {p, m, n, g_cols, x_cols, dW, lddw, dw_type, alpha, beta_w};
-        CHECK(launched(mxk::launch_gemm(g, mxk::WAY_AUTO, st)));
-    }
+    const mxk::Gemm gx = {m, p, n, g_rows, (const uint8_t*)Wt, dX, lddx, dx_type, alpha, beta_x};
+    const mxk::Gemm gw = {p, m, n, g_cols, x_cols, dW, lddw, dw_type, alpha, beta_w};
+    if (want_x && want_w) return launched(mxk::launch_gemm2(gx, gw, st));
+    if (want_x) return launched(mxk::launch_gemm(gx, mxk::WAY_AUTO, st));
+    if (want_w) return launched(mxk::launch_gemm(gw, mxk::WAY_AUTO, st));
     return OZIMMU_OK;
 }
 

@@ -59,15 +59,16 @@ template <int N> __device__ inline void finish_any(const Gemm& g, int64_t row, i
 //
 // For outputs too small for the tiles below: the waves share the inner tiles, TILES of them on their way at a time, and their sums meet in
 // LDS.
-template <int FB, int WAVES, int TILES> __global__ __launch_bounds__(64 * WAVES) void k_mx_direct(Gemm g, int64_t KT)
+constexpr int DIRECT_SLOTS = 4;
+template <int FB> constexpr int direct_pitch() { return 16 * FB + 4; }  // floats between the rows of a wave's sums: rows fall on different banks
+
+template <int FB, int WAVES, int TILES> __device__ inline void direct_block(const Gemm& g, int64_t block_row, int64_t block_col, float* sums)
 {
-    constexpr int PITCH = 16 * FB + 4;  // floats between the rows of a wave's sums: rows fall on different banks
-    constexpr int SLOTS = 4;
-    __shared__ __align__(16) float sums[SLOTS * 64 * PITCH];
+    constexpr int PITCH = direct_pitch<FB>(), SLOTS = DIRECT_SLOTS;
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int64_t row0 = (int64_t)blockIdx.y * 64, col0 = (int64_t)blockIdx.x / (4 / FB) * QUARTER_R;
-    const int f0 = (int)(blockIdx.x % (4 / FB)) * FB;  // first of the workgroup's fragments of the quarter
+    const int64_t KT = inner_tiles(g.n), row0 = block_row * 64, col0 = block_col / (4 / FB) * QUARTER_R;
+    const int f0 = (int)(block_col % (4 / FB)) * FB;  // first of the workgroup's fragments of the quarter
     const uint8_t* const A = g.A + row0 / TILE_R * KT * TILE_BYTES + row0 % TILE_R / QUARTER_R * QUARTER_BYTES;
     const uint8_t* const B = g.B + col0 / TILE_R * KT * TILE_BYTES + col0 % TILE_R / QUARTER_R * QUARTER_BYTES;
     v4f acc[4][FB];
@@ -140,25 +141,49 @@ template <int FB, int WAVES, int TILES> __global__ __launch_bounds__(64 * WAVES)
     }
 }
 
-template <int FB, int WAVES, int TILES> void direct(const Gemm& g, hipStream_t st)
+template <int FB, int WAVES, int TILES> __global__ __launch_bounds__(64 * WAVES) void k_mx_direct(Gemm g)
 {
-    const dim3 grid((unsigned)((g.p + QUARTER_R - 1) / QUARTER_R * (4 / FB)), (unsigned)((g.m + 63) / 64));
-    k_mx_direct<FB, WAVES, TILES><<<grid, dim3(64 * WAVES), 0, st>>>(g, inner_tiles(g.n));
+    __shared__ __align__(16) float sums[DIRECT_SLOTS * 64 * direct_pitch<FB>()];
+    direct_block<FB, WAVES, TILES>(g, blockIdx.y, blockIdx.x, sums);
+}
+
+// Two products in one launch (the gradients of a small layer)
+template <int FB, int WAVES, int TILES>
+__global__ __launch_bounds__(64 * WAVES) void k_mx_direct2(Gemm a, Gemm b, uint32_t cols_a, uint32_t cols_b, uint32_t blocks_a)
+{
+    __shared__ __align__(16) float sums[DIRECT_SLOTS * 64 * direct_pitch<FB>()];
+    const bool first = blockIdx.x < blocks_a;
+    const uint32_t at = first ? blockIdx.x : blockIdx.x - blocks_a, cols = first ? cols_a : cols_b;
+    const Gemm g = first ? a : b;
+    direct_block<FB, WAVES, TILES>(g, at / cols, at % cols, sums);
+}
+
+inline int64_t direct_units(const Gemm& g) { return (g.p + QUARTER_R - 1) / QUARTER_R * ((g.m + 63) / 64); }
+
+template <int FB, int WAVES, int TILES> void direct(const Gemm& g, const Gemm* also, hipStream_t st)
+{
+    const unsigned cols = (unsigned)((g.p + QUARTER_R - 1) / QUARTER_R * (4 / FB)), rows = (unsigned)((g.m + 63) / 64);
+    if (!also) {
+        k_mx_direct<FB, WAVES, TILES><<<dim3(cols, rows), dim3(64 * WAVES), 0, st>>>(g);
+    } else {
+        const unsigned cols_b = (unsigned)((also->p + QUARTER_R - 1) / QUARTER_R * (4 / FB)), rows_b = (unsigned)((also->m + 63) / 64);
+        k_mx_direct2<FB, WAVES, TILES><<<dim3(cols * rows + cols_b * rows_b), dim3(64 * WAVES), 0, st>>>(g, *also, cols, cols_b, cols * rows);
+    }
 }
 
 // Fewer fragments of B a workgroup where there are few workgroups (64 x 4096 x 4096, 1, 2, 4 fragments: 5.5, 5.9, 7.4 us; 256 rows: 8.0,
 // 7.2, 7.7; 1024 rows: 24, 18.9, 16.7); eight waves where they all run at once and have four tiles each (64 x 8192 x 1024, 8 and 4 waves: 7.5 and
 // 8.2 us; 64 x 2048 x 2048: 3.7 and 3.6).
-void direct(const Gemm& g, hipStream_t st)
+void direct(const Gemm& g, const Gemm* also, hipStream_t st)
 {
-    const int64_t units = (g.p + QUARTER_R - 1) / QUARTER_R * ((g.m + 63) / 64);
-    const bool deep = inner_tiles(g.n) >= 32;
+    const int64_t units = direct_units(g) + (also ? direct_units(*also) : 0);
+    const bool deep = inner_tiles(g.n) >= 32 || (also && inner_tiles(also->n) >= 32);
     if (units * 4 <= COMPUTE_UNITS)
-        deep ? direct<1, 8, 1>(g, st) : direct<1, 4, 1>(g, st);
+        deep ? direct<1, 8, 1>(g, also, st) : direct<1, 4, 1>(g, also, st);
     else if (units <= COMPUTE_UNITS * 5 / 4)
-        deep && units * 2 <= COMPUTE_UNITS ? direct<2, 8, 1>(g, st) : direct<2, 4, 1>(g, st);
+        deep && units * 2 <= COMPUTE_UNITS ? direct<2, 8, 1>(g, also, st) : direct<2, 4, 1>(g, also, st);
     else
-        direct<4, 4, 1>(g, st);
+        direct<4, 4, 1>(g, also, st);
 }
 
 // ---- 256 x 256 outputs by a workgroup of four waves, 128 x 128 each: 256 FP32 sums a lane, one wave a SIMD ----
@@ -825,7 +850,7 @@ template <int TYPE> void product(const Gemm& g, int way, hipStream_t st)
     else if (way == WAY_HALF)
         half<TYPE>(g, st);
     else
-        direct(g, st);
+        direct(g, nullptr, st);
 }
 
 }  // namespace
@@ -878,6 +903,18 @@ hipError_t launch_gemm(const Gemm& g, int way, hipStream_t st)
     if (g.dtype == BF16) product<BF16>(g, way, st);
     if (g.dtype == F16) product<F16>(g, way, st);
     return hipGetLastError();
+}
+
+// Two products that do not depend on each other: in one launch where both are small
+hipError_t launch_gemm2(const Gemm& a, const Gemm& b, hipStream_t st)
+{
+    if (choose(a.m, a.n, a.p, a.ldd) == WAY_DIRECT && choose(b.m, b.n, b.p, b.ldd) == WAY_DIRECT &&
+        direct_units(a) + direct_units(b) <= 4 * COMPUTE_UNITS) {
+        direct(a, &b, st);
+        return hipGetLastError();
+    }
+    const hipError_t e = launch_gemm(a, WAY_AUTO, st);
+    return e != hipSuccess ? e : launch_gemm(b, WAY_AUTO, st);
 }
 
 }  // namespace mxk

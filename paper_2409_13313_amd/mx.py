@@ -26,8 +26,8 @@ _SIGNATURES = {
     "ozimmu_mx_unpack": (_int, [_i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp]),
     "ozimmu_mx_workspace_bytes": (_sz, [_i64, _i64, _i64]),
     "ozimmu_mx_backward_workspace_bytes": (_sz, [_i64, _i64, _i64]),
-    "ozimmu_mx_gemm": (_int, [_i64, _i64, _i64, _float, _vp, _vp, _float, _int, _vp, _i64, _vp, _sz, _vp]),
-    "ozimmu_mx_gemm_way": (_int, [_int, _i64, _i64, _i64, _float, _vp, _vp, _float, _int, _vp, _i64, _vp, _sz, _vp]),
+    "ozimmu_mx_gemm": (_int, [_i64, _i64, _i64, _float, _vp, _vp, _float, _int, _vp, _i64, _vp]),
+    "ozimmu_mx_gemm_way": (_int, [_int, _i64, _i64, _i64, _float, _vp, _vp, _float, _int, _vp, _i64, _vp]),
     "ozimmu_mx_choose": (_int, [_i64, _i64, _i64, _i64]),
     "ozimmu_mx_linear": (_int, [_i64, _i64, _i64, _float, _int, _vp, _i64, _vp, _float, _int, _vp, _i64, _vp, _sz, _vp]),
     "ozimmu_mx_linear_backward": (_int, [_i64, _i64, _i64, _float, _int, _vp, _i64, _vp, _i64, _vp, _float, _int, _vp, _i64,
@@ -40,6 +40,7 @@ EXPORTS = list(_SIGNATURES)
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 BLOCK = 32
 WAYS = {"auto": -1, "direct": 0, "tile": 1, "half": 2}
+_uint8 = torch.uint8
 
 
 class Packed:
@@ -47,7 +48,7 @@ class Packed:
     __slots__ = ("data", "rows", "n")
 
     def __init__(self, data: torch.Tensor, rows: int, n: int):
-        if not (data.is_cuda and data.dtype is torch.uint8 and data.dim() == 1 and data.is_contiguous()):
+        if not (data.is_cuda and data.dtype is _uint8 and data.dim() == 1 and data.is_contiguous()):
             raise ValueError("packed data is a contiguous 1-D uint8 tensor on the GPU")
         if data.numel() < packed_bytes(rows, n):
             raise ValueError(f"{data.numel()} bytes for a packed matrix of {rows} x {n}, which takes {packed_bytes(rows, n)}")
@@ -65,23 +66,29 @@ def _matrix(t: torch.Tensor) -> Tuple[int, int, int, int]:
         raise ValueError(f"expected float32, bfloat16 or float16, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError("tensor must live on the GPU")
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError("expected a 2-D tensor")
-    (rows, cols), (ld, unit) = t.shape, t.stride()
+    rows, cols = shape
+    ld, unit = t.stride()
     if (cols > 1 and unit != 1) or (rows > 1 and ld < cols):
         raise ValueError("expected a 2-D tensor with unit stride along rows that do not overlap")
     return rows, cols, ld if rows > 1 else max(cols, ld, 1), kind
 
 
-def _output(D: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, dtype, beta: float) -> torch.Tensor:
-    """The caller's output, or a new one."""
+def _output(D: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, dtype, beta: float):
+    """The caller's output, or a new one; its leading dimension and type number."""
     if D is None:
         if beta != 0.0:
             raise ValueError("beta without the matrix that it multiplies")
-        return torch.empty((rows, cols), dtype=dtype, device=like.device)
-    if tuple(D.shape) != (rows, cols):
-        raise ValueError(f"output of {tuple(D.shape)} for a result of {rows} x {cols}")
-    return D
+        kind = TYPES.get(dtype)
+        if kind is None:
+            raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
+        return like.new_empty((rows, cols), dtype=dtype), max(cols, 1), kind
+    m, n, ldd, kind = _matrix(D)
+    if m != rows or n != cols:
+        raise ValueError(f"output of {m} x {n} for a result of {rows} x {cols}")
+    return D, ldd, kind
 
 
 def _packed(P: Packed, what: str) -> Packed:
@@ -108,17 +115,26 @@ def backward_workspace_bytes(m: int, n: int, p: int) -> int:
 
 
 def alloc_workspace(m: int, n: int, p: int, device="cuda", backward: bool = False) -> torch.Tensor:
-    """Workspace for gemm and linear with these sizes; with `backward` for linear_backward too."""
+    """Workspace for linear with these sizes; with `backward` for linear_backward too."""
     nbytes = max(workspace_bytes(m, n, p), backward_workspace_bytes(m, n, p) if backward else 0)
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    return torch.empty(max(nbytes, 256), dtype=_uint8, device=device)
 
 
-def _room(workspace: Optional[torch.Tensor]):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+def _workspace(workspace: Optional[torch.Tensor], nbytes: int, like: torch.Tensor):
+    """The caller's workspace, or a new one (none where none is needed): the tensor, its address and size."""
+    if workspace is None:
+        if not nbytes:
+            return None, None, 0
+        workspace = like.new_empty(nbytes, dtype=_uint8)
+    elif not (workspace.is_cuda and workspace.dtype is _uint8 and workspace.is_contiguous()):
+        raise ValueError("a workspace is a contiguous uint8 tensor on the GPU")
+    return workspace, workspace.data_ptr(), workspace.numel()
 
 
-def _empty(rows: int, n: int, device) -> Packed:
-    return Packed(torch.empty(packed_bytes(rows, n), dtype=torch.uint8, device=device), rows, n)
+def _empty(rows: int, n: int, like: torch.Tensor) -> Packed:
+    P = Packed.__new__(Packed)
+    P.data, P.rows, P.n = like.new_empty(_lib.ozimmu_mx_bytes(rows, n), dtype=_uint8), rows, n
+    return P
 
 
 def quantize(X: torch.Tensor, rows: bool = True, cols: bool = False) -> Tuple[Optional[Packed], Optional[Packed]]:
@@ -126,19 +142,22 @@ def quantize(X: torch.Tensor, rows: bool = True, cols: bool = False) -> Tuple[Op
     m, n, ldx, kind = _matrix(X)
     if not rows and not cols:
         raise ValueError("nothing asked for: rows, cols or both")
-    by_row = _empty(m, n, X.device) if rows else None
-    by_col = _empty(n, m, X.device) if cols else None
-    _check(_lib.ozimmu_mx_quantize(kind, m, n, X.data_ptr(), ldx, by_row.data.data_ptr() if rows else None,
-                                   by_col.data.data_ptr() if cols else None, ozimmu._stream()))
+    by_row = _empty(m, n, X) if rows else None
+    by_col = _empty(n, m, X) if cols else None
+    status = _lib.ozimmu_mx_quantize(kind, m, n, X.data_ptr(), ldx, by_row.data.data_ptr() if rows else None,
+                                     by_col.data.data_ptr() if cols else None, ozimmu._stream())
+    if status:
+        raise OzimmuError(status)
     return by_row, by_col
 
 
 def dequantize(P: Packed, dtype=torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values of a packed matrix."""
-    P = _packed(P, "the matrix")
-    X = _output(out, P.data, P.rows, P.n, dtype, 0.0)
-    _, _, ldx, kind = _matrix(X)
-    _check(_lib.ozimmu_mx_dequantize(kind, P.rows, P.n, P.data.data_ptr(), X.data_ptr(), ldx, ozimmu._stream()))
+    data = _packed(P, "the matrix").data
+    X, ldx, kind = _output(out, data, P.rows, P.n, dtype, 0.0)
+    status = _lib.ozimmu_mx_dequantize(kind, P.rows, P.n, data.data_ptr(), X.data_ptr(), ldx, ozimmu._stream())
+    if status:
+        raise OzimmuError(status)
     return X
 
 
@@ -160,7 +179,7 @@ def pack(codes: torch.Tensor, scales: torch.Tensor, n: Optional[int] = None) -> 
     if -(-n // BLOCK) != blocks:
         raise ValueError(f"{blocks} scales a row for {n} columns")
     ldc, lds = _bytes_matrix(codes, rows, blocks * BLOCK // 2, "codes"), _bytes_matrix(scales, rows, blocks, "scales")
-    P = _empty(rows, n, codes.device)
+    P = _empty(rows, n, codes)
     _check(_lib.ozimmu_mx_pack(rows, n, codes.data_ptr(), ldc, scales.data_ptr(), lds, P.data.data_ptr(), ozimmu._stream()))
     return P
 
@@ -177,16 +196,15 @@ def unpack(P: Packed) -> Tuple[torch.Tensor, torch.Tensor]:
 
 
 def gemm(A: Packed, B: Packed, dtype=torch.float32, alpha: float = 1.0, beta: float = 0.0, D: Optional[torch.Tensor] = None,
-         workspace: Optional[torch.Tensor] = None, way: str = "auto") -> torch.Tensor:
+         way: str = "auto") -> torch.Tensor:
     """D <- alpha A B^T + beta D from packed matrices; `way` forces how it is run (see ozimmu_mx_gemm_way in the header)."""
     A, B = _packed(A, "A"), _packed(B, "B")
     if A.n != B.n:
         raise ValueError("inner dimensions differ")
     m, n, p = A.rows, A.n, B.rows
-    D = _output(D, A.data, m, p, dtype, beta)
-    _, _, ldd, kind = _matrix(D)
+    D, ldd, kind = _output(D, A.data, m, p, dtype, beta)
     _check(_lib.ozimmu_mx_gemm_way(WAYS[way], m, n, p, alpha, A.data.data_ptr(), B.data.data_ptr(), beta, kind, D.data_ptr(), ldd,
-                                   None, 0, ozimmu._stream()))
+                                   ozimmu._stream()))
     return D
 
 
@@ -194,16 +212,16 @@ def linear(X: torch.Tensor, W: Packed, dtype=None, alpha: float = 1.0, beta: flo
            workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """D <- alpha Q(X) W^T + beta D for rows X as they come and packed weights W (D in the type of X unless said otherwise)."""
     m, n, ldx, xkind = _matrix(X)
-    W = _packed(W, "W")
-    if W.n != n:
+    if _packed(W, "W").n != n:
         raise ValueError("inner dimensions differ")
     p = W.rows
-    D = _output(D, X, m, p, dtype or X.dtype, beta)
-    _, _, ldd, dkind = _matrix(D)
-    if workspace is None and workspace_bytes(m, n, p):
-        workspace = alloc_workspace(m, n, p, X.device)
-    _check(_lib.ozimmu_mx_linear(m, n, p, alpha, xkind, X.data_ptr(), ldx, W.data.data_ptr(), beta, dkind, D.data_ptr(), ldd,
-                                 *_room(workspace), ozimmu._stream()))
+    D, ldd, dkind = _output(D, X, m, p, dtype or X.dtype, beta)
+    nbytes = _lib.ozimmu_mx_workspace_bytes(m, n, p) if workspace is None else 0
+    workspace, room, size = _workspace(workspace, nbytes, X)
+    status = _lib.ozimmu_mx_linear(m, n, p, alpha, xkind, X.data_ptr(), ldx, W.data.data_ptr(), beta, dkind, D.data_ptr(), ldd,
+                                   room, size, ozimmu._stream())
+    if status:
+        raise OzimmuError(status)
     return D
 
 
@@ -218,26 +236,27 @@ def linear_backward(G: torch.Tensor, X: Optional[torch.Tensor], Wt: Optional[Pac
         raise ValueError("neither X (for dW) nor Wt (for dX) given")
     if (X is None and dW is not None) or (Wt is None and dX is not None):
         raise ValueError("dW takes X, dX takes Wt")
-    n = X.shape[1] if X is not None and X.dim() == 2 else (Wt.rows if Wt is not None else 0)
     ldx = lddx = lddw = dxkind = dwkind = 0
+    x_at = wt_at = dx_at = dw_at = None
     if X is not None:
-        if X.dtype is not G.dtype:
+        rows, n, ldx, xkind = _matrix(X)
+        if xkind != kind:
             raise ValueError("X and G have to be of one type")
-        mx_, n, ldx, _ = _matrix(X)
-        if mx_ != m:
+        if rows != m:
             raise ValueError("X and G have to have as many rows")
-        dW = _output(dW, G, p, n, torch.float32, beta_w)
-        _, _, lddw, dwkind = _matrix(dW)
+        dW, lddw, dwkind = _output(dW, G, p, n, torch.float32, beta_w)
+        x_at, dw_at = X.data_ptr(), dW.data_ptr()
     if Wt is not None:
-        if _packed(Wt, "Wt").shape != (n, p):
-            raise ValueError(f"Wt of {Wt.shape} for a layer of {n} to {p}")
-        dX = _output(dX, G, m, n, G.dtype, beta_x)
-        _, _, lddx, dxkind = _matrix(dX)
-    if workspace is None:
-        workspace = torch.empty(max(backward_workspace_bytes(m, n, p), 256), dtype=torch.uint8, device=G.device)
-    _check(_lib.ozimmu_mx_linear_backward(m, n, p, alpha, kind, G.data_ptr(), ldg, X.data_ptr() if X is not None else None, ldx,
-                                          Wt.data.data_ptr() if Wt is not None else None, beta_x, dxkind,
-                                          dX.data_ptr() if dX is not None else None, lddx, beta_w, dwkind,
-                                          dW.data_ptr() if dW is not None else None, lddw, workspace.data_ptr(), workspace.numel(),
-                                          ozimmu._stream()))
+        if X is None:
+            n = _packed(Wt, "Wt").rows
+        if _packed(Wt, "Wt").rows != n or Wt.n != p:
+            raise ValueError(f"Wt of {Wt.rows} x {Wt.n} for a layer of {n} to {p}")
+        dX, lddx, dxkind = _output(dX, G, m, n, G.dtype, beta_x)
+        wt_at, dx_at = Wt.data.data_ptr(), dX.data_ptr()
+    nbytes = _lib.ozimmu_mx_backward_workspace_bytes(m, n, p) if workspace is None else 0
+    workspace, room, size = _workspace(workspace, nbytes, G)
+    status = _lib.ozimmu_mx_linear_backward(m, n, p, alpha, kind, G.data_ptr(), ldg, x_at, ldx, wt_at, beta_x, dxkind, dx_at, lddx, beta_w,
+                                            dwkind, dw_at, lddw, room, size, ozimmu._stream())
+    if status:
+        raise OzimmuError(status)
     return dX, dW
