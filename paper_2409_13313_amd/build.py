@@ -17,6 +17,7 @@ SOURCES = ["ozimmu_api.hip", "ozimmu_split.hip", "ozimmu_gemm.hip", "ozimmu_mx_a
 # ozimmu_resident.hip holds kernels specialised for a slice count: one compilation per count, all of them linked into
 # the object of the chunk GEMM (whoever links that object gets every way to run the schedule)
 RESIDENT_KS = range(3, 17)
+LOOKED_AT = ["ozimmu_mx_gemm.hip"]   # beside those: kernels with asm statements of their own
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]
@@ -45,7 +46,7 @@ def build(verbose: bool = False) -> str:
         with tempfile.TemporaryDirectory() as tmp:
             # (the assembly that becomes the object is kept beside it for a look)
             made = os.path.join(tmp, os.path.basename(obj))
-            cmd = ["hipcc", *FLAGS, *defs, *(["--save-temps=obj"] if defs else []), "-c", os.path.join(CSRC, src), "-o", made]
+            cmd = ["hipcc", *FLAGS, *defs, *(["--save-temps=obj"] if defs or src in LOOKED_AT else []), "-c", os.path.join(CSRC, src), "-o", made]
             if verbose:
                 print(" ".join(cmd), flush=True)
             pr = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -54,6 +55,9 @@ def build(verbose: bool = False) -> str:
                 raise RuntimeError(f"hipcc failed: {' '.join(cmd)}\n{out}")
             if verbose and out.strip():
                 print(out)
+            if src in LOOKED_AT:
+                text, = (open(f).read() for f in glob.glob(os.path.join(tmp, "*gfx950*.s")))
+                codegen.check_mx(text)
             if defs:
                 text, = (open(f).read() for f in glob.glob(os.path.join(tmp, "*gfx950*.s")))
                 seen = codegen.check_resident(text, int(defs[0].split("=")[1]))

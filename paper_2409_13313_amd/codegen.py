@@ -162,3 +162,111 @@ def check_kernels(text: str, k: int) -> dict:
 def check_resident(text: str, k: int) -> dict:
     """check_kernels, which looks at k_held too, with the counts of the others."""
     return {kind: count for kind, count in check_kernels(text, k).items() if kind != "k_held"}
+
+
+# ---- the product of microscaled 4-bit matrices (csrc/ozimmu_mx_gemm.hip) ----
+#
+# k_mx_tile and k_mx_half rest on asm statements too: copies into LDS counted by hand, whose operands have to be scalar registers that a scalar
+# instruction wrote (a vector instruction that writes a scalar register wants SGPR_WAIT_STATES before a memory instruction reads it, and the
+# compiler does not put them before an asm statement); M0 shared by the copies of a piece; sums that are read out of their accumulation registers.
+MX_MFMA = "v_mfma_scale_f32_16x16x128_f8f6f4"
+MX_KERNEL = re.compile(r"^(_ZN12_GLOBAL__N_1\d+(k_mx_tile|k_mx_half)ILi(\d)EEEv\w+):(.*?)^\.Lfunc_end", re.S | re.M)
+SGPR_WAIT_STATES = 5
+
+
+def scalar_registers(operand: str) -> set:
+    """numbers of the scalar registers in s5, s[4:7]"""
+    m = re.fullmatch(r"s(?:(\d+)|\[(\d+):(\d+)\])", operand.strip())
+    if not m:
+        return set()
+    lo, hi = (int(m.group(1)),) * 2 if m.group(1) else (int(m.group(2)), int(m.group(3)))
+    return set(range(lo, hi + 1))
+
+
+def _operands(code: str) -> list:
+    return re.findall(r"[sva](?:\d+|\[\d+:\d+\])", code.partition(" ")[2])
+
+
+def check_mx_scalars(code: list, by_hand: set, what: tuple) -> None:
+    """No vector instruction writes a scalar operand of a hand-written memory instruction within the wait states before it, on any way there."""
+    at_branch = {}
+    for i, c in enumerate(code):
+        m = re.match(r"s_c?branch\w* (\.LBB\w+)", c)
+        if m:
+            at_branch.setdefault(m.group(1) + ":", []).append(i)
+
+    def look(i, states, used, who):
+        while i >= 0 and states < SGPR_WAIT_STATES:
+            c = code[i]
+            if c.startswith(".LBB"):
+                for j in at_branch.get(c, []):
+                    look(j, states, used, who)
+            elif c.startswith("s_branch"):
+                return                       # (not reached from above)
+            else:
+                if c.startswith("v_") and not c.startswith("v_mfma"):
+                    first = _operands(c)[:1]
+                    _require(not (first and scalar_registers(first[0]) & used), what, c, who)
+                states += _wait_states(c)
+            i -= 1
+
+    for i in sorted(by_hand):
+        if re.match(r"(buffer|global)_", code[i]):
+            look(i - 1, 0, set().union(*map(scalar_registers, _operands(code[i]))), code[i])
+
+
+def check_mx_body(body: str, kind: str, what: tuple) -> None:
+    code, by_hand, hand = [], set(), False
+    for line in body.split("\n"):
+        if "#ASMSTART" in line or "#ASMEND" in line:
+            hand = "#ASMSTART" in line
+            continue
+        c = line.split(";")[0].strip()
+        if not c or (c.startswith(".") and not c.startswith(".LBB")):
+            continue
+        if hand:
+            by_hand.add(len(code))
+        code.append(c)
+    mfma = [i for i, c in enumerate(code) if c.startswith(MX_MFMA)]
+    _require(len(mfma) == {"k_mx_tile": 64, "k_mx_half": 32}[kind], what, "matrix instructions", len(mfma))
+    for i in mfma:
+        d, _, _, c = re.findall(r"[va]\[\d+:\d+\]", code[i])[:4]
+        _require(d == c and d.startswith("a"), what, code[i])
+    # (the loop: from its label to the branch back)
+    begin = max(i for i, c in enumerate(code) if c.startswith(".LBB") and i < mfma[0])
+    end = min(i for i, c in enumerate(code) if i > mfma[-1] and re.match(r"s_cbranch\w+ ", c))
+    waits = 0
+    for i, c in enumerate(code):
+        hand = i in by_hand
+        if re.search(r"\bm0\b", c):
+            _require(hand and c.startswith("s_mov_b32 m0, s") and code[i + 1] == "s_nop 0" and i + 1 in by_hand, what, c)
+        _require(not c.startswith("scratch_"), what, c)
+        if begin <= i <= end:
+            waits += "vmcnt" in c
+            _require(hand or "vmcnt" not in c, what, c)
+            _require(hand or not re.match(r"(buffer|global|flat)_|v_accvgpr", c), what, c)
+    _require(waits == 2, what, "waits for copies", waits)
+    _require(sum(c.startswith("s_barrier") for c in code[begin:end + 1]) == 1, what, "barriers in the loop")
+    reads = [i for i, c in enumerate(code) if c.startswith("v_accvgpr_read")]
+    _require(reads and all(i in by_hand for i in reads), what, "sums read by the compiler")
+    nops = [i for i in range(end, reads[0]) if code[i] == "s_nop 15" and i in by_hand]
+    _require(reads[0] > end and len(nops) == 2, what, "no wait states between the products and the reads of their sums")
+    for i in by_hand:
+        if code[i].startswith("global_store_dwordx4"):
+            _require(code[i + 1] == "s_nop 1" and i + 1 in by_hand, what, code[i])
+    check_mx_scalars(code, by_hand, what)
+
+
+def check_mx(text: str) -> dict:
+    """Looks at every tile kernel in the assembly of ozimmu_mx_gemm.hip; raises Wrong, also where one is missing."""
+    seen = {"k_mx_tile": 0, "k_mx_half": 0}
+    for m in MX_KERNEL.finditer(text):
+        name, kind, what = m.group(1), m.group(2), (m.group(2), int(m.group(3)))
+        check_mx_body(m.group(4), kind, what)
+        at = text.index(".name:           " + name)
+        about = text[text.rindex("- .agpr_count", 0, at):text.find("- .agpr_count", at)]
+        for key in ("private_segment_fixed_size", "vgpr_spill_count", "sgpr_spill_count"):
+            _require(re.search(r"\.%s:\s+(\d+)" % key, about).group(1) == "0", what, key)
+        seen[kind] += 1
+    _require(seen == {"k_mx_tile": 3, "k_mx_half": 3}, "kernels in the assembly", seen)
+    return seen

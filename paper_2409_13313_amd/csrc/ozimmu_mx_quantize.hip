@@ -9,9 +9,6 @@ namespace {
 using namespace mxk;
 using namespace mxl;
 
-// Blocks along the rows.  A workgroup takes 64 rows x 128 columns (a quarter of a tile): thread t the eight elements t % 16 of
-// the four rows at place t / 16 of the fragments, so that 16 lanes read 128 columns of a row side by side; four lanes hold a block and
-// share its maximum.
 // (largest of the four lanes of a quad, in all of them)
 __device__ inline uint32_t quad_max(uint32_t m)
 {
@@ -21,42 +18,52 @@ __device__ inline uint32_t quad_max(uint32_t m)
     return b > m ? b : m;
 }
 
-// COUNT (2 or 4) of the four fragments' rows at a place, from fragment `first` on
-template <int TYPE, int COUNT>
-__device__ inline void quantize_rows(const typename Elem<TYPE>::Bits (*x)[8], int64_t row0, int first, int64_t rows, uint8_t* tile, int chunk)
+constexpr int64_t BLOCKS_Y = 32768;  // (there may be more blocks of rows than a grid has in its second dimension)
+inline dim3 grid_of(int64_t cols, int64_t blocks)
 {
-    const int c = chunk >> 2, sub = chunk & 3;
+    return dim3((unsigned)cols, (unsigned)(blocks < BLOCKS_Y ? blocks : BLOCKS_Y), (unsigned)((blocks + BLOCKS_Y - 1) / BLOCKS_Y));
+}
+
+// Blocks along the rows.  A workgroup takes 32 rows x 128 columns (half a quarter of a tile, its fragments 0 and 1 or 2 and 3): thread t the
+// eight elements t % 16 of the two rows at place t / 16, so that 16 lanes read 128 columns of a row side by side; four lanes hold a block and
+// share its maximum.  (64 rows: 8192 x 4096 bf16 17.7 us.)
+struct RowsAt {
+    int64_t row0;  // the place's row in fragment 0 of the quarter
+    int first;     // the first of the two fragments
+    __device__ inline RowsAt(int64_t block) : row0(block / 2 * 64 + row_of(0, (int)threadIdx.x >> 4)), first((int)(block % 2) * 2) {}
+    __device__ inline int64_t row(int i) const { return row0 + row_of(first + i, 0); }
+};
+template <int TYPE>
+__device__ inline void load_rows(typename Elem<TYPE>::Bits (&x)[2][8], const typename Elem<TYPE>::Bits* X, int64_t ldx, int64_t rows, int64_t n,
+                                 const RowsAt& at, int64_t col)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_row<TYPE, 8>(X + at.row(i) * ldx + col, at.row(i) < rows ? n - col : 0, x[i]);
+}
+template <int TYPE>
+__device__ inline void quantize_rows(const typename Elem<TYPE>::Bits (&x)[2][8], const RowsAt& at, int64_t rows, uint8_t* row_tiles, int64_t KT, int64_t kt)
+{
+    const int chunk = threadIdx.x & 15, c = chunk >> 2, sub = chunk & 3;
+    uint8_t* const tile = row_tiles + ((at.row0 / TILE_R) * KT + kt) * TILE_BYTES;
     uint32_t scales = 0;
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
+    for (int i = 0; i < 2; ++i) {
         const uint32_t b = scale_byte(f32_bits<TYPE>(quad_max(max_magnitude<TYPE, 8>(x[i]))));
         scales |= b << (8 * i);
-        const int64_t row = row0 + row_of(first + i, 0);
-        if (row < rows) *(uint32_t*)(tile + code_offset((int)(row % TILE_R), c) + 4 * sub) = codes8<TYPE>(x[i], scale_value(b));
+        if (at.row(i) < rows) *(uint32_t*)(tile + code_offset((int)(at.row(i) % TILE_R), c) + 4 * sub) = codes8<TYPE>(x[i], scale_value(b));
     }
-    // (the scales of rows that are not there are those of zeros)
-    if (sub == 0 && row0 + row_of(first, 0) < rows) {
-        uint8_t* const at = tile + scale_offset((int)(row0 % TILE_R), c) + first;
-        if constexpr (COUNT == 4)
-            *(uint32_t*)at = scales;
-        else
-            *(uint16_t*)at = (uint16_t)scales;
-    }
+    // (the scale of a row that is not there is that of zeros)
+    if (sub == 0 && at.row(0) < rows) *(uint16_t*)(tile + scale_offset((int)(at.row(0) % TILE_R), c)) = (uint16_t)scales;
 }
 
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_mx_quantize_rows(int64_t rows, int64_t n, const typename Elem<TYPE>::Bits* X, int64_t ldx,
                                                           uint8_t* out, int64_t KT)
 {
-    typename Elem<TYPE>::Bits x[4][8];
-    const int t = threadIdx.x, chunk = t & 15;
-    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + row_of(0, t >> 4), col = kt * TILE_K + chunk * 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + row_of(i, 0);
-        load_row<TYPE, 8>(X + row * ldx + col, row < rows ? n - col : 0, x[i]);
-    }
-    quantize_rows<TYPE, 4>(x, row0, 0, rows, out + ((row0 / TILE_R) * KT + kt) * TILE_BYTES, chunk);
+    typename Elem<TYPE>::Bits x[2][8];
+    const RowsAt at((int64_t)blockIdx.z * BLOCKS_Y + blockIdx.y);
+    load_rows<TYPE>(x, X, ldx, rows, n, at, (int64_t)blockIdx.x * TILE_K + (threadIdx.x & 15) * 8);
+    quantize_rows<TYPE>(x, at, rows, out, KT, blockIdx.x);
 }
 
 // Blocks along the columns, and along the rows too where by_row is given.  A workgroup takes 32 rows x 128 columns, read as above (rows
@@ -75,18 +82,12 @@ template <int TYPE> struct Columns {
     {
         const int t = threadIdx.x, chunk = t & 15;
         const int64_t col0 = tile_col * 128;
-        // half a quarter of the rows: fragments 0 and 1, or 2 and 3
-        const int64_t row0 = block / 2 * 64 + row_of(0, t >> 4);
-        const int first = (int)(block % 2) * 2;
+        const RowsAt at(block);
         Bits x[2][8];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t row = row0 + row_of(first + i, 0);
-            load_row<TYPE, 8>(X + row * ldx + col0 + chunk * 8, row < rows ? n - col0 - chunk * 8 : 0, x[i]);
-        }
+        load_rows<TYPE>(x, X, ldx, rows, n, at, col0 + chunk * 8);
 #pragma unroll
         for (int i = 0; i < 2; ++i) __builtin_memcpy(held + row_of(i, t >> 4) * 128 + chunk * 8, x[i], 8 * sizeof(Bits));
-        if (by_row) quantize_rows<TYPE, 2>(x, row0, first, rows, by_row + ((row0 / TILE_R) * KT_row + tile_col) * TILE_BYTES, chunk);
+        if (by_row) quantize_rows<TYPE>(x, at, rows, by_row, KT_row, tile_col);
         __syncthreads();
         const int64_t col = col0 + t;
         if (t >= 128 || col >= n) return;
@@ -104,7 +105,6 @@ template <int TYPE> struct Columns {
     }
 };
 
-constexpr int64_t BLOCKS_Y = 32768;  // (there may be more blocks of rows than a grid has in its second dimension)
 template <int TYPE> __global__ __launch_bounds__(256) void k_mx_quantize_cols(Columns<TYPE> c)
 {
     __shared__ __align__(16) typename Elem<TYPE>::Bits held[BLOCK * 128];
@@ -123,29 +123,44 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_quantize_cols2(C
     c.run(at % tiles, at / tiles, held);
 }
 
-// Reading back: the same threads as k_mx_quantize_rows.
-template <int TYPE>
+// Reading back: a lane makes 16 bytes, E elements, of a row, side by side with its neighbours (FP32: half of the eight codes that it loads; 32 bytes a
+// lane in two stores: 16384 x 8192 183 us, so 154).  A workgroup takes 64 rows x 128 columns.  STREAM, where rows begin at multiples of 16 bytes: stores
+// past the caches (16384 x 8192 FP32 86 us = 7.1 TB/s, a large fill writes 6.9; bf16 49 and 64; rows that begin anywhere: 1001 x 4099 bf16 5.6 us,
+// plain stores 4.5).
+template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t n, const uint8_t* in, typename Elem<TYPE>::Bits* X,
                                                        int64_t ldx, int64_t KT)
 {
     typedef typename Elem<TYPE>::Bits Bits;
-    const int t = threadIdx.x, chunk = t & 15, c = chunk >> 2, sub = chunk & 3;
-    const int64_t kt = blockIdx.x, row0 = (int64_t)blockIdx.y * 64 + row_of(0, t >> 4);
-    const int64_t col = kt * TILE_K + chunk * 8;
-    if (row0 >= rows || col >= n) return;
-    const uint8_t* const tile = in + ((row0 / TILE_R) * KT + kt) * TILE_BYTES;
-    const uint32_t scales = *(const uint32_t*)(tile + scale_offset((int)(row0 % TILE_R), c));
-    uint32_t codes[4];
+    constexpr int E = 16 / sizeof(Bits), LANES = 128 / E, PLACES = 256 / LANES;  // lanes to a row, places of a fragment at a time
+    const int t = threadIdx.x, lane = t % LANES, chunk = lane * E / 8, c = chunk >> 2, sub = chunk & 3;
+    const int64_t kt = blockIdx.x, quarter = (int64_t)blockIdx.y * 64, col = kt * TILE_K + lane * E;
+    if (col >= n) return;
+    const uint8_t* const tile = in + ((quarter / TILE_R) * KT + kt) * TILE_BYTES;
+    uint32_t scales[16 / PLACES], codes[16 / PLACES][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) codes[i] = *(const uint32_t*)(tile + code_offset((int)(row0 % TILE_R) + row_of(i, 0), c) + 4 * sub);
+    for (int h = 0; h < 16 / PLACES; ++h) {
+        const int r = (int)(quarter % TILE_R) + row_of(0, h * PLACES + t / LANES);
+        scales[h] = *(const uint32_t*)(tile + scale_offset(r, c));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + row_of(i, 0);
-        if (row >= rows) break;
-        Bits x[8];
-        values8<TYPE>(codes[i], (scales >> (8 * i)) & 255u, x);
-        store_row<TYPE, 8>(X + row * ldx + col, n - col, x);
+        for (int i = 0; i < 4; ++i) codes[h][i] = *(const uint32_t*)(tile + code_offset(r + row_of(i, 0), c) + 4 * sub);
     }
+#pragma unroll
+    for (int h = 0; h < 16 / PLACES; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = quarter + row_of(i, h * PLACES + t / LANES);
+            if (row >= rows) continue;
+            Bits x[8];
+            values8<TYPE>(E == 4 ? codes[h][i] >> (lane % 2 * 16) : codes[h][i], (scales[h] >> (8 * i)) & 255u, x);
+            if (STREAM && n - col >= E) {
+                v4i y;
+                __builtin_memcpy(&y, x, 16);
+                __builtin_nontemporal_store(y, (v4i*)(X + row * ldx + col));
+            } else {
+                store_row<TYPE, E>(X + row * ldx + col, n - col, x);
+            }
+        }
 }
 
 // Plain layout -> packed and back: one thread a block.
@@ -192,14 +207,11 @@ template <int TYPE> Columns<TYPE> columns(const Quantize& q)
 
 template <int TYPE> void quantize(const Quantize& q, hipStream_t st)
 {
-    if (q.by_col) {
-        const int64_t blocks = 4 * inner_tiles(q.rows);
-        const dim3 grid((unsigned)inner_tiles(q.n), (unsigned)(blocks < BLOCKS_Y ? blocks : BLOCKS_Y), (unsigned)((blocks + BLOCKS_Y - 1) / BLOCKS_Y));
-        k_mx_quantize_cols<TYPE><<<grid, dim3(256), 0, st>>>(columns<TYPE>(q));
-    } else {
-        k_mx_quantize_rows<TYPE><<<dim3((unsigned)inner_tiles(q.n), (unsigned)((q.rows + 63) / 64)), dim3(256), 0, st>>>(
+    if (q.by_col)
+        k_mx_quantize_cols<TYPE><<<grid_of(inner_tiles(q.n), 4 * inner_tiles(q.rows)), dim3(256), 0, st>>>(columns<TYPE>(q));
+    else
+        k_mx_quantize_rows<TYPE><<<grid_of(inner_tiles(q.n), (q.rows + BLOCK - 1) / BLOCK), dim3(256), 0, st>>>(
             q.rows, q.n, (const typename Elem<TYPE>::Bits*)q.X, q.ldx, (uint8_t*)q.by_row, inner_tiles(q.n));
-    }
 }
 
 template <int TYPE> void quantize2(const Quantize& a, const Quantize& b, hipStream_t st)
@@ -210,8 +222,12 @@ template <int TYPE> void quantize2(const Quantize& a, const Quantize& b, hipStre
 
 template <int TYPE> void dequantize(int64_t rows, int64_t n, const void* packed, void* X, int64_t ldx, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_mx_dequantize<TYPE>, dim3((unsigned)inner_tiles(n), (unsigned)((rows + 63) / 64)), dim3(256), 0, st, rows, n,
-                       (const uint8_t*)packed, (typename Elem<TYPE>::Bits*)X, ldx, inner_tiles(n));
+    typedef typename Elem<TYPE>::Bits Bits;
+    const dim3 grid((unsigned)inner_tiles(n), (unsigned)((rows + 63) / 64));
+    if (((uintptr_t)X | (uintptr_t)(ldx * (int64_t)sizeof(Bits))) % 16 == 0)
+        k_mx_dequantize<TYPE, true><<<grid, dim3(256), 0, st>>>(rows, n, (const uint8_t*)packed, (Bits*)X, ldx, inner_tiles(n));
+    else
+        k_mx_dequantize<TYPE, false><<<grid, dim3(256), 0, st>>>(rows, n, (const uint8_t*)packed, (Bits*)X, ldx, inner_tiles(n));
 }
 
 }  // namespace
@@ -228,8 +244,8 @@ hipError_t launch_quantize(int type, const Quantize& q, hipStream_t st)
 
 hipError_t launch_quantize2(int type, const Quantize& a, const Quantize& b, hipStream_t st)
 {
-    // (work items of a launch are counted in 32 bits)
-    if (4 * (inner_tiles(a.rows) * inner_tiles(a.n) + inner_tiles(b.rows) * inner_tiles(b.n)) >= (int64_t)1 << 24) {
+    // (large ones one after the other: 8192 x 8192 both ways and 8192 x 4096 by columns 57 us, in one launch 71)
+    if (4 * (inner_tiles(a.rows) * inner_tiles(a.n) + inner_tiles(b.rows) * inner_tiles(b.n)) > 4096) {
         const hipError_t e = launch_quantize(type, a, st);
         return e != hipSuccess ? e : launch_quantize(type, b, st);
     }

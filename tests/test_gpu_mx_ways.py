@@ -63,3 +63,36 @@ def test_again_and_again(mx, way):
         D = torch.full((m, p), float("nan"), dtype=torch.bfloat16, device="cuda")
         mx.gemm(PA, PB, D=D, way=way)
         assert torch.equal(D, first), k
+
+
+# few rows, quantised on the way: every number of fragments a workgroup and of tiles at a time, more than one group of 16 rows
+FEW = [(3, 700, 200), (10, 700, 200), (4, 1030, 5000), (13, 1030, 5000), (2, 1100, 9000), (12, 1100, 9000), (12, 900, 20000), (16, 2050, 16500),
+       (40, 1500, 3000), (64, 33, 4000), (17, 4099, 64), (50, 129, 130)]
+
+
+@pytest.mark.parametrize("m,n,p", FEW)
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_few_rows(mx, m, n, p, kind):
+    print(f"few {m} x {n} x {p} {kind}", flush=True)
+    assert mx.workspace_bytes(m, n, p) == 0                 # (what takes one launch needs none)
+    W = matrix(p, n, "bf16", p + n)
+    PW, _ = mx.quantize(W)
+    qw = ref.read_back(f64(W))
+    for pad in (0, 1, 8):
+        X = matrix(m, n, kind, m + n + pad, pad=pad)
+        want, size = product(ref.read_back(f64(X)), qw)
+        bound = n * 2.0 ** -23 * size
+        for out in TYPES:
+            check(mx.linear(X, PW, dtype=TYPES[out]), want, bound, out, n, f"{kind} to {out}, pad {pad}")
+
+
+def test_gradient_of_a_large_layer(mx):
+    """Each launch by itself, tiles of every size."""
+    m, n, p = 4096, 2048, 2304
+    X, W, G = matrix(m, n, "bf16", 1), matrix(p, n, "bf16", 2), matrix(m, p, "bf16", 3, std=1e-3)
+    _, Wt = mx.quantize(W, rows=False, cols=True)
+    dX, dW = mx.linear_backward(G, X, Wt)
+    want, size = product(ref.read_back(f64(G)), ref.read_back(f64(W).T))
+    check(dX, want, p * 2.0 ** -23 * size, "bf16", p, "dX")
+    want, size = product(ref.read_back(f64(G).T), ref.read_back(f64(X).T))
+    check(dW, want, m * 2.0 ** -23 * size, "f32", m, "dW")
