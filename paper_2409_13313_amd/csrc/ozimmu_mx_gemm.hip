@@ -474,6 +474,9 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
                 acc[i][j] = v4f{0, 0, 0, 0};
                 asm volatile("" : "+a"(acc[i][j]));  // (in its accumulation registers from here on)
             }
+        // Nothing is outstanding here (lgkmcnt 0, said to the compiler): at the top of the loop it then waits for the loads that a stage
+        // begins with.  It would wait for all of them otherwise, the last of which was issued just before.
+        __builtin_amdgcn_s_waitcnt(0xc07f);
         for (int it = 0; it < KT; ++it) {
             // quarter 0: the upper half of B comes in, the first copies of B go out
             static_for<0, 4>([&](auto Q) {
@@ -783,6 +786,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_half(Gemm g, int
                 acc[i][j] = v4f{0, 0, 0, 0};
                 asm volatile("" : "+a"(acc[i][j]));
             }
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // (as above)
         for (int it = 0; it < KT; ++it) {
             // (A lo, B): the upper half of A comes in, early, so that it is there at the barrier; the rest of the copies
             static_for<0, 4>([&](auto Q) {
