@@ -228,25 +228,27 @@ def check_mx_body(body: str, kind: str, what: tuple) -> None:
             by_hand.add(len(code))
         code.append(c)
     mfma = [i for i, c in enumerate(code) if c.startswith(MX_MFMA)]
-    _require(len(mfma) == {"k_mx_tile": 64, "k_mx_half": 32}[kind], what, "matrix instructions", len(mfma))
+    stage = {"k_mx_tile": 64, "k_mx_half": 32}[kind]
+    _require(len(mfma) == 2 * stage, what, "matrix instructions", len(mfma))
     for i in mfma:
         d, _, _, c = re.findall(r"[va]\[\d+:\d+\]", code[i])[:4]
         _require(d == c and d.startswith("a"), what, code[i])
-    # (the loop: from its label to the branch back)
-    begin = max(i for i, c in enumerate(code) if c.startswith(".LBB") and i < mfma[0])
-    end = min(i for i, c in enumerate(code) if i > mfma[-1] and re.match(r"s_cbranch\w+ ", c))
-    waits = 0
     for i, c in enumerate(code):
-        hand = i in by_hand
         if re.search(r"\bm0\b", c):
-            _require(hand and c.startswith("s_mov_b32 m0, s") and code[i + 1] == "s_nop 0" and i + 1 in by_hand, what, c)
+            _require(i in by_hand and re.match(r"s_add_u32 m0, s\d+, s\d+$", c) and not code[i + 1].endswith(" lds"), what, c)
         _require(not c.startswith("scratch_"), what, c)
-        if begin <= i <= end:
-            waits += "vmcnt" in c
-            _require(hand or "vmcnt" not in c, what, c)
-            _require(hand or not re.match(r"(buffer|global|flat)_|v_accvgpr", c), what, c)
-    _require(waits == 2, what, "waits for copies", waits)
-    _require(sum(c.startswith("s_barrier") for c in code[begin:end + 1]) == 1, what, "barriers in the loop")
+    # (the two loops over stages: each from its label to the branch back)
+    for first, last in ((mfma[0], mfma[stage - 1]), (mfma[stage], mfma[-1])):
+        begin = max(i for i, c in enumerate(code) if c.startswith(".LBB") and i < first)
+        end = min(i for i, c in enumerate(code) if i > last and re.match(r"s_cbranch\w+ ", c))
+        _require(begin > mfma[stage - 1] or first == mfma[0], what, "stages that are not loops of their own")
+        waits = 0
+        for i in range(begin, end + 1):
+            waits += "vmcnt" in code[i]
+            _require(i in by_hand or "vmcnt" not in code[i], what, code[i])
+            _require(i in by_hand or not re.match(r"(buffer|global|flat)_|v_accvgpr", code[i]), what, code[i])
+        _require(waits == 1, what, "waits for copies", waits)
+        _require(sum(c.startswith("s_barrier") for c in code[begin:end + 1]) == 1, what, "barriers in the loop")
     reads = [i for i, c in enumerate(code) if c.startswith("v_accvgpr_read")]
     _require(reads and all(i in by_hand for i in reads), what, "sums read by the compiler")
     nops = [i for i in range(end, reads[0]) if code[i] == "s_nop 15" and i in by_hand]

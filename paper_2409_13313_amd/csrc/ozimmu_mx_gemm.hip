@@ -194,8 +194,8 @@ void direct(const Gemm& g, const Gemm* also, hipStream_t st)
 // matrix instructions a wave, run as four quarters of 4 x 4 fragments on four sets of four fragments (16 bytes a lane each) and one
 // register of scales: (A lo, B lo), (A lo, B hi), (A hi, B lo), (A hi, B hi).  Quarter 0 fetches B hi, quarter 1 A hi, quarters 2 and 3
 // A lo and B lo of the next stage, so that a fragment is on its way 8 to 16 matrix instructions ahead of its first use.
-// A scaled matrix instruction takes three of its four issue slots itself (a second vector instruction beside it costs 4 cycles), so
-// everything else is spread: one fetch every four of them, a copy every six.
+// A scaled matrix instruction takes three of its four issue slots itself (a second instruction beside it costs 4 cycles, a branch 40 and more),
+// so a stage has 52 other instructions for its 64, one behind a product at a time, and no branch but the one at its end.
 // One barrier a stage, in its middle, where every wave has fetched all of the stage and its own copies of the next one have landed: behind
 // it the stage's place in the ring takes the copies of the fourth stage from here.  Ten copies a wave and stage; those behind the last
 // stage are out of the buffer's range: they read nothing, but count, so that every stage waits alike.
@@ -203,6 +203,13 @@ constexpr int RING = 4, STAGE_BYTES = 2 * TILE_BYTES, COPIES = 10;
 constexpr int NXCD = 8, BAND = 8;
 constexpr int64_t MEMORY_SIDE_CACHE = (int64_t)256 << 20;
 
+// (by the builtin: the compiler then knows, and waits for none of them again)
+template <int N> __device__ inline void wait_lds()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f | N << 8);  // lgkmcnt(N)
+    asm volatile("" ::: "memory");
+}
 template <int N> __device__ inline void wait_vmcnt() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // Workgroup b runs on XCD b % 8.  The tiles are cut into eight contiguous ranges, one an XCD, in bands of 8 tile rows walked column by
@@ -229,34 +236,34 @@ struct Order {
     }
 };
 
-// What is copied next of an operand: the address of the tile (or half of it), its bytes (0: nothing is read), how many stages of the output
-// tile are left.  Copies are a ring ahead at most and an output tile has at least as many stages, so that the operand tiles behind it
-// (`after`) are looked up once an output tile, outside the loop over its stages: there is no branch in there.  (All of it stays in scalar
+// Where the copies of an operand come from, as buffers: of the output tile at hand, and of the next one (no bytes: behind the last; nothing is
+// read).  The copy of a stage is at the start of the buffer + the stage's offset, which runs from 0 to `stages` tiles in every output tile and
+// is the same for A and B; the copies are AHEAD stages ahead, so the buffer of this output tile starts that much later, and that of the next
+// one, which takes over within the loop, that much before its tiles.  The bytes are all that any offset reaches.  (All of it stays in scalar
 // registers that scalar instructions write: the copies below are asm statements, and the compiler would not put the wait states between a
 // vector instruction that writes their operands and them.)
 struct Source {
-    uint64_t at, after;
-    int bytes, bytes_after, left;
-    __device__ inline v4i resource() const { return v4i{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), bytes, 0x00020000}; }
-    __device__ inline void next(int stages)
-    {
-        --left;
-        const bool over = left == 0;
-        at = over ? after : at + TILE_BYTES;
-        bytes = over ? bytes_after : bytes;
-        left = over ? stages : left;
-    }
+    v4i now;
+    uint64_t after;
+    int bytes_after;
+    __device__ inline void point(uint64_t at, int bytes) { now = v4i{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), bytes, 0x00020000}; }
+    __device__ inline uint64_t at() const { return (uint64_t)(uint32_t)now[1] << 32 | (uint32_t)now[0]; }
+    __device__ inline void move(int64_t by) { point(at() + by, now[2]); }
+    // the next output tile from here on: copies of its stage 0 at offset `stage` x TILE_BYTES
+    __device__ inline void switch_over(int stage) { point(after - (uint64_t)stage * TILE_BYTES, bytes_after); }
 };
 
-// Copy Q of a quarter of a tile: 256 bytes of scales (Q = 0, which sets M0 to the quarter's place in LDS for the others too) or a fragment.
-// Lane i writes LDS bytes [M0 + offset + its 4 or 16 bytes); the instruction's offset moves both addresses alike; one wait state
-// separates the write of M0 from the copy.
-template <int Q> __device__ inline void copy_quarter(uint32_t m0, uint32_t voff4, uint32_t voff16, v4i source)
+// M0: the place in LDS that the next copies go to.  (At least one instruction has to stand between this and the first of them.)
+__device__ inline void copy_to(uint32_t place, uint32_t wave_part) { asm volatile("s_add_u32 m0, %0, %1" ::"s"(place), "s"(wave_part) : "memory", "scc"); }
+
+// Copy Q of a quarter of a tile: 256 bytes of scales (Q = 0) or a fragment.  Lane i writes LDS bytes [M0 + the instruction's offset + its 4 or
+// 16 bytes); that offset moves both addresses alike, `off` only the one in memory.
+template <int Q> __device__ inline void copy_quarter(uint32_t voff4, uint32_t voff16, v4i source, uint32_t off)
 {
     if constexpr (Q == 0)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(m0), "v"(voff4), "s"(source) : "memory");
+        asm volatile("buffer_load_dword %0, %1, %2 offen lds" ::"v"(voff4), "s"(source), "s"(off) : "memory");
     else
-        asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" ::"v"(voff16), "s"(source), "n"(SCALE_BYTES + (Q - 1) * FRAGMENT_BYTES)
+        asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" ::"v"(voff16), "s"(source), "s"(off), "n"(SCALE_BYTES + (Q - 1) * FRAGMENT_BYTES)
                      : "memory");
 }
 
@@ -320,7 +327,7 @@ __device__ inline void put8_whole(uint64_t base, uint32_t off, float alpha, cons
 // columns.  whole: all of the workgroup's tile lies inside D; true is returned where that many stores were made, one for every two fragments (in
 // FP32: each).
 template <int TYPE, int NJ>
-__device__ inline bool put_tile(const Gemm& g, v4f (&acc)[8][NJ], int64_t row0, int64_t col0, bool whole_tile, bool stream, int lane)
+__device__ __attribute__((always_inline)) inline bool put_tile(const Gemm& g, v4f (&acc)[8][NJ], int64_t row0, int64_t col0, bool whole_tile, bool stream, int lane)
 {
     typedef typename Elem<TYPE>::Bits Bits;
     typedef __attribute__((address_space(1))) Bits Global;
@@ -387,7 +394,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
     const int wm = wave >> 1, wn = wave & 1;
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
     const uint32_t voff4 = wave * QUARTER_BYTES + lane * 4, voff16 = wave * QUARTER_BYTES + lane * 16;
-    const uint32_t m0_wave = lds + wave * QUARTER_BYTES;
+    const uint32_t m0_a = lds + wave * QUARTER_BYTES, m0_b = m0_a + TILE_BYTES;
     typedef __attribute__((address_space(3))) const v4i* lds_v4i;
     typedef __attribute__((address_space(3))) const int* lds_int;
     // this lane's bytes of fragment 0 and of the scales in the wave's first quarter of A and of B, in ring place 0
@@ -396,49 +403,53 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
     const uint32_t scaleA = lds + 2 * wm * QUARTER_BYTES + lane * 4;
     const uint32_t scaleB = lds + TILE_BYTES + 2 * wn * QUARTER_BYTES + lane * 4;
 
-    Source a = {0, 0, 0, 0, KT}, b = {0, 0, 0, 0, KT};
+    Source a, b;
     Order copy_order(TM, TP);
+    const int operand_bytes = KT * TILE_BYTES;
     auto look_up = [&]() {
         int tm, tp;
         const bool any = copy_order.take(tm, tp);
-        a.bytes_after = b.bytes_after = any ? TILE_BYTES : 0;
+        a.bytes_after = b.bytes_after = any ? operand_bytes : 0;
         if (any) {
-            a.after = (uint64_t)(uintptr_t)g.A + (uint64_t)tm * KT * TILE_BYTES;
-            b.after = (uint64_t)(uintptr_t)g.B + (uint64_t)tp * KT * TILE_BYTES;
+            a.after = (uint64_t)(uintptr_t)g.A + (uint64_t)tm * operand_bytes;
+            b.after = (uint64_t)(uintptr_t)g.B + (uint64_t)tp * operand_bytes;
         }
     };
+    a.after = b.after = 0;
     look_up();
-    a.at = a.after;
-    b.at = b.after;
-    a.bytes = b.bytes = a.bytes_after;
+    a.switch_over(0);
+    b.switch_over(0);
     uint32_t here = 0, to = 0;  // ring offsets: the current stage, the stage that is copied
     auto advance = [](uint32_t& place) { place = place == (RING - 1) * STAGE_BYTES ? 0 : place + STAGE_BYTES; };
-    auto copy_a = [&](auto Q) { copy_quarter<decltype(Q)::value>(m0_wave + to, voff4, voff16, a.resource()); };
-    auto copy_b = [&](auto Q) { copy_quarter<decltype(Q)::value>(m0_wave + to + TILE_BYTES, voff4, voff16, b.resource()); };
+    uint32_t off = 0;  // of the stage, in the operands' buffers
+    auto copy_a = [&](auto Q) { copy_quarter<decltype(Q)::value>(voff4, voff16, a.now, off); };
+    auto copy_b = [&](auto Q) { copy_quarter<decltype(Q)::value>(voff4, voff16, b.now, off); };
     static_for<0, RING>([&](auto S) {
+        copy_to(to, m0_a);
+        asm volatile("s_nop 0");
         static_for<0, COPIES / 2>(copy_a);
         if constexpr (decltype(S)::value < RING - 1) {  // (the main loop begins with the last one's B)
-            a.next(KT);
+            copy_to(to, m0_b);
+            asm volatile("s_nop 0");
             static_for<0, COPIES / 2>(copy_b);
-            b.next(KT);
             advance(to);
+            off += TILE_BYTES;
         }
     });
+    a.move(RING * TILE_BYTES);
+    b.move((RING - 1) * TILE_BYTES);
 
     v4f acc[8][8];
     v4i faL[4], faH[4], fbL[4], fbH[4];
     int saL, saH, sbL, sbH;
-    // half of sub-step S of a quarter: two matrix instructions on fragment S of the set that was fetched last (B's with BY_B) and the other set
-    auto math = [&](const v4i* fa, int sa, const v4i* fb, int sb, auto I0, auto J0, auto S, auto BY_B, auto X0) {
-        static_for<0, 2>([&](auto X) {
-            constexpr int s = decltype(S)::value, x = decltype(X0)::value + decltype(X)::value, y = (s & 1) ? 3 - x : x;
-            constexpr int i = decltype(BY_B)::value ? y : s, j = decltype(BY_B)::value ? s : y;
-            v4f& c = acc[decltype(I0)::value + i][decltype(J0)::value + j];
-            c = mfma<j, i>(fb[j], sb, fa[i], sa, c);
-        });
+    // matrix instruction X of a quarter: four on each fragment of the set that was fetched last (B's with BY_B), there and back over the other
+    auto math = [&](const v4i* fa, int sa, const v4i* fb, int sb, auto I0, auto J0, auto X, auto BY_B) {
+        constexpr int s = decltype(X)::value / 4, x = decltype(X)::value % 4, y = (s & 1) ? 3 - x : x;
+        constexpr int i = decltype(BY_B)::value ? y : s, j = decltype(BY_B)::value ? s : y;
+        v4f& c = acc[decltype(I0)::value + i][decltype(J0)::value + j];
+        c = mfma<j, i>(fb[j], sb, fa[i], sa, c);
     };
     typedef std::integral_constant<int, 0> N0;
-    typedef std::integral_constant<int, 2> N2;
     typedef std::integral_constant<int, 4> N4;
     typedef std::true_type ByB;
     typedef std::false_type ByA;
@@ -454,15 +465,76 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
         fbL[q] = *(lds_v4i)(uintptr_t)(fb_at + q * FRAGMENT_BYTES);
     }
     saL = *(lds_int)(uintptr_t)sa_at;
-    saH = *(lds_int)(uintptr_t)(sa_at + QUARTER_BYTES);
     sbL = *(lds_int)(uintptr_t)sb_at;
-    sbH = *(lds_int)(uintptr_t)(sb_at + QUARTER_BYTES);
 
     // Stores count as copies do.  In the two stages behind the end of a tile, all of whose STORES stores were made, they are newer than
-    // the copies that are waited for and need not be over.
+    // the copies that are waited for and need not be over; those stages have a loop of their own (with the choice between two waits in one
+    // loop: a stage of k_mx_half 772 cycles, without 726).
     constexpr int STORES = TYPE == F32 ? 64 : 32, NEWER = (RING - 2) * COPIES;
     constexpr int NEWER_STORES = NEWER + STORES < 63 ? NEWER + STORES : 63;
-    int fresh = 0;  // stages for which that holds
+    uint32_t fresh = 0;  // the offset of the first stage of the others
+    // (forced inline: the state that it captures has to stay in registers)
+    auto stage = [&](auto FRESH) __attribute__((always_inline)) {
+        wait_lds<0>();
+        // quarter 0: the upper half of B comes in, the first copies of B go out
+        static_for<0, 16>([&](auto X) {
+            constexpr int x = decltype(X)::value;
+            if constexpr (x % 3 == 0 && x < 12) fbH[x / 3] = *(lds_v4i)(uintptr_t)(fb_at + QUARTER_BYTES + x / 3 * FRAGMENT_BYTES);
+            if constexpr (x == 1) copy_to(to, m0_b);
+            if constexpr (x == 2) copy_b(std::integral_constant<int, 0>{});
+            if constexpr (x == 4) sbH = *(lds_int)(uintptr_t)(sb_at + QUARTER_BYTES);
+            if constexpr (x == 5) saH = *(lds_int)(uintptr_t)(sa_at + QUARTER_BYTES);
+            if constexpr (x == 8) copy_b(std::integral_constant<int, 1>{});
+            if constexpr (x == 14) copy_b(std::integral_constant<int, 2>{});
+            math(faL, saL, fbL, sbL, N0{}, N0{}, X, ByB{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        wait_lds<0>();
+        // quarter 1: the upper half of A, early, so that it is there at the barrier
+        static_for<0, 16>([&](auto X) {
+            constexpr int x = decltype(X)::value;
+            if constexpr (x % 2 == 0 && x < 8) faH[x / 2] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + x / 2 * FRAGMENT_BYTES);
+            if constexpr (x == 3) copy_b(std::integral_constant<int, 3>{});
+            if constexpr (x == 9) copy_b(std::integral_constant<int, 4>{});
+            if constexpr (x == 10) {
+                to = here;
+                advance(here);
+            }
+            if constexpr (x == 12) fa_at = fragA + here;
+            if constexpr (x == 13) fb_at = fragB + here;
+            if constexpr (x == 14) sa_at = scaleA + here;
+            if constexpr (x == 15) sb_at = scaleB + here;
+            math(faL, saL, fbH, sbH, N0{}, N4{}, X, ByB{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        wait_vmcnt<decltype(FRESH)::value ? NEWER_STORES : NEWER>();
+        wait_lds<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        // quarter 2: the lower half of A of the next stage (behind the last one: what the ring holds, unused); copies of A
+        static_for<0, 16>([&](auto X) {
+            constexpr int x = decltype(X)::value;
+            if constexpr (x % 3 == 0 && x < 12) faL[x / 3] = *(lds_v4i)(uintptr_t)(fa_at + x / 3 * FRAGMENT_BYTES);
+            if constexpr (x == 1) copy_to(to, m0_a);
+            if constexpr (x == 2) copy_a(std::integral_constant<int, 0>{});
+            if constexpr (x == 4) saL = *(lds_int)(uintptr_t)sa_at;
+            if constexpr (x == 8) copy_a(std::integral_constant<int, 1>{});
+            if constexpr (x == 14) copy_a(std::integral_constant<int, 2>{});
+            math(faH, saH, fbL, sbL, N4{}, N0{}, X, ByA{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        // quarter 3: its lower half of B
+        static_for<0, 16>([&](auto X) {
+            constexpr int x = decltype(X)::value;
+            if constexpr (x % 2 == 0 && x < 8) fbL[x / 2] = *(lds_v4i)(uintptr_t)(fb_at + x / 2 * FRAGMENT_BYTES);
+            if constexpr (x == 1) sbL = *(lds_int)(uintptr_t)sb_at;
+            if constexpr (x == 4) copy_a(std::integral_constant<int, 3>{});
+            if constexpr (x == 10) copy_a(std::integral_constant<int, 4>{});
+            math(faH, saH, fbH, sbH, N4{}, N4{}, X, ByA{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        off += TILE_BYTES;
+    };
     Order order(TM, TP);
     int tm, tp;
     while (order.take(tm, tp)) {
@@ -474,86 +546,23 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
                 acc[i][j] = v4f{0, 0, 0, 0};
                 asm volatile("" : "+a"(acc[i][j]));  // (in its accumulation registers from here on)
             }
-        // Nothing is outstanding here (lgkmcnt 0, said to the compiler): at the top of the loop it then waits for the loads that a stage
-        // begins with.  It would wait for all of them otherwise, the last of which was issued just before.
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-        for (int it = 0; it < KT; ++it) {
-            // quarter 0: the upper half of B comes in, the first copies of B go out
-            static_for<0, 4>([&](auto Q) {
-                constexpr int q = decltype(Q)::value;
-                fbH[q] = *(lds_v4i)(uintptr_t)(fb_at + QUARTER_BYTES + q * FRAGMENT_BYTES);
-                math(faL, saL, fbL, sbL, N0{}, N0{}, Q, ByB{}, N0{});
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (q == 0 || q == 2) copy_b(std::integral_constant<int, q / 2>{});
-                if constexpr (q == 1) a.next(KT);
-                math(faL, saL, fbL, sbL, N0{}, N0{}, Q, ByB{}, N2{});
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            // quarter 1: the upper half of A, early, so that it is there at the barrier
-            static_for<0, 4>([&](auto Q) {
-                constexpr int q = decltype(Q)::value;
-                if constexpr (q < 2) faH[2 * q] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + 2 * q * FRAGMENT_BYTES);
-                if constexpr (q == 2) copy_b(std::integral_constant<int, 3>{});
-                math(faL, saL, fbH, sbH, N0{}, N4{}, Q, ByB{}, N0{});
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (q < 2) faH[2 * q + 1] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + (2 * q + 1) * FRAGMENT_BYTES);
-                if constexpr (q == 1) copy_b(std::integral_constant<int, 2>{});
-                if constexpr (q == 3) copy_b(std::integral_constant<int, 4>{});
-                math(faL, saL, fbH, sbH, N0{}, N4{}, Q, ByB{}, N2{});
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            // (a branch that the compiler does not see: at one that it sees it gathers the matrix instructions behind it)
-            asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(%1)\n1:\n\ts_waitcnt vmcnt(%2)" ::"s"(fresh), "n"(NEWER),
-                         "n"(NEWER_STORES)
-                         : "memory", "scc");
-            --fresh;
-            to = here;
-            advance(here);
-            fa_at = fragA + here;
-            fb_at = fragB + here;
-            sa_at = scaleA + here;
-            sb_at = scaleB + here;
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            // quarter 2: the lower half of A of the next stage (behind the last one: what the ring holds, unused); copies of A
-            int sa_next[2], sb_next[2];
-            static_for<0, 4>([&](auto Q) {
-                constexpr int q = decltype(Q)::value;
-                faL[q] = *(lds_v4i)(uintptr_t)(fa_at + q * FRAGMENT_BYTES);
-                math(faH, saH, fbL, sbL, N4{}, N0{}, Q, ByA{}, N0{});
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (q == 0 || q == 2) copy_a(std::integral_constant<int, q / 2>{});
-                if constexpr (q == 1) {
-                    sa_next[0] = *(lds_int)(uintptr_t)sa_at;
-                    sa_next[1] = *(lds_int)(uintptr_t)(sa_at + QUARTER_BYTES);
-                }
-                if constexpr (q == 3) {
-                    sb_next[0] = *(lds_int)(uintptr_t)sb_at;
-                    sb_next[1] = *(lds_int)(uintptr_t)(sb_at + QUARTER_BYTES);
-                }
-                math(faH, saH, fbL, sbL, N4{}, N0{}, Q, ByA{}, N2{});
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            // quarter 3: its lower half of B
-            static_for<0, 4>([&](auto Q) {
-                constexpr int q = decltype(Q)::value;
-                fbL[q] = *(lds_v4i)(uintptr_t)(fb_at + q * FRAGMENT_BYTES);
-                math(faH, saH, fbH, sbH, N4{}, N4{}, Q, ByA{}, N0{});
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (q == 0) b.next(KT);
-                if constexpr (q > 0) copy_a(std::integral_constant<int, 1 + q>{});
-                math(faH, saH, fbH, sbH, N4{}, N4{}, Q, ByA{}, N2{});
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            saL = sa_next[0];
-            saH = sa_next[1];
-            sbL = sb_next[0];
-            sbH = sb_next[1];
+        off = 0;
+        while (off != fresh) stage(std::true_type{});
+        // until the copies of A are the next output tile's, until those of B are, to the end (fresh stages end before)
+        uint32_t until = (uint32_t)(KT - RING) * TILE_BYTES;
+#pragma clang loop unroll(disable)
+        for (int part = 0; part < 3; ++part) {
+#pragma clang loop unroll(disable)
+            while (off != until) stage(std::false_type{});
+            if (part == 0) a.switch_over(KT - RING);
+            if (part == 1) b.switch_over(KT - RING + 1);
+            until = part == 0 ? (uint32_t)(KT - RING + 1) * TILE_BYTES : (uint32_t)operand_bytes;
         }
+        a.move(operand_bytes);
+        b.move(operand_bytes);
         fresh = put_tile<TYPE, 8>(g, acc, (int64_t)tm * TILE_R + wm * 128, (int64_t)tp * TILE_R + wn * 128,
                                   (int64_t)(tm + 1) * TILE_R <= g.m && (int64_t)(tp + 1) * TILE_R <= g.p, stream, lane)
-                    ? RING - 2
+                    ? (uint32_t)(KT - RING < RING - 2 ? KT - RING : RING - 2) * TILE_BYTES
                     : 0;
     }
     wait_vmcnt<0>();  // no copy may still be writing LDS when the workgroup retires
@@ -709,56 +718,55 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_half(Gemm g, int
     const uint32_t fragA = lds + 2 * wm * QUARTER_BYTES + SCALE_BYTES + lane * 16, scaleA = lds + 2 * wm * QUARTER_BYTES + lane * 4;
     const uint32_t fragB = lds + TILE_BYTES + 2 * wn * PIECE_BYTES + SCALE_BYTES + lane * 16, scaleB = lds + TILE_BYTES + 2 * wn * PIECE_BYTES + lane * 4;
 
-    Source a = {0, 0, 0, 0, KT}, b = {0, 0, 0, 0, KT};
+    Source a, b;
     Order copy_order(TM, TP);
+    const int operand_bytes = KT * TILE_BYTES;
     auto look_up = [&]() {
         int tm, tp;
         const bool any = copy_order.take(tm, tp);
-        a.bytes_after = any ? TILE_BYTES : 0;
-        b.bytes_after = any ? 2 * QUARTER_BYTES : 0;
+        a.bytes_after = b.bytes_after = any ? operand_bytes : 0;
         if (any) {
-            a.after = (uint64_t)(uintptr_t)g.A + (uint64_t)tm * KT * TILE_BYTES;
-            b.after = (uint64_t)(uintptr_t)g.B + (uint64_t)(tp >> 1) * KT * TILE_BYTES + (uint64_t)(tp & 1) * 2 * QUARTER_BYTES;
+            a.after = (uint64_t)(uintptr_t)g.A + (uint64_t)tm * operand_bytes;
+            b.after = (uint64_t)(uintptr_t)g.B + (uint64_t)(tp >> 1) * operand_bytes + (uint64_t)(tp & 1) * 2 * QUARTER_BYTES;
         }
     };
+    a.after = b.after = 0;
     look_up();
-    a.at = a.after;
-    b.at = b.after;
-    a.bytes = a.bytes_after;
-    b.bytes = b.bytes_after;
+    a.switch_over(0);
+    b.switch_over(0);
     uint32_t here = 0, to = 0;  // ring offsets: the current stage, the stage that is copied
     auto advance = [](uint32_t& place) { place = place == (HALF_RING - 1) * HALF_STAGE_BYTES ? 0 : place + HALF_STAGE_BYTES; };
-    auto copy_a = [&](auto Q) { copy_quarter<decltype(Q)::value>(m0_a + to, voffA4, voffA16, a.resource()); };
-    auto copy_b = [&](auto Q) { copy_quarter<decltype(Q)::value>(m0_b + to, voffB4, voffB16, b.resource()); };
-    // copies 0 .. 2 of A in the second half of a stage, the other two and B's in the first half of the next one
-    constexpr int EARLY = 3;
+    uint32_t off = 0;
+    auto copy_a = [&](auto Q) { copy_quarter<decltype(Q)::value>(voffA4, voffA16, a.now, off); };
+    auto copy_b = [&](auto Q) { copy_quarter<decltype(Q)::value>(voffB4, voffB16, b.now, off); };
     static_for<0, HALF_RING>([&](auto S) {
-        constexpr bool last = decltype(S)::value == HALF_RING - 1;
-        static_for<0, last ? EARLY : 5>(copy_a);
-        if constexpr (!last) {
-            a.next(KT);
+        copy_to(to, m0_a);
+        asm volatile("s_nop 0");
+        static_for<0, 5>(copy_a);
+        if constexpr (decltype(S)::value < HALF_RING - 1) {  // (the main loop begins with the last one's B)
+            copy_to(to, m0_b);
+            asm volatile("s_nop 0");
             static_for<0, 3>(copy_b);
-            b.next(KT);
             advance(to);
+            off += TILE_BYTES;
         }
     });
+    a.move(HALF_RING * TILE_BYTES);
+    b.move((HALF_RING - 1) * TILE_BYTES);
 
     v4f acc[8][4];
     v4i faL[4], faH[4], fb[4];
     int saL, saH, sb;
-    // half of sub-step S: two matrix instructions on fragment S of B and two of A
-    auto math = [&](const v4i* fa, int sa, auto I0, auto S, auto X0) {
-        static_for<0, 2>([&](auto X) {
-            constexpr int j = decltype(S)::value, x = decltype(X0)::value + decltype(X)::value, i = (j & 1) ? 3 - x : x;
-            v4f& c = acc[decltype(I0)::value + i][j];
-            c = mfma<j, i>(fb[j], sb, fa[i], sa, c);
-        });
+    // matrix instruction X of a half of A: four on each fragment of B, there and back over those of A
+    auto math = [&](const v4i* fa, int sa, auto I0, auto X) {
+        constexpr int j = decltype(X)::value / 4, x = decltype(X)::value % 4, i = (j & 1) ? 3 - x : x;
+        v4f& c = acc[decltype(I0)::value + i][j];
+        c = mfma<j, i>(fb[j], sb, fa[i], sa, c);
     };
     typedef std::integral_constant<int, 0> N0;
-    typedef std::integral_constant<int, 2> N2;
     typedef std::integral_constant<int, 4> N4;
 
-    wait_vmcnt<(HALF_RING - 2) * HALF_COPIES + EARLY>();
+    wait_vmcnt<(HALF_RING - 1) * HALF_COPIES - 3>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     uint32_t fa_at = fragA, fb_at = fragB, sa_at = scaleA, sb_at = scaleB;
@@ -774,7 +782,57 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_half(Gemm g, int
     // (as above: stores newer than the copies that are waited for need not be over; here in the four stages behind a tile)
     constexpr int STORES = TYPE == F32 ? 32 : 16, NEWER = (HALF_RING - 2) * HALF_COPIES;
     constexpr int NEWER_STORES = NEWER + STORES < 63 ? NEWER + STORES : 63;
-    int fresh = 0;
+    uint32_t fresh = 0;
+    // (forced inline: the state that it captures has to stay in registers)
+    auto stage = [&](auto FRESH) __attribute__((always_inline)) {
+        // (A lo, B): the upper half of A comes in, early, so that it is there at the barrier; copies of B
+        static_for<0, 16>([&](auto X) {
+            constexpr int x = decltype(X)::value;
+            if constexpr (x % 2 == 0 && x < 8) faH[x / 2] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + x / 2 * FRAGMENT_BYTES);
+            if constexpr (x == 1) copy_to(to, m0_b);
+            if constexpr (x == 3) copy_b(std::integral_constant<int, 0>{});
+            if constexpr (x == 5) saH = *(lds_int)(uintptr_t)(sa_at + QUARTER_BYTES);
+            if constexpr (x == 7) copy_b(std::integral_constant<int, 1>{});
+            if constexpr (x == 9) copy_b(std::integral_constant<int, 2>{});
+            if constexpr (x == 10) {
+                to = here;
+                advance(here);
+            }
+            if constexpr (x == 12) fa_at = fragA + here;
+            if constexpr (x == 13) fb_at = fragB + here;
+            if constexpr (x == 14) sa_at = scaleA + here;
+            if constexpr (x == 15) sb_at = scaleB + here;
+            math(faL, saL, N0{}, X);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        wait_vmcnt<decltype(FRESH)::value ? NEWER_STORES : NEWER>();
+        wait_lds<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        // (A hi, B): the lower half of A and B of the next stage (behind the last one: what the ring holds, unused); copies of A
+        int sb_next;
+        static_for<0, 16>([&](auto X) {
+            constexpr int x = decltype(X)::value;
+            if constexpr (x % 2 == 0 && x < 8) faL[x / 2] = *(lds_v4i)(uintptr_t)(fa_at + x / 2 * FRAGMENT_BYTES);
+            if constexpr (x == 1) copy_to(to, m0_a);
+            if constexpr (x == 3) copy_a(std::integral_constant<int, 0>{});
+            if constexpr (x == 5) saL = *(lds_int)(uintptr_t)sa_at;
+            if constexpr (x == 7) sb_next = *(lds_int)(uintptr_t)sb_at;
+            if constexpr (x == 9) copy_a(std::integral_constant<int, 1>{});
+            if constexpr (x == 11) copy_a(std::integral_constant<int, 2>{});
+            if constexpr (x == 13) copy_a(std::integral_constant<int, 3>{});
+            if constexpr (x == 14) copy_a(std::integral_constant<int, 4>{});
+            if constexpr (x == 8) fb[0] = *(lds_v4i)(uintptr_t)(fb_at + piece(0));
+            if constexpr (x == 10) fb[1] = *(lds_v4i)(uintptr_t)(fb_at + piece(1));
+            if constexpr (x == 12) fb[2] = *(lds_v4i)(uintptr_t)(fb_at + piece(2));
+            math(faH, saH, N4{}, X);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        fb[3] = *(lds_v4i)(uintptr_t)(fb_at + piece(3));
+        sb = sb_next;
+        off += TILE_BYTES;
+        wait_lds<2>();
+    };
     Order order(TM, TP);
     int tm, tp;
     while (order.take(tm, tp)) {
@@ -786,56 +844,23 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_half(Gemm g, int
                 acc[i][j] = v4f{0, 0, 0, 0};
                 asm volatile("" : "+a"(acc[i][j]));
             }
-        __builtin_amdgcn_s_waitcnt(0xc07f);  // (as above)
-        for (int it = 0; it < KT; ++it) {
-            // (A lo, B): the upper half of A comes in, early, so that it is there at the barrier; the rest of the copies
-            static_for<0, 4>([&](auto Q) {
-                constexpr int q = decltype(Q)::value;
-                if constexpr (q < 2) faH[2 * q] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + 2 * q * FRAGMENT_BYTES);
-                if constexpr (q == 0) saH = *(lds_int)(uintptr_t)(sa_at + QUARTER_BYTES);
-                if constexpr (q >= 2) copy_b(std::integral_constant<int, q - 2>{});
-                math(faL, saL, N0{}, Q, N0{});
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (q < 2) faH[2 * q + 1] = *(lds_v4i)(uintptr_t)(fa_at + QUARTER_BYTES + (2 * q + 1) * FRAGMENT_BYTES);
-                if constexpr (q < 2) copy_a(std::integral_constant<int, EARLY + q>{});
-                if constexpr (q == 2) a.next(KT);
-                if constexpr (q == 3) copy_b(std::integral_constant<int, 2>{});
-                math(faL, saL, N0{}, Q, N2{});
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(%1)\n1:\n\ts_waitcnt vmcnt(%2)" ::"s"(fresh), "n"(NEWER),
-                         "n"(NEWER_STORES)
-                         : "memory", "scc");
-            --fresh;
-            to = here;
-            advance(here);
-            fa_at = fragA + here;
-            fb_at = fragB + here;
-            sa_at = scaleA + here;
-            sb_at = scaleB + here;
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            // (A hi, B): the lower half of A and B of the next stage (behind the last one: what the ring holds, unused)
-            int sb_next;
-            static_for<0, 4>([&](auto Q) {
-                constexpr int q = decltype(Q)::value;
-                faL[q] = *(lds_v4i)(uintptr_t)(fa_at + q * FRAGMENT_BYTES);
-                if constexpr (q == 1) saL = *(lds_int)(uintptr_t)sa_at;
-                math(faH, saH, N4{}, Q, N0{});
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (q == 2) sb_next = *(lds_int)(uintptr_t)sb_at;
-                if constexpr (q == 0) b.next(KT);
-                if constexpr (q >= 1) copy_a(std::integral_constant<int, q - 1>{});
-                math(faH, saH, N4{}, Q, N2{});
-                __builtin_amdgcn_sched_barrier(0);
-                fb[q] = *(lds_v4i)(uintptr_t)(fb_at + piece(q));
-            });
-            sb = sb_next;
+        off = 0;
+        while (off != fresh) stage(std::true_type{});
+        uint32_t until = (uint32_t)(KT - HALF_RING) * TILE_BYTES;
+#pragma clang loop unroll(disable)
+        for (int part = 0; part < 3; ++part) {
+            wait_lds<0>();  // (here and not at every stage: its last fetch, which is the last to be used, may be on its way then)
+#pragma clang loop unroll(disable)
+            while (off != until) stage(std::false_type{});
+            if (part == 0) a.switch_over(KT - HALF_RING);
+            if (part == 1) b.switch_over(KT - HALF_RING + 1);
+            until = part == 0 ? (uint32_t)(KT - HALF_RING + 1) * TILE_BYTES : (uint32_t)operand_bytes;
         }
+        a.move(operand_bytes);
+        b.move(operand_bytes);
         fresh = put_tile<TYPE, 4>(g, acc, (int64_t)tm * TILE_R + wm * 128, (int64_t)tp * 128 + wn * 64,
                                   (int64_t)(tm + 1) * TILE_R <= g.m && (int64_t)(tp + 1) * 128 <= g.p, stream, lane)
-                    ? HALF_RING - 2
+                    ? (uint32_t)(KT - HALF_RING < HALF_RING - 2 ? KT - HALF_RING : HALF_RING - 2) * TILE_BYTES
                     : 0;
     }
     wait_vmcnt<0>();
@@ -865,7 +890,8 @@ namespace mxk {
 bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd)
 {
     if (way == WAY_TILE || way == WAY_HALF)
-        return inner_tiles(n) >= (way == WAY_TILE ? RING : HALF_RING) && ldd < (1 << 24) && row_tiles(m) * row_tiles(p) < ((int64_t)1 << 28);
+        return inner_tiles(n) >= (way == WAY_TILE ? RING : HALF_RING) && inner_tiles(n) < ((int64_t)1 << 31) / TILE_BYTES && ldd < (1 << 24) &&
+               row_tiles(m) * row_tiles(p) < ((int64_t)1 << 28);
     return way == WAY_DIRECT;
 }
 
