@@ -65,6 +65,22 @@ def test_again_and_again(mx, way):
         assert torch.equal(D, first), k
 
 
+# several tiles a workgroup, one behind the other: as many inner tiles as the ring has places, one more, several more; whole tiles, whose stores
+# may be on their way in the next one's first stages, and edges
+SEVERAL = [("tile", 4352, 512, 4096), ("tile", 4352, 513, 4100), ("tile", 4096, 1000, 4608), ("half", 4096, 700, 2560), ("half", 4096, 896, 2600),
+           ("half", 4090, 1281, 2560)]
+
+
+@pytest.mark.parametrize("way,m,n,p", SEVERAL)
+def test_several_tiles_a_workgroup(mx, way, m, n, p):
+    print(f"{way} {m} x {n} x {p}", flush=True)
+    A, B = matrix(m, n, "bf16", m + n), matrix(p, n, "bf16", p + n + 1)
+    want, size = product(ref.read_back(f64(A)), ref.read_back(f64(B)))
+    (PA, _), (PB, _) = mx.quantize(A), mx.quantize(B)
+    for kind in ("bf16", "f32"):
+        check(mx.gemm(PA, PB, TYPES[kind], way=way), want, n * 2.0 ** -23 * size, kind, n, kind)
+
+
 # few rows, quantised on the way: every number of fragments a workgroup and of tiles at a time, more than one group of 16 rows
 FEW = [(3, 700, 200), (10, 700, 200), (4, 1030, 5000), (13, 1030, 5000), (2, 1100, 9000), (12, 1100, 9000), (12, 900, 20000), (16, 2050, 16500),
        (40, 1500, 3000), (64, 33, 4000), (17, 4099, 64), (50, 129, 130)]
