@@ -288,17 +288,25 @@ __device__ inline void put8(__attribute__((address_space(1))) typename Elem<TYPE
 // left to write back (4096 x 2048 x 4096: 21.1 us, 22.5 with plain stores; 8192 x 2048 x 8192: 70 and 73.5).  STREAM: past the caches, for
 // outputs that with the operands exceed the memory-side cache (8192 x 8192 x 16384, 268 MB of D: 434 us, written through 471, plain 477;
 // 134 MB of D, inner dimension 4096: 128, 119, 117).  Two wait states keep what follows off the registers of a 16-byte store.
-template <bool STREAM, int OFFSET> __device__ inline void store16(uint64_t base, uint32_t off, v4i y)
+// EDGE: by the lanes alone of which NEED columns or more are left.
+enum Stores { THROUGH, STREAM, EDGE };
+template <int HOW, int OFFSET, int NEED> __device__ inline void store16(uint64_t base, uint32_t off, v4i y, int left)
 {
-    if constexpr (STREAM)
+    if constexpr (HOW == EDGE) {
+        uint64_t all;
+        asm volatile("v_cmp_le_i32 vcc, %5, %4\n\ts_and_saveexec_b64 %0, vcc\n\tglobal_store_dwordx4 %1, %2, %3 offset:%6 sc0 sc1\n\ts_nop 1\n\ts_mov_b64 exec, %0"
+                     : "=&s"(all)
+                     : "v"(off), "v"(y), "s"(base), "v"(left), "n"(NEED), "n"(OFFSET)
+                     : "memory", "vcc", "scc");
+    } else if constexpr (HOW == STREAM)
         asm volatile("global_store_dwordx4 %0, %1, %2 offset:%3 sc1 nt\n\ts_nop 1" ::"v"(off), "v"(y), "s"(base), "n"(OFFSET) : "memory");
     else
         asm volatile("global_store_dwordx4 %0, %1, %2 offset:%3 sc0 sc1\n\ts_nop 1" ::"v"(off), "v"(y), "s"(base), "n"(OFFSET) : "memory");
 }
 // 16-bit types: a lane stores its eight, and the four lanes of a row 64 bytes.  FP32: the lanes of a row first exchange theirs, so that
 // each of two stores covers 64 bytes of a row there too (16 bytes of every 32 at a time, written through: 210 us for 8192 x 8192 x 4096).
-template <int TYPE, bool STREAM, int COLUMN>
-__device__ inline void put8_whole(uint64_t base, uint32_t off, float alpha, const float* v)
+template <int TYPE, int HOW, int COLUMN>
+__device__ inline void put8_whole(uint64_t base, uint32_t off, float alpha, const float* v, int left)
 {
     if constexpr (TYPE == F32) {
         v4i lo, hi;
@@ -310,15 +318,15 @@ __device__ inline void put8_whole(uint64_t base, uint32_t off, float alpha, cons
             lo[e] = (int)y[0];
             hi[e] = (int)y[1];
         }
-        store16<STREAM, COLUMN * 4>(base, off, lo);
-        store16<STREAM, COLUMN * 4 + 64>(base, off, hi);
+        store16<HOW, COLUMN * 4, 4>(base, off, lo, left);
+        store16<HOW, COLUMN * 4 + 64, 20>(base, off, hi, left);
     } else {
         typename Elem<TYPE>::Bits x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = from_float<TYPE>(alpha * v[e]);
         v4i y;
         __builtin_memcpy(&y, x, 16);
-        store16<STREAM, COLUMN * 2>(base, off, y);
+        store16<HOW, COLUMN * 2, 8>(base, off, y, left);
     }
 }
 
@@ -360,27 +368,35 @@ __device__ __attribute__((always_inline)) inline bool put_tile(const Gemm& g, v4
             });
         });
     };
-    auto whole = [&](auto STREAM) {
+    // rows and columns of D from this lane's first ones on (FP32: it stores columns 4 lc .. 4 lc + 3 and the 16th behind them)
+    const int rows_left = (int)(g.m - row0 < 128 ? g.m - row0 : 128) - row_lane, cols = (int)(g.p - col0 < 128 ? g.p - col0 : 128);
+    // (none in rows behind the last one; by a minimum: conditions kept in scalar registers spilled others)
+    auto left = [&](int ri, int columns) { return min(columns, (rows_left - ri) * 256); };
+    auto eights = [&](auto HOW) {
         const uint32_t off16 = TYPE == F32 ? ((uint32_t)row_lane * (uint32_t)g.ldd + (uint32_t)lc * 4u) * 4u : off;
-        each([&](uint64_t base, auto, auto CJ, const float* v) { put8_whole<TYPE, decltype(STREAM)::value, decltype(CJ)::value>(base, off16, g.alpha, v); });
-    };
-    auto edge = [&](auto BETA) {
-        const int rows_left = (int)(g.m - row0 < 128 ? g.m - row0 : 128) - row_lane;
-        const int cols_left = (int)(g.p - col0 < 128 ? g.p - col0 : 128) - col_lane;
+        const int cols_left = cols - (TYPE == F32 ? lc * 4 : col_lane);
         each([&](uint64_t base, auto RI, auto CJ, const float* v) {
             constexpr int ri = decltype(RI)::value, cj = decltype(CJ)::value;
-            put8<TYPE, decltype(BETA)::value>((Global*)(base + off) + cj, ri < rows_left ? cols_left - cj : 0, g.alpha, g.beta, v);
+            put8_whole<TYPE, decltype(HOW)::value, cj>(base, off16, g.alpha, v, left(ri, cols_left - cj));
+        });
+    };
+    auto ones = [&](auto BETA) {
+        each([&](uint64_t base, auto RI, auto CJ, const float* v) {
+            constexpr int ri = decltype(RI)::value, cj = decltype(CJ)::value;
+            const int here = left(ri, cols - col_lane - cj);
+            put8<TYPE, decltype(BETA)::value>((Global*)(base + off) + cj, decltype(BETA)::value || here < 8 ? here : 0, g.alpha, g.beta, v);
         });
     };
     if (g.beta != 0.0f) {
-        edge(std::true_type{});
+        ones(std::true_type{});
     } else if (!whole_tile) {
-        edge(std::false_type{});
+        eights(std::integral_constant<int, EDGE>{});
+        if (cols > 0 && cols & 7) ones(std::false_type{});  // (the columns behind the last whole eight of a row)
     } else {
         if (stream)
-            whole(std::true_type{});
+            eights(std::integral_constant<int, STREAM>{});
         else
-            whole(std::false_type{});
+            eights(std::integral_constant<int, THROUGH>{});
         return true;
     }
     return false;
