@@ -911,17 +911,20 @@ bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd)
     return way == WAY_DIRECT;
 }
 
-// Microseconds that each way takes, roughly: the tiles by rounds of one for every compute unit, k_mx_direct by its workgroups.  Fitted to
-// (m x n x p: direct, half, tile)  256 x 4096 x 4096: 6.8, 16.8, 24.9;  1024 x 4096 x 4096: 17.3, 17.8, 25.5;  2048 x 4096 x 4096: 32.7, 21.5, 27.0;
-// 4096 x 4096 x 4096: 66, 39.0, 36.2;  512 x 8192 x 8192: 29.2, 29.1, 43.3;  1024 x 8192 x 8192: 60, 35.0, 44.3;  2048 x 8192 x 8192: 117, 68, 59;
-// 512 x 1024 x 8192: 9.8, 8.6, 11.7;  512 x 4096 x 14336: 33.6, 19.5, 27.6;  1024 x 4096 x 14336: 61, 36.0, 31.2;  4096 x 2051 x 1283: 19.5, 15.9, 24.8.
+// Microseconds that each way takes, roughly: the tiles by rounds of one for every compute unit, slower stages where more of those are at
+// work (`fill`: clock and memory), k_mx_direct by its workgroups.  Fitted to
+// (m x n x p: direct, half, tile)  256 x 4096 x 4096: 6.8, 15.4, 23.6;  1024 x 4096 x 4096: 17.0, 16.1, 23.5;  2048 x 4096 x 4096: 32.4, 20.0, 25.0;
+// 4096 x 4096 x 4096: 63, 35.6, 33.7;  512 x 8192 x 8192: 29.2, 26.5, 40.3;  1024 x 8192 x 8192: 56, 32.9, 41.8;  2048 x 8192 x 8192: 112, 62, 56;
+// 512 x 1024 x 8192: 9.6, 8.3, 11.4;  256 x 4096 x 14336: 17.8, 16.7, 24.4;  512 x 4096 x 14336: 33.0, 17.9, 25.0;  1024 x 4096 x 14336: 58, 32.5, 29.0;
+// 768 x 4096 x 14336: 47, 31.2, 26.1;  2048 x 2048 x 2048: 11.9, 11.1, 15.7;  8192 x 2048 x 8192: 152, 74.5, 66.6;  4096 x 2051 x 1283: 19.8, 15.3, 24.1.
 double estimate_us(int way, int64_t m, int64_t n, int64_t p)
 {
     const double KT = (double)inner_tiles(n);
-    const auto rounds = [](int64_t tiles) { return (double)((tiles + COMPUTE_UNITS - 1) / COMPUTE_UNITS); };
-    if (way == WAY_TILE) return rounds(row_tiles(m) * row_tiles(p)) * (7.5 + 0.62 * KT);
-    if (way == WAY_HALF) return rounds(row_tiles(m) * ((p + 127) / 128)) * (5.5 + 0.42 * KT);
-    return 3.0 + (double)(((m + 63) / 64) * ((p + 63) / 64)) * (0.0035 + 0.0004 * KT);
+    if (way == WAY_DIRECT) return 3.0 + (double)(((m + 63) / 64) * ((p + 63) / 64)) * (0.0035 + 0.0004 * KT);
+    const int64_t tiles = way == WAY_TILE ? row_tiles(m) * row_tiles(p) : row_tiles(m) * ((p + 127) / 128);
+    const double rounds = (double)((tiles + COMPUTE_UNITS - 1) / COMPUTE_UNITS), fill = (double)tiles / (rounds * COMPUTE_UNITS);
+    if (way == WAY_TILE) return 4.3 + rounds * (2.9 + KT * (0.51 + 0.28 * fill * fill));
+    return 2.5 + rounds * (3.0 + KT * (0.32 + 0.10 * fill));
 }
 
 int choose(int64_t m, int64_t n, int64_t p, int64_t ldd)
