@@ -200,7 +200,7 @@ void direct(const Gemm& g, const Gemm* also, hipStream_t st)
 // it the stage's place in the ring takes the copies of the fourth stage from here.  Ten copies a wave and stage; those behind the last
 // stage are out of the buffer's range: they read nothing, but count, so that every stage waits alike.
 constexpr int RING = 4, STAGE_BYTES = 2 * TILE_BYTES, COPIES = 10;
-constexpr int NXCD = 8, BAND = 8;
+constexpr int NXCD = 8;
 constexpr int64_t MEMORY_SIDE_CACHE = (int64_t)256 << 20;
 
 // (by the builtin: the compiler then knows, and waits for none of them again)
@@ -212,9 +212,10 @@ template <int N> __device__ inline void wait_lds()
 }
 template <int N> __device__ inline void wait_vmcnt() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-// Workgroup b runs on XCD b % 8.  The tiles are cut into eight contiguous ranges, one an XCD, in bands of 8 tile rows walked column by
-// column: the 32 tiles that an XCD works on at a time share 8 panels of A and 4 of B in its L2.
-struct Order {
+// Workgroup b runs on XCD b % 8.  The tiles are cut into eight contiguous ranges, one an XCD, in bands of BAND tile rows walked column by
+// column: the 32 tiles that an XCD works on at a time share BAND panels of A and 32 / BAND of B in its L2.  8 for tiles of 256 x 256, 4 for
+// those of 256 x 128, where 8 would take a quarter more of A and B together (2048 x 4096 x 4096 with cold operands 20.4 and 20.9 us).
+template <int BAND> struct Order {
     int TM, TP, next, last, step;
     __device__ inline Order(int TM_, int TP_) : TM(TM_), TP(TP_)
     {
@@ -420,7 +421,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
     const uint32_t scaleB = lds + TILE_BYTES + 2 * wn * QUARTER_BYTES + lane * 4;
 
     Source a, b;
-    Order copy_order(TM, TP);
+    Order<8> copy_order(TM, TP);
     const int operand_bytes = KT * TILE_BYTES;
     auto look_up = [&]() {
         int tm, tp;
@@ -551,7 +552,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_tile(Gemm g, int
         });
         off += TILE_BYTES;
     };
-    Order order(TM, TP);
+    Order<8> order(TM, TP);
     int tm, tp;
     while (order.take(tm, tp)) {
         look_up();
@@ -735,7 +736,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_half(Gemm g, int
     const uint32_t fragB = lds + TILE_BYTES + 2 * wn * PIECE_BYTES + SCALE_BYTES + lane * 16, scaleB = lds + TILE_BYTES + 2 * wn * PIECE_BYTES + lane * 4;
 
     Source a, b;
-    Order copy_order(TM, TP);
+    Order<4> copy_order(TM, TP);
     const int operand_bytes = KT * TILE_BYTES;
     auto look_up = [&]() {
         int tm, tp;
@@ -849,7 +850,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_half(Gemm g, int
         off += TILE_BYTES;
         wait_lds<2>();
     };
-    Order order(TM, TP);
+    Order<4> order(TM, TP);
     int tm, tp;
     while (order.take(tm, tp)) {
         look_up();
