@@ -57,8 +57,9 @@ template <int N> __device__ inline void finish_any(const Gemm& g, int64_t row, i
 
 // ---- 64 rows x FB fragments of B (16 columns each) by a workgroup, operands straight from memory into registers ----
 //
-// For outputs too small for the tiles below: the waves share the inner tiles, TILES of them on their way at a time, and their sums meet in
-// LDS.
+// For outputs too small for the tiles below, where the time is that of a launch, of the way of the operands and of one wave's share of the inner
+// dimension: the waves share the inner tiles, TILES of them on their way at a time, and their sums meet in LDS, in a fixed order.  256 x 4096 x
+// 4096 6.8 us (10 MB, 1.3 PF; a launch alone is 2.5), 512 x 4096 x 4096 9.5; beyond that operands read again by every workgroup bound it.
 constexpr int DIRECT_SLOTS = 4;
 template <int FB> constexpr int direct_pitch() { return 16 * FB + 4; }  // floats between the rows of a wave's sums: rows fall on different banks
 
@@ -199,6 +200,8 @@ void direct(const Gemm& g, const Gemm* also, hipStream_t st)
 // One barrier a stage, in its middle, where every wave has fetched all of the stage and its own copies of the next one have landed: behind
 // it the stage's place in the ring takes the copies of the fourth stage from here.  Ten copies a wave and stage; those behind the last
 // stage are out of the buffer's range: they read nothing, but count, so that every stage waits alike.
+// Bound by power where the product is large: 8192 x 8192 x 16384 416 us (5.3 PF) from cool, 513 (4.3) call after call with changing operands, 330 on
+// zeros, which are the same instructions.  A register-only loop of the instruction gives 7.6 PF (with 32 x 32 x 64 6.7).  8192 x 4096 x 8192 112 us.
 constexpr int RING = 4, STAGE_BYTES = 2 * TILE_BYTES, COPIES = 10;
 constexpr int NXCD = 8;
 constexpr int64_t MEMORY_SIDE_CACHE = (int64_t)256 << 20;
@@ -214,7 +217,8 @@ template <int N> __device__ inline void wait_vmcnt() { asm volatile("s_waitcnt v
 
 // Workgroup b runs on XCD b % 8.  The tiles are cut into eight contiguous ranges, one an XCD, in bands of BAND tile rows walked column by
 // column: the 32 tiles that an XCD works on at a time share BAND panels of A and 32 / BAND of B in its L2.  8 for tiles of 256 x 256, 4 for
-// those of 256 x 128, where 8 would take a quarter more of A and B together (2048 x 4096 x 4096 with cold operands 20.4 and 20.9 us).
+// those of 256 x 128, where 8 would take a quarter more of A and B together (a linear layer of 2048 x 4096 x 4096, its quantisation included,
+// 27.3 and 27.8 us).
 template <int BAND> struct Order {
     int TM, TP, next, last, step;
     __device__ inline Order(int TM_, int TP_) : TM(TM_), TP(TP_)
@@ -599,10 +603,11 @@ template <int TYPE> void tile(const Gemm& g, hipStream_t st)
 
 // ---- few rows of X, quantised on the way: 16 rows and FB fragments of W's (16 columns each) by a workgroup ----
 //
-// The time of such a call is that of reading W once and of its launches, so this is one launch: eight waves share the inner tiles, each
-// takes its fragments of W straight from memory into registers, four tiles at a time, and quantises the blocks of X that meet them - a lane
+// The time of such a call is that of reading W once and of its launches, so this is one launch: the waves share the inner tiles, each
+// takes its fragments of W straight from memory into registers, TILES of its tiles at a time, and quantises the blocks of X that meet them - a lane
 // holds a block as the matrix instruction wants it, so that its scale takes no exchange between lanes.  The waves' sums meet in LDS.
 // Every workgroup quantises all of X: FB is as large as leaves a workgroup for every compute unit.
+// 16 rows through 16384 x 8192: 13.8 us, 72 MB at 5.2 TB/s, a large copy's rate; one row through 4096 x 4096: 4.9 us on the GPU.
 constexpr int FEW_ROWS = 16;
 
 template <int XTYPE, int FB, int WAVES, int TILES>
@@ -718,6 +723,8 @@ template <int XTYPE> void few(const Gemm& g, const void* X, int64_t ldx, hipStre
 // A wave has 128 x 64 outputs; a stage (26 KiB) is 32 matrix instructions of it, (A lo, B) and (A hi, B), and the ring has six places.  A fragment
 // of B gives way to the next stage's as soon as its last four products are done.  In LDS B is four pieces of two fragments, each behind the
 // scales of its quarter, one from each wave.
+// 2048 x 4096 x 4096, one tile for each compute unit: 20.3 us (3.4 PF), of 37000 cycles 23000 the stages (726 each; 512 were the matrix
+// instructions alone, 70 the loop, 55 the barrier, 45 the copies, 30 LDS), 5000 the ring's first filling, 5000 the stores, 2000 their end.  A ring of four: within 2 %.
 constexpr int HALF_RING = 6, PIECE_BYTES = SCALE_BYTES + 2 * FRAGMENT_BYTES, HALF_STAGE_BYTES = TILE_BYTES + 4 * PIECE_BYTES, HALF_COPIES = 8;
 
 template <int TYPE> __global__ __launch_bounds__(256) void k_mx_half(Gemm g, int KT, int TM, int TP, int stream)

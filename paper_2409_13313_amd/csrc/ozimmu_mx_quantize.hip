@@ -26,7 +26,7 @@ inline dim3 grid_of(int64_t cols, int64_t blocks)
 
 // Blocks along the rows.  A workgroup takes 32 rows x 128 columns (half a quarter of a tile, its fragments 0 and 1 or 2 and 3): thread t the
 // eight elements t % 16 of the two rows at place t / 16, so that 16 lanes read 128 columns of a row side by side; four lanes hold a block and
-// share its maximum.  (64 rows: 8192 x 4096 bf16 17.7 us.)
+// share its maximum.  (8192 x 8192 bf16 30.5 us, 170 MB at 5.6 TB/s, a large copy moves 5.0.)
 struct RowsAt {
     int64_t row0;  // the place's row in fragment 0 of the quarter
     int first;     // the first of the two fragments
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t n, 
         }
 }
 
-// Plain layout -> packed and back: one thread a block.
+// Plain layout -> packed and back: one thread a block.  (16384 x 8192: 35 and 28 us, 143 MB at 4.1 and 5.0 TB/s.)
 __global__ __launch_bounds__(256) void k_mx_pack(int64_t rows, int64_t n, const uint8_t* codes, int64_t ldc, const uint8_t* scales,
                                                  int64_t lds, uint8_t* out, int64_t KT)
 {
