@@ -71,6 +71,7 @@ struct Gemm {
     int64_t ldd;
     int dtype;
     float alpha, beta;
+    bool read_later = false;  // D is not what the next work reads (a gradient of weights)
 };
 // How a product is run (OZIMMU_MX_WAY_*); WAY_AUTO: choose() says
 enum { WAY_AUTO = -1, WAY_DIRECT = 0, WAY_TILE = 1, WAY_HALF = 2 };

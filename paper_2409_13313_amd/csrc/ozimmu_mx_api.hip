@@ -179,7 +179,7 @@ int ozimmu_mx_linear_backward(int64_t m, int64_t n, int64_t p, float alpha, int 
             CHECK(launched(mxk::launch_quantize(type, gq, st)));
     }
     const mxk::Gemm gx = {m, p, n, g_rows, (const uint8_t*)Wt, dX, lddx, dx_type, alpha, beta_x};
-    const mxk::Gemm gw = {p, m, n, g_cols, x_cols, dW, lddw, dw_type, alpha, beta_w};
+    const mxk::Gemm gw = {p, m, n, g_cols, x_cols, dW, lddw, dw_type, alpha, beta_w, true};
     if (want_x && want_w) return launched(mxk::launch_gemm2(gx, gw, st));
     if (want_x) return launched(mxk::launch_gemm(gx, mxk::WAY_AUTO, st));
     if (want_w) return launched(mxk::launch_gemm(gw, mxk::WAY_AUTO, st));
