@@ -81,6 +81,29 @@ def test_several_tiles_a_workgroup(mx, way, m, n, p):
         check(mx.gemm(PA, PB, TYPES[kind], way=way), want, n * 2.0 ** -23 * size, kind, n, kind)
 
 
+# results that are written past the caches: large gradients of weights (whole tiles and edges, both tile kernels), a product that with its
+# operands is larger than the memory-side cache
+@pytest.mark.parametrize("m,n,p,kind", [(1000, 2200, 2100, "f32"), (600, 2304, 4096, "f32"), (1000, 2304, 4096, "bf16"), (600, 4100, 2304, "f32")])
+def test_large_gradient_of_weights(mx, m, n, p, kind):
+    print(f"gradient of weights {m} x {n} x {p} {kind}", flush=True)
+    X, G = matrix(m, n, "bf16", 1), matrix(m, p, "bf16", 2)
+    want, size = product(ref.read_back(f64(G).T), ref.read_back(f64(X).T))
+    dW = torch.full((p, n), float("nan"), dtype=TYPES[kind], device="cuda")
+    mx.linear_backward(G, X, None, dW=dW)
+    check(dW, want, m * 2.0 ** -23 * size, kind, m, "dW")
+
+
+def test_product_larger_than_the_caches(mx):
+    m, n, p = 8192, 512, 8192
+    A, B = matrix(m, n, "bf16", 1), matrix(p, n, "bf16", 2)
+    (PA, _), (PB, _) = mx.quantize(A), mx.quantize(B)
+    whole = mx.gemm(PA, PB, torch.float32)
+    rows = np.r_[0:40, 4090:4130, 8150:8192]
+    a, b = torch.from_numpy(ref.read_back(f64(A)[rows])), torch.from_numpy(ref.read_back(f64(B)))
+    want, size = (a @ b.t()).numpy(), (a.abs() @ b.abs().t()).numpy()
+    check(whole[torch.from_numpy(rows).cuda()], want, n * 2.0 ** -23 * size, "f32", n)
+
+
 # few rows, quantised on the way: every number of fragments a workgroup and of tiles at a time, more than one group of 16 rows
 FEW = [(3, 700, 200), (10, 700, 200), (4, 1030, 5000), (13, 1030, 5000), (2, 1100, 9000), (12, 1100, 9000), (12, 900, 20000), (16, 2050, 16500),
        (40, 1500, 3000), (64, 33, 4000), (17, 4099, 64), (50, 129, 130)]
