@@ -124,43 +124,47 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_quantize_cols2(C
 }
 
 // Reading back: a lane makes 16 bytes, E elements, of a row, side by side with its neighbours (FP32: half of the eight codes that it loads; 32 bytes a
-// lane in two stores: 16384 x 8192 183 us, so 154).  A workgroup takes 64 rows x 128 columns.  STREAM, where rows begin at multiples of 16 bytes: stores
-// past the caches (16384 x 8192 FP32 86 us = 7.1 TB/s, a large fill writes 6.9; bf16 49 and 64; rows that begin anywhere: 1001 x 4099 bf16 5.6 us,
-// plain stores 4.5).
+// lane in two stores: 16384 x 8192 183 us, so 154, today 84).  A workgroup takes 16 rows x 128 columns (64 rows: 4096 x 4096 FP32 13.6 us, 16 rows 11.5;
+// 513 x 1001 3.6 and 2.9; 16384 x 8192 85.7 and 84.5).  STREAM, where rows begin at multiples of 16 bytes: stores
+// past the caches (16384 x 8192 FP32 84.5 us = 7.2 TB/s, a large fill writes 6.9; bf16 47.7 and 64).  Rows that begin anywhere: plain stores (1001 x 4099
+// bf16 4.2 us, past the caches 5.6), in FP32 of 8 bytes (1001 x 4099 6.0 us; 4, 16 bytes: 7.4, 7.0; bf16 of 2, 4, 8, 16 bytes: 6.9, 5.3, 4.7, 4.2).
+constexpr int BACK_ROWS = 16;
 template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t n, const uint8_t* in, typename Elem<TYPE>::Bits* X,
                                                        int64_t ldx, int64_t KT)
 {
     typedef typename Elem<TYPE>::Bits Bits;
-    constexpr int E = 16 / sizeof(Bits), LANES = 128 / E, PLACES = 256 / LANES;  // lanes to a row, places of a fragment at a time
-    const int t = threadIdx.x, lane = t % LANES, chunk = lane * E / 8, c = chunk >> 2, sub = chunk & 3;
-    const int64_t kt = blockIdx.x, quarter = (int64_t)blockIdx.y * 64, col = kt * TILE_K + lane * E;
-    if (col >= n) return;
+    constexpr int E = TYPE != F32 ? 8 : STREAM ? 4 : 2, LANES = 128 / E, PLACES = 256 / LANES;  // lanes to a row, places of a fragment at a time
+    constexpr int STEPS = BACK_ROWS / PLACES;                                                   // rows of a thread
+    const int t = threadIdx.x, lane = t % LANES, first = lane * E, chunk = first / 8, c = chunk >> 2, sub = chunk & 3;
+    const int64_t block = ((int64_t)blockIdx.z * BLOCKS_Y + blockIdx.y) * BACK_ROWS, quarter = block / 64 * 64;
+    const int64_t kt = blockIdx.x, col = kt * TILE_K + first;
+    if (block >= (rows + 63) / 64 * 64 || col >= n) return;
     const uint8_t* const tile = in + ((quarter / TILE_R) * KT + kt) * TILE_BYTES;
-    uint32_t scales[16 / PLACES], codes[16 / PLACES][4];
+    const int step0 = (int)(block % 64) / PLACES;
+    uint32_t scales[STEPS], codes[STEPS];
+    // step: four fragments of the places at hand, then the next places
+    const auto row_at = [&](int step) { return row_of(step % 4, step / 4 * PLACES + t / LANES); };
 #pragma unroll
-    for (int h = 0; h < 16 / PLACES; ++h) {
-        const int r = (int)(quarter % TILE_R) + row_of(0, h * PLACES + t / LANES);
-        scales[h] = *(const uint32_t*)(tile + scale_offset(r, c));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) codes[h][i] = *(const uint32_t*)(tile + code_offset(r + row_of(i, 0), c) + 4 * sub);
+    for (int s = 0; s < STEPS; ++s) {
+        const int r = (int)(quarter % TILE_R) + row_at(step0 + s);
+        scales[s] = tile[scale_offset(r, c)];
+        codes[s] = *(const uint32_t*)(tile + code_offset(r, c) + 4 * sub) >> (first % 8 * 4);
     }
 #pragma unroll
-    for (int h = 0; h < 16 / PLACES; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t row = quarter + row_of(i, h * PLACES + t / LANES);
-            if (row >= rows) continue;
-            Bits x[8];
-            values8<TYPE>(E == 4 ? codes[h][i] >> (lane % 2 * 16) : codes[h][i], (scales[h] >> (8 * i)) & 255u, x);
-            if (STREAM && n - col >= E) {
-                v4i y;
-                __builtin_memcpy(&y, x, 16);
-                __builtin_nontemporal_store(y, (v4i*)(X + row * ldx + col));
-            } else {
-                store_row<TYPE, E>(X + row * ldx + col, n - col, x);
-            }
+    for (int s = 0; s < STEPS; ++s) {
+        const int64_t row = quarter + row_at(step0 + s);
+        if (row >= rows) continue;
+        Bits x[8];
+        values8<TYPE>(codes[s], scales[s], x);
+        if (STREAM && n - col >= E) {
+            v4i y;
+            __builtin_memcpy(&y, x, 16);
+            __builtin_nontemporal_store(y, (v4i*)(X + row * ldx + col));
+        } else {
+            store_row<TYPE, E>(X + row * ldx + col, n - col, x);
         }
+    }
 }
 
 // Plain layout -> packed and back: one thread a block.  (16384 x 8192: 35 and 28 us, 143 MB at 4.1 and 5.0 TB/s.)
@@ -223,7 +227,7 @@ template <int TYPE> void quantize2(const Quantize& a, const Quantize& b, hipStre
 template <int TYPE> void dequantize(int64_t rows, int64_t n, const void* packed, void* X, int64_t ldx, hipStream_t st)
 {
     typedef typename Elem<TYPE>::Bits Bits;
-    const dim3 grid((unsigned)inner_tiles(n), (unsigned)((rows + 63) / 64));
+    const dim3 grid = grid_of(inner_tiles(n), (rows + 63) / 64 * (64 / BACK_ROWS));
     if (((uintptr_t)X | (uintptr_t)(ldx * (int64_t)sizeof(Bits))) % 16 == 0)
         k_mx_dequantize<TYPE, true><<<grid, dim3(256), 0, st>>>(rows, n, (const uint8_t*)packed, (Bits*)X, ldx, inner_tiles(n));
     else
