@@ -39,6 +39,7 @@ EXPORTS = list(_SIGNATURES)
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 BLOCK = 32
+FEW_ROWS = 16  # up to here a layer takes no workspace, whatever its sizes (asking the library for it is a quarter of a microsecond)
 WAYS = {"auto": -1, "direct": 0, "tile": 1, "half": 2}
 _uint8 = torch.uint8
 
@@ -216,7 +217,7 @@ def linear(X: torch.Tensor, W: Packed, dtype=None, alpha: float = 1.0, beta: flo
         raise ValueError("inner dimensions differ")
     p = W.rows
     D, ldd, dkind = _output(D, X, m, p, dtype or X.dtype, beta)
-    nbytes = _lib.ozimmu_mx_workspace_bytes(m, n, p) if workspace is None else 0
+    nbytes = _lib.ozimmu_mx_workspace_bytes(m, n, p) if workspace is None and m > FEW_ROWS else 0
     workspace, room, size = _workspace(workspace, nbytes, X)
     status = _lib.ozimmu_mx_linear(m, n, p, alpha, xkind, X.data_ptr(), ldx, W.data.data_ptr(), beta, dkind, D.data_ptr(), ldd,
                                    room, size, ozimmu._stream())

@@ -46,6 +46,7 @@ def test_sizes_of_packed_matrices_and_workspaces(mx):
     assert mx.packed_bytes(1, 1) == 17408 and mx.packed_bytes(256, 128) == 17408 and mx.packed_bytes(257, 129) == 4 * 17408
     assert mx.packed_bytes(0, 5) == 0 and mx.packed_bytes(2 ** 22, 5) == 0 and mx.packed_bytes(5, 2 ** 29 + 1) == 0
     # few rows take one launch and no workspace; others hold X packed
+    assert all(mx.workspace_bytes(m, n, p) == 0 for m in range(mx.FEW_ROWS + 1) for n in (1, 4096, 2 ** 20) for p in (1, 8192, 2 ** 21))
     assert mx.workspace_bytes(1, 4096, 4096) == 0 and mx.workspace_bytes(16, 8192, 2 ** 20) == 0
     assert mx.workspace_bytes(64, 4096, 4096) == 0 and mx.workspace_bytes(64, 4096, 8192) == mx.packed_bytes(64, 4096)
     assert mx.workspace_bytes(300, 512, 512) == mx.packed_bytes(300, 512)
