@@ -13,9 +13,9 @@
  *
  * Conventions are those of ozimmu.h: row-major matrices with leading dimensions counted in elements, device pointers owned by the
  * caller, no allocation, all work enqueued on `stream`, OZIMMU_OK or a negative status, nothing enqueued when a check fails.
- * Rows may begin at any element: leading dimensions and pointers need the alignment of their element type only.  Inputs
- * and outputs of a call must not overlap.  No state is kept between calls, and every call may be captured into a HIP graph.
- * Results do not depend on timing: the same call gives the same bits.
+ * Rows may begin at any element: leading dimensions (below 2^40, and rows x leading dimension below 2^60) and pointers need the
+ * alignment of their element type only.  Inputs and outputs of a call must not overlap.  No state is kept between calls, and
+ * every call may be captured into a HIP graph.  Results do not depend on timing: the same call gives the same bits.
  */
 #ifndef OZIMMU_MX_H
 #define OZIMMU_MX_H

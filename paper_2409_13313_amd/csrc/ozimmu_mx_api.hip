@@ -9,7 +9,10 @@ namespace {
 // rows <= 2^22 - 256: every grid dimension stays within the HIP limits (64 rows a workgroup along y)
 constexpr int64_t MAX_ROWS = ((int64_t)1 << 22) - 256;
 constexpr int64_t MAX_INNER = (int64_t)1 << 29;
-constexpr int64_t MAX_LD = ((int64_t)1 << 40) - 1;  // products of a row number and a leading dimension stay within 64 bits
+constexpr int64_t MAX_LD = ((int64_t)1 << 40) - 1;
+// rows x leading dimension: offsets in bytes stay within 64 bits, those of the rows that fill up a tile too (up to 2^29 rows where blocks
+// lie along the columns; MAX_ROWS x MAX_LD bytes of codes or scales are below that by themselves)
+constexpr int64_t MAX_SPAN = ((int64_t)1 << 60) - 1;
 
 inline bool sizes_ok(int64_t rows, int64_t n) { return rows >= 0 && n >= 0 && rows <= MAX_ROWS && n <= MAX_INNER; }
 inline bool type_ok(int type) { return type == OZIMMU_MX_F32 || type == OZIMMU_MX_BF16 || type == OZIMMU_MX_F16; }
@@ -29,7 +32,7 @@ int packed_status(const void* p, int64_t rows, int64_t n)
 int matrix_status(int type, const void* p, int64_t rows, int64_t n, int64_t ld)
 {
     if (!type_ok(type)) return OZIMMU_ERR_TYPE;
-    if (!ld_ok(ld, n)) return OZIMMU_ERR_DIM;
+    if (!ld_ok(ld, n) || (rows > 0 && ld > MAX_SPAN / rows)) return OZIMMU_ERR_DIM;
     if (rows == 0 || n == 0) return OZIMMU_OK;
     if (!p) return OZIMMU_ERR_NULL;
     return aligned_to_type(p, type) ? OZIMMU_OK : OZIMMU_ERR_TYPE;
