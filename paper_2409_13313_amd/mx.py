@@ -3,7 +3,8 @@ linear layer with its gradient.
 
 Argument marshalling only: device pointers of torch tensors and the current HIP stream go to the entry points of the same name.
 There is no CPU fallback.  Matrices are 2-D tensors with unit stride along their rows, in float32, bfloat16 or float16; results that
-are not handed over are allocated, workspaces too.
+are not handed over are allocated, workspaces too.  All tensors of a call have to be on the current device (torch.cuda.device), whose
+current stream it goes to.
 """
 from __future__ import annotations
 
@@ -42,6 +43,13 @@ BLOCK = 32
 FEW_ROWS = 16  # up to here a layer takes no workspace, whatever its sizes (asking the library for it is a quarter of a microsecond)
 WAYS = {"auto": -1, "direct": 0, "tile": 1, "half": 2}
 _uint8 = torch.uint8
+_several_devices = torch.cuda.device_count() > 1  # (where there is one, there is nothing to tell apart)
+
+
+def _on_current_device(t) -> None:
+    device = getattr(t, "device", None)
+    if device is not None and device.index != ozimmu._current_device():
+        raise ValueError(f"tensor on {device}, while the current device is cuda:{ozimmu._current_device()}")
 
 
 class Packed:
@@ -67,6 +75,8 @@ def _matrix(t: torch.Tensor) -> Tuple[int, int, int, int]:
         raise ValueError(f"expected float32, bfloat16 or float16, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError("tensor must live on the GPU")
+    if _several_devices:
+        _on_current_device(t)
     shape = t.shape
     if len(shape) != 2:
         raise ValueError("expected a 2-D tensor")
@@ -95,6 +105,8 @@ def _output(D: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int,
 def _packed(P: Packed, what: str) -> Packed:
     if not isinstance(P, Packed):
         raise ValueError(f"{what} has to be a packed matrix (see quantize and pack), got {type(P).__name__}")
+    if _several_devices:
+        _on_current_device(P.data)
     return P
 
 
@@ -129,6 +141,8 @@ def _workspace(workspace: Optional[torch.Tensor], nbytes: int, like: torch.Tenso
         workspace = like.new_empty(nbytes, dtype=_uint8)
     elif not (workspace.is_cuda and workspace.dtype is _uint8 and workspace.is_contiguous()):
         raise ValueError("a workspace is a contiguous uint8 tensor on the GPU")
+    elif _several_devices:
+        _on_current_device(workspace)
     return workspace, workspace.data_ptr(), workspace.numel()
 
 
@@ -165,6 +179,8 @@ def dequantize(P: Packed, dtype=torch.float32, out: Optional[torch.Tensor] = Non
 def _bytes_matrix(t: torch.Tensor, rows: int, width: int, what: str) -> int:
     if not t.is_cuda or t.dtype is not torch.uint8 or t.dim() != 2 or tuple(t.shape) != (rows, width):
         raise ValueError(f"{what}: expected uint8 of {rows} x {width} on the GPU, got {t.dtype} of {tuple(t.shape)}")
+    if _several_devices:
+        _on_current_device(t)
     if width > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < width:
         raise ValueError(f"{what}: expected unit stride along rows that do not overlap")
     return t.stride(0) if rows > 1 else max(width, 1)
