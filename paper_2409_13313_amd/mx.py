@@ -5,6 +5,9 @@ Argument marshalling only: device pointers of torch tensors and the current HIP 
 There is no CPU fallback.  Matrices are 2-D tensors with unit stride along their rows, in float32, bfloat16 or float16; results that
 are not handed over are allocated, workspaces too.  All tensors of a call have to be on the current device (torch.cuda.device), whose
 current stream it goes to.
+
+No operations are recorded for torch's autograd: linear_backward is called by the user, in torch.no_grad() or in the backward of a
+torch.autograd.Function.  linear and linear_backward refuse a tensor that requires a gradient while torch records.
 """
 from __future__ import annotations
 
@@ -50,6 +53,11 @@ def _on_current_device(t) -> None:
     device = getattr(t, "device", None)
     if device is not None and device.index != ozimmu._current_device():
         raise ValueError(f"tensor on {device}, while the current device is cuda:{ozimmu._current_device()}")
+
+
+def _not_recorded(t, what: str) -> None:
+    if getattr(t, "requires_grad", False) and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which the result would not carry: call this in torch.no_grad() or a torch.autograd.Function")
 
 
 class Packed:
@@ -229,6 +237,7 @@ def linear(X: torch.Tensor, W: Packed, dtype=None, alpha: float = 1.0, beta: flo
            workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """D <- alpha Q(X) W^T + beta D for rows X as they come and packed weights W (D in the type of X unless said otherwise)."""
     m, n, ldx, xkind = _matrix(X)
+    _not_recorded(X, "X")
     if _packed(W, "W").n != n:
         raise ValueError("inner dimensions differ")
     p = W.rows
@@ -253,6 +262,8 @@ def linear_backward(G: torch.Tensor, X: Optional[torch.Tensor], Wt: Optional[Pac
         raise ValueError("neither X (for dW) nor Wt (for dX) given")
     if (X is None and dW is not None) or (Wt is None and dX is not None):
         raise ValueError("dW takes X, dX takes Wt")
+    _not_recorded(G, "G")
+    _not_recorded(X, "X")
     ldx = lddx = lddw = dxkind = dwkind = 0
     x_at = wt_at = dx_at = dw_at = None
     if X is not None:
