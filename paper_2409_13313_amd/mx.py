@@ -95,16 +95,19 @@ def _matrix(t: torch.Tensor) -> Tuple[int, int, int, int]:
     return rows, cols, ld if rows > 1 else max(cols, ld, 1), kind
 
 
-def _output(D: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, dtype, beta: float):
-    """The caller's output, or a new one; its leading dimension and type number."""
+def _output(D: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, dtype, usual, beta: float):
+    """The caller's output, or a new one, of type `dtype` (None: the caller's, or `usual`); its leading dimension and type number."""
     if D is None:
         if beta != 0.0:
             raise ValueError("beta without the matrix that it multiplies")
+        dtype = dtype or usual
         kind = TYPES.get(dtype)
         if kind is None:
             raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
         return like.new_empty((rows, cols), dtype=dtype), max(cols, 1), kind
     m, n, ldd, kind = _matrix(D)
+    if dtype is not None and dtype is not D.dtype:
+        raise ValueError(f"output of {D.dtype} for a result of {dtype}")
     if m != rows or n != cols:
         raise ValueError(f"output of {m} x {n} for a result of {rows} x {cols}")
     return D, ldd, kind
@@ -174,10 +177,10 @@ def quantize(X: torch.Tensor, rows: bool = True, cols: bool = False) -> Tuple[Op
     return by_row, by_col
 
 
-def dequantize(P: Packed, dtype=torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """The values of a packed matrix."""
+def dequantize(P: Packed, dtype=None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values of a packed matrix (in float32, or the type of `out`, unless said otherwise)."""
     data = _packed(P, "the matrix").data
-    X, ldx, kind = _output(out, data, P.rows, P.n, dtype, 0.0)
+    X, ldx, kind = _output(out, data, P.rows, P.n, dtype, torch.float32, 0.0)
     status = _lib.ozimmu_mx_dequantize(kind, P.rows, P.n, data.data_ptr(), X.data_ptr(), ldx, ozimmu._stream())
     if status:
         raise OzimmuError(status)
@@ -220,14 +223,15 @@ def unpack(P: Packed) -> Tuple[torch.Tensor, torch.Tensor]:
     return codes, scales
 
 
-def gemm(A: Packed, B: Packed, dtype=torch.float32, alpha: float = 1.0, beta: float = 0.0, D: Optional[torch.Tensor] = None,
+def gemm(A: Packed, B: Packed, dtype=None, alpha: float = 1.0, beta: float = 0.0, D: Optional[torch.Tensor] = None,
          way: str = "auto") -> torch.Tensor:
-    """D <- alpha A B^T + beta D from packed matrices; `way` forces how it is run (see ozimmu_mx_gemm_way in the header)."""
+    """D <- alpha A B^T + beta D from packed matrices (a new D in float32 unless said otherwise); `way` forces how it is run (see
+    ozimmu_mx_gemm_way in the header)."""
     A, B = _packed(A, "A"), _packed(B, "B")
     if A.n != B.n:
         raise ValueError("inner dimensions differ")
     m, n, p = A.rows, A.n, B.rows
-    D, ldd, kind = _output(D, A.data, m, p, dtype, beta)
+    D, ldd, kind = _output(D, A.data, m, p, dtype, torch.float32, beta)
     _check(_lib.ozimmu_mx_gemm_way(WAYS[way], m, n, p, alpha, A.data.data_ptr(), B.data.data_ptr(), beta, kind, D.data_ptr(), ldd,
                                    ozimmu._stream()))
     return D
@@ -235,13 +239,13 @@ def gemm(A: Packed, B: Packed, dtype=torch.float32, alpha: float = 1.0, beta: fl
 
 def linear(X: torch.Tensor, W: Packed, dtype=None, alpha: float = 1.0, beta: float = 0.0, D: Optional[torch.Tensor] = None,
            workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """D <- alpha Q(X) W^T + beta D for rows X as they come and packed weights W (D in the type of X unless said otherwise)."""
+    """D <- alpha Q(X) W^T + beta D for rows X as they come and packed weights W (a new D in the type of X unless said otherwise)."""
     m, n, ldx, xkind = _matrix(X)
     _not_recorded(X, "X")
     if _packed(W, "W").n != n:
         raise ValueError("inner dimensions differ")
     p = W.rows
-    D, ldd, dkind = _output(D, X, m, p, dtype or X.dtype, beta)
+    D, ldd, dkind = _output(D, X, m, p, dtype, X.dtype, beta)
     nbytes = _lib.ozimmu_mx_workspace_bytes(m, n, p) if workspace is None and m > FEW_ROWS else 0
     workspace, room, size = _workspace(workspace, nbytes, X)
     status = _lib.ozimmu_mx_linear(m, n, p, alpha, xkind, X.data_ptr(), ldx, W.data.data_ptr(), beta, dkind, D.data_ptr(), ldd,
@@ -272,14 +276,14 @@ def linear_backward(G: torch.Tensor, X: Optional[torch.Tensor], Wt: Optional[Pac
             raise ValueError("X and G have to be of one type")
         if rows != m:
             raise ValueError("X and G have to have as many rows")
-        dW, lddw, dwkind = _output(dW, G, p, n, torch.float32, beta_w)
+        dW, lddw, dwkind = _output(dW, G, p, n, None, torch.float32, beta_w)
         x_at, dw_at = X.data_ptr(), dW.data_ptr()
     if Wt is not None:
         if X is None:
             n = _packed(Wt, "Wt").rows
         if _packed(Wt, "Wt").rows != n or Wt.n != p:
             raise ValueError(f"Wt of {Wt.rows} x {Wt.n} for a layer of {n} to {p}")
-        dX, lddx, dxkind = _output(dX, G, m, n, G.dtype, beta_x)
+        dX, lddx, dxkind = _output(dX, G, m, n, None, G.dtype, beta_x)
         wt_at, dx_at = Wt.data.data_ptr(), dX.data_ptr()
     nbytes = _lib.ozimmu_mx_backward_workspace_bytes(m, n, p) if workspace is None else 0
     workspace, room, size = _workspace(workspace, nbytes, G)
