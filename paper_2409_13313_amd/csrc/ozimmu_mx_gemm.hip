@@ -58,12 +58,12 @@ template <int N> __device__ inline void finish_any(const Gemm& g, int64_t row, i
 // ---- 64 rows x FB fragments of B (16 columns each) by a workgroup, operands straight from memory into registers ----
 //
 // For outputs too small for the tiles below, where the time is that of a launch, of the way of the operands and of one wave's share of the inner
-// dimension: the waves share the inner tiles, TILES of them on their way at a time, and their sums meet in LDS, in a fixed order.  256 x 4096 x
+// dimension: the waves share the inner tiles, each has one on its way at a time, and their sums meet in LDS, in a fixed order.  256 x 4096 x
 // 4096 6.8 us (10 MB, 1.3 PF; a launch alone is 2.5), 512 x 4096 x 4096 9.5; beyond that operands read again by every workgroup bound it.
 constexpr int DIRECT_SLOTS = 4;
 template <int FB> constexpr int direct_pitch() { return 16 * FB + 4; }  // floats between the rows of a wave's sums: rows fall on different banks
 
-template <int FB, int WAVES, int TILES> __device__ inline void direct_block(const Gemm& g, int64_t block_row, int64_t block_col, float* sums)
+template <int FB, int WAVES> __device__ inline void direct_block(const Gemm& g, int64_t block_row, int64_t block_col, float* sums)
 {
     constexpr int PITCH = direct_pitch<FB>(), SLOTS = DIRECT_SLOTS;
     const int t = threadIdx.x, lane = t & 63;
@@ -77,32 +77,22 @@ template <int FB, int WAVES, int TILES> __device__ inline void direct_block(cons
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < FB; ++j) acc[i][j] = v4f{0, 0, 0, 0};
-    for (int64_t kt0 = wave; kt0 < KT; kt0 += WAVES * TILES) {
-        v4i fa[TILES][4], fb[TILES][FB];
-        int sa[TILES], sb[TILES];
+    for (int64_t kt = wave; kt < KT; kt += WAVES) {
+        v4i fa[4], fb[FB];
+        const uint8_t* const ta = A + kt * TILE_BYTES;
+        const uint8_t* const tb = B + kt * TILE_BYTES;
 #pragma unroll
-        for (int u = 0; u < TILES; ++u) {
-            const int64_t kt = kt0 + u * WAVES < KT ? kt0 + u * WAVES : KT - 1;
-            const uint8_t* const ta = A + kt * TILE_BYTES;
-            const uint8_t* const tb = B + kt * TILE_BYTES;
+        for (int j = 0; j < FB; ++j) fb[j] = *(const v4i*)(tb + SCALE_BYTES + (f0 + j) * FRAGMENT_BYTES + lane * 16);
+        const int sb = *(const int*)(tb + lane * 4) >> (8 * f0);
 #pragma unroll
-            for (int j = 0; j < FB; ++j) fb[u][j] = *(const v4i*)(tb + SCALE_BYTES + (f0 + j) * FRAGMENT_BYTES + lane * 16);
-            sb[u] = *(const int*)(tb + lane * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) fa[u][i] = *(const v4i*)(ta + SCALE_BYTES + i * FRAGMENT_BYTES + lane * 16);
-            sa[u] = *(const int*)(ta + lane * 4);
-        }
-#pragma unroll
-        for (int u = 0; u < TILES; ++u) {
-            if (kt0 + u * WAVES >= KT) break;
-            const int s = sb[u] >> (8 * f0);
-            static_for<0, 4>([&](auto I) {
-                static_for<0, FB>([&](auto J) {
-                    constexpr int i = decltype(I)::value, j = decltype(J)::value;
-                    acc[i][j] = mfma<j, i>(fb[u][j], s, fa[u][i], sa[u], acc[i][j]);
-                });
+        for (int i = 0; i < 4; ++i) fa[i] = *(const v4i*)(ta + SCALE_BYTES + i * FRAGMENT_BYTES + lane * 16);
+        const int sa = *(const int*)(ta + lane * 4);
+        static_for<0, 4>([&](auto I) {
+            static_for<0, FB>([&](auto J) {
+                constexpr int i = decltype(I)::value, j = decltype(J)::value;
+                acc[i][j] = mfma<j, i>(fb[j], sb, fa[i], sa, acc[i][j]);
             });
-        }
+        });
     }
     // of the row at place l % 16 of fragment i, lane l holds the columns at places 4 (l / 16) .. + 3 of fragment j
     auto slot = [&](int w, int i, int j) { return (v4f*)(sums + (w * 64 + row_of(i, lane & 15)) * PITCH + j * 16 + (lane >> 4 << 2)); };
@@ -142,33 +132,33 @@ template <int FB, int WAVES, int TILES> __device__ inline void direct_block(cons
     }
 }
 
-template <int FB, int WAVES, int TILES> __global__ __launch_bounds__(64 * WAVES) void k_mx_direct(Gemm g)
+template <int FB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void k_mx_direct(Gemm g)
 {
     __shared__ __align__(16) float sums[DIRECT_SLOTS * 64 * direct_pitch<FB>()];
-    direct_block<FB, WAVES, TILES>(g, blockIdx.y, blockIdx.x, sums);
+    direct_block<FB, WAVES>(g, blockIdx.y, blockIdx.x, sums);
 }
 
 // Two products in one launch (the gradients of a small layer)
-template <int FB, int WAVES, int TILES>
+template <int FB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_mx_direct2(Gemm a, Gemm b, uint32_t cols_a, uint32_t cols_b, uint32_t blocks_a)
 {
     __shared__ __align__(16) float sums[DIRECT_SLOTS * 64 * direct_pitch<FB>()];
     const bool first = blockIdx.x < blocks_a;
     const uint32_t at = first ? blockIdx.x : blockIdx.x - blocks_a, cols = first ? cols_a : cols_b;
     const Gemm g = first ? a : b;
-    direct_block<FB, WAVES, TILES>(g, at / cols, at % cols, sums);
+    direct_block<FB, WAVES>(g, at / cols, at % cols, sums);
 }
 
 inline int64_t direct_units(const Gemm& g) { return (g.p + QUARTER_R - 1) / QUARTER_R * ((g.m + 63) / 64); }
 
-template <int FB, int WAVES, int TILES> void direct(const Gemm& g, const Gemm* also, hipStream_t st)
+template <int FB, int WAVES> void direct(const Gemm& g, const Gemm* also, hipStream_t st)
 {
     const unsigned cols = (unsigned)((g.p + QUARTER_R - 1) / QUARTER_R * (4 / FB)), rows = (unsigned)((g.m + 63) / 64);
     if (!also) {
-        k_mx_direct<FB, WAVES, TILES><<<dim3(cols, rows), dim3(64 * WAVES), 0, st>>>(g);
+        k_mx_direct<FB, WAVES><<<dim3(cols, rows), dim3(64 * WAVES), 0, st>>>(g);
     } else {
         const unsigned cols_b = (unsigned)((also->p + QUARTER_R - 1) / QUARTER_R * (4 / FB)), rows_b = (unsigned)((also->m + 63) / 64);
-        k_mx_direct2<FB, WAVES, TILES><<<dim3(cols * rows + cols_b * rows_b), dim3(64 * WAVES), 0, st>>>(g, *also, cols, cols_b, cols * rows);
+        k_mx_direct2<FB, WAVES><<<dim3(cols * rows + cols_b * rows_b), dim3(64 * WAVES), 0, st>>>(g, *also, cols, cols_b, cols * rows);
     }
 }
 
@@ -180,11 +170,11 @@ void direct(const Gemm& g, const Gemm* also, hipStream_t st)
     const int64_t units = direct_units(g) + (also ? direct_units(*also) : 0);
     const bool deep = inner_tiles(g.n) >= 32 || (also && inner_tiles(also->n) >= 32);
     if (units * 4 <= COMPUTE_UNITS)
-        deep ? direct<1, 8, 1>(g, also, st) : direct<1, 4, 1>(g, also, st);
+        deep ? direct<1, 8>(g, also, st) : direct<1, 4>(g, also, st);
     else if (units <= COMPUTE_UNITS * 5 / 4)
-        deep && units * 2 <= COMPUTE_UNITS ? direct<2, 8, 1>(g, also, st) : direct<2, 4, 1>(g, also, st);
+        deep && units * 2 <= COMPUTE_UNITS ? direct<2, 8>(g, also, st) : direct<2, 4>(g, also, st);
     else
-        direct<4, 4, 1>(g, also, st);
+        direct<4, 4>(g, also, st);
 }
 
 // ---- 256 x 256 outputs by a workgroup of four waves, 128 x 128 each: 256 FP32 sums a lane, one wave a SIMD ----
