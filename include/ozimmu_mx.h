@@ -53,8 +53,8 @@ int ozimmu_mx_unpack(int64_t rows, int64_t n, const void *packed, uint8_t *codes
                      void *stream);
 
 /* Bytes of device workspace (256-byte aligned, contents irrelevant) that ozimmu_mx_linear needs for X of m x n and D of m x p, 0 where it
- * takes one launch and needs none (workspace may be NULL then), and ozimmu_mx_linear_backward for X of m x n and G of m x p.  Calls that may
- * run at the same time must not share one.  0 for sizes out of range.  Host, pure. */
+ * takes one launch and needs none (workspace may be NULL then), and ozimmu_mx_linear_backward for X of m x n and G of m x p (one size,
+ * whichever of the gradients are asked for).  Calls that may run at the same time must not share one.  0 for sizes out of range.  Host, pure. */
 size_t ozimmu_mx_workspace_bytes(int64_t m, int64_t n, int64_t p);
 size_t ozimmu_mx_backward_workspace_bytes(int64_t m, int64_t n, int64_t p);
 
@@ -75,7 +75,8 @@ int ozimmu_mx_gemm_way(int way, int64_t m, int64_t n, int64_t p, float alpha, co
 int ozimmu_mx_choose(int64_t m, int64_t n, int64_t p, int64_t ldd);
 
 /* The forward pass of a linear layer: D <- alpha Q(X) W^T + beta D, X (device, m x n, ldx >= n) of type `xtype`, W packed
- * p x n, D of type `dtype`.  The same as ozimmu_mx_quantize(X) and ozimmu_mx_gemm; for few rows in one launch. */
+ * p x n, D of type `dtype`.  The product that ozimmu_mx_quantize(X) and ozimmu_mx_gemm make; for few rows in one launch, whose FP32 sums are
+ * formed in another order (the last bits of D may differ from theirs). */
 int ozimmu_mx_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void *X, int64_t ldx, const void *W, float beta,
                      int dtype, void *D, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);
 

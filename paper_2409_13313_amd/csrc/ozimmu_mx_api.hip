@@ -103,7 +103,7 @@ int ozimmu_mx_unpack(int64_t rows, int64_t n, const void* packed, uint8_t* codes
     return launched(mxk::launch_unpack(rows, n, packed, codes, ldc, scales, lds, (hipStream_t)stream));
 }
 
-// workspace of a product whose A is quantised in the call: A packed, then what the product itself needs
+// workspace of a product whose A is quantised in the call: A packed
 size_t ozimmu_mx_workspace_bytes(int64_t m, int64_t n, int64_t p)
 {
     if (!sizes_ok(m, n) || !sizes_ok(p, n) || mxk::few_rows(m, p)) return 0;

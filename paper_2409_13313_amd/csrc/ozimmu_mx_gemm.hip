@@ -190,8 +190,8 @@ void direct(const Gemm& g, const Gemm* also, hipStream_t st)
 // One barrier a stage, in its middle, where every wave has fetched all of the stage and its own copies of the next one have landed: behind
 // it the stage's place in the ring takes the copies of the fourth stage from here.  Ten copies a wave and stage; those behind the last
 // stage are out of the buffer's range: they read nothing, but count, so that every stage waits alike.
-// Bound by power where the product is large: 8192 x 8192 x 16384 416 us (5.3 PF) from cool, 513 (4.3) call after call with changing operands, 330 on
-// zeros, which are the same instructions.  A register-only loop of the instruction gives 7.6 PF (with 32 x 32 x 64 6.7).  8192 x 4096 x 8192 112 us.
+// Bound by power where the product is large: 8192 x 8192 x 16384 440 to 546 us (5.0 to 4.0 PF) on random operands, by what ran before (416 the
+// least seen), 325 to 420 on zeros, which are the same instructions.  A register-only loop of the instruction gives 7.6 PF (with 32 x 32 x 64 6.7).  8192 x 4096 x 8192 112 us.
 constexpr int RING = 4, STAGE_BYTES = 2 * TILE_BYTES, COPIES = 10;
 constexpr int NXCD = 8;
 constexpr int64_t MEMORY_SIDE_CACHE = (int64_t)256 << 20;
@@ -921,6 +921,9 @@ bool way_fits(int way, int64_t m, int64_t n, int64_t p, int64_t ldd)
 // 4096 x 4096 x 4096: 63, 35.6, 33.7;  512 x 8192 x 8192: 29.2, 26.5, 40.3;  1024 x 8192 x 8192: 56, 32.9, 41.8;  2048 x 8192 x 8192: 112, 62, 56;
 // 512 x 1024 x 8192: 9.6, 8.3, 11.4;  256 x 4096 x 14336: 17.8, 16.7, 24.4;  512 x 4096 x 14336: 33.0, 17.9, 25.0;  1024 x 4096 x 14336: 58, 32.5, 29.0;
 // 768 x 4096 x 14336: 47, 31.2, 26.1;  2048 x 2048 x 2048: 11.9, 11.1, 15.7;  8192 x 2048 x 8192: 152, 74.5, 66.6;  4096 x 2051 x 1283: 19.8, 15.3, 24.1.
+// Not in it, as it decides nothing at these: the writing of a large D of a short inner dimension (8192 x 512 x 8192: 110, -, 58, estimated 87, -, 29) and
+// the length of the walk in few workgroups (64 x 8192 x 1024: 7.6, 23.6, 37.3, estimated 3.5, 26.2, 39.8).  beta != 0 takes longer in the tiles (2048 x 4096 x
+// 4096: 20.4 us and 29.7) and in k_mx_direct (8192 x 128 x 8192: 88 and 160).
 double estimate_us(int way, int64_t m, int64_t n, int64_t p)
 {
     const double KT = (double)inner_tiles(n);

@@ -126,8 +126,10 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_mx_quantize_cols2(C
 // Reading back: a lane makes 16 bytes, E elements, of a row, side by side with its neighbours (FP32: half of the eight codes that it loads; 32 bytes a
 // lane in two stores: 16384 x 8192 183 us, so 154, today 84).  A workgroup takes 16 rows x 128 columns (64 rows: 4096 x 4096 FP32 13.6 us, 16 rows 11.5;
 // 513 x 1001 3.6 and 2.9; 16384 x 8192 85.7 and 84.5).  STREAM, where rows begin at multiples of 16 bytes: stores
-// past the caches (16384 x 8192 FP32 84.5 us = 7.2 TB/s, a large fill writes 6.9; bf16 47.7 and 64).  Rows that begin anywhere: plain stores (1001 x 4099
-// bf16 4.2 us, past the caches 5.6), in FP32 of 8 bytes (1001 x 4099 6.0 us; 4, 16 bytes: 7.4, 7.0; bf16 of 2, 4, 8, 16 bytes: 6.9, 5.3, 4.7, 4.2).
+// past the caches (16384 x 8192 FP32 84.5 us = 7.2 TB/s, a large fill writes 6.9; bf16 47.7 and 64).  What reads X right behind them loses up to 5 %
+// of the two, and gains where X is large (past the caches and plain, bf16: read back and a product of 16 rows with it, 4096 x 4096 27.1 and 26.3 us,
+// 8192 x 8192 63 and 69, 16384 x 8192 132 and 137; read back and 1 added to it, 22.9 and 21.8, 79 and 76, 154 and 162).  Rows that begin anywhere: plain
+// stores (1001 x 4099 bf16 4.2 us, past the caches 5.6), in FP32 of 8 bytes (1001 x 4099 6.0 us; 4, 16 bytes: 7.4, 7.0; bf16 of 2, 4, 8, 16 bytes: 6.9, 5.3, 4.7, 4.2).
 constexpr int BACK_ROWS = 16;
 template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(256) void k_mx_dequantize(int64_t rows, int64_t n, const uint8_t* in, typename Elem<TYPE>::Bits* X,
