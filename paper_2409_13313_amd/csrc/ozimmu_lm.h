@@ -1,0 +1,121 @@
+// Operators around a model's output layer (include/ozimmu_lm.h): the stored form of 4-bit weights and the launchers of their kernels
+// (ozimmu_lm_*.hip).
+//
+// Weights in 4 bits, p rows of n elements.  Codes come in blocks of 16 rows x 128 elements, 1 KiB each, the blocks of 16 rows one behind the
+// other along the row: 16 bytes for each lane l of a wave, the codes of row l % 16 that it holds in four matrix instructions (16x16x32).
+// Word j of them (j < 4) is elements 32 j + 8 (l / 16) .. + 7, element 2 i at bits 4 i and 2 i + 1 at bits 16 + 4 i, so that one mask
+// and one or makes a pair of 16-bit numbers of two neighbouring elements.
+// Behind the codes of all blocks come their scales, [block][row][128 / group] numbers of 16 bits (0 behind the end of a row), and behind those,
+// where the weights have zero points, these as bytes in the same order.  Codes behind the end of a row are 0.  Padding rows are not written:
+// what they give is not stored.
+#pragma once
+#include "ozimmu_mx_convert.h"
+
+namespace lml {
+
+constexpr int ROWS = 16, INNER = 128, BLOCK_BYTES = 1024;
+
+struct Shape {
+    int64_t p, n;
+    int group;   // 32, 64 or 128
+    bool zeros;
+    __host__ __device__ inline int64_t row_blocks() const { return (p + ROWS - 1) / ROWS; }
+    __host__ __device__ inline int64_t inner_blocks() const { return (n + INNER - 1) / INNER; }
+    __host__ __device__ inline int64_t blocks() const { return row_blocks() * inner_blocks(); }
+    __host__ __device__ inline int groups() const { return INNER / group; }  // of a block's row
+    __host__ __device__ inline int64_t scales_at() const { return blocks() * BLOCK_BYTES; }
+    __host__ __device__ inline int64_t zeros_at() const { return scales_at() + (blocks() * ROWS * groups() * 2 + 255) / 256 * 256; }
+    __host__ __device__ inline int64_t bytes() const { return zeros_at() + (zeros ? (blocks() * ROWS * groups() + 255) / 256 * 256 : 0); }
+};
+
+}  // namespace lml
+
+namespace lmk {
+
+using mxk::BF16;
+using mxk::F16;
+using mxk::F32;
+
+struct Weights {
+    lml::Shape shape;
+    int stype;            // type of the scales: BF16 or F16
+    const uint8_t* data;
+};
+
+hipError_t launch_quantize(int type, const void* W, int64_t ldw, const lml::Shape& s, int stype, void* packed, hipStream_t st);
+// rows row0 .. row0 + rows - 1 into X (of `type`); columns n .. cols - 1 become zeros
+hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, hipStream_t st);
+hipError_t launch_pack(const lml::Shape& s, const uint8_t* codes, int64_t ldc, const void* scales, int64_t lds, const uint8_t* zeros, int64_t ldz,
+                       void* packed, hipStream_t st);
+hipError_t launch_unpack(const lml::Shape& s, const void* packed, uint8_t* codes, int64_t ldc, void* scales, int64_t lds, uint8_t* zeros,
+                         int64_t ldz, hipStream_t st);
+
+// D <- alpha X W^T + beta D straight from the stored weights (m rows of X)
+struct Linear {
+    int64_t m;
+    const void* X;
+    int64_t ldx;
+    int xtype;
+    void* D;
+    int64_t ldd;
+    int dtype;
+    float alpha, beta;
+};
+hipError_t launch_direct(const Linear& l, const Weights& w, hipStream_t st);
+
+// ---- products of 16-bit matrices in tiles of 256 x 256 (ozimmu_lm_tile.hip) ----
+
+// What is made of the sums C (m x p, over the inner dimension n):
+enum Kind {
+    LINEAR,   // A: m x n, B: p x n.  D <- alpha C + beta D
+    LOSS,     // A: m x n, B: p x n.  per row and 128 columns: log2(e) times the largest sum, and the sum of 2^(log2(e) c - that) (without the target's)
+    SLOPE,    // A: m x n, B: p x n.  D <- exp(C - lse) - [column = target] in 16 bits (0 in rows without a target)
+    STATES,   // A: m x n, B: n x p.  D (FP32, one for each split of n) <- C, or C + D
+    WEIGHTS,  // A: n x m, B: n x p.  D <- alpha C + beta D, alpha from the device
+};
+
+struct Tile {
+    int kind, type;       // type: of A and B
+    int64_t m, n, p;
+    const void *A, *B;    // 16-byte aligned; leading dimensions multiples of 8 elements; where rows lie along n, n a multiple of 8
+    int64_t lda, ldb;
+    int64_t b_rows;       // of B: p, or where its rows lie across n how many of n there are (the others count as zeros)
+    void* D = nullptr;
+    int64_t ldd = 0;
+    int dtype = 0;
+    float alpha = 1, beta = 0;
+    const float* alpha_at = nullptr;   // WEIGHTS: alpha is multiplied by this
+    int splits = 1;                    // STATES: of the inner dimension
+    int64_t split_stride = 0;          // STATES: elements between the D of splits
+    const int* targets = nullptr;      // LOSS, SLOPE: per row of whole tiles; < 0: NO_TARGET, BAD_TARGET
+    int column0 = 0;                   // LOSS, SLOPE: what number the first column is to them
+    const float* lse2 = nullptr;       // SLOPE: log2(e) lse per row of whole tiles
+    float* at_target = nullptr;        // LOSS: the sums at the targets
+    float2* parts = nullptr;           // LOSS: [128 columns][row]
+    int64_t parts_ld = 0;
+};
+bool tile_fits(const Tile& t);
+hipError_t launch_tile(const Tile& t, hipStream_t st);
+
+// ---- what stands around them in the loss (ozimmu_lm_loss.hip) ----
+
+constexpr int NO_TARGET = -1, BAD_TARGET = -2;  // an ignored row; a target that no column has
+constexpr float SLOPE_SCALE_F16 = 32768.0f;     // slopes in FP16 are held times this: most of them are far below 2^-14
+
+// rows x cols of X (16 bits) into Y, columns cols .. width - 1 zeros; with `ratio`, times ratio[row] (0: zeros whatever X holds)
+hipError_t launch_lay_out(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, const float* ratio, void* Y, int64_t ldy, int64_t width,
+                          hipStream_t st);
+// targets as Tile has them (rows .. padded - 1: NO_TARGET)
+hipError_t launch_targets(int64_t rows, int64_t padded, int64_t words, const int64_t* y, int64_t stride, int64_t ignore, int* targets, hipStream_t st);
+hipError_t launch_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const int* targets, const float* at_target, float* loss,
+                       float* lse, hipStream_t st);
+// targets, log2(e) lse (NaN where the target is bad), the largest |g| of rows with a target and each row's share of it
+hipError_t launch_slopes(int64_t rows, int64_t padded, int64_t words, const int64_t* y, int64_t stride, int64_t ignore, const float* g, int64_t g_stride,
+                         const float* lse, int* targets, float* lse2, float* ratio, float* largest, hipStream_t st);
+// dX <- g (the sum of the splits) / scale, zeros in rows without a target
+hipError_t launch_states(int type, int64_t rows, int64_t cols, const float* parts, int64_t ld, int splits, int64_t split_stride, const float* g,
+                         int64_t g_stride, const int* targets, float scale, void* dX, int64_t ldx, hipStream_t st);
+// X <- beta X (beta == 0: zeros)
+hipError_t launch_scale(int type, int64_t rows, int64_t cols, float beta, void* X, int64_t ldx, hipStream_t st);
+
+}  // namespace lmk

@@ -1,0 +1,469 @@
+// C ABI of the operators around a model's output layer (declared in include/ozimmu_lm.h): argument checks, workspace carving and launches.
+// No allocation, no host synchronisation, no state between calls.
+#include "../../include/ozimmu.h"
+#include "../../include/ozimmu_lm.h"
+#include "ozimmu_lm.h"
+
+namespace {
+
+using lmk::Tile;
+using lml::Shape;
+
+constexpr int64_t MAX_ROWS = ((int64_t)1 << 22) - 256, MAX_INNER = (int64_t)1 << 20, MAX_LD = ((int64_t)1 << 40) - 1;
+constexpr int64_t MAX_SPAN = ((int64_t)1 << 60) - 1;   // rows x leading dimension: byte offsets stay within 64 bits
+constexpr int64_t MAX_STATES = ((int64_t)1 << 31) - (1 << 20);
+constexpr int64_t COMPUTE_UNITS = 256;
+
+inline int64_t round_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+inline bool rows_ok(int64_t r) { return r >= 0 && r <= MAX_ROWS; }
+inline bool sizes_ok(int64_t p, int64_t n) { return rows_ok(p) && n >= 0 && n <= MAX_INNER; }
+inline bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
+inline bool type_ok(int type) { return type == OZIMMU_LM_F32 || type == OZIMMU_LM_BF16 || type == OZIMMU_LM_F16; }
+inline bool type16_ok(int type) { return type == OZIMMU_LM_BF16 || type == OZIMMU_LM_F16; }
+inline bool aligned(const void* p) { return ((uintptr_t)p & 255u) == 0; }
+
+// a matrix in memory: given, aligned for its type, its rows apart
+int matrix_status(int type, const void* p, int64_t rows, int64_t n, int64_t ld)
+{
+    if (!type_ok(type)) return OZIMMU_ERR_TYPE;
+    if (ld < n || ld > MAX_LD || (rows > 0 && ld > MAX_SPAN / rows)) return OZIMMU_ERR_DIM;
+    if (rows == 0 || n == 0) return OZIMMU_OK;
+    if (!p) return OZIMMU_ERR_NULL;
+    return ((uintptr_t)p & (type == OZIMMU_LM_F32 ? 3u : 1u)) == 0 ? OZIMMU_OK : OZIMMU_ERR_TYPE;
+}
+// numbers of `size` bytes, `stride` apart
+int vector_status(const void* p, int64_t rows, int64_t stride, unsigned size)
+{
+    if (stride < 0 || stride > MAX_LD) return OZIMMU_ERR_DIM;
+    if (rows == 0) return OZIMMU_OK;
+    if (!p) return OZIMMU_ERR_NULL;
+    return (uintptr_t)p % size == 0 ? OZIMMU_OK : OZIMMU_ERR_TYPE;
+}
+int packed_status(const void* p, int64_t rows, int64_t n, int group, int scale_type)
+{
+    if (!group_ok(group)) return OZIMMU_ERR_DIM;
+    if (!type16_ok(scale_type)) return OZIMMU_ERR_TYPE;
+    if (rows == 0 || n == 0) return OZIMMU_OK;
+    if (!p) return OZIMMU_ERR_NULL;
+    return aligned(p) ? OZIMMU_OK : OZIMMU_ERR_WORKSPACE;
+}
+int workspace_status(const void* p, size_t bytes, size_t need)
+{
+    if (need == 0) return OZIMMU_OK;
+    if (!p) return OZIMMU_ERR_NULL;
+    return bytes >= need && aligned(p) ? OZIMMU_OK : OZIMMU_ERR_WORKSPACE;
+}
+#define CHECK(x)                                  \
+    do {                                          \
+        const int status_ = (x);                  \
+        if (status_ != OZIMMU_OK) return status_; \
+    } while (0)
+
+inline int launched(hipError_t e) { return e == hipSuccess ? OZIMMU_OK : OZIMMU_ERR_HIP; }
+
+// Pieces of a workspace, one behind the other (without a workspace: their sizes)
+struct Room {
+    uint8_t* base;
+    size_t used = 0;
+    template <class T> T* take(int64_t count)
+    {
+        T* const at = base ? (T*)(base + used) : nullptr;
+        used += (size_t)round_to(count * (int64_t)sizeof(T), 256);
+        return at;
+    }
+};
+
+// whether the tiles can take rows along the inner dimension as they are
+bool as_it_is(const void* p, int64_t n, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && n % 8 == 0 && ld * 2 < (1 << 22); }
+
+// ---- the linear layer from the stored form ----
+
+struct LinearPlan {
+    int64_t width, rows;   // of a piece of weights read back
+    uint16_t *W, *X;
+    size_t bytes;
+    LinearPlan(int64_t m, int64_t n, int64_t p, void* workspace)
+    {
+        Room room{(uint8_t*)workspace};
+        width = round_to(n, 64);
+        // pieces of at most 128 MB, which stay in the memory-side cache until they are multiplied
+        const int64_t most = ((int64_t)1 << 27) / (width * 2) / 256 * 256;
+        rows = most < 256 ? 256 : most;
+        if (rows > round_to(p, 256)) rows = round_to(p, 256);
+        W = room.take<uint16_t>(rows * width);
+        X = room.take<uint16_t>(m * width);
+        bytes = room.used;
+    }
+};
+
+int choose(int64_t m, int64_t n, int64_t p)
+{
+    (void)n;
+    (void)p;
+    return m <= 128 ? OZIMMU_LM_WAY_DIRECT : OZIMMU_LM_WAY_TILE;
+}
+
+int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void* X, int64_t ldx, const lmk::Weights& w, float beta, int dtype, void* D,
+                int64_t ldd, void* workspace, hipStream_t st)
+{
+    const LinearPlan plan(m, n, p, workspace);
+    Tile t{lmk::LINEAR, xtype};
+    t.m = m;
+    t.n = n;
+    t.A = X;
+    t.lda = ldx;
+    if (!as_it_is(X, n, ldx)) {
+        t.n = plan.width;
+        CHECK(launched(lmk::launch_lay_out(xtype, m, n, X, ldx, nullptr, plan.X, plan.width, plan.width, st)));
+        t.A = plan.X;
+        t.lda = plan.width;
+    }
+    t.B = plan.W;
+    t.ldb = plan.width;
+    t.ldd = ldd;
+    t.dtype = dtype;
+    t.alpha = alpha;
+    t.beta = beta;
+    const int64_t size = dtype == OZIMMU_LM_F32 ? 4 : 2;
+    for (int64_t at = 0; at < p; at += plan.rows) {
+        t.p = t.b_rows = p - at < plan.rows ? p - at : plan.rows;
+        CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, st)));
+        t.D = (uint8_t*)D + at * size;
+        CHECK(launched(lmk::launch_tile(t, st)));
+    }
+    return OZIMMU_OK;
+}
+
+// ---- cross entropy ----
+
+bool loss_sizes_ok(int64_t m, int64_t n, int64_t p)
+{
+    return rows_ok(m) && p >= 1 && p <= MAX_ROWS && n >= 1 && n <= MAX_INNER && round_to(m, 256) * round_to(n, 256) < MAX_STATES;
+}
+
+// W in pieces of rows that are laid out anew where the tiles cannot take it as it is: at most 256 MB (there are enough tiles in those)
+int64_t laid_out_rows(int64_t width, int64_t p)
+{
+    int64_t rows = ((int64_t)1 << 28) / (width * 2) / 256 * 256;
+    if (rows < 256) rows = 256;
+    return rows < round_to(p, 256) ? rows : round_to(p, 256);
+}
+
+struct LossPlan {
+    int64_t width, tokens, words;   // of a row laid out; tokens at a time; rows of W laid out at a time
+    int* targets;
+    float* at_target;
+    float2* parts;
+    uint16_t *X, *W;
+    size_t bytes;
+    LossPlan(int64_t m, int64_t n, int64_t p, void* workspace)
+    {
+        Room room{(uint8_t*)workspace};
+        width = round_to(n, 64);
+        const int64_t blocks = (p + 127) / 128;
+        // tokens at a time: parts of at most 256 MB
+        tokens = ((int64_t)1 << 25) / blocks / 256 * 256;
+        if (tokens < 256) tokens = 256;
+        if (tokens > round_to(m, 256)) tokens = round_to(m, 256);
+        words = laid_out_rows(width, p);
+        targets = room.take<int>(tokens);
+        at_target = room.take<float>(tokens);
+        parts = room.take<float2>(blocks * tokens);
+        X = room.take<uint16_t>(tokens * width);
+        W = room.take<uint16_t>(words * width);
+        bytes = room.used;
+    }
+};
+
+struct GradientPlan {
+    int64_t padded, width, states_ld, words;   // rows and columns of whole tiles; words at a time
+    int splits;
+    int* targets;
+    float *lse2, *ratio, *largest, *states;
+    uint16_t *slopes, *X, *scaled, *W;
+    size_t bytes;
+    GradientPlan(int64_t m, int64_t n, int64_t p, void* workspace)
+    {
+        Room room{(uint8_t*)workspace};
+        padded = round_to(m, 256);
+        width = round_to(n, 64);
+        states_ld = round_to(n, 256);
+        // slopes of at most 128 MB, which stay in the memory-side cache for the two products that read them, and pieces of W of at most 1 GB
+        words = ((int64_t)1 << 26) / padded / 256 * 256;
+        const int64_t most = ((int64_t)1 << 29) / width / 256 * 256;
+        if (words > most) words = most;
+        if (words < 256) words = 256;
+        if (words > round_to(p, 256)) words = round_to(p, 256);
+        // the states' gradient: with few tiles the words are shared by several workgroups
+        const int64_t tiles = padded / 256 * (states_ld / 256);
+        const int64_t most_splits = words / 64 / 4 < 1 ? 1 : words / 64 / 4;
+        int64_t s = COMPUTE_UNITS / (tiles < 1 ? 1 : tiles);
+        s = s < 1 ? 1 : s;
+        splits = (int)(s < most_splits ? s : most_splits);
+        targets = room.take<int>(padded);
+        lse2 = room.take<float>(padded);
+        ratio = room.take<float>(padded);
+        largest = room.take<float>(1);
+        slopes = room.take<uint16_t>(padded * words);
+        states = room.take<float>(splits * padded * states_ld);
+        X = room.take<uint16_t>(m * width);
+        scaled = room.take<uint16_t>(m * width);
+        W = room.take<uint16_t>(words * width);
+        bytes = room.used;
+    }
+};
+
+}  // namespace
+
+extern "C" {
+
+size_t ozimmu_lm_bytes(int64_t p, int64_t n, int group, int zeros)
+{
+    return sizes_ok(p, n) && group_ok(group) ? (size_t)Shape{p, n, group, zeros != 0}.bytes() : 0;
+}
+
+int ozimmu_lm_quantize(int type, int64_t p, int64_t n, const void* W, int64_t ldw, int group, int zeros, int scale_type, void* packed, void* stream)
+{
+    if (!sizes_ok(p, n)) return OZIMMU_ERR_DIM;
+    CHECK(matrix_status(type, W, p, n, ldw));
+    CHECK(packed_status(packed, p, n, group, scale_type));
+    if (p == 0 || n == 0) return OZIMMU_OK;
+    return launched(lmk::launch_quantize(type, W, ldw, Shape{p, n, group, zeros != 0}, scale_type, packed, (hipStream_t)stream));
+}
+
+int ozimmu_lm_dequantize(int type, int64_t p, int64_t n, int group, int zeros, int scale_type, const void* packed, void* W, int64_t ldw, void* stream)
+{
+    if (!sizes_ok(p, n)) return OZIMMU_ERR_DIM;
+    CHECK(matrix_status(type, W, p, n, ldw));
+    CHECK(packed_status(packed, p, n, group, scale_type));
+    if (p == 0 || n == 0) return OZIMMU_OK;
+    const lmk::Weights w{Shape{p, n, group, zeros != 0}, scale_type, (const uint8_t*)packed};
+    return launched(lmk::launch_dequantize(type, w, 0, p, n, W, ldw, (hipStream_t)stream));
+}
+
+static int plain_status(int64_t p, int64_t n, int group, const void* codes, int64_t ldc, const void* scales, int64_t lds, const void* zeros, int64_t ldz,
+                        const void* packed)
+{
+    if (!sizes_ok(p, n) || !group_ok(group)) return OZIMMU_ERR_DIM;
+    const int64_t groups = (n + group - 1) / group;
+    if (ldc < (n + 1) / 2 || ldc > MAX_LD || lds < groups || lds > MAX_LD || (zeros && (ldz < groups || ldz > MAX_LD))) return OZIMMU_ERR_DIM;
+    if (p > 0 && n > 0 && (!codes || !scales)) return OZIMMU_ERR_NULL;
+    if ((uintptr_t)scales & 1u) return OZIMMU_ERR_TYPE;
+    return packed_status(packed, p, n, group, OZIMMU_LM_F16);
+}
+
+int ozimmu_lm_pack(int64_t p, int64_t n, int group, const uint8_t* codes, int64_t ldc, const void* scales, int64_t lds, const uint8_t* zeros, int64_t ldz,
+                   void* packed, void* stream)
+{
+    CHECK(plain_status(p, n, group, codes, ldc, scales, lds, zeros, ldz, packed));
+    if (p == 0 || n == 0) return OZIMMU_OK;
+    return launched(lmk::launch_pack(Shape{p, n, group, zeros != nullptr}, codes, ldc, scales, lds, zeros, ldz, packed, (hipStream_t)stream));
+}
+
+int ozimmu_lm_unpack(int64_t p, int64_t n, int group, const void* packed, uint8_t* codes, int64_t ldc, void* scales, int64_t lds, uint8_t* zeros,
+                     int64_t ldz, void* stream)
+{
+    CHECK(plain_status(p, n, group, codes, ldc, scales, lds, zeros, ldz, packed));
+    if (p == 0 || n == 0) return OZIMMU_OK;
+    return launched(lmk::launch_unpack(Shape{p, n, group, zeros != nullptr}, packed, codes, ldc, scales, lds, zeros, ldz, (hipStream_t)stream));
+}
+
+int ozimmu_lm_linear_choose(int64_t m, int64_t n, int64_t p) { return choose(m, n, p); }
+
+size_t ozimmu_lm_linear_way_workspace_bytes(int way, int64_t m, int64_t n, int64_t p)
+{
+    if (!sizes_ok(p, n) || !rows_ok(m)) return 0;
+    if (way == OZIMMU_LM_WAY_AUTO) way = choose(m, n, p);
+    return way == OZIMMU_LM_WAY_TILE && m > 0 && n > 0 && p > 0 ? LinearPlan(m, n, p, nullptr).bytes : 0;
+}
+size_t ozimmu_lm_linear_workspace_bytes(int64_t m, int64_t n, int64_t p) { return ozimmu_lm_linear_way_workspace_bytes(OZIMMU_LM_WAY_AUTO, m, n, p); }
+
+int ozimmu_lm_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void* X, int64_t ldx, int group, int zeros, int scale_type,
+                     const void* W, float beta, int dtype, void* D, int64_t ldd, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return ozimmu_lm_linear_way(OZIMMU_LM_WAY_AUTO, m, n, p, alpha, xtype, X, ldx, group, zeros, scale_type, W, beta, dtype, D, ldd, workspace,
+                                workspace_bytes, stream);
+}
+
+int ozimmu_lm_linear_way(int way, int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void* X, int64_t ldx, int group, int zeros, int scale_type,
+                         const void* W, float beta, int dtype, void* D, int64_t ldd, void* workspace, size_t workspace_bytes, void* stream)
+{
+    // (an empty inner dimension: the sum would be zero, but there is nothing stored to read it from)
+    if (!sizes_ok(p, n) || !rows_ok(m) || n == 0) return OZIMMU_ERR_DIM;
+    if (!type16_ok(xtype)) return OZIMMU_ERR_TYPE;
+    CHECK(matrix_status(xtype, X, m, n, ldx));
+    CHECK(matrix_status(dtype, D, m, p, ldd));
+    if (way == OZIMMU_LM_WAY_AUTO) way = choose(m, n, p);
+    if (way != OZIMMU_LM_WAY_DIRECT && way != OZIMMU_LM_WAY_TILE) return OZIMMU_ERR_WAY;
+    CHECK(packed_status(W, p, n, group, scale_type));
+    if (m == 0 || p == 0) return OZIMMU_OK;
+    CHECK(workspace_status(workspace, workspace_bytes, ozimmu_lm_linear_way_workspace_bytes(way, m, n, p)));
+    const lmk::Weights w{Shape{p, n, group, zeros != 0}, scale_type, (const uint8_t*)W};
+    const hipStream_t st = (hipStream_t)stream;
+    if (way == OZIMMU_LM_WAY_TILE) return linear_tile(m, n, p, alpha, xtype, X, ldx, w, beta, dtype, D, ldd, workspace, st);
+    return launched(lmk::launch_direct({m, X, ldx, xtype, D, ldd, dtype, alpha, beta}, w, st));
+}
+
+size_t ozimmu_lm_cross_entropy_workspace_bytes(int64_t m, int64_t n, int64_t p)
+{
+    return loss_sizes_ok(m, n, p) && m > 0 ? LossPlan(m, n, p, nullptr).bytes : 0;
+}
+
+int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* y,
+                            int64_t y_stride, int64_t ignore, float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!loss_sizes_ok(m, n, p)) return OZIMMU_ERR_DIM;
+    if (!type16_ok(type)) return OZIMMU_ERR_TYPE;
+    CHECK(matrix_status(type, X, m, n, ldx));
+    CHECK(matrix_status(type, W, p, n, ldw));
+    CHECK(vector_status(y, m, y_stride, 8));
+    CHECK(vector_status(loss, m, 1, 4));
+    CHECK(vector_status(lse, m, 1, 4));
+    CHECK(workspace_status(workspace, workspace_bytes, ozimmu_lm_cross_entropy_workspace_bytes(m, n, p)));
+    if (m == 0) return OZIMMU_OK;
+    const LossPlan plan(m, n, p, workspace);
+    const hipStream_t st = (hipStream_t)stream;
+    const bool x_as_it_is = as_it_is(X, n, ldx), w_as_it_is = as_it_is(W, n, ldw);
+    for (int64_t t0 = 0; t0 < m; t0 += plan.tokens) {
+        const int64_t rows = m - t0 < plan.tokens ? m - t0 : plan.tokens;
+        Tile t{lmk::LOSS, type};
+        t.m = rows;
+        t.n = x_as_it_is && w_as_it_is ? n : plan.width;
+        t.A = (const uint16_t*)X + t0 * ldx;
+        t.lda = ldx;
+        // (one that is laid out has zeros up to `width`; the other must not then be read beyond n, so both are)
+        if (t.n != n || !x_as_it_is) {
+            CHECK(launched(lmk::launch_lay_out(type, rows, n, t.A, ldx, nullptr, plan.X, plan.width, plan.width, st)));
+            t.A = plan.X;
+            t.lda = plan.width;
+        }
+        const bool lay_out = t.n != n || !w_as_it_is;
+        CHECK(launched(lmk::launch_targets(rows, round_to(rows, 256), p, y + t0 * y_stride, y_stride, ignore, plan.targets, st)));
+        t.targets = plan.targets;
+        t.at_target = plan.at_target;
+        t.parts_ld = plan.tokens;
+        const int64_t step = lay_out ? plan.words : p;
+        for (int64_t v0 = 0; v0 < p; v0 += step) {
+            t.p = t.b_rows = p - v0 < step ? p - v0 : step;
+            t.B = (const uint16_t*)W + v0 * ldw;
+            t.ldb = ldw;
+            if (lay_out) {
+                CHECK(launched(lmk::launch_lay_out(type, t.p, n, t.B, ldw, nullptr, plan.W, plan.width, plan.width, st)));
+                t.B = plan.W;
+                t.ldb = plan.width;
+            }
+            t.column0 = (int)v0;
+            t.parts = plan.parts + v0 / 128 * plan.tokens;
+            if (!lmk::tile_fits(t)) return OZIMMU_ERR_DIM;
+            CHECK(launched(lmk::launch_tile(t, st)));
+        }
+        CHECK(launched(lmk::launch_join(rows, (p + 127) / 128, plan.parts, plan.tokens, plan.targets, plan.at_target, loss + t0, lse + t0, st)));
+    }
+    return OZIMMU_OK;
+}
+
+size_t ozimmu_lm_cross_entropy_backward_workspace_bytes(int64_t m, int64_t n, int64_t p)
+{
+    return loss_sizes_ok(m, n, p) && m > 0 ? GradientPlan(m, n, p, nullptr).bytes : 0;
+}
+
+int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, const float* g, int64_t g_stride, const void* X, int64_t ldx, const void* W,
+                                     int64_t ldw, const int64_t* y, int64_t y_stride, int64_t ignore, const float* lse, int dx_type, void* dX,
+                                     int64_t lddx, float beta, int dw_type, void* dW, int64_t lddw, void* workspace, size_t workspace_bytes,
+                                     void* stream)
+{
+    if (!loss_sizes_ok(m, n, p)) return OZIMMU_ERR_DIM;
+    if (!type16_ok(type)) return OZIMMU_ERR_TYPE;
+    CHECK(matrix_status(type, X, m, n, ldx));
+    CHECK(matrix_status(type, W, p, n, ldw));
+    if (dX) CHECK(matrix_status(dx_type, dX, m, n, lddx));
+    if (dW) CHECK(matrix_status(dw_type, dW, p, n, lddw));
+    CHECK(vector_status(y, m, y_stride, 8));
+    CHECK(vector_status(g, m, g_stride, 4));
+    CHECK(vector_status(lse, m, 1, 4));
+    const hipStream_t st = (hipStream_t)stream;
+    CHECK(workspace_status(workspace, workspace_bytes, ozimmu_lm_cross_entropy_backward_workspace_bytes(m, n, p)));
+    if (!dX && !dW) return OZIMMU_OK;
+    if (m == 0) {
+        if (dW && beta != 1.0f) return launched(lmk::launch_scale(dw_type, p, n, beta, dW, lddw, st));
+        return OZIMMU_OK;
+    }
+    const GradientPlan plan(m, n, p, workspace);
+    CHECK(launched(lmk::launch_slopes(m, plan.padded, p, y, y_stride, ignore, g, g_stride, lse, plan.targets, plan.lse2, plan.ratio, plan.largest, st)));
+    const bool x_as_it_is = as_it_is(X, n, ldx);
+    // (W is read along its rows and across them, a piece of `words` rows at a time)
+    const bool w_as_it_is = as_it_is(W, n, ldw) && plan.words * ldw * 2 < ((int64_t)1 << 32) - (1 << 20);
+    const bool lay_out = !x_as_it_is || !w_as_it_is;
+    const float unscale = type == OZIMMU_LM_F16 ? 1.0f / lmk::SLOPE_SCALE_F16 : 1.0f;
+    if (lay_out) CHECK(launched(lmk::launch_lay_out(type, m, n, X, ldx, nullptr, plan.X, plan.width, plan.width, st)));
+    if (dW) CHECK(launched(lmk::launch_lay_out(type, m, n, X, ldx, plan.ratio, plan.scaled, plan.width, plan.width, st)));
+    int splits = 0;
+    for (int64_t v0 = 0; v0 < p; v0 += plan.words) {
+        const int64_t words = p - v0 < plan.words ? p - v0 : plan.words, whole = round_to(words, 256);
+        const uint16_t* W_at = (const uint16_t*)W + v0 * ldw;
+        int64_t ldw_at = ldw;
+        if (lay_out) {
+            CHECK(launched(lmk::launch_lay_out(type, words, n, W_at, ldw, nullptr, plan.W, plan.width, plan.width, st)));
+            W_at = plan.W;
+            ldw_at = plan.width;
+        }
+        Tile t{lmk::SLOPE, type};
+        t.m = m;
+        t.n = lay_out ? plan.width : n;
+        t.p = t.b_rows = words;
+        t.A = lay_out ? (const void*)plan.X : X;
+        t.lda = lay_out ? plan.width : ldx;
+        t.B = W_at;
+        t.ldb = ldw_at;
+        t.D = plan.slopes;
+        t.ldd = whole;
+        t.targets = plan.targets;
+        t.column0 = (int)v0;
+        t.lse2 = plan.lse2;
+        if (!lmk::tile_fits(t)) return OZIMMU_ERR_DIM;
+        CHECK(launched(lmk::launch_tile(t, st)));
+        if (dX) {
+            Tile s{lmk::STATES, type};
+            s.m = m;
+            s.n = whole;
+            s.p = round_to(n, 8);
+            s.b_rows = words;
+            s.A = plan.slopes;
+            s.lda = whole;
+            s.B = W_at;
+            s.ldb = ldw_at;
+            s.D = plan.states;
+            s.ldd = plan.states_ld;
+            s.split_stride = plan.padded * plan.states_ld;
+            s.beta = v0 > 0 ? 1.0f : 0.0f;
+            s.splits = plan.splits < (int)(whole / 64) ? plan.splits : (int)(whole / 64);
+            if (v0 == 0) splits = s.splits;
+            if (!lmk::tile_fits(s)) return OZIMMU_ERR_DIM;
+            CHECK(launched(lmk::launch_tile(s, st)));
+        }
+        if (dW) {
+            Tile s{lmk::WEIGHTS, type};
+            s.m = words;
+            s.n = s.b_rows = m;
+            s.p = n;
+            s.A = plan.slopes;
+            s.lda = whole;
+            s.B = plan.scaled;
+            s.ldb = plan.width;
+            s.D = (uint8_t*)dW + v0 * lddw * (dw_type == OZIMMU_LM_F32 ? 4 : 2);
+            s.ldd = lddw;
+            s.dtype = dw_type;
+            s.alpha = unscale;
+            s.alpha_at = plan.largest;
+            s.beta = beta;
+            if (!lmk::tile_fits(s)) return OZIMMU_ERR_DIM;
+            CHECK(launched(lmk::launch_tile(s, st)));
+        }
+    }
+    if (dX)
+        CHECK(launched(lmk::launch_states(dx_type, m, n, plan.states, plan.states_ld, splits, plan.padded * plan.states_ld, g, g_stride, plan.targets, unscale, dX,
+                                          lddx, st)));
+    return OZIMMU_OK;
+}
+
+}  // extern "C"
