@@ -10,7 +10,8 @@ using lmk::Tile;
 
 constexpr int64_t COMPUTE_UNITS = 256;
 constexpr int NXCD = 8, TILE = 256, STAGE_K = 64;
-constexpr int OPERAND_BYTES = TILE * STAGE_K * 2, PLACE_BYTES = 2 * OPERAND_BYTES, COPIES = 8;  // 32 KiB, 64 KiB; copies a wave and operand
+constexpr int OPERAND_BYTES = TILE * STAGE_K * 2, COPIES = 8;  // 32 KiB of a stage; copies a wave
+constexpr int A_PLACES = 2, B_PLACES = 3;                      // in LDS: 160 KiB
 constexpr float LOG2E = 1.44269504088896341f;
 
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -102,38 +103,40 @@ struct Order {
     }
 };
 
-// An operand on its way: a stage (64 inner elements of a tile's 256 rows) is 32 copies of 1 KiB, eight a wave.
+// An operand on its way: a stage (64 inner elements of a tile's 256 rows) is 32 copies of 1 KiB, eight a wave, into one of PLACES places.
 //
-// ACROSS false: rows lie along the inner dimension.  A copy takes 128 bytes of eight rows, a row by eight neighbouring lanes.  In LDS a fragment (16
-// rows) is 2 KiB, its rows one behind the other, the eight 16-byte pieces of a row exchanged by the row's last three bits: the 16 lanes that
-// read one piece of each row fall on different banks.
+// ACROSS false: rows lie along the inner dimension.  A copy takes 128 bytes, a whole line, of eight rows, a row by eight neighbouring lanes.  In
+// LDS a fragment (16 rows) is 2 KiB, its rows one behind the other, the eight 16-byte pieces of a row exchanged by the last three bits of its
+// place: the lanes that read one piece of eight rows fall on different banks.
 // ACROSS true: the inner dimension lies across the rows.  A copy takes 512 bytes of two inner positions.  In LDS they lie one behind the other, the
-// eight pieces of 64 bytes (two fragments) of a position exchanged by bits 0, 1 and 3 of its number; the transposing read gives a lane
-// four inner positions of its column, 16 lanes of it read four positions on different banks.
-template <bool ACROSS> struct Operand {
+// pieces of 32 bytes (a fragment) of a position exchanged by bits 0, 1 and 3 of its number: the transposing read, which gives a lane four inner
+// positions of its column, has 32 lanes read eight positions, which then fall on different banks.
+template <bool ACROSS, int PLACES> struct Operand {
     v4i now;          // the buffer: this tile's panel
     uint32_t off;     // of the stage that is copied next
     uint32_t stride;  // between stages
     uint32_t part[COPIES];
     uint32_t voff[ACROSS ? 4 : 1], tail;
     bool tail_lane;
-    uint32_t at[ACROSS ? 4 : 2];
+    uint32_t base[ACROSS ? 8 : 2], at[ACROSS ? 8 : 2];
+    uint32_t to;      // where this wave's copies go next
+    uint32_t first;   // .. in the first place
+    uint32_t from;    // offset of the place that is read
 
     __device__ inline void set(uint32_t ld, uint32_t lds, int wave, int half, int lane, int64_t n)
     {
+        stride = ACROSS ? STAGE_K * ld : STAGE_K * 2;
+        first = to = lds + wave * (COPIES * 1024);
         if constexpr (ACROSS) {
-            stride = STAGE_K * ld;
 #pragma unroll
             for (int i = 0; i < COPIES; ++i) part[i] = (uint32_t)(16 * wave + 2 * i) * ld;
 #pragma unroll
             for (int v = 0; v < 4; ++v)  // copy i: v = i % 2 + 2 (i / 4)
-                voff[v] = (uint32_t)(lane >> 5) * ld + (uint32_t)(((lane & 31) >> 2) ^ (2 * (v & 1) + (lane >> 5) + 4 * (v >> 1))) * 64u + (lane & 3) * 16u;
+                voff[v] = (uint32_t)(lane >> 5) * ld + (uint32_t)(((lane & 31) >> 1) ^ (2 * (v & 1) + (lane >> 5) + 4 * (v >> 1))) * 32u + (lane & 1) * 16u;
             const int i = lane & 15, q = lane >> 4;
 #pragma unroll
-            for (int f = 0; f < 4; ++f)
-                at[f] = lds + (8 * q + (i >> 2)) * 512 + ((half ^ (q & 1)) * 4 + (f ^ (i >> 2))) * 64 + (i & 3) * 16;
+            for (int f = 0; f < 8; ++f) base[f] = lds + (8 * q + (i >> 2)) * 512 + half * 256 + (f ^ ((i >> 2) + 4 * (q & 1))) * 32 + (i & 3) * 8;
         } else {
-            stride = STAGE_K * 2;
 #pragma unroll
             for (int i = 0; i < COPIES; ++i) part[i] = (uint32_t)((2 * wave + i / 4) * 32 + (i / 2 % 2) * 4 + (i % 2) * 16) * ld;
             const int r = lane >> 3, piece = (lane & 7) ^ r;
@@ -141,9 +144,21 @@ template <bool ACROSS> struct Operand {
             // pieces behind the end of a row, in the last stage: out of the buffer, which gives zeros
             tail_lane = (n - 1) / STAGE_K * STAGE_K + piece * 8 >= n;
             const int place = lane & 15, q = lane >> 4;
-            at[0] = lds + half * (OPERAND_BYTES / 2) + (place >> 3) * 1024 + (place & 7) * 128 + ((q ^ (place & 7)) << 4);
-            at[1] = at[0] ^ 64u;
+            base[0] = lds + half * (OPERAND_BYTES / 2) + (place >> 3) * 1024 + (place & 7) * 128 + ((q ^ (place & 7)) << 4);
+            base[1] = base[0] ^ 64u;
         }
+        from = 0;
+        read_from();
+    }
+    __device__ inline void read_from()
+    {
+#pragma unroll
+        for (int f = 0; f < (ACROSS ? 8 : 2); ++f) at[f] = base[f] + from;
+    }
+    __device__ inline void read_next()
+    {
+        from = from == (PLACES - 1) * OPERAND_BYTES ? 0 : from + OPERAND_BYTES;
+        read_from();
     }
     // the panel of a tile, from stage k0 on; `rows`: of the operand (along the tile), `n`: inner
     __device__ inline void point(uint64_t base, uint32_t ld, int tile, int k0, int64_t rows, int64_t n)
@@ -169,6 +184,7 @@ template <bool ACROSS> struct Operand {
         stride = 0;
     }
     __device__ inline void last_stage(bool is) { if constexpr (!ACROSS) tail = is && tail_lane ? 0x70000000u : voff[0]; }
+    template <int I> __device__ inline void set_m0() const { copy_to<I * 1024>(to); }
     template <int I> __device__ inline void issue() const
     {
         if constexpr (ACROSS)
@@ -176,19 +192,54 @@ template <bool ACROSS> struct Operand {
         else
             copy(tail, now, off + part[I]);
     }
-    __device__ inline void turn() { for (auto& a : at) a ^= PLACE_BYTES; }
+    __device__ inline void issued()
+    {
+        off += stride;
+        to = to == first + (PLACES - 1) * OPERAND_BYTES ? first : to + OPERAND_BYTES;
+    }
     // fragment F (0 .. 7 of the wave's half) of the stage's inner elements 32 KS .. + 31
     template <int F, int KS> __device__ inline v4i fetch() const
     {
         if constexpr (ACROSS) {
             typedef __attribute__((address_space(3))) v4s* lds_v4s;
-            constexpr int D = F % 2 * 8 + KS * 32 * 512;
-            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(at[F / 2] + D));
-            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(at[F / 2] + D + 4 * 512));
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(at[F] + KS * 32 * 512));
+            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(at[F] + KS * 32 * 512 + 4 * 512));
             return __builtin_bit_cast(v4i, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             return *(lds_v4i)(uintptr_t)(at[KS] + F * 2048);
         }
+    }
+    // row (column) of fragment f's place in the tile's half
+    static __host__ __device__ constexpr int row(int fragment, int place) { return ACROSS ? 16 * fragment + place : row_of(fragment, place); }
+};
+
+// One operand's way through the items of a workgroup, some stages ahead of the products
+template <bool ACROSS, int PLACES, bool IS_A> struct Stream : Operand<ACROSS, PLACES> {
+    Order order;
+    int left = 0, stage = 0;
+    __device__ inline explicit Stream(const Args& g) : order(g) {}
+    __device__ inline void look_up(const Args& g)
+    {
+        int tm, tp, split, k0, k1;
+        if (order.take(tm, tp, split, k0, k1)) {
+            if constexpr (IS_A)
+                this->point(g.A, g.lda, tm, k0, g.m, g.n);
+            else
+                this->point(g.B, g.ldb, tp, k0, g.p, ACROSS ? g.b_rows : g.n);
+            left = k1 - k0;
+            stage = k0;
+        } else {
+            this->nothing();
+            left = 1 << 30;
+            stage = -(1 << 30);
+        }
+    }
+    __device__ inline void begin(const Args& g) { this->last_stage(stage == g.KT - 1); }
+    __device__ inline void end(const Args& g)
+    {
+        this->issued();
+        ++stage;
+        if (--left == 0) look_up(g);
     }
 };
 
@@ -222,136 +273,86 @@ template <int TYPE, int DTYPE> __device__ inline void put(const Args& g, float a
 }
 
 // A workgroup of four waves, 128 x 128 sums each in 256 registers a lane, one wave a SIMD, takes one item after the other.  A stage is 64
-// inner elements of A and B, 64 KiB, and LDS holds two: while one is multiplied the other arrives, and the stages of all items are one
-// stream, so that the first of an item arrive while the sums of the one before are written out.  A stage is two steps of 64 matrix instructions a
-// wave, each run as four quarters of 4 x 4 fragments on four sets of four: (A lo, B lo), (A lo, B hi), (A hi, B lo), (A hi, B hi), each fetching
-// the set that the quarter after the next needs.  One barrier a stage, before the last two quarters: behind it the stage's place takes the
-// copies of the stage after the next.
+// inner elements of A and B.  The stages of all items are one stream, so that the first of an item arrive while the sums of the one before are
+// written out.  A stage is two halves of 64 matrix instructions a wave; during each the 16 fragments of the next half come from LDS into a second
+// set of registers.  So both places of a stage are free at the end of its first half, where the one barrier of a stage is; behind it they take
+// the copies of A two stages and of B three stages on.
 template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(Args g)
 {
     constexpr bool A_ACROSS = KIND == lmk::WEIGHTS, B_ACROSS = KIND == lmk::WEIGHTS || KIND == lmk::STATES;
-    __shared__ __align__(16) uint8_t ring[2 * PLACE_BYTES];
+    __shared__ __align__(16) uint8_t places[(A_PLACES + B_PLACES) * OPERAND_BYTES];
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)places;
 
-    Operand<A_ACROSS> a;
-    Operand<B_ACROSS> b;
+    Stream<A_ACROSS, A_PLACES, true> a(g);
+    Stream<B_ACROSS, B_PLACES, false> b(g);
     a.set(g.lda, lds, wave, wm, lane, g.n);
-    b.set(g.ldb, lds + OPERAND_BYTES, wave, wn, lane, g.n);
-    Order copy_order(g);
-    int stages_left = 0, stage_now = 0;
-    auto look_up = [&]() {
-        int tm, tp, split, k0, k1;
-        if (copy_order.take(tm, tp, split, k0, k1)) {
-            a.point(g.A, g.lda, tm, k0, g.m, g.n);
-            b.point(g.B, g.ldb, tp, k0, g.p, B_ACROSS ? g.b_rows : g.n);
-            stages_left = k1 - k0;
-            stage_now = k0;
-        } else {
-            a.nothing();
-            b.nothing();
-            stages_left = 1 << 30;
-            stage_now = -(1 << 30);
-        }
-    };
-    auto begin_copies = [&]() {
-        const bool last = stage_now == g.KT - 1;
-        a.last_stage(last);
-        b.last_stage(last);
-    };
-    auto end_copies = [&]() {
-        a.off += a.stride;
-        b.off += b.stride;
-        ++stage_now;
-        if (--stages_left == 0) look_up();
-    };
-    uint32_t to = lds + wave * (COPIES * 1024);  // the place that is copied to, this wave's part
-    look_up();
-    static_for<0, 2>([&](auto) {
-        begin_copies();
+    b.set(g.ldb, lds + A_PLACES * OPERAND_BYTES, wave, wn, lane, g.n);
+    a.look_up(g);
+    b.look_up(g);
+    auto whole_stage = [&](auto& o) {
+        o.begin(g);
         static_for<0, COPIES>([&](auto I) {
-            constexpr int i = decltype(I)::value;
-            copy_to<i * 1024>(to);
+            o.template set_m0<decltype(I)::value>();
             asm volatile("s_nop 4");
-            a.template issue<i>();
-            copy_to<OPERAND_BYTES + i * 1024>(to);
-            asm volatile("s_nop 4");
-            b.template issue<i>();
+            o.template issue<decltype(I)::value>();
         });
-        end_copies();
-        to = to + PLACE_BYTES < lds + 2 * PLACE_BYTES ? to + PLACE_BYTES : to - PLACE_BYTES;
-    });
+        o.end(g);
+    };
+    whole_stage(a);
+    whole_stage(b);
+    whole_stage(b);
+    whole_stage(a);
+    whole_stage(b);
 
     v4f acc[8][8];
-    v4i faL[4], faH[4], fbL[4], fbH[4];
-    // matrix instruction X of a quarter, there and back over the fragments of A
-    auto math = [&](const v4i* fa, const v4i* fb, auto I0, auto J0, auto X) __attribute__((always_inline)) {
-        constexpr int j = decltype(X)::value / 4, x = decltype(X)::value % 4, i = (j & 1) ? 3 - x : x;
-        v4f& c = acc[decltype(I0)::value + i][decltype(J0)::value + j];
-        c = mfma<TYPE>(fb[j], fa[i], c);
-    };
-    typedef std::integral_constant<int, 0> N0;
-    typedef std::integral_constant<int, 4> N4;
-
-    wait_vmcnt<2 * COPIES>();
+    v4i fa[2][8], fb[2][8];   // the fragments of this half and of the next
+    wait_vmcnt<3 * COPIES>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    static_for<0, 4>([&](auto Q) {
-        constexpr int q = decltype(Q)::value;
-        faL[q] = a.template fetch<q, 0>();
-        fbL[q] = b.template fetch<q, 0>();
+    static_for<0, 8>([&](auto F) __attribute__((always_inline)) {
+        fa[0][decltype(F)::value] = a.template fetch<decltype(F)::value, 0>();
+        fb[0][decltype(F)::value] = b.template fetch<decltype(F)::value, 0>();
     });
 
-    auto stage = [&]() __attribute__((always_inline)) {
-        static_for<0, 2>([&](auto KS) __attribute__((always_inline)) {
-            constexpr int ks = decltype(KS)::value;
-            static_for<0, 16>([&](auto X) __attribute__((always_inline)) {
-                constexpr int x = decltype(X)::value;
-                if constexpr (x % 2 == 0 && x < 8) fbH[x / 2] = b.template fetch<4 + x / 2, ks>();
-                math(faL, fbL, N0{}, N0{}, X);
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            static_for<0, 16>([&](auto X) __attribute__((always_inline)) {
-                constexpr int x = decltype(X)::value;
-                if constexpr (x % 2 == 0 && x < 8) faH[x / 2] = a.template fetch<4 + x / 2, ks>();
-                math(faL, fbH, N0{}, N4{}, X);
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            if constexpr (ks == 1) {
-                wait_vmcnt<0>();
-                wait_lds();
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-                a.turn();
-                b.turn();
-                begin_copies();
+    auto half = [&](auto H) __attribute__((always_inline)) {
+        constexpr int h = decltype(H)::value;
+        if constexpr (h == 1) {
+            a.begin(g);
+            b.begin(g);
+        }
+        static_for<0, 64>([&](auto X) __attribute__((always_inline)) {
+            constexpr int x = decltype(X)::value, j = x / 8, i = j & 1 ? 7 - x % 8 : x % 8;
+            if constexpr (x % 3 == 0 && x < 48) {
+                constexpr int f = x / 3;
+                if constexpr (f < 8)
+                    fa[1 - h][f] = a.template fetch<f % 8, 1 - h>();
+                else
+                    fb[1 - h][f - 8] = b.template fetch<f % 8, 1 - h>();
             }
-            static_for<0, 16>([&](auto X) __attribute__((always_inline)) {
-                constexpr int x = decltype(X)::value;
-                if constexpr (ks == 1) {
-                    // copies: B's eight here, A's in the next quarter
-                    if constexpr (x % 2 == 0) copy_to<OPERAND_BYTES + x / 2 * 1024>(to);
-                    if constexpr (x % 2 == 1) b.template issue<x / 2>();
-                }
-                if constexpr (x % 2 == 0 && x < 8) faL[x / 2] = a.template fetch<x / 2, 1 - ks>();
-                math(faH, fbL, N4{}, N0{}, X);
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            static_for<0, 16>([&](auto X) __attribute__((always_inline)) {
-                constexpr int x = decltype(X)::value;
-                if constexpr (ks == 1) {
-                    if constexpr (x % 2 == 0) copy_to<x / 2 * 1024>(to);
-                    if constexpr (x % 2 == 1) a.template issue<x / 2>();
-                }
-                if constexpr (x % 2 == 0 && x < 8) fbL[x / 2] = b.template fetch<x / 2, 1 - ks>();
-                math(faH, fbH, N4{}, N4{}, X);
-                __builtin_amdgcn_sched_barrier(0);
-            });
+            if constexpr (h == 1) {
+                if constexpr (x % 4 == 1 && x < 32) a.template set_m0<x / 4>();
+                if constexpr (x % 4 == 2 && x < 32) a.template issue<x / 4>();
+                if constexpr (x % 4 == 1 && x >= 32) b.template set_m0<x / 4 - 8>();
+                if constexpr (x % 4 == 2 && x >= 32) b.template issue<x / 4 - 8>();
+            }
+            acc[i][j] = mfma<TYPE>(fb[h][j], fa[h][i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
         });
-        end_copies();
-        to = to < lds + PLACE_BYTES ? to + PLACE_BYTES : to - PLACE_BYTES;
+        if constexpr (h == 0) {
+            // all of this stage is read, and A and B of the next one are there (B of the one after may be on its way)
+            wait_vmcnt<COPIES>();
+            wait_lds();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            a.read_next();
+            b.read_next();
+        } else {
+            a.end(g);
+            b.end(g);
+        }
     };
 
     Order order(g);
@@ -365,7 +366,10 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
                 asm volatile("" : "+a"(acc[i][j]));  // (in its accumulation registers from here on)
             }
 #pragma clang loop unroll(disable)
-        for (int k = k0; k < k1; ++k) stage();
+        for (int k = k0; k < k1; ++k) {
+            half(std::integral_constant<int, 0>{});
+            half(std::integral_constant<int, 1>{});
+        }
 
         // (read by asm statements, or the register allocator parks sums in scratch memory; the wait states behind the last matrix instruction are
         // written out)
@@ -376,16 +380,16 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
         asm volatile("s_nop 15\n\ts_nop 15");
         int lr = lane & 15, lc = lane >> 4;
         asm volatile("" : "+v"(lr), "+v"(lc));
-        const int64_t row0 = (int64_t)tm * TILE + wm * 128 + row_of(0, lr), col0 = (int64_t)tp * TILE + wn * 128;
-        const int row_lane = wm * 128 + row_of(0, lr);
-        // this lane's 32 sums of a row, eight neighbouring columns at a time: v[8 J + e] is column 32 J + 8 lc + e
+        const int row_lane = wm * 128 + a.row(0, lr);
+        const int64_t row0 = (int64_t)tm * TILE + row_lane, col0 = (int64_t)tp * TILE + wn * 128;
+        // this lane's 32 sums of a row: v[4 j + r] is of place 4 lc + r of B's fragment j (B along: v[8 J + e] is column 32 J + 8 lc + e)
         auto rows = [&](auto&& f) __attribute__((always_inline)) {
             static_for<0, 8>([&](auto I) __attribute__((always_inline)) {
                 constexpr int i = decltype(I)::value;
                 float v[32];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][e / 8 * 2 + e / 4 % 2][e % 4]));
-                f(I, std::integral_constant<int, row_of(i, 0)>{}, v);
+                f(I, std::integral_constant<int, a.row(i, 0)>{}, v);
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
@@ -465,27 +469,38 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
         } else if constexpr (KIND == lmk::STATES) {
             rows([&](auto, auto RI, float* v) __attribute__((always_inline)) {
                 constexpr int ri = decltype(RI)::value;
-                float* const out = (float*)g.D + split * g.split_stride + (row0 + ri) * g.ldd + col0 + lc * 8;
+                float* const out = (float*)g.D + split * g.split_stride + (row0 + ri) * g.ldd + col0 + lc * 4;
                 if (g.beta != 0.0f) {
                     v4f old[8];
 #pragma unroll
-                    for (int jj = 0; jj < 8; ++jj) old[jj] = *(const v4f*)(out + jj / 2 * 32 + jj % 2 * 4);
+                    for (int j = 0; j < 8; ++j) old[j] = *(const v4f*)(out + 16 * j);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] += old[e / 4][e % 4];
                 }
 #pragma unroll
-                for (int jj = 0; jj < 8; ++jj) *(v4f*)(out + jj / 2 * 32 + jj % 2 * 4) = v4f{v[4 * jj], v[4 * jj + 1], v[4 * jj + 2], v[4 * jj + 3]};
+                for (int j = 0; j < 8; ++j) *(v4f*)(out + 16 * j) = v4f{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
             });
         } else {
             float alpha = g.alpha;
             if constexpr (KIND == lmk::WEIGHTS) alpha *= *g.alpha_at;
             rows([&](auto, auto RI, float* v) __attribute__((always_inline)) {
                 constexpr int ri = decltype(RI)::value;
+                if constexpr (B_ACROSS) {
+                    // two fragments' fours into eights: the odd sixteens of lanes give theirs of the first for the even ones' of the second
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (e / 4 % 2 == 0) {
+                            const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[e]), __float_as_uint(v[e + 4]), false, false);
+                            v[e] = __uint_as_float(x[0]);
+                            v[e + 4] = __uint_as_float(x[1]);
+                        }
+                }
+                const int eight = B_ACROSS ? (lc & 1) * 16 + (lc >> 1) * 8 : lc * 8;  // of 32 columns
 #pragma unroll
                 for (int jj = 0; jj < 4; ++jj) {
-                    if (g.dtype == F32) put<TYPE, F32>(g, alpha, row0 + ri, col0 + jj * 32 + lc * 8, v + 8 * jj);
-                    if (g.dtype == BF16) put<TYPE, BF16>(g, alpha, row0 + ri, col0 + jj * 32 + lc * 8, v + 8 * jj);
-                    if (g.dtype == F16) put<TYPE, F16>(g, alpha, row0 + ri, col0 + jj * 32 + lc * 8, v + 8 * jj);
+                    if (g.dtype == F32) put<TYPE, F32>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
+                    if (g.dtype == BF16) put<TYPE, BF16>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
+                    if (g.dtype == F16) put<TYPE, F16>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
                 }
             });
         }
