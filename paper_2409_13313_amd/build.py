@@ -14,10 +14,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libozimmu.so")
 SOURCES = ["ozimmu_api.hip", "ozimmu_split.hip", "ozimmu_gemm.hip", "ozimmu_mx_api.hip", "ozimmu_mx_quantize.hip", "ozimmu_mx_gemm.hip",
-           "ozimmu_lm_api.hip", "ozimmu_lm_weights.hip", "ozimmu_lm_tile.hip", "ozimmu_lm_loss.hip"]
+           "ozimmu_lm_api.hip", "ozimmu_lm_weights.hip", "ozimmu_lm_loss.hip"]
 # ozimmu_resident.hip holds kernels specialised for a slice count: one compilation per count, all of them linked into
 # the object of the chunk GEMM (whoever links that object gets every way to run the schedule)
 RESIDENT_KS = range(3, 17)
+LM_TYPES = (1, 2)   # ozimmu_lm_tile.hip: one compilation for each 16-bit type
 LOOKED_AT = ["ozimmu_mx_gemm.hip"]   # beside those: kernels with asm statements of their own
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -40,6 +41,8 @@ def build(verbose: bool = False) -> str:
     core = os.path.join(CSRC, "ozimmu_gemm_core.o")
     resident = [os.path.join(CSRC, f"ozimmu_resident_k{k}.o") for k in RESIDENT_KS]
     jobs = [(src, [], core if obj.endswith("ozimmu_gemm.o") else obj) for src, obj in zip(SOURCES, objs)]
+    tiles = [os.path.join(CSRC, f"ozimmu_lm_tile_{t}.o") for t in LM_TYPES]
+    jobs += [("ozimmu_lm_tile.hip", [f"-DLM_TYPE={t}"], obj) for t, obj in zip(LM_TYPES, tiles)]
     jobs += [("ozimmu_resident.hip", [f"-DOZ_RES_K={k}"], obj) for k, obj in zip(RESIDENT_KS, resident)]
 
     def compile_one(job):
@@ -59,7 +62,7 @@ def build(verbose: bool = False) -> str:
             if src in LOOKED_AT:
                 text, = (open(f).read() for f in glob.glob(os.path.join(tmp, "*gfx950*.s")))
                 codegen.check_mx(text)
-            if defs:
+            if src == "ozimmu_resident.hip":
                 text, = (open(f).read() for f in glob.glob(os.path.join(tmp, "*gfx950*.s")))
                 seen = codegen.check_resident(text, int(defs[0].split("=")[1]))
                 if not all(seen[kind] for kind in ("k_resident", "k_cut")):
@@ -69,7 +72,7 @@ def build(verbose: bool = False) -> str:
     with ThreadPoolExecutor(max_workers=8) as pool:
         list(pool.map(compile_one, jobs))
     subprocess.run(["ld", "-r", "-o", os.path.join(CSRC, "ozimmu_gemm.o"), core, *resident], check=True)
-    cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
+    cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs, *tiles]
     subprocess.run(cmd, check=True)
     return LIB
 

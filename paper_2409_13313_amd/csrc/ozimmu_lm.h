@@ -76,6 +76,7 @@ enum Kind {
 
 struct Tile {
     int kind, type;       // type: of A and B
+    bool half = false;    // tiles of 128 x 256 instead of 256 x 256
     int64_t m, n, p;
     const void *A, *B;    // 16-byte aligned; leading dimensions multiples of 8 elements; where rows lie along n, n a multiple of 8
     int64_t lda, ldb;
@@ -95,7 +96,10 @@ struct Tile {
     int64_t parts_ld = 0;
 };
 bool tile_fits(const Tile& t);
+bool half_tiles(int64_t m, int64_t p, int splits);   // whether tiles of 128 x 256 take less time
 hipError_t launch_tile(const Tile& t, hipStream_t st);
+hipError_t launch_tile_1(const Tile& t, hipStream_t st);  // BF16
+hipError_t launch_tile_2(const Tile& t, hipStream_t st);  // F16
 
 // ---- what stands around them in the loss (ozimmu_lm_loss.hip) ----
 

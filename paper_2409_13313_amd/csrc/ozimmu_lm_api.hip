@@ -129,6 +129,7 @@ int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const v
         t.p = t.b_rows = p - at < plan.rows ? p - at : plan.rows;
         CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, st)));
         t.D = (uint8_t*)D + at * size;
+        t.half = lmk::half_tiles(t.m, t.p, t.splits);
         CHECK(launched(lmk::launch_tile(t, st)));
     }
     return OZIMMU_OK;
@@ -214,6 +215,29 @@ struct GradientPlan {
 };
 
 }  // namespace
+
+namespace lmk {
+
+// (32-bit offsets inside a panel, 30 bits where rows lie along the inner dimension: pieces behind a row's end are sent behind those)
+bool tile_fits(const Tile& t)
+{
+    auto along = [](int64_t ld) { return ld * 2 < (1 << 22); };
+    auto across = [&](int64_t ld) { return t.n * ld * 2 < ((int64_t)1 << 32) - (1 << 20); };
+    const bool a = t.kind == WEIGHTS ? across(t.lda) : along(t.lda);
+    const bool b = t.kind == WEIGHTS || t.kind == STATES ? across(t.ldb) : along(t.ldb);
+    return a && b && t.n > 0 && (t.m + 127) / 128 * ((t.p + 255) / 256) * t.splits < ((int64_t)1 << 28);
+}
+
+bool half_tiles(int64_t m, int64_t p, int splits)
+{
+    const int64_t columns = (p + 255) / 256 * splits, whole = (m + 255) / 256 * columns, half = (m + 127) / 128 * columns;
+    auto rounds = [](int64_t items) { return (double)((items + COMPUTE_UNITS - 1) / COMPUTE_UNITS); };
+    return rounds(half) * 0.6 < rounds(whole);
+}
+
+hipError_t launch_tile(const Tile& t, hipStream_t st) { return t.type == BF16 ? launch_tile_1(t, st) : launch_tile_2(t, st); }
+
+}  // namespace lmk
 
 extern "C" {
 
@@ -355,6 +379,7 @@ int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const voi
             t.column0 = (int)v0;
             t.parts = plan.parts + v0 / 128 * plan.tokens;
             if (!lmk::tile_fits(t)) return OZIMMU_ERR_DIM;
+            t.half = lmk::half_tiles(t.m, t.p, t.splits);
             CHECK(launched(lmk::launch_tile(t, st)));
         }
         CHECK(launched(lmk::launch_join(rows, (p + 127) / 128, plan.parts, plan.tokens, plan.targets, plan.at_target, loss + t0, lse + t0, st)));
@@ -421,6 +446,7 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
         t.column0 = (int)v0;
         t.lse2 = plan.lse2;
         if (!lmk::tile_fits(t)) return OZIMMU_ERR_DIM;
+        t.half = lmk::half_tiles(t.m, t.p, t.splits);
         CHECK(launched(lmk::launch_tile(t, st)));
         if (dX) {
             Tile s{lmk::STATES, type};
@@ -439,6 +465,7 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
             s.splits = plan.splits < (int)(whole / 64) ? plan.splits : (int)(whole / 64);
             if (v0 == 0) splits = s.splits;
             if (!lmk::tile_fits(s)) return OZIMMU_ERR_DIM;
+            s.half = lmk::half_tiles(s.m, s.p, s.splits);
             CHECK(launched(lmk::launch_tile(s, st)));
         }
         if (dW) {
@@ -457,6 +484,7 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
             s.alpha_at = plan.largest;
             s.beta = beta;
             if (!lmk::tile_fits(s)) return OZIMMU_ERR_DIM;
+            s.half = lmk::half_tiles(s.m, s.p, s.splits);
             CHECK(launched(lmk::launch_tile(s, st)));
         }
     }

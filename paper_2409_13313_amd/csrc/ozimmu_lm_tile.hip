@@ -9,9 +9,8 @@ using lmk::BAD_TARGET;
 using lmk::Tile;
 
 constexpr int64_t COMPUTE_UNITS = 256;
-constexpr int NXCD = 8, TILE = 256, STAGE_K = 64;
-constexpr int OPERAND_BYTES = TILE * STAGE_K * 2, COPIES = 8;  // 32 KiB of a stage; copies a wave
-constexpr int A_PLACES = 2, B_PLACES = 3;                      // in LDS: 160 KiB
+constexpr int NXCD = 8, STAGE_K = 64;
+constexpr int FB = 8, TILE_B = 32 * FB;  // fragments of B a wave, columns of a tile
 constexpr float LOG2E = 1.44269504088896341f;
 
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -103,22 +102,25 @@ struct Order {
     }
 };
 
-// An operand on its way: a stage (64 inner elements of a tile's 256 rows) is 32 copies of 1 KiB, eight a wave, into one of PLACES places.
+// An operand on its way: a stage (64 inner elements of a tile's 32 F rows) is 4 F copies of 1 KiB, F a wave, into one of PLACES places.
 //
 // ACROSS false: rows lie along the inner dimension.  A copy takes 128 bytes, a whole line, of eight rows, a row by eight neighbouring lanes.  In
 // LDS a fragment (16 rows) is 2 KiB, its rows one behind the other, the eight 16-byte pieces of a row exchanged by the last three bits of its
 // place: the lanes that read one piece of eight rows fall on different banks.
-// ACROSS true: the inner dimension lies across the rows.  A copy takes 512 bytes of two inner positions.  In LDS they lie one behind the other, the
+// ACROSS true: the inner dimension lies across the rows.  A copy takes 1 KiB of two (F = 4: four) inner positions.  In LDS they lie one behind the other, the
 // pieces of 32 bytes (a fragment) of a position exchanged by bits 0, 1 and 3 of its number: the transposing read, which gives a lane four inner
 // positions of its column, has 32 lanes read eight positions, which then fall on different banks.
-template <bool ACROSS, int PLACES> struct Operand {
+template <bool ACROSS, int F, int PLACES> struct Operand {
+    static constexpr int TILE = 32 * F, COPIES = F, BYTES = TILE * STAGE_K * 2, ROW = 2 * TILE;  // of a stage in LDS; of an inner position there
+    static constexpr int POSITIONS = 1024 / ROW, LANES = 64 / POSITIONS;  // ACROSS: of a copy; lanes for each
+    static constexpr int VOFFS = F == 8 ? 4 : 2;
     v4i now;          // the buffer: this tile's panel
     uint32_t off;     // of the stage that is copied next
     uint32_t stride;  // between stages
     uint32_t part[COPIES];
-    uint32_t voff[ACROSS ? 4 : 1], tail;
+    uint32_t voff[ACROSS ? VOFFS : 1], tail;
     bool tail_lane;
-    uint32_t base[ACROSS ? 8 : 2], at[ACROSS ? 8 : 2];
+    uint32_t base[ACROSS ? F : 2], at[ACROSS ? F : 2];
     uint32_t to;      // where this wave's copies go next
     uint32_t first;   // .. in the first place
     uint32_t from;    // offset of the place that is read
@@ -129,22 +131,25 @@ template <bool ACROSS, int PLACES> struct Operand {
         first = to = lds + wave * (COPIES * 1024);
         if constexpr (ACROSS) {
 #pragma unroll
-            for (int i = 0; i < COPIES; ++i) part[i] = (uint32_t)(16 * wave + 2 * i) * ld;
+            for (int i = 0; i < COPIES; ++i) part[i] = (uint32_t)(16 * wave + POSITIONS * i) * ld;
+            const int position = lane / LANES, slot = lane % LANES;
 #pragma unroll
-            for (int v = 0; v < 4; ++v)  // copy i: v = i % 2 + 2 (i / 4)
-                voff[v] = (uint32_t)(lane >> 5) * ld + (uint32_t)(((lane & 31) >> 1) ^ (2 * (v & 1) + (lane >> 5) + 4 * (v >> 1))) * 32u + (lane & 1) * 16u;
+            for (int v = 0; v < VOFFS; ++v) {  // of copy i: F = 8: v = i % 2 + 2 (i / 4), F = 4: v = i / 2
+                const int swap = F == 8 ? 2 * (v & 1) + position + 4 * (v >> 1) : position + 4 * v;
+                voff[v] = (uint32_t)position * ld + (uint32_t)((slot >> 1) ^ swap) * 32u + (slot & 1) * 16u;
+            }
             const int i = lane & 15, q = lane >> 4;
 #pragma unroll
-            for (int f = 0; f < 8; ++f) base[f] = lds + (8 * q + (i >> 2)) * 512 + half * 256 + (f ^ ((i >> 2) + 4 * (q & 1))) * 32 + (i & 3) * 8;
+            for (int f = 0; f < F; ++f) base[f] = lds + (8 * q + (i >> 2)) * ROW + ((half * F + f) ^ ((i >> 2) + 4 * (q & 1))) * 32 + (i & 3) * 8;
         } else {
 #pragma unroll
-            for (int i = 0; i < COPIES; ++i) part[i] = (uint32_t)((2 * wave + i / 4) * 32 + (i / 2 % 2) * 4 + (i % 2) * 16) * ld;
+            for (int i = 0; i < COPIES; ++i) part[i] = (uint32_t)(row_of(wave * (F / 2), 0) + row_of(i / 2, i % 2 * 8)) * ld;
             const int r = lane >> 3, piece = (lane & 7) ^ r;
             voff[0] = (uint32_t)row_of(0, r) * ld + (uint32_t)piece * 16u;
             // pieces behind the end of a row, in the last stage: out of the buffer, which gives zeros
             tail_lane = (n - 1) / STAGE_K * STAGE_K + piece * 8 >= n;
             const int place = lane & 15, q = lane >> 4;
-            base[0] = lds + half * (OPERAND_BYTES / 2) + (place >> 3) * 1024 + (place & 7) * 128 + ((q ^ (place & 7)) << 4);
+            base[0] = lds + half * (BYTES / 2) + (place >> 3) * 1024 + (place & 7) * 128 + ((q ^ (place & 7)) << 4);
             base[1] = base[0] ^ 64u;
         }
         from = 0;
@@ -153,11 +158,11 @@ template <bool ACROSS, int PLACES> struct Operand {
     __device__ inline void read_from()
     {
 #pragma unroll
-        for (int f = 0; f < (ACROSS ? 8 : 2); ++f) at[f] = base[f] + from;
+        for (int f = 0; f < (ACROSS ? F : 2); ++f) at[f] = base[f] + from;
     }
     __device__ inline void read_next()
     {
-        from = from == (PLACES - 1) * OPERAND_BYTES ? 0 : from + OPERAND_BYTES;
+        from = from == (PLACES - 1) * BYTES ? 0 : from + BYTES;
         read_from();
     }
     // the panel of a tile, from stage k0 on; `rows`: of the operand (along the tile), `n`: inner
@@ -188,25 +193,25 @@ template <bool ACROSS, int PLACES> struct Operand {
     template <int I> __device__ inline void issue() const
     {
         if constexpr (ACROSS)
-            copy(voff[I % 2 + 2 * (I / 4)], now, off + part[I]);
+            copy(voff[F == 8 ? I % 2 + 2 * (I / 4) : I / 2], now, off + part[I]);
         else
             copy(tail, now, off + part[I]);
     }
     __device__ inline void issued()
     {
         off += stride;
-        to = to == first + (PLACES - 1) * OPERAND_BYTES ? first : to + OPERAND_BYTES;
+        to = to == first + (PLACES - 1) * BYTES ? first : to + BYTES;
     }
-    // fragment F (0 .. 7 of the wave's half) of the stage's inner elements 32 KS .. + 31
-    template <int F, int KS> __device__ inline v4i fetch() const
+    // fragment I (0 .. F - 1 of the wave's half) of the stage's inner elements 32 KS .. + 31
+    template <int I, int KS> __device__ inline v4i fetch() const
     {
         if constexpr (ACROSS) {
             typedef __attribute__((address_space(3))) v4s* lds_v4s;
-            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(at[F] + KS * 32 * 512));
-            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(at[F] + KS * 32 * 512 + 4 * 512));
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(at[I] + KS * 32 * ROW));
+            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)(at[I] + KS * 32 * ROW + 4 * ROW));
             return __builtin_bit_cast(v4i, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            return *(lds_v4i)(uintptr_t)(at[KS] + F * 2048);
+            return *(lds_v4i)(uintptr_t)(at[KS] + I * 2048);
         }
     }
     // row (column) of fragment f's place in the tile's half
@@ -214,7 +219,7 @@ template <bool ACROSS, int PLACES> struct Operand {
 };
 
 // One operand's way through the items of a workgroup, some stages ahead of the products
-template <bool ACROSS, int PLACES, bool IS_A> struct Stream : Operand<ACROSS, PLACES> {
+template <bool ACROSS, int F, int PLACES, bool IS_A> struct Stream : Operand<ACROSS, F, PLACES> {
     Order order;
     int left = 0, stage = 0;
     __device__ inline explicit Stream(const Args& g) : order(g) {}
@@ -277,24 +282,29 @@ template <int TYPE, int DTYPE> __device__ inline void put(const Args& g, float a
 // written out.  A stage is two halves of 64 matrix instructions a wave; during each the 16 fragments of the next half come from LDS into a second
 // set of registers.  So both places of a stage are free at the end of its first half, where the one barrier of a stage is; behind it they take
 // the copies of A two stages and of B three stages on.
-template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(Args g)
+//
+// FA = 8: 256 x 256 sums a workgroup; FA = 4: 128 x 256, for outputs of too few tiles.
+template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_lm_tile(Args g)
 {
     constexpr bool A_ACROSS = KIND == lmk::WEIGHTS, B_ACROSS = KIND == lmk::WEIGHTS || KIND == lmk::STATES;
-    __shared__ __align__(16) uint8_t places[(A_PLACES + B_PLACES) * OPERAND_BYTES];
+    constexpr int A_PLACES = FA == 8 ? 2 : 3, B_PLACES = 3, M = FA * FB, TILE_A = 32 * FA;
+    typedef Stream<A_ACROSS, FA, A_PLACES, true> StreamA;
+    typedef Stream<B_ACROSS, FB, B_PLACES, false> StreamB;
+    __shared__ __align__(16) uint8_t places[A_PLACES * StreamA::BYTES + B_PLACES * StreamB::BYTES];  // 160 KiB; FA = 4: 144
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave >> 1, wn = wave & 1;
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)places;
 
-    Stream<A_ACROSS, A_PLACES, true> a(g);
-    Stream<B_ACROSS, B_PLACES, false> b(g);
+    StreamA a(g);
+    StreamB b(g);
     a.set(g.lda, lds, wave, wm, lane, g.n);
-    b.set(g.ldb, lds + A_PLACES * OPERAND_BYTES, wave, wn, lane, g.n);
+    b.set(g.ldb, lds + A_PLACES * StreamA::BYTES, wave, wn, lane, g.n);
     a.look_up(g);
     b.look_up(g);
-    auto whole_stage = [&](auto& o) {
+    auto whole_stage = [&](auto& o) __attribute__((always_inline)) {
         o.begin(g);
-        static_for<0, COPIES>([&](auto I) {
+        static_for<0, std::remove_reference_t<decltype(o)>::COPIES>([&](auto I) __attribute__((always_inline)) {
             o.template set_m0<decltype(I)::value>();
             asm volatile("s_nop 4");
             o.template issue<decltype(I)::value>();
@@ -305,45 +315,47 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
     whole_stage(b);
     whole_stage(b);
     whole_stage(a);
+    if constexpr (A_PLACES == 3) whole_stage(a);
     whole_stage(b);
+    constexpr int ON_THE_WAY = (A_PLACES - 2) * FA + FB;  // copies of a wave that need not be there yet when the next stage is looked at
 
-    v4f acc[8][8];
-    v4i fa[2][8], fb[2][8];   // the fragments of this half and of the next
-    wait_vmcnt<3 * COPIES>();
+    v4f acc[FA][FB];
+    v4i fa[2][FA], fb[2][FB];   // the fragments of this half and of the next
+    wait_vmcnt<FA + FB + ON_THE_WAY>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    static_for<0, 8>([&](auto F) __attribute__((always_inline)) {
-        fa[0][decltype(F)::value] = a.template fetch<decltype(F)::value, 0>();
-        fb[0][decltype(F)::value] = b.template fetch<decltype(F)::value, 0>();
-    });
+    static_for<0, FA>([&](auto F) __attribute__((always_inline)) { fa[0][decltype(F)::value] = a.template fetch<decltype(F)::value, 0>(); });
+    static_for<0, FB>([&](auto F) __attribute__((always_inline)) { fb[0][decltype(F)::value] = b.template fetch<decltype(F)::value, 0>(); });
 
     auto half = [&](auto H) __attribute__((always_inline)) {
-        constexpr int h = decltype(H)::value;
+        constexpr int h = decltype(H)::value, READS = FA + FB, EVERY = M / READS;
         if constexpr (h == 1) {
             a.begin(g);
             b.begin(g);
         }
-        static_for<0, 64>([&](auto X) __attribute__((always_inline)) {
-            constexpr int x = decltype(X)::value, j = x / 8, i = j & 1 ? 7 - x % 8 : x % 8;
-            if constexpr (x % 3 == 0 && x < 48) {
-                constexpr int f = x / 3;
-                if constexpr (f < 8)
-                    fa[1 - h][f] = a.template fetch<f % 8, 1 - h>();
+        static_for<0, M>([&](auto X) __attribute__((always_inline)) {
+            constexpr int x = decltype(X)::value, j = x / FA, i = j & 1 ? FA - 1 - x % FA : x % FA;
+            // (early, so that the last of them is there at the end: three steps of four)
+            constexpr int f = x * READS / (M * 3 / 4);
+            if constexpr (f < READS && f * (M * 3 / 4) / READS + ((f * (M * 3 / 4)) % READS != 0) == x) {
+                if constexpr (f < FA)
+                    fa[1 - h][f % FA] = a.template fetch<f % FA, 1 - h>();
                 else
-                    fb[1 - h][f - 8] = b.template fetch<f % 8, 1 - h>();
+                    fb[1 - h][f % READS - FA] = b.template fetch<(f - FA) & (FB - 1), 1 - h>();
             }
             if constexpr (h == 1) {
-                if constexpr (x % 4 == 1 && x < 32) a.template set_m0<x / 4>();
-                if constexpr (x % 4 == 2 && x < 32) a.template issue<x / 4>();
-                if constexpr (x % 4 == 1 && x >= 32) b.template set_m0<x / 4 - 8>();
-                if constexpr (x % 4 == 2 && x >= 32) b.template issue<x / 4 - 8>();
+                constexpr int c = x / EVERY;
+                if constexpr (x % EVERY == 0 && c < FA) a.template set_m0<c>();
+                if constexpr (x % EVERY == 1 && c < FA) a.template issue<c>();
+                if constexpr (x % EVERY == 0 && c >= FA && c < READS) b.template set_m0<c - FA>();
+                if constexpr (x % EVERY == 1 && c >= FA && c < READS) b.template issue<c - FA>();
             }
             acc[i][j] = mfma<TYPE>(fb[h][j], fa[h][i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (h == 0) {
-            // all of this stage is read, and A and B of the next one are there (B of the one after may be on its way)
-            wait_vmcnt<COPIES>();
+            // all of this stage is read, and the next one is there
+            wait_vmcnt<ON_THE_WAY>();
             wait_lds();
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
@@ -359,9 +371,9 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
     int tm, tp, split, k0, k1;
     while (order.take(tm, tp, split, k0, k1)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < FA; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < FB; ++j) {
                 acc[i][j] = v4f{0, 0, 0, 0};
                 asm volatile("" : "+a"(acc[i][j]));  // (in its accumulation registers from here on)
             }
@@ -374,17 +386,16 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
         // (read by asm statements, or the register allocator parks sums in scratch memory; the wait states behind the last matrix instruction are
         // written out)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < FA; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+            for (int j = 0; j < FB; ++j) asm volatile("" : "+a"(acc[i][j]));
         asm volatile("s_nop 15\n\ts_nop 15");
         int lr = lane & 15, lc = lane >> 4;
         asm volatile("" : "+v"(lr), "+v"(lc));
-        const int row_lane = wm * 128 + a.row(0, lr);
-        const int64_t row0 = (int64_t)tm * TILE + row_lane, col0 = (int64_t)tp * TILE + wn * 128;
+        const int64_t row0 = (int64_t)tm * TILE_A + wm * (TILE_A / 2) + a.row(0, lr), col0 = (int64_t)tp * TILE_B + wn * (TILE_B / 2);
         // this lane's 32 sums of a row: v[4 j + r] is of place 4 lc + r of B's fragment j (B along: v[8 J + e] is column 32 J + 8 lc + e)
         auto rows = [&](auto&& f) __attribute__((always_inline)) {
-            static_for<0, 8>([&](auto I) __attribute__((always_inline)) {
+            static_for<0, FA>([&](auto I) __attribute__((always_inline)) {
                 constexpr int i = decltype(I)::value;
                 float v[32];
 #pragma unroll
@@ -395,11 +406,11 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
         };
         if constexpr (KIND == lmk::LOSS || KIND == lmk::SLOPE) {
             // the targets of the lane's rows, as columns of this wave's 128
-            int target[8];
+            int target[FA];
             bool any = false;
-            static_for<0, 8>([&](auto I) {
+            static_for<0, FA>([&](auto I) {
                 constexpr int i = decltype(I)::value;
-                target[i] = g.targets[(int64_t)tm * TILE + row_lane + row_of(i, 0)];
+                target[i] = g.targets[row0 + row_of(i, 0)];
                 const int c = target[i] - g.column0 - (int)col0;
                 target[i] = target[i] < 0 ? target[i] : (c >= 0 && c < 128 ? c : 128);
                 any |= target[i] >= 0 && target[i] < 128;
@@ -434,9 +445,9 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
                         if (lc == 0) g.parts[(col0 >> 7) * g.parts_ld + row0 + ri] = make_float2(m, s);
                     });
             } else {
-                float lse2[8];
+                float lse2[FA];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) lse2[i] = g.lse2[(int64_t)tm * TILE + row_lane + row_of(i, 0)];
+                for (int i = 0; i < FA; ++i) lse2[i] = g.lse2[row0 + row_of(i, 0)];
                 typedef typename Elem<TYPE>::Bits Bits;
                 rows([&](auto I, auto RI, float* v) __attribute__((always_inline)) {
                     constexpr int i = decltype(I)::value, ri = decltype(RI)::value;
@@ -508,41 +519,31 @@ template <int TYPE, int KIND> __global__ __launch_bounds__(256) void k_lm_tile(A
     wait_vmcnt<0>();  // no copy may still be writing LDS when the workgroup retires
 }
 
-template <int TYPE, int KIND> void run(const Args& g, hipStream_t st)
+template <int TYPE, int KIND, int FA> void run(Args g, hipStream_t st)
 {
+    g.TM = (int)((g.m + 32 * FA - 1) / (32 * FA));
     const int64_t items = (int64_t)g.TM * g.TP * g.splits;
-    k_lm_tile<TYPE, KIND><<<dim3((unsigned)(items < COMPUTE_UNITS ? items : COMPUTE_UNITS)), dim3(256), 0, st>>>(g);
+    k_lm_tile<TYPE, KIND, FA><<<dim3((unsigned)(items < COMPUTE_UNITS ? items : COMPUTE_UNITS)), dim3(256), 0, st>>>(g);
 }
-template <int TYPE> void run(int kind, const Args& g, hipStream_t st)
-{
-    if (kind == lmk::LINEAR) run<TYPE, lmk::LINEAR>(g, st);
-    if (kind == lmk::LOSS) run<TYPE, lmk::LOSS>(g, st);
-    if (kind == lmk::SLOPE) run<TYPE, lmk::SLOPE>(g, st);
-    if (kind == lmk::STATES) run<TYPE, lmk::STATES>(g, st);
-    if (kind == lmk::WEIGHTS) run<TYPE, lmk::WEIGHTS>(g, st);
-}
+template <int TYPE, int KIND> void run(const Args& g, bool half, hipStream_t st) { half ? run<TYPE, KIND, 4>(g, st) : run<TYPE, KIND, 8>(g, st); }
 
 }  // namespace
 
 namespace lmk {
 
-// (32-bit offsets inside a panel, 30 bits where rows lie along the inner dimension: pieces behind a row's end are sent behind those)
-bool tile_fits(const Tile& t)
-{
-    auto along = [](int64_t ld) { return ld * 2 < (1 << 22); };
-    auto across = [&](int64_t ld) { return t.n * ld * 2 < ((int64_t)1 << 32) - (1 << 20); };
-    const bool a = t.kind == WEIGHTS ? across(t.lda) : along(t.lda);
-    const bool b = t.kind == WEIGHTS || t.kind == STATES ? across(t.ldb) : along(t.ldb);
-    return a && b && t.n > 0 && (t.m + TILE - 1) / TILE * ((t.p + TILE - 1) / TILE) * t.splits < ((int64_t)1 << 28);
-}
-
-hipError_t launch_tile(const Tile& t, hipStream_t st)
+// LM_TYPE: the element type that this compilation is of (the instances of both take long)
+#define NAME2(type) launch_tile_##type
+#define NAME(type) NAME2(type)
+hipError_t NAME(LM_TYPE)(const Tile& t, hipStream_t st)
 {
     const Args g = {t.m, t.n, t.p, t.b_rows, (uint64_t)(uintptr_t)t.A, (uint64_t)(uintptr_t)t.B, (uint32_t)(t.lda * 2), (uint32_t)(t.ldb * 2),
-                    (int)((t.m + TILE - 1) / TILE), (int)((t.p + TILE - 1) / TILE), (int)((t.n + STAGE_K - 1) / STAGE_K), t.splits, t.D, t.ldd, t.dtype,
+                    0, (int)((t.p + TILE_B - 1) / TILE_B), (int)((t.n + STAGE_K - 1) / STAGE_K), t.splits, t.D, t.ldd, t.dtype,
                     t.alpha, t.beta, t.alpha_at, t.split_stride, t.targets, t.column0, t.lse2, t.at_target, t.parts, t.parts_ld};
-    if (t.type == BF16) run<BF16>(t.kind, g, st);
-    if (t.type == F16) run<F16>(t.kind, g, st);
+    if (t.kind == LINEAR) run<LM_TYPE, LINEAR>(g, t.half, st);
+    if (t.kind == LOSS) run<LM_TYPE, LOSS>(g, t.half, st);
+    if (t.kind == SLOPE) run<LM_TYPE, SLOPE>(g, t.half, st);
+    if (t.kind == STATES) run<LM_TYPE, STATES>(g, t.half, st);
+    if (t.kind == WEIGHTS) run<LM_TYPE, WEIGHTS>(g, t.half, st);
     return hipGetLastError();
 }
 
