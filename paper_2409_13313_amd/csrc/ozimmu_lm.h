@@ -68,15 +68,17 @@ hipError_t launch_direct(const Linear& l, const Weights& w, hipStream_t st);
 // What is made of the sums C (m x p, over the inner dimension n):
 enum Kind {
     LINEAR,   // A: m x n, B: p x n.  D <- alpha C + beta D
-    LOSS,     // A: m x n, B: p x n.  per row and 128 columns: log2(e) times the largest sum, and the sum of 2^(log2(e) c - that) (without the target's)
+    LOSS,     // A: m x n, B: p x n.  per row and part_columns: log2(e) times the largest sum, and the sum of 2^(log2(e) c - that) (without the target's)
     SLOPE,    // A: m x n, B: p x n.  D <- exp(C - lse) - [column = target] in 16 bits (0 in rows without a target)
     STATES,   // A: m x n, B: n x p.  D (FP32, one for each split of n) <- C, or C + D
     WEIGHTS,  // A: n x m, B: n x p.  D <- alpha C + beta D, alpha from the device
 };
 
+enum TileShape { TILE_256, TILE_128_256, TILE_128 };  // sums a workgroup: 256 x 256, 128 x 256, 128 x 128
+
 struct Tile {
     int kind, type;       // type: of A and B
-    bool half = false;    // tiles of 128 x 256 instead of 256 x 256
+    int shape = TILE_256;
     int64_t m, n, p;
     const void *A, *B;    // 16-byte aligned; leading dimensions multiples of 8 elements; where rows lie along n, n a multiple of 8
     int64_t lda, ldb;
@@ -92,11 +94,13 @@ struct Tile {
     int column0 = 0;                   // LOSS, SLOPE: what number the first column is to them
     const float* lse2 = nullptr;       // SLOPE: log2(e) lse per row of whole tiles
     float* at_target = nullptr;        // LOSS: the sums at the targets
-    float2* parts = nullptr;           // LOSS: [128 columns][row]
+    float2* parts = nullptr;           // LOSS: [part_columns][row]
     int64_t parts_ld = 0;
 };
 bool tile_fits(const Tile& t);
-bool half_tiles(int64_t m, int64_t p, int splits);   // whether tiles of 128 x 256 take less time
+int tile_shape(int64_t m, int64_t n, int64_t p, int splits);   // the one that takes the least time, by an estimate
+int tile_splits(int64_t m, int64_t n, int64_t p);             // STATES: the number of splits that does
+inline int part_columns(int shape) { return shape == TILE_128 ? 64 : 128; }  // LOSS: columns of a part
 hipError_t launch_tile(const Tile& t, hipStream_t st);
 hipError_t launch_tile_1(const Tile& t, hipStream_t st);  // BF16
 hipError_t launch_tile_2(const Tile& t, hipStream_t st);  // F16

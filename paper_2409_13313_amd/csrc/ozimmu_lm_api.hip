@@ -4,6 +4,73 @@
 #include "../../include/ozimmu_lm.h"
 #include "ozimmu_lm.h"
 
+namespace lmk {
+
+constexpr int64_t COMPUTE_UNITS = 256;
+
+// (32-bit offsets inside a panel, 30 bits where rows lie along the inner dimension: pieces behind a row's end are sent behind those)
+bool tile_fits(const Tile& t)
+{
+    auto along = [](int64_t ld) { return ld * 2 < (1 << 22); };
+    auto across = [&](int64_t ld) { return t.n * ld * 2 < ((int64_t)1 << 32) - (1 << 20); };
+    const bool a = t.kind == WEIGHTS ? across(t.lda) : along(t.lda);
+    const bool b = t.kind == WEIGHTS || t.kind == STATES ? across(t.ldb) : along(t.ldb);
+    return a && b && t.n > 0 && (t.m + 127) / 128 * ((t.p + 255) / 256) * t.splits < ((int64_t)1 << 28);
+}
+
+// Microseconds of an output of that many tiles over KT stages each, roughly: rounds of one tile for every compute unit, of two with 128 x 128.
+// Fitted to (loss alone, without its small launches; tokens x inner x words: 256 x 256, 128 x 256, 128 x 128)  133 x 1024 x 5003: 30, 18, 12;
+// 777 x 1024 x 10007: 33, 38, 28;  2048 x 4096 x 4096: 85, 57, 59;  512 x 4096 x 4096: 78, 49, 36;  1024 x 1024 x 32768: 65, 75, 66;
+// 4096 x 1024 x 32768: 255, 282, 275;  1 x 4096 x 32768: 77, 49, 42;  2048 x 4096 x 131072: 1570, 1820, -.
+static double estimate_us(int shape, int64_t tiles, double KT)
+{
+    const double rounds = (double)((tiles + COMPUTE_UNITS - 1) / COMPUTE_UNITS);
+    if (shape == TILE_256) return rounds * (13 + KT * (1.12 + 0.2 * (double)tiles / (rounds * COMPUTE_UNITS)));
+    if (shape == TILE_128_256) return rounds * (5 + KT * 0.81);
+    const int64_t pairs = tiles / (2 * COMPUTE_UNITS), rest = tiles % (2 * COMPUTE_UNITS);
+    return (double)pairs * (3.5 + KT * 0.86) + (rest == 0 ? 0 : rest > COMPUTE_UNITS ? 3.5 + KT * 0.86 : 4 + KT * 0.5);
+}
+
+static int64_t tiles_of(int shape, int64_t m, int64_t p)
+{
+    const int64_t rows = shape == TILE_256 ? 256 : 128, columns = shape == TILE_128 ? 128 : 256;
+    return (m + rows - 1) / rows * ((p + columns - 1) / columns);
+}
+
+int tile_shape(int64_t m, int64_t n, int64_t p, int splits)
+{
+#ifdef VAR_SHAPE
+    return VAR_SHAPE;
+#endif
+    int best = TILE_256;
+    for (int s : {TILE_128_256, TILE_128})
+        if (estimate_us(s, tiles_of(s, m, p) * splits, (double)((n + 63) / 64) / splits) <
+            estimate_us(best, tiles_of(best, m, p) * splits, (double)((n + 63) / 64) / splits))
+            best = s;
+    return best;
+}
+
+// The number of splits of n, four stages each at the least, that takes the least time; the sums of each are written and read again in FP32
+int tile_splits(int64_t m, int64_t n, int64_t p)
+{
+    const int64_t KT = (n + 63) / 64;
+    int best = 1;
+    double least = 0;
+    for (int64_t s = 1; s <= 256 && (s == 1 || s * 4 <= KT); s += s < 4 ? 1 : s / 4) {
+        const int shape = tile_shape(m, n, p, (int)s);
+        const double us = estimate_us(shape, tiles_of(shape, m, p) * s, (double)KT / (double)s) + (double)(s * m * p) * 8 / 4e6;
+        if (s == 1 || us < least) {
+            least = us;
+            best = (int)s;
+        }
+    }
+    return best;
+}
+
+hipError_t launch_tile(const Tile& t, hipStream_t st) { return t.type == BF16 ? launch_tile_1(t, st) : launch_tile_2(t, st); }
+
+}  // namespace lmk
+
 namespace {
 
 using lmk::Tile;
@@ -12,7 +79,6 @@ using lml::Shape;
 constexpr int64_t MAX_ROWS = ((int64_t)1 << 22) - 256, MAX_INNER = (int64_t)1 << 20, MAX_LD = ((int64_t)1 << 40) - 1;
 constexpr int64_t MAX_SPAN = ((int64_t)1 << 60) - 1;   // rows x leading dimension: byte offsets stay within 64 bits
 constexpr int64_t MAX_STATES = ((int64_t)1 << 31) - (1 << 20);
-constexpr int64_t COMPUTE_UNITS = 256;
 
 inline int64_t round_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 inline bool rows_ok(int64_t r) { return r >= 0 && r <= MAX_ROWS; }
@@ -129,7 +195,7 @@ int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const v
         t.p = t.b_rows = p - at < plan.rows ? p - at : plan.rows;
         CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, st)));
         t.D = (uint8_t*)D + at * size;
-        t.half = lmk::half_tiles(t.m, t.p, t.splits);
+        t.shape = lmk::tile_shape(t.m, t.n, t.p, t.splits);
         CHECK(launched(lmk::launch_tile(t, st)));
     }
     return OZIMMU_OK;
@@ -161,7 +227,7 @@ struct LossPlan {
     {
         Room room{(uint8_t*)workspace};
         width = round_to(n, 64);
-        const int64_t blocks = (p + 127) / 128;
+        const int64_t blocks = (p + 63) / 64;
         // tokens at a time: parts of at most 256 MB
         tokens = ((int64_t)1 << 25) / blocks / 256 * 256;
         if (tokens < 256) tokens = 256;
@@ -195,12 +261,7 @@ struct GradientPlan {
         if (words > most) words = most;
         if (words < 256) words = 256;
         if (words > round_to(p, 256)) words = round_to(p, 256);
-        // the states' gradient: with few tiles the words are shared by several workgroups
-        const int64_t tiles = padded / 256 * (states_ld / 256);
-        const int64_t most_splits = words / 64 / 4 < 1 ? 1 : words / 64 / 4;
-        int64_t s = COMPUTE_UNITS / (tiles < 1 ? 1 : tiles);
-        s = s < 1 ? 1 : s;
-        splits = (int)(s < most_splits ? s : most_splits);
+        splits = lmk::tile_splits(m, words, n);
         targets = room.take<int>(padded);
         lse2 = room.take<float>(padded);
         ratio = room.take<float>(padded);
@@ -215,29 +276,6 @@ struct GradientPlan {
 };
 
 }  // namespace
-
-namespace lmk {
-
-// (32-bit offsets inside a panel, 30 bits where rows lie along the inner dimension: pieces behind a row's end are sent behind those)
-bool tile_fits(const Tile& t)
-{
-    auto along = [](int64_t ld) { return ld * 2 < (1 << 22); };
-    auto across = [&](int64_t ld) { return t.n * ld * 2 < ((int64_t)1 << 32) - (1 << 20); };
-    const bool a = t.kind == WEIGHTS ? across(t.lda) : along(t.lda);
-    const bool b = t.kind == WEIGHTS || t.kind == STATES ? across(t.ldb) : along(t.ldb);
-    return a && b && t.n > 0 && (t.m + 127) / 128 * ((t.p + 255) / 256) * t.splits < ((int64_t)1 << 28);
-}
-
-bool half_tiles(int64_t m, int64_t p, int splits)
-{
-    const int64_t columns = (p + 255) / 256 * splits, whole = (m + 255) / 256 * columns, half = (m + 127) / 128 * columns;
-    auto rounds = [](int64_t items) { return (double)((items + COMPUTE_UNITS - 1) / COMPUTE_UNITS); };
-    return rounds(half) * 0.6 < rounds(whole);
-}
-
-hipError_t launch_tile(const Tile& t, hipStream_t st) { return t.type == BF16 ? launch_tile_1(t, st) : launch_tile_2(t, st); }
-
-}  // namespace lmk
 
 extern "C" {
 
@@ -367,6 +405,7 @@ int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const voi
         t.at_target = plan.at_target;
         t.parts_ld = plan.tokens;
         const int64_t step = lay_out ? plan.words : p;
+        const int shape = lmk::tile_shape(rows, t.n, step, 1);
         for (int64_t v0 = 0; v0 < p; v0 += step) {
             t.p = t.b_rows = p - v0 < step ? p - v0 : step;
             t.B = (const uint16_t*)W + v0 * ldw;
@@ -377,12 +416,12 @@ int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const voi
                 t.ldb = plan.width;
             }
             t.column0 = (int)v0;
-            t.parts = plan.parts + v0 / 128 * plan.tokens;
+            t.parts = plan.parts + v0 / lmk::part_columns(shape) * plan.tokens;
+            t.shape = shape;
             if (!lmk::tile_fits(t)) return OZIMMU_ERR_DIM;
-            t.half = lmk::half_tiles(t.m, t.p, t.splits);
             CHECK(launched(lmk::launch_tile(t, st)));
         }
-        CHECK(launched(lmk::launch_join(rows, (p + 127) / 128, plan.parts, plan.tokens, plan.targets, plan.at_target, loss + t0, lse + t0, st)));
+        CHECK(launched(lmk::launch_join(rows, (p + lmk::part_columns(shape) - 1) / lmk::part_columns(shape), plan.parts, plan.tokens, plan.targets, plan.at_target, loss + t0, lse + t0, st)));
     }
     return OZIMMU_OK;
 }
@@ -446,12 +485,12 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
         t.column0 = (int)v0;
         t.lse2 = plan.lse2;
         if (!lmk::tile_fits(t)) return OZIMMU_ERR_DIM;
-        t.half = lmk::half_tiles(t.m, t.p, t.splits);
+        t.shape = lmk::tile_shape(t.m, t.n, t.p, t.splits);
         CHECK(launched(lmk::launch_tile(t, st)));
         if (dX) {
             Tile s{lmk::STATES, type};
             s.m = m;
-            s.n = whole;
+            s.n = round_to(words, 64);  // (columns of slopes behind the words: zeros, as far as tiles reach, which is here at the least)
             s.p = round_to(n, 8);
             s.b_rows = words;
             s.A = plan.slopes;
@@ -462,10 +501,10 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
             s.ldd = plan.states_ld;
             s.split_stride = plan.padded * plan.states_ld;
             s.beta = v0 > 0 ? 1.0f : 0.0f;
-            s.splits = plan.splits < (int)(whole / 64) ? plan.splits : (int)(whole / 64);
+            s.splits = plan.splits < (int)(s.n / 64) ? plan.splits : (int)(s.n / 64);
             if (v0 == 0) splits = s.splits;
             if (!lmk::tile_fits(s)) return OZIMMU_ERR_DIM;
-            s.half = lmk::half_tiles(s.m, s.p, s.splits);
+            s.shape = lmk::tile_shape(s.m, s.n, s.p, s.splits);
             CHECK(launched(lmk::launch_tile(s, st)));
         }
         if (dW) {
@@ -484,7 +523,7 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
             s.alpha_at = plan.largest;
             s.beta = beta;
             if (!lmk::tile_fits(s)) return OZIMMU_ERR_DIM;
-            s.half = lmk::half_tiles(s.m, s.p, s.splits);
+            s.shape = lmk::tile_shape(s.m, s.n, s.p, s.splits);
             CHECK(launched(lmk::launch_tile(s, st)));
         }
     }

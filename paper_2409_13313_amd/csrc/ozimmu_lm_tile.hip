@@ -10,7 +10,6 @@ using lmk::Tile;
 
 constexpr int64_t COMPUTE_UNITS = 256;
 constexpr int NXCD = 8, STAGE_K = 64;
-constexpr int FB = 8, TILE_B = 32 * FB;  // fragments of B a wave, columns of a tile
 constexpr float LOG2E = 1.44269504088896341f;
 
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -283,14 +282,15 @@ template <int TYPE, int DTYPE> __device__ inline void put(const Args& g, float a
 // set of registers.  So both places of a stage are free at the end of its first half, where the one barrier of a stage is; behind it they take
 // the copies of A two stages and of B three stages on.
 //
-// FA = 8: 256 x 256 sums a workgroup; FA = 4: 128 x 256, for outputs of too few tiles.
-template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_lm_tile(Args g)
+// A wave has FA fragments of A and FB of B, a workgroup 32 FA x 32 FB sums: 256 x 256, one workgroup a compute unit; 128 x 256 and 128 x 128 (two
+// workgroups a compute unit, the one at work while the other begins or ends) for outputs of too few tiles.
+template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, FB == 4 ? 2 : 1) void k_lm_tile(Args g)
 {
     constexpr bool A_ACROSS = KIND == lmk::WEIGHTS, B_ACROSS = KIND == lmk::WEIGHTS || KIND == lmk::STATES;
-    constexpr int A_PLACES = FA == 8 ? 2 : 3, B_PLACES = 3, M = FA * FB, TILE_A = 32 * FA;
+    constexpr int A_PLACES = FA == 8 || FB == 4 ? 2 : 3, B_PLACES = 3, M = FA * FB, TILE_A = 32 * FA, TILE_B = 32 * FB, N = 4 * FB;
     typedef Stream<A_ACROSS, FA, A_PLACES, true> StreamA;
     typedef Stream<B_ACROSS, FB, B_PLACES, false> StreamB;
-    __shared__ __align__(16) uint8_t places[A_PLACES * StreamA::BYTES + B_PLACES * StreamB::BYTES];  // 160 KiB; FA = 4: 144
+    __shared__ __align__(16) uint8_t places[A_PLACES * StreamA::BYTES + B_PLACES * StreamB::BYTES];  // 160, 144, 80 KiB
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave >> 1, wn = wave & 1;
@@ -367,6 +367,7 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
         }
     };
 
+    const float alpha = KIND == lmk::WEIGHTS ? g.alpha * *g.alpha_at : g.alpha;
     Order order(g);
     int tm, tp, split, k0, k1;
     while (order.take(tm, tp, split, k0, k1)) {
@@ -393,13 +394,13 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
         int lr = lane & 15, lc = lane >> 4;
         asm volatile("" : "+v"(lr), "+v"(lc));
         const int64_t row0 = (int64_t)tm * TILE_A + wm * (TILE_A / 2) + a.row(0, lr), col0 = (int64_t)tp * TILE_B + wn * (TILE_B / 2);
-        // this lane's 32 sums of a row: v[4 j + r] is of place 4 lc + r of B's fragment j (B along: v[8 J + e] is column 32 J + 8 lc + e)
+        // this lane's N sums of a row: v[4 j + r] is of place 4 lc + r of B's fragment j (B along: v[8 J + e] is column 32 J + 8 lc + e)
         auto rows = [&](auto&& f) __attribute__((always_inline)) {
             static_for<0, FA>([&](auto I) __attribute__((always_inline)) {
                 constexpr int i = decltype(I)::value;
-                float v[32];
+                float v[N];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][e / 8 * 2 + e / 4 % 2][e % 4]));
+                for (int e = 0; e < N; ++e) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][e / 8 * 2 + e / 4 % 2][e % 4]));
                 f(I, std::integral_constant<int, a.row(i, 0)>{}, v);
                 __builtin_amdgcn_sched_barrier(0);
             });
@@ -412,11 +413,11 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
                 constexpr int i = decltype(I)::value;
                 target[i] = g.targets[row0 + row_of(i, 0)];
                 const int c = target[i] - g.column0 - (int)col0;
-                target[i] = target[i] < 0 ? target[i] : (c >= 0 && c < 128 ? c : 128);
-                any |= target[i] >= 0 && target[i] < 128;
+                target[i] = target[i] < 0 ? target[i] : (c >= 0 && c < TILE_B / 2 ? c : TILE_B);
+                any |= target[i] >= 0 && target[i] < TILE_B;
             });
-            const bool found = __any(any), edge = col0 + 128 > g.p;
-            const int cols = (int)(g.p - col0 < 128 ? g.p - col0 : 128);
+            const bool found = __any(any), edge = col0 + TILE_B / 2 > g.p;
+            const int cols = (int)(g.p - col0 < TILE_B / 2 ? g.p - col0 : TILE_B / 2);
             if constexpr (KIND == lmk::LOSS) {
                 if (col0 < g.p)
                     rows([&](auto I, auto RI, float* v) __attribute__((always_inline)) {
@@ -424,10 +425,10 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
                         const float none = -__builtin_inff();
                         if (edge)
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = e / 8 * 32 + lc * 8 + e % 8 < cols ? v[e] : none;
+                            for (int e = 0; e < N; ++e) v[e] = e / 8 * 32 + lc * 8 + e % 8 < cols ? v[e] : none;
                         if (found) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
+                            for (int e = 0; e < N; ++e)
                                 if (target[i] == e / 8 * 32 + lc * 8 + e % 8) {
                                     g.at_target[row0 + ri] = v[e];
                                     v[e] = none;
@@ -435,14 +436,14 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
                         }
                         float m = none;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) m = fmaxf(m, v[e]);
+                        for (int e = 0; e < N; ++e) m = fmaxf(m, v[e]);
                         m = over_quarters_max(m) * LOG2E;
                         const float m2 = m == none ? 0.0f : m;
                         float s = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], LOG2E, -m2));
+                        for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], LOG2E, -m2));
                         s = over_quarters_sum(s);
-                        if (lc == 0) g.parts[(col0 >> 7) * g.parts_ld + row0 + ri] = make_float2(m, s);
+                        if (lc == 0) g.parts[col0 / (TILE_B / 2) * g.parts_ld + row0 + ri] = make_float2(m, s);
                     });
             } else {
                 float lse2[FA];
@@ -455,13 +456,13 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
                     float target_slope = 0.0f;
                     if (found) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
+                        for (int e = 0; e < N; ++e)
                             if (target[i] == e / 8 * 32 + lc * 8 + e % 8) target_slope = expm1f((v[e] * LOG2E - lse2[i]) * 0.693147180559945309f);
                     }
                     const uint32_t keep = target[i] == lmk::NO_TARGET ? 0u : 0xffffffffu;
                     Bits* const out = (Bits*)g.D + (row0 + ri) * g.ldd + col0 + lc * 8;
 #pragma unroll
-                    for (int jj = 0; jj < 4; ++jj) {
+                    for (int jj = 0; jj < FB / 2; ++jj) {
                         Bits x[8];
                         uint32_t w[4];
 #pragma unroll
@@ -482,24 +483,22 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
                 constexpr int ri = decltype(RI)::value;
                 float* const out = (float*)g.D + split * g.split_stride + (row0 + ri) * g.ldd + col0 + lc * 4;
                 if (g.beta != 0.0f) {
-                    v4f old[8];
+                    v4f old[FB];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) old[j] = *(const v4f*)(out + 16 * j);
+                    for (int j = 0; j < FB; ++j) old[j] = *(const v4f*)(out + 16 * j);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] += old[e / 4][e % 4];
+                    for (int e = 0; e < N; ++e) v[e] += old[e / 4][e % 4];
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) *(v4f*)(out + 16 * j) = v4f{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+                for (int j = 0; j < FB; ++j) *(v4f*)(out + 16 * j) = v4f{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
             });
         } else {
-            float alpha = g.alpha;
-            if constexpr (KIND == lmk::WEIGHTS) alpha *= *g.alpha_at;
             rows([&](auto, auto RI, float* v) __attribute__((always_inline)) {
                 constexpr int ri = decltype(RI)::value;
                 if constexpr (B_ACROSS) {
                     // two fragments' fours into eights: the odd sixteens of lanes give theirs of the first for the even ones' of the second
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
+                    for (int e = 0; e < N; ++e)
                         if (e / 4 % 2 == 0) {
                             const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[e]), __float_as_uint(v[e + 4]), false, false);
                             v[e] = __uint_as_float(x[0]);
@@ -508,7 +507,7 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
                 }
                 const int eight = B_ACROSS ? (lc & 1) * 16 + (lc >> 1) * 8 : lc * 8;  // of 32 columns
 #pragma unroll
-                for (int jj = 0; jj < 4; ++jj) {
+                for (int jj = 0; jj < FB / 2; ++jj) {
                     if (g.dtype == F32) put<TYPE, F32>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
                     if (g.dtype == BF16) put<TYPE, BF16>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
                     if (g.dtype == F16) put<TYPE, F16>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
@@ -519,13 +518,19 @@ template <int TYPE, int KIND, int FA> __global__ __launch_bounds__(256) void k_l
     wait_vmcnt<0>();  // no copy may still be writing LDS when the workgroup retires
 }
 
-template <int TYPE, int KIND, int FA> void run(Args g, hipStream_t st)
+template <int TYPE, int KIND, int FA, int FB> void run(Args g, hipStream_t st)
 {
     g.TM = (int)((g.m + 32 * FA - 1) / (32 * FA));
-    const int64_t items = (int64_t)g.TM * g.TP * g.splits;
-    k_lm_tile<TYPE, KIND, FA><<<dim3((unsigned)(items < COMPUTE_UNITS ? items : COMPUTE_UNITS)), dim3(256), 0, st>>>(g);
+    g.TP = (int)((g.p + 32 * FB - 1) / (32 * FB));
+    const int64_t items = (int64_t)g.TM * g.TP * g.splits, most = FB == 4 ? 2 * COMPUTE_UNITS : COMPUTE_UNITS;
+    k_lm_tile<TYPE, KIND, FA, FB><<<dim3((unsigned)(items < most ? items : most)), dim3(256), 0, st>>>(g);
 }
-template <int TYPE, int KIND> void run(const Args& g, bool half, hipStream_t st) { half ? run<TYPE, KIND, 4>(g, st) : run<TYPE, KIND, 8>(g, st); }
+template <int TYPE, int KIND> void run(const Args& g, int shape, hipStream_t st)
+{
+    if (shape == lmk::TILE_256) run<TYPE, KIND, 8, 8>(g, st);
+    if (shape == lmk::TILE_128_256) run<TYPE, KIND, 4, 8>(g, st);
+    if (shape == lmk::TILE_128) run<TYPE, KIND, 4, 4>(g, st);
+}
 
 }  // namespace
 
@@ -537,13 +542,13 @@ namespace lmk {
 hipError_t NAME(LM_TYPE)(const Tile& t, hipStream_t st)
 {
     const Args g = {t.m, t.n, t.p, t.b_rows, (uint64_t)(uintptr_t)t.A, (uint64_t)(uintptr_t)t.B, (uint32_t)(t.lda * 2), (uint32_t)(t.ldb * 2),
-                    0, (int)((t.p + TILE_B - 1) / TILE_B), (int)((t.n + STAGE_K - 1) / STAGE_K), t.splits, t.D, t.ldd, t.dtype,
+                    0, 0, (int)((t.n + STAGE_K - 1) / STAGE_K), t.splits, t.D, t.ldd, t.dtype,
                     t.alpha, t.beta, t.alpha_at, t.split_stride, t.targets, t.column0, t.lse2, t.at_target, t.parts, t.parts_ld};
-    if (t.kind == LINEAR) run<LM_TYPE, LINEAR>(g, t.half, st);
-    if (t.kind == LOSS) run<LM_TYPE, LOSS>(g, t.half, st);
-    if (t.kind == SLOPE) run<LM_TYPE, SLOPE>(g, t.half, st);
-    if (t.kind == STATES) run<LM_TYPE, STATES>(g, t.half, st);
-    if (t.kind == WEIGHTS) run<LM_TYPE, WEIGHTS>(g, t.half, st);
+    if (t.kind == LINEAR) run<LM_TYPE, LINEAR>(g, t.shape, st);
+    if (t.kind == LOSS) run<LM_TYPE, LOSS>(g, t.shape, st);
+    if (t.kind == SLOPE) run<LM_TYPE, SLOPE>(g, t.shape, st);
+    if (t.kind == STATES) run<LM_TYPE, STATES>(g, t.shape, st);
+    if (t.kind == WEIGHTS) run<LM_TYPE, WEIGHTS>(g, t.shape, st);
     return hipGetLastError();
 }
 
