@@ -5,9 +5,9 @@
 // other along the row: 16 bytes for each lane l of a wave, the codes of row l % 16 that it holds in four matrix instructions (16x16x32).
 // Word j of them (j < 4) is elements 32 j + 8 (l / 16) .. + 7, element 2 i at bits 4 i and 2 i + 1 at bits 16 + 4 i, so that one mask
 // and one or makes a pair of 16-bit numbers of two neighbouring elements.
-// Behind the codes of all blocks come their scales, [block][row][128 / group] numbers of 16 bits (0 behind the end of a row), and behind those,
-// where the weights have zero points, these as bytes in the same order.  Codes behind the end of a row are 0.  Padding rows are not written:
-// what they give is not stored.
+// Behind the codes of all blocks comes a record for each of their rows, [block][row]: 128 / group scales of 16 bits (0 behind the end of a row), then,
+// where the weights have zero points, as many of these as bytes; so a lane has what its row needs beside the codes in one load.  Codes behind the
+// end of a row are 0.  Padding rows are not written: what they give is not stored.
 #pragma once
 #include "ozimmu_mx_convert.h"
 
@@ -23,9 +23,10 @@ struct Shape {
     __host__ __device__ inline int64_t inner_blocks() const { return (n + INNER - 1) / INNER; }
     __host__ __device__ inline int64_t blocks() const { return row_blocks() * inner_blocks(); }
     __host__ __device__ inline int groups() const { return INNER / group; }  // of a block's row
-    __host__ __device__ inline int64_t scales_at() const { return blocks() * BLOCK_BYTES; }
-    __host__ __device__ inline int64_t zeros_at() const { return scales_at() + (blocks() * ROWS * groups() * 2 + 255) / 256 * 256; }
-    __host__ __device__ inline int64_t bytes() const { return zeros_at() + (zeros ? (blocks() * ROWS * groups() + 255) / 256 * 256 : 0); }
+    __host__ __device__ inline int record() const { return groups() * (zeros ? 3 : 2); }
+    __host__ __device__ inline int64_t records_at() const { return blocks() * BLOCK_BYTES; }
+    // (16 bytes more: records are read as whole dwords)
+    __host__ __device__ inline int64_t bytes() const { return blocks() ? records_at() + (blocks() * ROWS * record() + 16 + 255) / 256 * 256 : 0; }
 };
 
 }  // namespace lml
@@ -43,8 +44,8 @@ struct Weights {
 };
 
 hipError_t launch_quantize(int type, const void* W, int64_t ldw, const lml::Shape& s, int stype, void* packed, hipStream_t st);
-// rows row0 .. row0 + rows - 1 into X (of `type`); columns n .. cols - 1 become zeros
-hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, hipStream_t st);
+// rows row0 .. row0 + rows - 1 into X (of `type`); columns n .. cols - 1 (no more than whole blocks have) become zeros; stream: past the caches
+hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, bool stream, hipStream_t st);
 hipError_t launch_pack(const lml::Shape& s, const uint8_t* codes, int64_t ldc, const void* scales, int64_t lds, const uint8_t* zeros, int64_t ldz,
                        void* packed, hipStream_t st);
 hipError_t launch_unpack(const lml::Shape& s, const void* packed, uint8_t* codes, int64_t ldc, void* scales, int64_t lds, uint8_t* zeros,
@@ -74,6 +75,18 @@ enum Kind {
     WEIGHTS,  // A: n x m, B: n x p.  D <- alpha C + beta D, alpha from the device
 };
 
+constexpr int NO_TARGET = -1, BAD_TARGET = -2;  // an ignored row; a target that no column has
+
+struct Targets {
+    const int64_t* y;
+    int64_t stride, ignore, words;
+    __device__ inline int operator[](int64_t row) const
+    {
+        const int64_t v = y[row * stride];
+        return v == ignore ? NO_TARGET : (v >= 0 && v < words ? (int)v : BAD_TARGET);
+    }
+};
+
 enum TileShape { TILE_256, TILE_128_256, TILE_128 };  // sums a workgroup: 256 x 256, 128 x 256, 128 x 128
 
 struct Tile {
@@ -90,7 +103,8 @@ struct Tile {
     const float* alpha_at = nullptr;   // WEIGHTS: alpha is multiplied by this
     int splits = 1;                    // STATES: of the inner dimension
     int64_t split_stride = 0;          // STATES: elements between the D of splits
-    const int* targets = nullptr;      // LOSS, SLOPE: per row of whole tiles; < 0: NO_TARGET, BAD_TARGET
+    Targets targets{};                 // LOSS
+    const int* known = nullptr;        // SLOPE: targets per row of whole tiles, as target_of has them
     int column0 = 0;                   // LOSS, SLOPE: what number the first column is to them
     const float* lse2 = nullptr;       // SLOPE: log2(e) lse per row of whole tiles
     float* at_target = nullptr;        // LOSS: the sums at the targets
@@ -107,19 +121,34 @@ hipError_t launch_tile_2(const Tile& t, hipStream_t st);  // F16
 
 // ---- what stands around them in the loss (ozimmu_lm_loss.hip) ----
 
-constexpr int NO_TARGET = -1, BAD_TARGET = -2;  // an ignored row; a target that no column has
 constexpr float SLOPE_SCALE_F16 = 32768.0f;     // slopes in FP16 are held times this: most of them are far below 2^-14
 
-// rows x cols of X (16 bits) into Y, columns cols .. width - 1 zeros; with `ratio`, times ratio[row] (0: zeros whatever X holds)
-hipError_t launch_lay_out(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, const float* ratio, void* Y, int64_t ldy, int64_t width,
-                          hipStream_t st);
-// targets as Tile has them (rows .. padded - 1: NO_TARGET)
-hipError_t launch_targets(int64_t rows, int64_t padded, int64_t words, const int64_t* y, int64_t stride, int64_t ignore, int* targets, hipStream_t st);
-hipError_t launch_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const int* targets, const float* at_target, float* loss,
+// rows x cols of X (16 bits) into Y (nullptr: not wanted), columns cols .. width - 1 zeros (width: a multiple of 8; Y's rows 16-byte aligned)
+struct LayOut {
+    int64_t rows, cols;
+    const void* X;
+    int64_t ldx;
+    void* Y;
+    int64_t width;
+};
+hipError_t launch_lay_out(int type, const LayOut& a, const LayOut& b, hipStream_t st);  // both, of one type
+hipError_t launch_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const Targets& targets, const float* at_target, float* loss,
                        float* lse, hipStream_t st);
-// targets, log2(e) lse (NaN where the target is bad), the largest |g| of rows with a target and each row's share of it
-hipError_t launch_slopes(int64_t rows, int64_t padded, int64_t words, const int64_t* y, int64_t stride, int64_t ignore, const float* g, int64_t g_stride,
-                         const float* lse, int* targets, float* lse2, float* ratio, float* largest, hipStream_t st);
+// What the gradient begins with: targets and log2(e) lse (NaN where the target is bad) per row, `padded` of them, the largest |g| of rows with a
+// target, X laid out (as x says) and, in `scaled` (nullptr: not wanted), X times each row's share of that |g|, zeros in rows without a target; and W laid out
+struct Prepare {
+    int64_t rows, padded;
+    Targets targets;
+    const float* g;
+    int64_t g_stride;
+    const float* lse;
+    int* known;
+    float *lse2, *largest;
+    LayOut x;
+    void* scaled;
+    LayOut w;
+};
+hipError_t launch_prepare(int type, const Prepare& p, hipStream_t st);
 // dX <- g (the sum of the splits) / scale, zeros in rows without a target
 hipError_t launch_states(int type, int64_t rows, int64_t cols, const float* parts, int64_t ld, int splits, int64_t split_stride, const float* g,
                          int64_t g_stride, const int* targets, float scale, void* dX, int64_t ldx, hipStream_t st);

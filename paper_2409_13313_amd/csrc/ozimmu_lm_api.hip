@@ -180,7 +180,7 @@ int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const v
     t.lda = ldx;
     if (!as_it_is(X, n, ldx)) {
         t.n = plan.width;
-        CHECK(launched(lmk::launch_lay_out(xtype, m, n, X, ldx, nullptr, plan.X, plan.width, plan.width, st)));
+        CHECK(launched(lmk::launch_lay_out(xtype, {m, n, X, ldx, plan.X, plan.width}, {}, st)));
         t.A = plan.X;
         t.lda = plan.width;
     }
@@ -193,7 +193,7 @@ int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const v
     const int64_t size = dtype == OZIMMU_LM_F32 ? 4 : 2;
     for (int64_t at = 0; at < p; at += plan.rows) {
         t.p = t.b_rows = p - at < plan.rows ? p - at : plan.rows;
-        CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, st)));
+        CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, false, st)));
         t.D = (uint8_t*)D + at * size;
         t.shape = lmk::tile_shape(t.m, t.n, t.p, t.splits);
         CHECK(launched(lmk::launch_tile(t, st)));
@@ -218,7 +218,6 @@ int64_t laid_out_rows(int64_t width, int64_t p)
 
 struct LossPlan {
     int64_t width, tokens, words;   // of a row laid out; tokens at a time; rows of W laid out at a time
-    int* targets;
     float* at_target;
     float2* parts;
     uint16_t *X, *W;
@@ -233,7 +232,6 @@ struct LossPlan {
         if (tokens < 256) tokens = 256;
         if (tokens > round_to(m, 256)) tokens = round_to(m, 256);
         words = laid_out_rows(width, p);
-        targets = room.take<int>(tokens);
         at_target = room.take<float>(tokens);
         parts = room.take<float2>(blocks * tokens);
         X = room.take<uint16_t>(tokens * width);
@@ -245,8 +243,8 @@ struct LossPlan {
 struct GradientPlan {
     int64_t padded, width, states_ld, words;   // rows and columns of whole tiles; words at a time
     int splits;
-    int* targets;
-    float *lse2, *ratio, *largest, *states;
+    int* known;
+    float *lse2, *largest, *states;
     uint16_t *slopes, *X, *scaled, *W;
     size_t bytes;
     GradientPlan(int64_t m, int64_t n, int64_t p, void* workspace)
@@ -262,9 +260,8 @@ struct GradientPlan {
         if (words < 256) words = 256;
         if (words > round_to(p, 256)) words = round_to(p, 256);
         splits = lmk::tile_splits(m, words, n);
-        targets = room.take<int>(padded);
+        known = room.take<int>(padded);
         lse2 = room.take<float>(padded);
-        ratio = room.take<float>(padded);
         largest = room.take<float>(1);
         slopes = room.take<uint16_t>(padded * words);
         states = room.take<float>(splits * padded * states_ld);
@@ -300,7 +297,7 @@ int ozimmu_lm_dequantize(int type, int64_t p, int64_t n, int group, int zeros, i
     CHECK(packed_status(packed, p, n, group, scale_type));
     if (p == 0 || n == 0) return OZIMMU_OK;
     const lmk::Weights w{Shape{p, n, group, zeros != 0}, scale_type, (const uint8_t*)packed};
-    return launched(lmk::launch_dequantize(type, w, 0, p, n, W, ldw, (hipStream_t)stream));
+    return launched(lmk::launch_dequantize(type, w, 0, p, n, W, ldw, true, (hipStream_t)stream));
 }
 
 static int plain_status(int64_t p, int64_t n, int group, const void* codes, int64_t ldc, const void* scales, int64_t lds, const void* zeros, int64_t ldz,
@@ -385,43 +382,36 @@ int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const voi
     if (m == 0) return OZIMMU_OK;
     const LossPlan plan(m, n, p, workspace);
     const hipStream_t st = (hipStream_t)stream;
-    const bool x_as_it_is = as_it_is(X, n, ldx), w_as_it_is = as_it_is(W, n, ldw);
+    // (one that is laid out has zeros up to `width`; where that is beyond n the other may not be read so far, so both are)
+    const bool x_as_it_is = as_it_is(X, n, ldx) && (n == plan.width || as_it_is(W, n, ldw));
+    const bool w_as_it_is = as_it_is(W, n, ldw) && (n == plan.width || as_it_is(X, n, ldx));
     for (int64_t t0 = 0; t0 < m; t0 += plan.tokens) {
-        const int64_t rows = m - t0 < plan.tokens ? m - t0 : plan.tokens;
+        const int64_t rows = m - t0 < plan.tokens ? m - t0 : plan.tokens, step = w_as_it_is ? p : plan.words;
+        const lmk::Targets targets{y + t0 * y_stride, y_stride, ignore, p};
+        const lmk::LayOut x{rows, n, (const uint16_t*)X + t0 * ldx, ldx, plan.X, plan.width};
         Tile t{lmk::LOSS, type};
         t.m = rows;
         t.n = x_as_it_is && w_as_it_is ? n : plan.width;
-        t.A = (const uint16_t*)X + t0 * ldx;
-        t.lda = ldx;
-        // (one that is laid out has zeros up to `width`; the other must not then be read beyond n, so both are)
-        if (t.n != n || !x_as_it_is) {
-            CHECK(launched(lmk::launch_lay_out(type, rows, n, t.A, ldx, nullptr, plan.X, plan.width, plan.width, st)));
-            t.A = plan.X;
-            t.lda = plan.width;
-        }
-        const bool lay_out = t.n != n || !w_as_it_is;
-        CHECK(launched(lmk::launch_targets(rows, round_to(rows, 256), p, y + t0 * y_stride, y_stride, ignore, plan.targets, st)));
-        t.targets = plan.targets;
+        t.A = x_as_it_is ? x.X : plan.X;
+        t.lda = x_as_it_is ? ldx : plan.width;
+        t.targets = targets;
         t.at_target = plan.at_target;
         t.parts_ld = plan.tokens;
-        const int64_t step = lay_out ? plan.words : p;
-        const int shape = lmk::tile_shape(rows, t.n, step, 1);
+        t.shape = lmk::tile_shape(rows, t.n, step < p ? step : p, 1);
+        const int64_t part = lmk::part_columns(t.shape);
         for (int64_t v0 = 0; v0 < p; v0 += step) {
             t.p = t.b_rows = p - v0 < step ? p - v0 : step;
-            t.B = (const uint16_t*)W + v0 * ldw;
-            t.ldb = ldw;
-            if (lay_out) {
-                CHECK(launched(lmk::launch_lay_out(type, t.p, n, t.B, ldw, nullptr, plan.W, plan.width, plan.width, st)));
-                t.B = plan.W;
-                t.ldb = plan.width;
-            }
+            const lmk::LayOut w{t.p, n, (const uint16_t*)W + v0 * ldw, ldw, plan.W, plan.width}, none{};
+            const bool lay_x = !x_as_it_is && v0 == 0;
+            if (lay_x || !w_as_it_is) CHECK(launched(lmk::launch_lay_out(type, lay_x ? x : none, w_as_it_is ? none : w, st)));
+            t.B = w_as_it_is ? w.X : plan.W;
+            t.ldb = w_as_it_is ? ldw : plan.width;
             t.column0 = (int)v0;
-            t.parts = plan.parts + v0 / lmk::part_columns(shape) * plan.tokens;
-            t.shape = shape;
+            t.parts = plan.parts + v0 / part * plan.tokens;
             if (!lmk::tile_fits(t)) return OZIMMU_ERR_DIM;
             CHECK(launched(lmk::launch_tile(t, st)));
         }
-        CHECK(launched(lmk::launch_join(rows, (p + lmk::part_columns(shape) - 1) / lmk::part_columns(shape), plan.parts, plan.tokens, plan.targets, plan.at_target, loss + t0, lse + t0, st)));
+        CHECK(launched(lmk::launch_join(rows, (p + part - 1) / part, plan.parts, plan.tokens, targets, plan.at_target, loss + t0, lse + t0, st)));
     }
     return OZIMMU_OK;
 }
@@ -453,23 +443,21 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
         return OZIMMU_OK;
     }
     const GradientPlan plan(m, n, p, workspace);
-    CHECK(launched(lmk::launch_slopes(m, plan.padded, p, y, y_stride, ignore, g, g_stride, lse, plan.targets, plan.lse2, plan.ratio, plan.largest, st)));
-    const bool x_as_it_is = as_it_is(X, n, ldx);
     // (W is read along its rows and across them, a piece of `words` rows at a time)
-    const bool w_as_it_is = as_it_is(W, n, ldw) && plan.words * ldw * 2 < ((int64_t)1 << 32) - (1 << 20);
-    const bool lay_out = !x_as_it_is || !w_as_it_is;
+    const bool lay_out = !as_it_is(X, n, ldx) || !as_it_is(W, n, ldw) || plan.words * ldw * 2 >= ((int64_t)1 << 32) - (1 << 20);
     const float unscale = type == OZIMMU_LM_F16 ? 1.0f / lmk::SLOPE_SCALE_F16 : 1.0f;
-    if (lay_out) CHECK(launched(lmk::launch_lay_out(type, m, n, X, ldx, nullptr, plan.X, plan.width, plan.width, st)));
-    if (dW) CHECK(launched(lmk::launch_lay_out(type, m, n, X, ldx, plan.ratio, plan.scaled, plan.width, plan.width, st)));
     int splits = 0;
     for (int64_t v0 = 0; v0 < p; v0 += plan.words) {
         const int64_t words = p - v0 < plan.words ? p - v0 : plan.words, whole = round_to(words, 256);
-        const uint16_t* W_at = (const uint16_t*)W + v0 * ldw;
-        int64_t ldw_at = ldw;
-        if (lay_out) {
-            CHECK(launched(lmk::launch_lay_out(type, words, n, W_at, ldw, nullptr, plan.W, plan.width, plan.width, st)));
-            W_at = plan.W;
-            ldw_at = plan.width;
+        const lmk::LayOut w{words, n, (const uint16_t*)W + v0 * ldw, ldw, lay_out ? plan.W : nullptr, plan.width};
+        const void* const W_at = lay_out ? (const void*)plan.W : w.X;
+        const int64_t ldw_at = lay_out ? plan.width : ldw;
+        if (v0 == 0) {
+            const lmk::LayOut x{m, n, X, ldx, lay_out ? plan.X : nullptr, plan.width};
+            CHECK(launched(lmk::launch_prepare(type, {m, plan.padded, {y, y_stride, ignore, p}, g, g_stride, lse, plan.known, plan.lse2, plan.largest, x,
+                                                      dW ? plan.scaled : nullptr, w}, st)));
+        } else if (lay_out) {
+            CHECK(launched(lmk::launch_lay_out(type, w, {}, st)));
         }
         Tile t{lmk::SLOPE, type};
         t.m = m;
@@ -481,7 +469,7 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
         t.ldb = ldw_at;
         t.D = plan.slopes;
         t.ldd = whole;
-        t.targets = plan.targets;
+        t.known = plan.known;
         t.column0 = (int)v0;
         t.lse2 = plan.lse2;
         if (!lmk::tile_fits(t)) return OZIMMU_ERR_DIM;
@@ -528,7 +516,7 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
         }
     }
     if (dX)
-        CHECK(launched(lmk::launch_states(dx_type, m, n, plan.states, plan.states_ld, splits, plan.padded * plan.states_ld, g, g_stride, plan.targets, unscale, dX,
+        CHECK(launched(lmk::launch_states(dx_type, m, n, plan.states, plan.states_ld, splits, plan.padded * plan.states_ld, g, g_stride, plan.known, unscale, dX,
                                           lddx, st)));
     return OZIMMU_OK;
 }

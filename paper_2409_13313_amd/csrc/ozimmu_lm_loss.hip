@@ -6,34 +6,66 @@ namespace {
 
 using namespace mxk;
 using lmk::BAD_TARGET;
+using lmk::LayOut;
 using lmk::NO_TARGET;
+using lmk::Prepare;
+using lmk::Targets;
 
 constexpr float LN2 = 0.693147180559945309f, LOG2E = 1.44269504088896341f;
 
-__device__ inline int target_of(int64_t y, int64_t words, int64_t ignore) { return y == ignore ? NO_TARGET : (y >= 0 && y < words ? (int)y : BAD_TARGET); }
-
-// 8 elements a thread; `width` is a multiple of 8 and Y's rows are 16-byte aligned
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_lay_out(int64_t rows, int64_t cols, const uint16_t* X, int64_t ldx, const float* ratio, uint16_t* Y, int64_t ldy,
-                                                 int64_t width)
+// Eight elements from `at` (a number of eights) of what is laid out; x: the eight, whose row is returned
+template <int TYPE> __device__ inline int64_t lay_out(const LayOut& o, int64_t at, uint16_t* x)
 {
-    const int64_t eights = width / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= rows * eights) return;
-    const int64_t row = at / eights, col = at % eights * 8;
-    uint16_t x[8];
-    load_row<TYPE, 8>(X + row * ldx + col, cols - col, x);
-    if (ratio) {
-        const float r = ratio[row];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = r == 0.0f ? 0 : from_float<TYPE>(r * to_float<TYPE>(x[e]));
-    }
-    __builtin_memcpy(Y + row * ldy + col, x, 16);
+    const int64_t eights = o.width / 8, row = at / eights, col = at % eights * 8;
+    load_row<TYPE, 8>((const uint16_t*)o.X + row * o.ldx + col, o.cols - col, x);
+    if (o.Y) __builtin_memcpy((uint16_t*)o.Y + at * 8, x, 16);
+    return row;
 }
 
-__global__ __launch_bounds__(256) void k_targets(int64_t rows, int64_t padded, int64_t words, const int64_t* y, int64_t stride, int64_t ignore, int* targets)
+template <int TYPE> __global__ __launch_bounds__(256) void k_lay_out(LayOut a, LayOut b)
 {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t < padded) targets[t] = t < rows ? target_of(y[t * stride], words, ignore) : NO_TARGET;
+    const int64_t of_a = a.rows * (a.width / 8), all = of_a + b.rows * (b.width / 8);
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
+        uint16_t x[8];
+        at < of_a ? lay_out<TYPE>(a, at, x) : lay_out<TYPE>(b, at - of_a, x);
+    }
+}
+
+// Every workgroup finds the largest |g| for itself, so that one launch does.  (With it in front, the slopes and each row's share of it lie in -1 .. 1, and
+// a g that is the same for all rows costs no rounding.)
+template <int TYPE> __global__ __launch_bounds__(256) void k_prepare(Prepare p)
+{
+    __shared__ float of_wave[4];
+    const int t = threadIdx.x;
+    const bool first = blockIdx.x == 0;
+    float most = 0.0f;
+    for (int64_t r = t; r < p.padded; r += 256) {
+        const int target = r < p.rows ? p.targets[r] : NO_TARGET;
+        if (target != NO_TARGET) most = fmaxf(most, fabsf(p.g[r * p.g_stride]));
+        if (first) {
+            p.known[r] = target;
+            p.lse2[r] = target == BAD_TARGET ? __builtin_nanf("") : (target == NO_TARGET ? 0.0f : p.lse[r] * LOG2E);
+        }
+    }
+    for (int far = 1; far < 64; far *= 2) most = fmaxf(most, __shfl_xor(most, far));
+    if ((t & 63) == 0) of_wave[t >> 6] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
+    if (first && t == 0) *p.largest = most;
+    const int64_t of_x = p.x.Y || p.scaled ? p.x.rows * (p.x.width / 8) : 0, all = of_x + (p.w.Y ? p.w.rows * (p.w.width / 8) : 0);
+    for (int64_t at = (int64_t)blockIdx.x * 256 + t; at < all; at += (int64_t)gridDim.x * 256) {
+        uint16_t x[8];
+        if (at >= of_x) {
+            lay_out<TYPE>(p.w, at - of_x, x);
+            continue;
+        }
+        const int64_t row = lay_out<TYPE>(p.x, at, x);
+        if (!p.scaled) continue;
+        const float own = p.targets[row] == NO_TARGET ? 0.0f : p.g[row * p.g_stride], ratio = own == 0.0f ? 0.0f : own / most;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = ratio == 0.0f ? 0 : from_float<TYPE>(ratio * to_float<TYPE>(x[e]));
+        __builtin_memcpy((uint16_t*)p.scaled + at * 8, x, 16);
+    }
 }
 
 // (m, s) stands for s 2^m; the sum of two of them.  A part of nothing is (-inf, 0).
@@ -45,7 +77,7 @@ __device__ inline float2 join(float2 a, float2 b)
 
 // 16 rows a workgroup, their parts shared by 64 threads each, joined in a fixed order.  The parts leave out the target's own exponential, so that
 // loss = log(1 + others / own) keeps its digits where the target has nearly all of the row.
-__global__ __launch_bounds__(1024) void k_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const int* targets, const float* at_target,
+__global__ __launch_bounds__(1024) void k_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, Targets targets, const float* at_target,
                                                float* loss, float* lse)
 {
     __shared__ float2 of_wave[16][16];
@@ -72,31 +104,6 @@ __global__ __launch_bounds__(1024) void k_join(int64_t rows, int64_t blocks, con
     } else {
         loss[row] = target == BAD_TARGET ? __builtin_nanf("") : 0.0f;
         lse[row] = LN2 * (sum.x + log2f(sum.y));
-    }
-}
-
-// One workgroup: the largest |g| is the same for all.  (With it in front, the slopes and each row's share of it lie in -1 .. 1, and a g that is
-// the same for all rows costs no rounding.)
-__global__ __launch_bounds__(1024) void k_slopes(int64_t rows, int64_t padded, int64_t words, const int64_t* y, int64_t stride, int64_t ignore, const float* g,
-                                                 int64_t g_stride, const float* lse, int* targets, float* lse2, float* ratio, float* largest)
-{
-    __shared__ float of_wave[16];
-    const int t = threadIdx.x;
-    float most = 0.0f;
-    for (int64_t r = t; r < padded; r += 1024) {
-        const int target = r < rows ? target_of(y[r * stride], words, ignore) : NO_TARGET;
-        targets[r] = target;
-        lse2[r] = target == BAD_TARGET ? __builtin_nanf("") : (target == NO_TARGET ? 0.0f : lse[r] * LOG2E);
-        if (target != NO_TARGET) most = fmaxf(most, fabsf(g[r * g_stride]));
-    }
-    for (int far = 1; far < 64; far *= 2) most = fmaxf(most, __shfl_xor(most, far));
-    if ((t & 63) == 0) of_wave[t >> 6] = most;
-    __syncthreads();
-    for (int w = 0; w < 16; ++w) most = fmaxf(most, of_wave[w]);
-    if (t == 0) *largest = most;
-    for (int64_t r = t; r < rows; r += 1024) {
-        const float own = g[r * g_stride];
-        ratio[r] = targets[r] == NO_TARGET || own == 0.0f ? 0.0f : own / most;
     }
 }
 
@@ -140,32 +147,33 @@ inline unsigned blocks_of(int64_t threads) { return (unsigned)((threads + 255) /
 
 namespace lmk {
 
-hipError_t launch_lay_out(int type, int64_t rows, int64_t cols, const void* X, int64_t ldx, const float* ratio, void* Y, int64_t ldy, int64_t width,
-                          hipStream_t st)
+// (workgroups for that many threads, some rounds of them for many)
+inline unsigned rounds_of(int64_t threads)
 {
-    const dim3 grid(blocks_of(rows * (width / 8)));
-    if (type == BF16) k_lay_out<BF16><<<grid, dim3(256), 0, st>>>(rows, cols, (const uint16_t*)X, ldx, ratio, (uint16_t*)Y, ldy, width);
-    if (type == F16) k_lay_out<F16><<<grid, dim3(256), 0, st>>>(rows, cols, (const uint16_t*)X, ldx, ratio, (uint16_t*)Y, ldy, width);
+    const int64_t blocks = (threads + 255) / 256;
+    return (unsigned)(blocks < 1 ? 1 : blocks < 4096 ? blocks : 4096);
+}
+
+hipError_t launch_lay_out(int type, const LayOut& a, const LayOut& b, hipStream_t st)
+{
+    const dim3 grid(rounds_of(a.rows * (a.width / 8) + b.rows * (b.width / 8)));
+    if (type == BF16) k_lay_out<BF16><<<grid, dim3(256), 0, st>>>(a, b);
+    if (type == F16) k_lay_out<F16><<<grid, dim3(256), 0, st>>>(a, b);
     return hipGetLastError();
 }
 
-hipError_t launch_targets(int64_t rows, int64_t padded, int64_t words, const int64_t* y, int64_t stride, int64_t ignore, int* targets, hipStream_t st)
+hipError_t launch_prepare(int type, const Prepare& p, hipStream_t st)
 {
-    k_targets<<<dim3(blocks_of(padded)), dim3(256), 0, st>>>(rows, padded, words, y, stride, ignore, targets);
+    const dim3 grid(rounds_of((p.x.Y || p.scaled ? p.x.rows * (p.x.width / 8) : 0) + (p.w.Y ? p.w.rows * (p.w.width / 8) : 0)));
+    if (type == BF16) k_prepare<BF16><<<grid, dim3(256), 0, st>>>(p);
+    if (type == F16) k_prepare<F16><<<grid, dim3(256), 0, st>>>(p);
     return hipGetLastError();
 }
 
-hipError_t launch_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const int* targets, const float* at_target, float* loss,
+hipError_t launch_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const Targets& targets, const float* at_target, float* loss,
                        float* lse, hipStream_t st)
 {
     k_join<<<dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, st>>>(rows, blocks, parts, parts_ld, targets, at_target, loss, lse);
-    return hipGetLastError();
-}
-
-hipError_t launch_slopes(int64_t rows, int64_t padded, int64_t words, const int64_t* y, int64_t stride, int64_t ignore, const float* g, int64_t g_stride,
-                         const float* lse, int* targets, float* lse2, float* ratio, float* largest, hipStream_t st)
-{
-    k_slopes<<<dim3(1), dim3(1024), 0, st>>>(rows, padded, words, y, stride, ignore, g, g_stride, lse, targets, lse2, ratio, largest);
     return hipGetLastError();
 }
 

@@ -64,7 +64,8 @@ struct Args {
     float alpha, beta;
     const float* alpha_at;
     int64_t split_stride;
-    const int* targets;
+    lmk::Targets targets;
+    const int* known;
     int column0;
     const float* lse2;
     float* at_target;
@@ -411,7 +412,11 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
             bool any = false;
             static_for<0, FA>([&](auto I) {
                 constexpr int i = decltype(I)::value;
-                target[i] = g.targets[row0 + row_of(i, 0)];
+                const int64_t row = row0 + row_of(i, 0);
+                if constexpr (KIND == lmk::LOSS)
+                    target[i] = row < g.m ? g.targets[row] : lmk::NO_TARGET;
+                else
+                    target[i] = g.known[row];
                 const int c = target[i] - g.column0 - (int)col0;
                 target[i] = target[i] < 0 ? target[i] : (c >= 0 && c < TILE_B / 2 ? c : TILE_B);
                 any |= target[i] >= 0 && target[i] < TILE_B;
@@ -543,7 +548,7 @@ hipError_t NAME(LM_TYPE)(const Tile& t, hipStream_t st)
 {
     const Args g = {t.m, t.n, t.p, t.b_rows, (uint64_t)(uintptr_t)t.A, (uint64_t)(uintptr_t)t.B, (uint32_t)(t.lda * 2), (uint32_t)(t.ldb * 2),
                     0, 0, (int)((t.n + STAGE_K - 1) / STAGE_K), t.splits, t.D, t.ldd, t.dtype,
-                    t.alpha, t.beta, t.alpha_at, t.split_stride, t.targets, t.column0, t.lse2, t.at_target, t.parts, t.parts_ld};
+                    t.alpha, t.beta, t.alpha_at, t.split_stride, t.targets, t.known, t.column0, t.lse2, t.at_target, t.parts, t.parts_ld};
     if (t.kind == LINEAR) run<LM_TYPE, LINEAR>(g, t.shape, st);
     if (t.kind == LOSS) run<LM_TYPE, LOSS>(g, t.shape, st);
     if (t.kind == SLOPE) run<LM_TYPE, SLOPE>(g, t.shape, st);

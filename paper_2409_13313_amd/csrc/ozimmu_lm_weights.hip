@@ -42,121 +42,205 @@ __device__ inline int code_at(uint32_t stored, int e) { return (int)(stored >> (
 
 __device__ inline float scale_float(int stype, uint16_t s) { return stype == BF16 ? to_float<BF16>(s) : to_float<F16>(s); }
 
-// The place of a wave: a block of 16 rows x 128 elements, of which lane l has row l % 16 and 8 elements at 32 j + 8 (l / 16), j < 4
-struct Place {
-    int64_t block, row, col;
-    int lane;
-    __device__ inline Place(const Shape& s, int64_t wave) : block(wave), lane(threadIdx.x & 63)
-    {
-        const int64_t kb = s.inner_blocks();
-        row = wave / kb * ROWS + (lane & 15);
-        col = wave % kb * INNER + (lane >> 4) * 8;
-    }
-    __device__ inline int64_t codes() const { return block * BLOCK_BYTES + lane * 16; }
-    __device__ inline int64_t scale(const Shape& s, int group) const { return (block * ROWS + (lane & 15)) * s.groups() + group; }  // number
+// A row's record, as much of it as a block has
+template <int GROUP> struct Record {
+    static constexpr int GROUPS = INNER / GROUP, WORDS = (GROUPS * 3 + 3) / 4;
+    uint32_t w[WORDS];
+    __device__ inline void load(const uint8_t* p) { __builtin_memcpy(w, p, sizeof(w)); }
+    __device__ inline uint16_t scale(int q) const { return (uint16_t)(w[q / 2] >> (q % 2 * 16)); }
+    __device__ inline uint32_t zero(int q) const { return w[(2 * GROUPS + q) / 4] >> ((2 * GROUPS + q) % 4 * 8) & 255u; }
 };
 
-__device__ inline float over_lanes_max(float v)
+// A workgroup of 256 threads takes a block of 16 rows x 128 elements, thread t the eight elements t % 16 of row t / 16: 16 lanes read or write 128
+// elements side by side, and a group lies in 4, 8 or 16 neighbouring lanes.
+constexpr int64_t BLOCKS_Y = 32768;  // (there may be more blocks of rows than a grid has in its second dimension)
+__device__ inline int64_t row_block() { return (int64_t)blockIdx.z * BLOCKS_Y + blockIdx.y; }
+inline dim3 grid_of(int64_t inner_blocks, int64_t row_blocks)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    return dim3((unsigned)inner_blocks, (unsigned)(row_blocks < BLOCKS_Y ? row_blocks : BLOCKS_Y), (unsigned)((row_blocks + BLOCKS_Y - 1) / BLOCKS_Y));
+}
+struct Place {
+    int64_t block, row, col;
+    int place, chunk;  // of the row in the block, of the eight in the row
+    __device__ inline Place(const Shape& s, int64_t row_block)
+    {
+        place = threadIdx.x >> 4;
+        chunk = threadIdx.x & 15;
+        block = row_block * s.inner_blocks() + blockIdx.x;
+        row = row_block * ROWS + place;
+        col = (int64_t)blockIdx.x * INNER + chunk * 8;
+    }
+    // where the word of the eight codes is, and the row's record
+    __device__ inline int64_t word() const { return block * BLOCK_BYTES + ((chunk & 3) * 16 + place) * 16 + (chunk >> 2) * 4; }
+    __device__ inline int64_t record(const Shape& s) const { return s.records_at() + (block * ROWS + place) * s.record(); }
+};
+
+// over neighbouring lanes: 4, 8 or 16 of them
+template <int LANES, class T, class F> __device__ inline T over_lanes(T v, F&& f)
+{
+    auto moved = [&](auto CTRL) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(CTRL)::value, 0xf, 0xf, false));
+    };
+    v = f(v, moved(std::integral_constant<int, 0xb1>{}));                            // lane ^ 1
+    v = f(v, moved(std::integral_constant<int, 0x4e>{}));                            // lane ^ 2
+    if constexpr (LANES >= 8) v = f(v, moved(std::integral_constant<int, 0x141>{}));   // the other four of eight
+    if constexpr (LANES >= 16) v = f(v, moved(std::integral_constant<int, 0x140>{}));  // the other eight of sixteen
+    return v;
 }
 
-// ---- quantisation: a wave a block, so that a group's elements are in four lanes ----
-template <int TYPE, int GROUP>
+// ---- quantisation ----
+
+// x / D, rounded once: with r the FP32 number nearest to 1 / D, q = x r and what q is short of, x - D q, exactly, q + (x - D q) r is the nearest
+// number to the quotient (Markstein 1990).  Below 2^-100, where x - D q may not be a normal number, by a division.
+template <int D> __device__ inline float over(float x)
+{
+    constexpr float r = 1.0f / D;
+    const float q = x * r;
+    float y = __builtin_fmaf(__builtin_fmaf(-(float)D, q, x), r, q);
+    if (__any(x < 0x1p-100f && x != 0.0f)) {
+        asm volatile("");  // (a branch, and not both)
+        y = x / (float)D;
+    }
+    return y;
+}
+
+// x / scale rounded to a whole number is x times the hardware's 1 / scale rounded, unless that lies so near to half way between two whole numbers that the
+// quotient, as an FP32 number, may round the other way: the two differ by at most 2^-22 of them (1 / scale by 2^-23, the quotient by 2^-24), below
+// 2^-17 up to 16, and what is beyond 16 becomes 0 or 15 in either form.  Where a lane has such a one the wave looks again: elements of 16 bits
+// are half way then (quotients of two numbers of 11 bits are 2^-14 off it or not at all, and x = scale / 2 is no rare number), and the even
+// neighbour is taken; those of 32 bits are divided.  The rounding is that of an addition to 1.5 x 2^23, whose last bits are the code then.
+template <int TYPE, int GROUP, bool ZEROS>
+__device__ inline void quantize_eight(const Shape& s, int stype, const typename Elem<TYPE>::Bits (&raw)[8], const Place& at, bool tail, uint8_t* out)
+{
+    constexpr int LANES = GROUP / 8;
+    constexpr float WHOLE = 12582912.0f, NEAR = 0.5f - 0x1p-17f;
+    const auto larger = [](auto a, auto b) { return a > b ? a : b; };
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = to_float<TYPE>(raw[e]);
+    // (magnitudes as whole numbers: NaN above infinity above all others)
+    const float amax = __uint_as_float(over_lanes<LANES>(f32_bits<TYPE>(max_magnitude<TYPE, 8>(raw)), larger));
+    const bool finite = amax < __builtin_inff();
+    float range, lo = 0.0f;
+    if constexpr (ZEROS) {
+        float hi = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            hi = fmaxf(hi, x[e]);
+            lo = fminf(lo, x[e]);
+        }
+        hi = over_lanes<LANES>(hi, larger);
+        lo = -over_lanes<LANES>(-lo, larger);
+        range = over<15>(hi - lo);
+    } else {
+        range = over<7>(amax);
+    }
+    uint16_t bits;  // (a range that the type cannot hold: its largest number)
+    if (stype == BF16) {
+        bits = from_float<BF16>(range);
+        if (bits == 0x7f80u) bits = 0x7f7fu;
+        if (!finite) bits = 0x7fc0u;
+    } else {
+        bits = from_float<F16>(range);
+        if (bits == 0x7c00u) bits = 0x7bffu;
+        if (!finite) bits = 0x7e00u;
+    }
+    const float scale = scale_float(stype, bits);
+    const bool some = scale > 0.0f;
+    // (it overflows, and more, for the smallest scales in BF16)
+    const float inverse = some ? __builtin_amdgcn_rcpf(scale) : 0.0f;
+    const auto short_of = [&](float v, float rounded) { return __builtin_fmaf(v, inverse, -rounded); };
+    float zero = 8.0f, near = 0.0f;
+    if constexpr (ZEROS) {
+        zero = __builtin_fmaf(-lo, inverse, WHOLE) - WHOLE;
+        near = fabsf(short_of(-lo, zero));
+    }
+    float q[8];  // the quotients rounded, + zero, + 1.5 x 2^23
+    const float base = WHOLE + (ZEROS ? __builtin_amdgcn_fmed3f(zero, 0.0f, 15.0f) : 8.0f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        q[e] = __builtin_fmaf(x[e], inverse, base);
+        near = fmaxf(near, fabsf(short_of(x[e], q[e] - base)));
+    }
+    const bool close = !(near < NEAR), by_division = !finite || (some && scale < 0x1p-120f) || (TYPE == F32 && close);
+    if (__any(by_division)) {
+        if constexpr (ZEROS) zero = some ? rintf(-lo / scale) : 0.0f;
+        zero = __builtin_amdgcn_fmed3f(zero, 0.0f, 15.0f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = WHOLE + zero + (some ? __builtin_amdgcn_fmed3f(rintf(x[e] / scale), -16.0f, 16.0f) : 0.0f);
+    } else if (TYPE != F32 && __any(close)) {
+        // (half way: to the even neighbour)
+        const auto even = [&](float v, float rounded) {
+            const float e = short_of(v, rounded), half = 0.5f * rounded;
+            return fabsf(e) >= NEAR && fabsf(e) <= 0.5f + 0x1p-17f && rintf(half) != half ? rounded + copysignf(1.0f, e) : rounded;
+        };
+        if constexpr (ZEROS) zero = even(-lo, zero);
+        zero = __builtin_amdgcn_fmed3f(zero, 0.0f, 15.0f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = WHOLE + zero + even(x[e], __builtin_amdgcn_fmed3f(q[e] - base, -32.0f, 32.0f));
+    }
+    if constexpr (ZEROS) zero = __builtin_amdgcn_fmed3f(zero, 0.0f, 15.0f);
+    uint32_t codes[2] = {0, 0};  // of even and of odd elements
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        uint32_t c = __float_as_uint(__builtin_amdgcn_fmed3f(q[e], WHOLE, WHOLE + 15.0f));
+        if (tail && at.col + e >= s.n) c = __float_as_uint(WHOLE);
+        codes[e % 2] += c << (e / 2 * 4);
+    }
+    constexpr uint32_t FOUR = 0x4b400000u * 0x1111u;
+    if (at.row >= s.p) return;
+    *(uint32_t*)(out + at.word()) = (codes[0] - FOUR) | (codes[1] - FOUR) << 16;
+    if (at.chunk % LANES == 0) {
+        if (tail && at.col >= s.n) bits = 0;
+        uint8_t* const record = out + at.record(s);
+        __builtin_memcpy(record + 2 * (at.chunk / LANES), &bits, 2);
+        if (ZEROS) record[2 * s.groups() + at.chunk / LANES] = (uint8_t)zero;
+    }
+}
+
+// A thread takes eight elements of each of two rows.
+template <int TYPE, int GROUP, bool ZEROS>
 __global__ __launch_bounds__(256) void k_lm_quantize(Shape s, int stype, const typename Elem<TYPE>::Bits* W, int64_t ldw, uint8_t* out)
 {
-    typedef typename Elem<TYPE>::Bits Bits;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (wave >= s.blocks()) return;
-    const Place at(s, wave);
-    const bool inside = at.row < s.p;
-    float x[4][8];
+    typename Elem<TYPE>::Bits raw[2][8];
+    const int64_t pair = row_block();
+    if (2 * pair >= s.row_blocks()) return;
+    const bool tail = blockIdx.x == gridDim.x - 1;
+    const Place at[2] = {Place(s, 2 * pair), Place(s, 2 * pair + 1)};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        Bits raw[8];
-        load_row<TYPE, 8>(W + at.row * ldw + at.col + 32 * j, inside ? s.n - at.col - 32 * j : 0, raw);
+    for (int i = 0; i < 2; ++i) load_row<TYPE, 8>(W + at[i].row * ldw + at[i].col, at[i].row < s.p ? (tail ? s.n - at[i].col : 8) : 0, raw[i]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[j][e] = to_float<TYPE>(raw[e]);
-    }
-    constexpr int STEPS = GROUP / 32, GROUPS = 4 / STEPS;
-    v4i codes;
-    uint16_t scales[GROUPS];
-    uint8_t zeros[GROUPS];
-#pragma unroll
-    for (int q = 0; q < GROUPS; ++q) {
-        float hi = 0.0f, lo = 0.0f;
-        bool finite = true;
-#pragma unroll
-        for (int j = q * STEPS; j < (q + 1) * STEPS; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                hi = fmaxf(hi, x[j][e]);
-                lo = fminf(lo, x[j][e]);
-                finite &= fabsf(x[j][e]) < __builtin_inff();
-            }
-        hi = over_lanes_max(hi);
-        lo = -over_lanes_max(-lo);
-        finite = over_lanes_max(finite ? 0.0f : 1.0f) == 0.0f;
-        const float range = s.zeros ? (hi - lo) / 15.0f : fmaxf(hi, -lo) / 7.0f;
-        // (a range that the type cannot hold: its largest number)
-        if (stype == BF16) {
-            scales[q] = from_float<BF16>(range);
-            if (scales[q] == 0x7f80u) scales[q] = 0x7f7fu;
-            if (!finite) scales[q] = 0x7fc0u;
-        } else {
-            scales[q] = from_float<F16>(range);
-            if (scales[q] == 0x7c00u) scales[q] = 0x7bffu;
-            if (!finite) scales[q] = 0x7e00u;
-        }
-        const float scale = scale_float(stype, scales[q]);
-        const bool some = scale > 0.0f;
-        const float zero = s.zeros ? (some ? fminf(fmaxf(rintf(-lo / scale), 0.0f), 15.0f) : 0.0f) : 8.0f;
-        zeros[q] = (uint8_t)zero;
-#pragma unroll
-        for (int j = q * STEPS; j < (q + 1) * STEPS; ++j) {
-            uint32_t w = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float c = some ? fminf(fmaxf(rintf(x[j][e] / scale) + zero, 0.0f), 15.0f) : zero;
-                w |= (uint32_t)(at.col + 32 * j + e < s.n ? (int)c : 0) << (e % 2 * 16 + e / 2 * 4);
-            }
-            codes[j] = (int)w;
-        }
-        if (at.col - (at.lane >> 4) * 8 + q * GROUP >= s.n) scales[q] = 0;
-    }
-    if (!inside) return;
-    *(v4i*)(out + at.codes()) = codes;
-    if (at.lane < 16) {
-#pragma unroll
-        for (int q = 0; q < GROUPS; ++q) {
-            ((uint16_t*)(out + s.scales_at()))[at.scale(s, q)] = scales[q];
-            if (s.zeros) (out + s.zeros_at())[at.scale(s, q)] = zeros[q];
-        }
-    }
+    for (int i = 0; i < 2; ++i) quantize_eight<TYPE, GROUP, ZEROS>(s, stype, raw[i], at[i], tail, out);
 }
 
 // ---- reading back ----
-template <int TYPE>
+// STREAM, where rows begin at multiples of 16 bytes: stores past the caches.
+template <int TYPE, int GROUP, bool STREAM>
 __global__ __launch_bounds__(256) void k_lm_dequantize(Weights w, int64_t row0, int64_t rows, int64_t cols, typename Elem<TYPE>::Bits* X, int64_t ldx)
 {
     typedef typename Elem<TYPE>::Bits Bits;
     const Shape& s = w.shape;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) + row0 / ROWS * s.inner_blocks();  // (row0: a multiple of 16)
-    if (wave >= (row0 + rows + ROWS - 1) / ROWS * s.inner_blocks()) return;
-    const Place at(s, wave);
-    if (at.row >= row0 + rows) return;
-    const v4i codes = *(const v4i*)(w.data + at.codes());
+    const Place at(s, row0 / ROWS + row_block());  // (row0: a multiple of 16)
+    const int64_t left = cols - at.col;
+    if (at.row >= row0 + rows || left <= 0) return;
+    const uint32_t codes = *(const uint32_t*)(w.data + at.word());
+    const uint8_t* const record = w.data + at.record(s);
+    const int g = at.chunk / (GROUP / 8);
+    uint16_t bits;
+    __builtin_memcpy(&bits, record + 2 * g, 2);
+    const int zero = s.zeros ? record[2 * s.groups() + g] : 8;
+    const float scale = scale_float(w.stype, bits);
+    Bits x[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int q = j * 32 / s.group;
-        const float scale = scale_float(w.stype, ((const uint16_t*)(w.data + s.scales_at()))[at.scale(s, q)]);
-        const int zero = s.zeros ? (w.data + s.zeros_at())[at.scale(s, q)] : 8;
-        Bits x[8];
+    for (int e = 0; e < 8; ++e) x[e] = at.col + e < s.n ? from_float<TYPE>((float)(code_at(codes, e) - zero) * scale) : 0;
+    Bits* const to = X + (at.row - row0) * ldx + at.col;
+    if (STREAM && left >= 8) {
+        v4i y[sizeof(x) / 16];
+        __builtin_memcpy(y, x, sizeof(x));
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            x[e] = at.col + 32 * j + e < s.n ? from_float<TYPE>((float)(code_at((uint32_t)codes[j], e) - zero) * scale) : 0;
-        store_row<TYPE, 8>(X + (at.row - row0) * ldx + at.col + 32 * j, cols - at.col - 32 * j, x);
+        for (int h = 0; h < (int)(sizeof(x) / 16); ++h) __builtin_nontemporal_store(y[h], (v4i*)to + h);
+    } else {
+        store_row<TYPE, 8>(to, left, x);
     }
 }
 
@@ -164,57 +248,53 @@ __global__ __launch_bounds__(256) void k_lm_dequantize(Weights w, int64_t row0, 
 __global__ __launch_bounds__(256) void k_lm_pack(Shape s, const uint8_t* codes, int64_t ldc, const uint16_t* scales, int64_t lds, const uint8_t* zeros,
                                                  int64_t ldz, uint8_t* out)
 {
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (wave >= s.blocks()) return;
-    const Place at(s, wave);
+    const Place at(s, row_block());
     if (at.row >= s.p) return;
-    v4i words;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t w = 0;
-        const int64_t col = at.col + 32 * j;
+    uint32_t w = 0;
+    const uint8_t* const from = codes + at.row * ldc + at.col / 2;
+    if (at.col + 8 <= s.n) {
+        __builtin_memcpy(&w, from, 4);
+    } else {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            if (col + 2 * b >= s.n) break;
-            uint32_t c = codes[at.row * ldc + col / 2 + b];
-            if (col + 2 * b + 1 >= s.n) c &= 15u;
-            w |= c << (8 * b);
+            if (at.col + 2 * b >= s.n) break;
+            w |= (at.col + 2 * b + 1 >= s.n ? from[b] & 15u : (uint32_t)from[b]) << (8 * b);
         }
-        words[j] = (int)stored_order(w);
     }
-    *(v4i*)(out + at.codes()) = words;
-    if (at.lane < 16) {
-        const int64_t first = (at.col - (at.lane >> 4) * 8) / s.group, all = (s.n + s.group - 1) / s.group;
-        for (int q = 0; q < s.groups(); ++q) {
-            const bool real = first + q < all;
-            ((uint16_t*)(out + s.scales_at()))[at.scale(s, q)] = real ? scales[at.row * lds + first + q] : 0;
-            if (s.zeros) (out + s.zeros_at())[at.scale(s, q)] = real ? zeros[at.row * ldz + first + q] & 15 : 0;
-        }
+    *(uint32_t*)(out + at.word()) = stored_order(w);
+    const int per = s.group / 8;
+    if (at.chunk % per == 0) {
+        const int64_t g = at.col / s.group;
+        const bool real = at.col < s.n;
+        const uint16_t scale = real ? scales[at.row * lds + g] : 0;
+        uint8_t* const record = out + at.record(s);
+        __builtin_memcpy(record + 2 * (at.chunk / per), &scale, 2);
+        if (s.zeros) record[2 * s.groups() + at.chunk / per] = real ? zeros[at.row * ldz + g] & 15 : 0;
     }
 }
 
 __global__ __launch_bounds__(256) void k_lm_unpack(Shape s, const uint8_t* in, uint8_t* codes, int64_t ldc, uint16_t* scales, int64_t lds, uint8_t* zeros,
                                                    int64_t ldz)
 {
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (wave >= s.blocks()) return;
-    const Place at(s, wave);
-    if (at.row >= s.p) return;
-    const v4i words = *(const v4i*)(in + at.codes());
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t w = plain_order((uint32_t)words[j]);
-        const int64_t col = at.col + 32 * j;
+    const Place at(s, row_block());
+    if (at.row >= s.p || at.col >= s.n) return;
+    const uint32_t w = plain_order(*(const uint32_t*)(in + at.word()));
+    uint8_t* const to = codes + at.row * ldc + at.col / 2;
+    if (at.col + 8 <= s.n) {
+        __builtin_memcpy(to, &w, 4);
+    } else {
 #pragma unroll
         for (int b = 0; b < 4; ++b)
-            if (col + 2 * b < s.n) codes[at.row * ldc + col / 2 + b] = (uint8_t)(w >> (8 * b));
+            if (at.col + 2 * b < s.n) to[b] = (uint8_t)(w >> (8 * b));
     }
-    if (at.lane < 16) {
-        const int64_t first = (at.col - (at.lane >> 4) * 8) / s.group, all = (s.n + s.group - 1) / s.group;
-        for (int q = 0; q < s.groups() && first + q < all; ++q) {
-            scales[at.row * lds + first + q] = ((const uint16_t*)(in + s.scales_at()))[at.scale(s, q)];
-            if (s.zeros) zeros[at.row * ldz + first + q] = (in + s.zeros_at())[at.scale(s, q)];
-        }
+    const int per = s.group / 8;
+    if (at.chunk % per == 0) {
+        const int64_t g = at.col / s.group;
+        const uint8_t* const record = in + at.record(s);
+        uint16_t scale;
+        __builtin_memcpy(&scale, record + 2 * (at.chunk / per), 2);
+        scales[at.row * lds + g] = scale;
+        if (s.zeros) zeros[at.row * ldz + g] = record[2 * s.groups() + at.chunk / per];
     }
 }
 
@@ -250,7 +330,7 @@ template <int XTYPE> __device__ inline v4i numbers(uint32_t w, float zero)
 }
 
 // FOUR: at most four rows, row i at place 4 i of the fragment, so that a lane's first sum is the one that counts
-template <int XTYPE, int GROUP, int MF, int PF, int WAVES, int BLOCKS, bool FOUR>
+template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR>
 __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
 {
     static_assert(!FOUR || MF == 1, "four rows are one fragment");
@@ -260,18 +340,18 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
     const Shape& s = w.shape;
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int64_t KB = s.inner_blocks(), last_rows = s.row_blocks() - 1;
+    const int KB = (int)s.inner_blocks();
+    const int64_t last_rows = s.row_blocks() - 1;
     const int64_t pb0 = (int64_t)blockIdx.x * PF, row0 = (int64_t)blockIdx.y * (16 * MF);
     const uint8_t* code_at[PF];
-    const uint8_t* scale_at[PF];
-    const uint8_t* zero_at[PF];
+    const uint8_t* record_at[PF];
+    const int record = s.record();
 #pragma unroll
     for (int f = 0; f < PF; ++f) {
         // (blocks of rows behind the last one: the last one again, not stored)
         const int64_t block = (pb0 + f < last_rows ? pb0 + f : last_rows) * KB;
         code_at[f] = w.data + block * BLOCK_BYTES + lane * 16;
-        scale_at[f] = w.data + s.scales_at() + (block * ROWS + (lane & 15)) * (GROUPS * 2);
-        zero_at[f] = w.data + s.zeros_at() + (block * ROWS + (lane & 15)) * GROUPS;
+        record_at[f] = w.data + s.records_at() + (block * ROWS + (lane & 15)) * record;
     }
     const Bits* x_at[MF];
 #pragma unroll
@@ -279,7 +359,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
         const int64_t row = row0 + 16 * i + (FOUR ? (lane & 15) >> 2 : lane & 15);
         x_at[i] = (const Bits*)g.X + (row < g.m ? row : g.m - 1) * g.ldx + (lane >> 4) * 8;
     }
-    const int64_t left = s.n - (lane >> 4) * 8;  // elements of a row from this lane's first on
+    const int left = (int)s.n - (lane >> 4) * 8;  // elements of a row from this lane's first on
 
     float acc[MF][PF][R];
 #pragma unroll
@@ -291,17 +371,21 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
 
     struct Stored {
         v4i code;
-        uint16_t scale[GROUPS];
-        uint8_t zero[GROUPS];
+        Record<GROUP> record;
     };
-    auto load = [&](int f, int64_t kb, Stored& o) __attribute__((always_inline)) {
-        o.code = *(const v4i*)(code_at[f] + kb * BLOCK_BYTES);
-        __builtin_memcpy(o.scale, __builtin_assume_aligned(scale_at[f] + kb * (ROWS * GROUPS * 2), 2 * GROUPS), sizeof(o.scale));
-        if (s.zeros)
-            __builtin_memcpy(o.zero, __builtin_assume_aligned(zero_at[f] + kb * (ROWS * GROUPS), GROUPS), sizeof(o.zero));
-        else
+    auto load = [&](int kb, Stored (&o)[PF], v4i (&x)[MF][4]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int q = 0; q < GROUPS; ++q) o.zero[q] = 8;
+        for (int f = 0; f < PF; ++f) {
+            o[f].code = *(const v4i*)(code_at[f] + (int64_t)kb * BLOCK_BYTES);
+            o[f].record.load(record_at[f] + (int64_t)kb * (ROWS * record));
+        }
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[i][j] = v4i{0, 0, 0, 0};
+                if (left - kb * INNER - 32 * j >= 8) __builtin_memcpy(&x[i][j], x_at[i] + kb * INNER + 32 * j, 16);
+            }
     };
     const v4i ones = {0x3f803f80, 0x3f803f80, 0x3f803f80, 0x3f803f80};
     auto multiply = [&](const Stored (&o)[PF], const v4i (&x)[MF][4]) __attribute__((always_inline)) {
@@ -317,7 +401,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
                 }
 #pragma unroll
             for (int f = 0; f < PF; ++f) {
-                const float scale = scale_float(w.stype, o[f].scale[q]), zero = (float)o[f].zero[q];
+                const float scale = scale_float(w.stype, o[f].record.scale(q)), zero = s.zeros ? (float)o[f].record.zero(q) : 8.0f;
                 v4f c[MF];
 #pragma unroll
                 for (int i = 0; i < MF; ++i) c[i] = v4f{0, 0, 0, 0};
@@ -338,43 +422,32 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
         });
     };
 
-    for (int64_t kb0 = wave; kb0 < KB; kb0 += WAVES * BLOCKS) {
-        Stored o[BLOCKS][PF];
-        v4i x[BLOCKS][MF][4];
-#pragma unroll
-        for (int u = 0; u < BLOCKS; ++u) {
-            // (a block behind the last one: the last one again, with zeros for X)
-            const int64_t kb = kb0 + u * WAVES, there = kb < KB ? kb : KB - 1;
-#pragma unroll
-            for (int f = 0; f < PF; ++f) load(f, there, o[u][f]);
-#pragma unroll
-            for (int i = 0; i < MF; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[u][i][j] = v4i{0, 0, 0, 0};
-                    if (kb < KB && left - kb * INNER - 32 * j >= 8) __builtin_memcpy(&x[u][i][j], x_at[i] + kb * INNER + 32 * j, 16);
-                }
+    // one block on its way while the other is multiplied
+    Stored o[2][PF];
+    v4i x[2][MF][4];
+    if (wave < KB) load(wave, o[0], x[0]);
+    for (int kb = wave; kb < KB; kb += 2 * WAVES) {
+        if (kb + WAVES < KB) load(kb + WAVES, o[1], x[1]);
+        multiply(o[0], x[0]);
+        if (kb + WAVES < KB) {
+            if (kb + 2 * WAVES < KB) load(kb + 2 * WAVES, o[0], x[0]);
+            multiply(o[1], x[1]);
         }
-#pragma unroll
-        for (int u = 0; u < BLOCKS; ++u) multiply(o[u], x[u]);
     }
     // the eight elements that a row ends in, where they are not whole: zeros for the others
-    if (s.n % 8 != 0 && wave == (int)((KB - 1) % WAVES)) {
-        Stored o[PF];
-        v4i x[MF][4];
-#pragma unroll
-        for (int f = 0; f < PF; ++f) load(f, KB - 1, o[f]);
+    if (s.n % 8 != 0 && wave == (KB - 1) % WAVES) {
+        load(KB - 1, o[0], x[0]);
 #pragma unroll
         for (int i = 0; i < MF; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int64_t here = left - (KB - 1) * INNER - 32 * j;
+                const int here = left - (KB - 1) * INNER - 32 * j;
                 Bits e[8];
 #pragma unroll
                 for (int n = 0; n < 8; ++n) e[n] = here < 8 && n < here ? x_at[i][(KB - 1) * INNER + 32 * j + n] : 0;
-                __builtin_memcpy(&x[i][j], e, 16);
+                __builtin_memcpy(&x[0][i][j], e, 16);
             }
-        multiply(o, x);
+        multiply(o[0], x[0]);
     }
 #pragma unroll
     for (int i = 0; i < MF; ++i)
@@ -408,27 +481,35 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
     }
 }
 
-template <int XTYPE, int GROUP, int MF, int PF, int WAVES, int BLOCKS, bool FOUR> void direct(const Linear& g, const Weights& w, hipStream_t st)
+template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR> void direct(const Linear& g, const Weights& w, hipStream_t st)
 {
     const dim3 grid((unsigned)((w.shape.row_blocks() + PF - 1) / PF), (unsigned)((g.m + 16 * MF - 1) / (16 * MF)));
-    k_lm_direct<XTYPE, GROUP, MF, PF, WAVES, BLOCKS, FOUR><<<grid, dim3(64 * WAVES), 0, st>>>(g, w);
+    k_lm_direct<XTYPE, GROUP, MF, PF, WAVES, FOUR><<<grid, dim3(64 * WAVES), 0, st>>>(g, w);
 }
 
 template <int XTYPE, int GROUP> void direct(const Linear& g, const Weights& w, hipStream_t st)
 {
     const int64_t units = w.shape.row_blocks();
     if (g.m <= 4) {
-        if (units <= COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 1, 16, 2, true>(g, w, st);
-        if (units <= 2 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 2, 16, 1, true>(g, w, st);
-        return direct<XTYPE, GROUP, 1, 4, 8, 1, true>(g, w, st);
+        if (units <= COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 1, 16, true>(g, w, st);
+        if (units <= 4 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 2, 16, true>(g, w, st);
+        if (units <= 16 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 2, 8, true>(g, w, st);
+        return direct<XTYPE, GROUP, 1, 4, 4, true>(g, w, st);
     }
     if (g.m <= 16) {
-        if (units <= COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 1, 8, 2, false>(g, w, st);
-        if (units <= 2 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 2, 8, 2, false>(g, w, st);
-        return direct<XTYPE, GROUP, 1, 4, 8, 1, false>(g, w, st);
+        if (units <= COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 1, 8, false>(g, w, st);
+        if (units < 4 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 2, 8, false>(g, w, st);
+        if (units <= 16 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 4, 8, false>(g, w, st);
+        return direct<XTYPE, GROUP, 1, 4, 4, false>(g, w, st);
     }
-    if (g.m <= 32) return direct<XTYPE, GROUP, 2, 2, 8, 1, false>(g, w, st);
-    return direct<XTYPE, GROUP, 4, 2, 8, 1, false>(g, w, st);
+    if (g.m <= 32) {
+        if (units < 2 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 2, 1, 8, false>(g, w, st);
+        return direct<XTYPE, GROUP, 2, 2, 8, false>(g, w, st);
+    }
+    const int64_t all = units * ((g.m + 63) / 64);
+    if (all < 2 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 4, 1, 8, false>(g, w, st);
+    if (all < 8 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 4, 2, 8, false>(g, w, st);
+    return direct<XTYPE, GROUP, 4, 4, 4, false>(g, w, st);
 }
 template <int XTYPE> void direct(const Linear& g, const Weights& w, hipStream_t st)
 {
@@ -437,15 +518,34 @@ template <int XTYPE> void direct(const Linear& g, const Weights& w, hipStream_t 
     if (w.shape.group == 128) direct<XTYPE, 128>(g, w, st);
 }
 
-inline unsigned four_waves_each(int64_t waves) { return (unsigned)((waves + 3) / 4); }
+inline dim3 grid_of(const Shape& s) { return grid_of(s.inner_blocks(), s.row_blocks()); }
 
+template <int TYPE, int GROUP> void quantize(const void* W, int64_t ldw, const Shape& s, int stype, void* packed, hipStream_t st)
+{
+    const dim3 grid = grid_of(s.inner_blocks(), (s.row_blocks() + 1) / 2);
+    const auto* w = (const typename Elem<TYPE>::Bits*)W;
+    s.zeros ? k_lm_quantize<TYPE, GROUP, true><<<grid, dim3(256), 0, st>>>(s, stype, w, ldw, (uint8_t*)packed)
+            : k_lm_quantize<TYPE, GROUP, false><<<grid, dim3(256), 0, st>>>(s, stype, w, ldw, (uint8_t*)packed);
+}
 template <int TYPE> void quantize(const void* W, int64_t ldw, const Shape& s, int stype, void* packed, hipStream_t st)
 {
-    const dim3 grid(four_waves_each(s.blocks()));
-    const auto* w = (const typename Elem<TYPE>::Bits*)W;
-    if (s.group == 32) k_lm_quantize<TYPE, 32><<<grid, dim3(256), 0, st>>>(s, stype, w, ldw, (uint8_t*)packed);
-    if (s.group == 64) k_lm_quantize<TYPE, 64><<<grid, dim3(256), 0, st>>>(s, stype, w, ldw, (uint8_t*)packed);
-    if (s.group == 128) k_lm_quantize<TYPE, 128><<<grid, dim3(256), 0, st>>>(s, stype, w, ldw, (uint8_t*)packed);
+    if (s.group == 32) quantize<TYPE, 32>(W, ldw, s, stype, packed, st);
+    if (s.group == 64) quantize<TYPE, 64>(W, ldw, s, stype, packed, st);
+    if (s.group == 128) quantize<TYPE, 128>(W, ldw, s, stype, packed, st);
+}
+
+template <int TYPE, int GROUP> void dequantize(const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, bool stream, hipStream_t st)
+{
+    const dim3 grid = grid_of((cols + INNER - 1) / INNER, (rows + ROWS - 1) / ROWS);
+    auto* const x = (typename Elem<TYPE>::Bits*)X;
+    stream && (uintptr_t)X % 16 == 0 && ldx * sizeof(*x) % 16 == 0 ? k_lm_dequantize<TYPE, GROUP, true><<<grid, dim3(256), 0, st>>>(w, row0, rows, cols, x, ldx)
+                                                                   : k_lm_dequantize<TYPE, GROUP, false><<<grid, dim3(256), 0, st>>>(w, row0, rows, cols, x, ldx);
+}
+template <int TYPE> void dequantize(const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, bool stream, hipStream_t st)
+{
+    if (w.shape.group == 32) dequantize<TYPE, 32>(w, row0, rows, cols, X, ldx, stream, st);
+    if (w.shape.group == 64) dequantize<TYPE, 64>(w, row0, rows, cols, X, ldx, stream, st);
+    if (w.shape.group == 128) dequantize<TYPE, 128>(w, row0, rows, cols, X, ldx, stream, st);
 }
 
 }  // namespace
@@ -460,26 +560,25 @@ hipError_t launch_quantize(int type, const void* W, int64_t ldw, const Shape& s,
     return hipGetLastError();
 }
 
-hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, hipStream_t st)
+hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, bool stream, hipStream_t st)
 {
-    const dim3 grid(four_waves_each(((row0 + rows + ROWS - 1) / ROWS - row0 / ROWS) * w.shape.inner_blocks()));
-    if (type == F32) k_lm_dequantize<F32><<<grid, dim3(256), 0, st>>>(w, row0, rows, cols, (uint32_t*)X, ldx);
-    if (type == BF16) k_lm_dequantize<BF16><<<grid, dim3(256), 0, st>>>(w, row0, rows, cols, (uint16_t*)X, ldx);
-    if (type == F16) k_lm_dequantize<F16><<<grid, dim3(256), 0, st>>>(w, row0, rows, cols, (uint16_t*)X, ldx);
+    if (type == F32) dequantize<F32>(w, row0, rows, cols, X, ldx, stream, st);
+    if (type == BF16) dequantize<BF16>(w, row0, rows, cols, X, ldx, stream, st);
+    if (type == F16) dequantize<F16>(w, row0, rows, cols, X, ldx, stream, st);
     return hipGetLastError();
 }
 
 hipError_t launch_pack(const Shape& s, const uint8_t* codes, int64_t ldc, const void* scales, int64_t lds, const uint8_t* zeros, int64_t ldz, void* packed,
                        hipStream_t st)
 {
-    k_lm_pack<<<dim3(four_waves_each(s.blocks())), dim3(256), 0, st>>>(s, codes, ldc, (const uint16_t*)scales, lds, zeros, ldz, (uint8_t*)packed);
+    k_lm_pack<<<grid_of(s), dim3(256), 0, st>>>(s, codes, ldc, (const uint16_t*)scales, lds, zeros, ldz, (uint8_t*)packed);
     return hipGetLastError();
 }
 
 hipError_t launch_unpack(const Shape& s, const void* packed, uint8_t* codes, int64_t ldc, void* scales, int64_t lds, uint8_t* zeros, int64_t ldz,
                          hipStream_t st)
 {
-    k_lm_unpack<<<dim3(four_waves_each(s.blocks())), dim3(256), 0, st>>>(s, (const uint8_t*)packed, codes, ldc, (uint16_t*)scales, lds, zeros, ldz);
+    k_lm_unpack<<<grid_of(s), dim3(256), 0, st>>>(s, (const uint8_t*)packed, codes, ldc, (uint16_t*)scales, lds, zeros, ldz);
     return hipGetLastError();
 }
 
