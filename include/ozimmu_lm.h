@@ -72,7 +72,8 @@ int ozimmu_lm_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, co
  * way needs; and that choice.  Debug / test helpers; the last two are host, pure. */
 enum { OZIMMU_LM_WAY_AUTO = -1,
        OZIMMU_LM_WAY_DIRECT = 0,   /* from the stored codes into registers */
-       OZIMMU_LM_WAY_TILE = 1 };   /* weights read back, 256 x 256 outputs a workgroup at a time */
+       OZIMMU_LM_WAY_TILE = 1,     /* weights read back, tiles of 128 x 128 to 256 x 256 outputs a workgroup at a time */
+       OZIMMU_LM_WAY_SHARED = 2 }; /* from the stored codes, rows of X shared in LDS, the inner dimension split where outputs are few */
 int ozimmu_lm_linear_way(int way, int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void *X, int64_t ldx, int group, int zeros,
                          int scale_type, const void *W, float beta, int dtype, void *D, int64_t ldd, void *workspace, size_t workspace_bytes,
                          void *stream);

@@ -63,6 +63,12 @@ struct Linear {
     float alpha, beta;
 };
 hipError_t launch_direct(const Linear& l, const Weights& w, hipStream_t st);
+// The same with X in LDS: rows (32, 64) x columns (128, 256) a workgroup, the inner dimension in `splits` parts, whose sums meet in `parts`
+// (splits > 1: that many matrices of whole workgroups in FP32)
+struct SharedPlan {
+    int rows, columns, splits;
+};
+hipError_t launch_shared(const Linear& l, const Weights& w, const SharedPlan& plan, float* parts, hipStream_t st);
 
 // ---- products of 16-bit matrices in tiles of 256 x 256 (ozimmu_lm_tile.hip) ----
 
@@ -113,6 +119,7 @@ struct Tile {
 };
 bool tile_fits(const Tile& t);
 int tile_shape(int64_t m, int64_t n, int64_t p, int splits);   // the one that takes the least time, by an estimate
+double tile_us(int64_t m, int64_t n, int64_t p);                // that estimate
 int tile_splits(int64_t m, int64_t n, int64_t p);             // STATES: the number of splits that does
 inline int part_columns(int shape) { return shape == TILE_128 ? 64 : 128; }  // LOSS: columns of a part
 hipError_t launch_tile(const Tile& t, hipStream_t st);

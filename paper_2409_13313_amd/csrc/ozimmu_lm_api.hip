@@ -50,6 +50,12 @@ int tile_shape(int64_t m, int64_t n, int64_t p, int splits)
     return best;
 }
 
+double tile_us(int64_t m, int64_t n, int64_t p)
+{
+    const int shape = tile_shape(m, n, p, 1);
+    return estimate_us(shape, tiles_of(shape, m, p), (double)((n + 63) / 64));
+}
+
 // The number of splits of n, four stages each at the least, that takes the least time; the sums of each are written and read again in FP32
 int tile_splits(int64_t m, int64_t n, int64_t p)
 {
@@ -162,11 +168,35 @@ struct LinearPlan {
     }
 };
 
+// Two workgroups for every compute unit where the sizes give as many, by splits of four blocks of the inner dimension at the least (4096 x 4096, rows:
+// splits and us  32: 4 12.3, 8 11.4, 16 13.8;  128: 2 19.4, 4 18.2;  512, of 64 rows a workgroup: 1 41, 2 34.3, 3 34.4;  1024: 1 53.5, 2 60).  32 rows a
+// workgroup up to 128 (64 rows 13.6 and 15.7 us, 256 25.1 and 25.2, 512 35.6 and 34.3); 256 columns from 1024 workgroups on (2048 rows 90 and 102 us,
+// 1024 rows 54 and 68).
+lmk::SharedPlan shared_plan(int64_t m, int64_t n, int64_t p)
+{
+    const int rows = m <= 128 ? 32 : 64;
+    const int64_t row_blocks = (m + rows - 1) / rows, most = (n + 511) / 512;
+    const int columns = row_blocks * ((p + 127) / 128) >= 4 * lmk::COMPUTE_UNITS ? 256 : 128;
+    const int64_t splits = 2 * lmk::COMPUTE_UNITS / (row_blocks * ((p + columns - 1) / columns));
+    return {rows, columns, (int)(splits < 2 ? 1 : splits < most ? splits : most)};
+}
+size_t shared_bytes(int64_t m, int64_t n, int64_t p)
+{
+    const lmk::SharedPlan plan = shared_plan(m, n, p);
+    return plan.splits < 2 ? 0 : (size_t)round_to(plan.splits * round_to(m, plan.rows) * round_to(p, plan.columns) * 4, 256);
+}
+
+// Up to 16 rows from the codes in one launch, in any case (callers need not ask for a workspace then), and more of them where there is little to do (128
+// rows through 512 x 512: 5.6 us, with X in LDS 6.9; 37 rows through 2051 x 1283: 9.4, 11.1; 32 rows through 4096 x 4096: 11.5 and 11.4; 256 rows: 38 and 25).  Beyond, estimates
+// fitted to (rows x n x p: X in LDS, weights read back)  256 x 1024 x 16384: 22, 38;  512 x 4096 x 4096: 34, 52;  1024 x 4096 x 4096: 53, 53;  2048 x 4096 x
+// 4096: 90, 75;  4096 x 4096 x 16384: 630, 460.
+constexpr int64_t DIRECT_ROWS = 16;
 int choose(int64_t m, int64_t n, int64_t p)
 {
-    (void)n;
-    (void)p;
-    return m <= 128 ? OZIMMU_LM_WAY_DIRECT : OZIMMU_LM_WAY_TILE;
+    const double weights = (double)p * (double)n;
+    if (m <= DIRECT_ROWS || (m <= 128 && (double)m * weights < 1 << 27)) return OZIMMU_LM_WAY_DIRECT;
+    const double shared = 8 + 2.4e-6 * (double)round_to(m, 64) * weights * 1e-3, tile = 3 + weights / 1.8e6 + lmk::tile_us(m, n, p);
+    return shared <= tile ? OZIMMU_LM_WAY_SHARED : OZIMMU_LM_WAY_TILE;
 }
 
 int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void* X, int64_t ldx, const lmk::Weights& w, float beta, int dtype, void* D,
@@ -333,7 +363,9 @@ size_t ozimmu_lm_linear_way_workspace_bytes(int way, int64_t m, int64_t n, int64
 {
     if (!sizes_ok(p, n) || !rows_ok(m)) return 0;
     if (way == OZIMMU_LM_WAY_AUTO) way = choose(m, n, p);
-    return way == OZIMMU_LM_WAY_TILE && m > 0 && n > 0 && p > 0 ? LinearPlan(m, n, p, nullptr).bytes : 0;
+    if (m == 0 || n == 0 || p == 0) return 0;
+    if (way == OZIMMU_LM_WAY_SHARED) return shared_bytes(m, n, p);
+    return way == OZIMMU_LM_WAY_TILE ? LinearPlan(m, n, p, nullptr).bytes : 0;
 }
 size_t ozimmu_lm_linear_workspace_bytes(int64_t m, int64_t n, int64_t p) { return ozimmu_lm_linear_way_workspace_bytes(OZIMMU_LM_WAY_AUTO, m, n, p); }
 
@@ -353,14 +385,16 @@ int ozimmu_lm_linear_way(int way, int64_t m, int64_t n, int64_t p, float alpha, 
     CHECK(matrix_status(xtype, X, m, n, ldx));
     CHECK(matrix_status(dtype, D, m, p, ldd));
     if (way == OZIMMU_LM_WAY_AUTO) way = choose(m, n, p);
-    if (way != OZIMMU_LM_WAY_DIRECT && way != OZIMMU_LM_WAY_TILE) return OZIMMU_ERR_WAY;
+    if (way != OZIMMU_LM_WAY_DIRECT && way != OZIMMU_LM_WAY_TILE && way != OZIMMU_LM_WAY_SHARED) return OZIMMU_ERR_WAY;
     CHECK(packed_status(W, p, n, group, scale_type));
     if (m == 0 || p == 0) return OZIMMU_OK;
     CHECK(workspace_status(workspace, workspace_bytes, ozimmu_lm_linear_way_workspace_bytes(way, m, n, p)));
     const lmk::Weights w{Shape{p, n, group, zeros != 0}, scale_type, (const uint8_t*)W};
     const hipStream_t st = (hipStream_t)stream;
     if (way == OZIMMU_LM_WAY_TILE) return linear_tile(m, n, p, alpha, xtype, X, ldx, w, beta, dtype, D, ldd, workspace, st);
-    return launched(lmk::launch_direct({m, X, ldx, xtype, D, ldd, dtype, alpha, beta}, w, st));
+    const lmk::Linear l{m, X, ldx, xtype, D, ldd, dtype, alpha, beta};
+    if (way == OZIMMU_LM_WAY_SHARED) return launched(lmk::launch_shared(l, w, shared_plan(m, n, p), (float*)workspace, st));
+    return launched(lmk::launch_direct(l, w, st));
 }
 
 size_t ozimmu_lm_cross_entropy_workspace_bytes(int64_t m, int64_t n, int64_t p)

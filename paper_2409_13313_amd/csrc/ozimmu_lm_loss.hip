@@ -84,7 +84,20 @@ __global__ __launch_bounds__(1024) void k_join(int64_t rows, int64_t blocks, con
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int64_t row = (int64_t)blockIdx.x * 16 + (lane & 15);  // (parts have rows of whole tiles)
     float2 sum = make_float2(-__builtin_inff(), 0.0f);
-    for (int64_t b = t >> 4; b < blocks; b += 64) sum = join(sum, parts[b * parts_ld + row]);
+    // (eight loads on their way at a time: one after the other, they are what one token's join takes)
+    for (int64_t b = t >> 4; b < blocks; b += 64 * 8) {
+        float2 part[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) part[u] = b + 64 * u < blocks ? parts[(b + 64 * u) * parts_ld + row] : make_float2(-__builtin_inff(), 0.0f);
+        float most = sum.x;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) most = fmaxf(most, part[u].x);
+        const float base = most == -__builtin_inff() ? 0.0f : most;
+        float s = sum.y * exp2f(sum.x - base);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += part[u].y * exp2f(part[u].x - base);
+        sum = make_float2(most, s);
+    }
     for (int far = 16; far < 64; far *= 2) {
         const float2 other = make_float2(__shfl_xor(sum.x, far), __shfl_xor(sum.y, far));
         sum = lane & far ? join(other, sum) : join(sum, other);

@@ -314,17 +314,15 @@ template <int XTYPE> __device__ inline v4f mfma(v4i x, v4i w, v4f c)
 
 template <int XTYPE> __device__ inline v4i numbers(uint32_t w, float zero)
 {
+    // (in a vector register: an instruction takes one scalar operand, and the mask is one)
+    uint32_t one = XTYPE == BF16 ? 0x43004300u : 0x64006400u;
+    asm("" : "+v"(one));
+    const _Float16 off = (_Float16)(-1024.0f - zero);
     v4i r;
-    if constexpr (XTYPE == BF16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = (int)((w >> (4 * i) & 0x000f000fu) | 0x43004300u);
-    } else {
-        const _Float16 off = (_Float16)(-1024.0f - zero);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const v2h v = __builtin_bit_cast(v2h, (w >> (4 * i) & 0x000f000fu) | 0x64006400u) + v2h{off, off};
-            r[i] = __builtin_bit_cast(int, v);
-        }
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t v = (w >> (4 * i) & 0x000f000fu) | one;
+        r[i] = XTYPE == BF16 ? (int)v : __builtin_bit_cast(int, __builtin_bit_cast(v2h, v) + v2h{off, off});
     }
     return r;
 }
@@ -481,6 +479,244 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
     }
 }
 
+// ---- the same for more rows: X goes through LDS, 16 MF rows of it and 64 PF columns of the result by a workgroup ----
+//
+// Four waves take 16 PF columns each and share blocks of 16 MF rows x 128 of X, which come through registers (so that rows may begin anywhere)
+// into two places in LDS: while one block is multiplied the next is on its way, and the codes as well.  In LDS the 16-byte pieces of a
+// fragment's 16 rows are exchanged by their number in the row, so that neither the writes, of a row's 16 pieces, nor the reads, of a piece
+// of 16 rows, fall on the same banks.  What a workgroup reads of X serves 64 PF columns (k_lm_direct: 16 PF), so for few rows the inner
+// dimension is split over workgroups, whose sums meet in a second launch.
+struct Shared {
+    Linear g;
+    Weights w;
+    int splits;
+    float* parts;        // splits > 1: [split][row][column] of whole workgroups
+    int64_t parts_ld, parts_stride;
+};
+
+// the sum of eight elements in BF16
+__device__ inline float sum_of(v4i x)
+{
+    float even = 0.0f, odd = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        even += __uint_as_float((uint32_t)x[i] << 16);
+        odd += __uint_as_float((uint32_t)x[i] & 0xffff0000u);
+    }
+    return even + odd;
+}
+
+template <int XTYPE, int GROUP, int MF, int PF> __global__ __launch_bounds__(256, MF * PF > 8 ? 2 : 3) void k_lm_shared(Shared a)
+{
+    typedef typename Elem<XTYPE>::Bits Bits;
+    constexpr int STEPS = GROUP / 32, GROUPS = 4 / STEPS, ROWS_X = 16 * MF;
+    constexpr bool SUMS = XTYPE == BF16;
+    __shared__ __align__(16) uint8_t held[2][MF * 4096];
+    __shared__ __align__(16) float sums[2][SUMS ? GROUPS : 1][ROWS_X];
+    const Linear& g = a.g;
+    const Weights& w = a.w;
+    const Shape& s = w.shape;
+    const int t = threadIdx.x, lane = t & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int KB = (int)s.inner_blocks(), k0 = (int)((int64_t)KB * blockIdx.z / a.splits), k1 = (int)((int64_t)KB * (blockIdx.z + 1) / a.splits);
+    const int64_t last_rows = s.row_blocks() - 1, pb0 = (int64_t)blockIdx.x * (4 * PF) + wave * PF, row0 = (int64_t)blockIdx.y * ROWS_X;
+    const uint8_t* code_at[PF];
+    const uint8_t* record_at[PF];
+    const int record = s.record();
+#pragma unroll
+    for (int f = 0; f < PF; ++f) {
+        // (blocks of rows behind the last one: the last one again, not stored)
+        const int64_t block = (pb0 + f < last_rows ? pb0 + f : last_rows) * KB;
+        code_at[f] = w.data + block * BLOCK_BYTES + lane * 16;
+        record_at[f] = w.data + s.records_at() + (block * ROWS + (lane & 15)) * record;
+    }
+    // X: thread t has piece t % 16 of rows t / 16 + 16 i
+    const int piece = t & 15, x_row = t >> 4;
+    const Bits* x_at[MF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+        const int64_t row = row0 + 16 * i + x_row;
+        x_at[i] = (const Bits*)g.X + (row < g.m ? row : g.m - 1) * g.ldx + piece * 8;
+    }
+    const int left = (int)s.n - piece * 8, to = (piece >> 2) * 1024 + (piece & 3) * 256 + ((x_row ^ piece) << 4);
+
+    struct Stored {
+        v4i code;
+        Record<GROUP> record;
+    };
+    Stored o[2][PF];
+    v4i x[MF];
+    auto load = [&](int kb, Stored (&o)[PF]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int f = 0; f < PF; ++f) {
+            o[f].code = *(const v4i*)(code_at[f] + (int64_t)kb * BLOCK_BYTES);
+            o[f].record.load(record_at[f] + (int64_t)kb * (ROWS * record));
+        }
+    };
+    auto load_x = [&](int kb) __attribute__((always_inline)) {
+        const int here = left - kb * INNER;
+        if (here >= 8) {
+#pragma unroll
+            for (int i = 0; i < MF; ++i) __builtin_memcpy(&x[i], x_at[i] + kb * INNER, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                Bits e[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) e[n] = n < here ? x_at[i][kb * INNER + n] : 0;
+                __builtin_memcpy(&x[i], e, 16);
+            }
+        }
+    };
+    auto hold = [&](int place) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            *(v4i*)(held[place] + i * 4096 + to) = x[i];
+            if constexpr (SUMS) {
+                const float sum = over_lanes<GROUP / 8>(sum_of(x[i]), [](float p, float q) { return p + q; });
+                if (piece % (GROUP / 8) == 0) sums[place][piece / (GROUP / 8)][16 * i + x_row] = sum;
+            }
+        }
+    };
+
+    float acc[MF][PF][4];
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int f = 0; f < PF; ++f)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][f][r] = 0.0f;
+    const int q = lane >> 4, place_x = lane & 15;
+    auto multiply = [&](int place, const Stored (&o)[PF]) __attribute__((always_inline)) {
+        static_for<0, GROUPS>([&](auto Q) __attribute__((always_inline)) {
+            constexpr int n = decltype(Q)::value;
+            v4f c[MF][PF];
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int f = 0; f < PF; ++f) c[i][f] = v4f{0, 0, 0, 0};
+#pragma unroll
+            for (int j = n * STEPS; j < (n + 1) * STEPS; ++j) {
+                v4i xf[MF];
+#pragma unroll
+                for (int i = 0; i < MF; ++i) xf[i] = *(const v4i*)(held[place] + i * 4096 + j * 1024 + q * 256 + ((place_x ^ (4 * j + q)) << 4));
+#pragma unroll
+                for (int f = 0; f < PF; ++f) {
+                    const v4i b = numbers<XTYPE>((uint32_t)o[f].code[j], s.zeros ? (float)o[f].record.zero(n) : 8.0f);
+#pragma unroll
+                    for (int i = 0; i < MF; ++i) c[i][f] = mfma<XTYPE>(xf[i], b, c[i][f]);
+                }
+                __builtin_amdgcn_sched_barrier(0);  // (fetched one step ahead of all, X would fill the registers)
+            }
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                v4f xs = {0, 0, 0, 0};
+                if constexpr (SUMS) xs = *(const v4f*)&sums[place][n][16 * i + 4 * q];
+#pragma unroll
+                for (int f = 0; f < PF; ++f) {
+                    const float scale = scale_float(w.stype, o[f].record.scale(n)), zero = s.zeros ? (float)o[f].record.zero(n) : 8.0f;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[i][f][r] = __builtin_fmaf(scale, SUMS ? __builtin_fmaf(-128.0f - zero, xs[r], c[i][f][r]) : c[i][f][r], acc[i][f][r]);
+                }
+            }
+            // (added here and now: put off, the sums of all groups would fill the registers)
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int f = 0; f < PF; ++f)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) asm volatile("" : "+v"(acc[i][f][r]));
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+
+    if (k0 < k1) {
+        load(k0, o[0]);
+        load_x(k0);
+        hold(0);
+    }
+    __syncthreads();
+    auto step = [&](int kb, auto PLACE) __attribute__((always_inline)) {
+        constexpr int place = decltype(PLACE)::value;
+        const bool more = kb + 1 < k1;
+        if (more) {
+            load(kb + 1, o[1 - place]);
+            load_x(kb + 1);
+        }
+        multiply(place, o[place]);
+        if (more) hold(1 - place);
+        __syncthreads();
+    };
+    for (int kb = k0; kb < k1; kb += 2) {
+        step(kb, std::integral_constant<int, 0>{});
+        if (kb + 1 < k1) step(kb + 1, std::integral_constant<int, 1>{});
+    }
+
+    // lane l: column l % 16 of fragment f, rows 4 (l / 16) + r of fragment i
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int f = 0; f < PF; ++f)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t row = row0 + 16 * i + 4 * q + r, col = (pb0 + f) * ROWS + place_x;
+                const float v = acc[i][f][r];
+                if (a.splits > 1) {
+                    a.parts[(int64_t)blockIdx.z * a.parts_stride + row * a.parts_ld + col] = v;
+                    continue;
+                }
+                if (row >= g.m || col >= s.p) continue;
+                auto out = [&](auto D) {
+                    constexpr int DTYPE = decltype(D)::value;
+                    auto* const d = (typename Elem<DTYPE>::Bits*)g.D + row * g.ldd + col;
+                    *d = from_float<DTYPE>(g.beta != 0.0f ? g.alpha * v + g.beta * to_float<DTYPE>(*d) : g.alpha * v);
+                };
+                if (g.dtype == F32) out(std::integral_constant<int, F32>{});
+                if (g.dtype == BF16) out(std::integral_constant<int, BF16>{});
+                if (g.dtype == F16) out(std::integral_constant<int, F16>{});
+            }
+}
+
+// The sums of the splits, in their order
+template <int DTYPE> __global__ __launch_bounds__(256) void k_lm_meet(Shared a)
+{
+    typedef typename Elem<DTYPE>::Bits Bits;
+    const Linear& g = a.g;
+    const int64_t p = a.w.shape.p, fours = (p + 3) / 4;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < g.m * fours; at += (int64_t)gridDim.x * 256) {
+        const int64_t row = at / fours, col = at % fours * 4;
+        const float* const from = a.parts + row * a.parts_ld + col;
+        v4f v = *(const v4f*)from;
+        for (int s = 1; s < a.splits; ++s) v += *(const v4f*)(from + s * a.parts_stride);
+        Bits* const d = (Bits*)g.D + row * g.ldd + col;
+        Bits y[4];
+        if (g.beta != 0.0f) load_row<DTYPE, 4>(d, p - col, y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = from_float<DTYPE>(g.beta != 0.0f ? g.alpha * v[e] + g.beta * to_float<DTYPE>(y[e]) : g.alpha * v[e]);
+        store_row<DTYPE, 4>(d, p - col, y);
+    }
+}
+
+template <int XTYPE, int GROUP, int MF, int PF> void shared(const Shared& a, hipStream_t st)
+{
+    const dim3 grid((unsigned)((a.w.shape.row_blocks() + 4 * PF - 1) / (4 * PF)), (unsigned)((a.g.m + 16 * MF - 1) / (16 * MF)), (unsigned)a.splits);
+    k_lm_shared<XTYPE, GROUP, MF, PF><<<grid, dim3(256), 0, st>>>(a);
+}
+template <int XTYPE, int GROUP> void shared(const Shared& a, const lmk::SharedPlan& plan, hipStream_t st)
+{
+    if (plan.rows == 32 && plan.columns == 128) shared<XTYPE, GROUP, 2, 2>(a, st);
+    if (plan.rows == 32 && plan.columns == 256) shared<XTYPE, GROUP, 2, 4>(a, st);
+    if (plan.rows == 64 && plan.columns == 128) shared<XTYPE, GROUP, 4, 2>(a, st);
+    if (plan.rows == 64 && plan.columns == 256) shared<XTYPE, GROUP, 4, 4>(a, st);
+}
+template <int XTYPE> void shared(const Shared& a, const lmk::SharedPlan& plan, hipStream_t st)
+{
+    if (a.w.shape.group == 32) shared<XTYPE, 32>(a, plan, st);
+    if (a.w.shape.group == 64) shared<XTYPE, 64>(a, plan, st);
+    if (a.w.shape.group == 128) shared<XTYPE, 128>(a, plan, st);
+}
+
 template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR> void direct(const Linear& g, const Weights& w, hipStream_t st)
 {
     const dim3 grid((unsigned)((w.shape.row_blocks() + PF - 1) / PF), (unsigned)((g.m + 16 * MF - 1) / (16 * MF)));
@@ -579,6 +815,22 @@ hipError_t launch_unpack(const Shape& s, const void* packed, uint8_t* codes, int
                          hipStream_t st)
 {
     k_lm_unpack<<<grid_of(s), dim3(256), 0, st>>>(s, (const uint8_t*)packed, codes, ldc, (uint16_t*)scales, lds, zeros, ldz);
+    return hipGetLastError();
+}
+
+hipError_t launch_shared(const Linear& l, const Weights& w, const SharedPlan& plan, float* parts, hipStream_t st)
+{
+    const int64_t rows = (l.m + plan.rows - 1) / plan.rows * plan.rows, columns = (w.shape.p + plan.columns - 1) / plan.columns * plan.columns;
+    const Shared a{l, w, plan.splits, parts, columns, rows * columns};
+    if (l.xtype == BF16) shared<BF16>(a, plan, st);
+    if (l.xtype == F16) shared<F16>(a, plan, st);
+    if (plan.splits > 1) {
+        const int64_t blocks = (l.m * ((w.shape.p + 3) / 4) + 255) / 256;
+        const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192));
+        if (l.dtype == F32) k_lm_meet<F32><<<grid, dim3(256), 0, st>>>(a);
+        if (l.dtype == BF16) k_lm_meet<BF16><<<grid, dim3(256), 0, st>>>(a);
+        if (l.dtype == F16) k_lm_meet<F16><<<grid, dim3(256), 0, st>>>(a);
+    }
     return hipGetLastError();
 }
 

@@ -46,8 +46,9 @@ EXPORTS = list(_SIGNATURES)
 
 GROUPS = (32, 64, 128)
 SCALE_TYPES = (torch.bfloat16, torch.float16)
-WAYS = {"auto": -1, "direct": 0, "tile": 1}
+WAYS = {"auto": -1, "direct": 0, "tile": 1, "shared": 2}
 IGNORE = -100
+DIRECT_ROWS = 16  # up to here a layer takes no workspace, whatever its sizes (asking the library for it is most of a microsecond)
 _uint8 = torch.uint8
 
 
@@ -156,12 +157,6 @@ def unpack(P: Packed) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor
     return codes, scales, zeros
 
 
-def _matrix16(t: torch.Tensor, what: str) -> Tuple[int, int, int, int]:
-    if t.dtype is torch.float32:
-        raise ValueError(f"{what}: expected bfloat16 or float16, got {t.dtype}")
-    return _matrix(t)
-
-
 def linear_workspace_bytes(m: int, n: int, p: int, way: str = "auto") -> int:
     return int(_lib.ozimmu_lm_linear_way_workspace_bytes(WAYS[way], m, n, p))
 
@@ -170,15 +165,19 @@ def linear(X: torch.Tensor, W: Packed, dtype=None, alpha: float = 1.0, beta: flo
            workspace: Optional[torch.Tensor] = None, way: str = "auto") -> torch.Tensor:
     """D <- alpha X W^T + beta D for rows X in 16 bits and packed weights W (a new D in the type of X unless said otherwise); `way` forces how
     it is run (see ozimmu_lm_linear_way in the header)."""
-    m, n, ldx, xkind = _matrix16(X, "X")
+    m, n, ldx, xkind = _matrix(X)
+    if not xkind:
+        raise ValueError("X: expected bfloat16 or float16, got torch.float32")
     _not_recorded(X, "X")
     if _packed(W, "W").n != n:
         raise ValueError("inner dimensions differ")
-    p = W.rows
+    p, number = W.rows, WAYS[way]
     D, ldd, dkind = _output(D, X, m, p, dtype, X.dtype, beta)
-    number = WAYS[way]
-    nbytes = _lib.ozimmu_lm_linear_way_workspace_bytes(number, m, n, p) if workspace is None else 0
-    workspace, room, size = _workspace(workspace, nbytes, X)
+    if workspace is None and (number == 0 or (number < 0 and m <= DIRECT_ROWS)):
+        room, size = None, 0
+    else:
+        nbytes = _lib.ozimmu_lm_linear_way_workspace_bytes(number, m, n, p) if workspace is None else 0
+        workspace, room, size = _workspace(workspace, nbytes, X)
     status = _lib.ozimmu_lm_linear_way(number, m, n, p, alpha, xkind, X.data_ptr(), ldx, W.group, W.zeros, W.kind, W.data.data_ptr(), beta, dkind,
                                        D.data_ptr(), ldd, room, size, ozimmu._stream())
     if status:
@@ -197,8 +196,10 @@ def _vector(t: torch.Tensor, m: int, dtype, what: str) -> int:
 
 def _layer(X: torch.Tensor, W: torch.Tensor, y: torch.Tensor):
     """Sizes, leading dimensions, type number and the targets' stride of a layer with its loss."""
-    m, n, ldx, kind = _matrix16(X, "X")
-    p, nw, ldw, wkind = _matrix16(W, "W")
+    m, n, ldx, kind = _matrix(X)
+    p, nw, ldw, wkind = _matrix(W)
+    if not kind or not wkind:
+        raise ValueError(f"X and W: expected bfloat16 or float16, got {X.dtype} and {W.dtype}")
     if wkind != kind:
         raise ValueError("X and W have to be of one type")
     if nw != n:
