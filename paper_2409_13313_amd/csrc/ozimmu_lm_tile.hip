@@ -115,9 +115,11 @@ template <bool ACROSS, int F, int PLACES> struct Operand {
     static constexpr int POSITIONS = 1024 / ROW, LANES = 64 / POSITIONS;  // ACROSS: of a copy; lanes for each
     static constexpr int VOFFS = F == 8 ? 4 : 2;
     v4i now;          // the buffer: this tile's panel
-    uint32_t off;     // of the stage that is copied next
+    uint32_t off;     // of this wave's part of the stage that is copied next
     uint32_t stride;  // between stages
-    uint32_t part[COPIES];
+    uint32_t step[2]; // between its copies (from an even one, from an odd one)
+    uint32_t at_copy; // offset of the next copy
+    uint32_t wave_part;
     uint32_t voff[ACROSS ? VOFFS : 1], tail;
     bool tail_lane;
     uint32_t base[ACROSS ? F : 2], at[ACROSS ? F : 2];
@@ -130,8 +132,8 @@ template <bool ACROSS, int F, int PLACES> struct Operand {
         stride = ACROSS ? STAGE_K * ld : STAGE_K * 2;
         first = to = lds + wave * (COPIES * 1024);
         if constexpr (ACROSS) {
-#pragma unroll
-            for (int i = 0; i < COPIES; ++i) part[i] = (uint32_t)(16 * wave + POSITIONS * i) * ld;
+            wave_part = (uint32_t)(16 * wave) * ld;
+            step[0] = step[1] = POSITIONS * ld;
             const int position = lane / LANES, slot = lane % LANES;
 #pragma unroll
             for (int v = 0; v < VOFFS; ++v) {  // of copy i: F = 8: v = i % 2 + 2 (i / 4), F = 4: v = i / 2
@@ -142,8 +144,10 @@ template <bool ACROSS, int F, int PLACES> struct Operand {
 #pragma unroll
             for (int f = 0; f < F; ++f) base[f] = lds + (8 * q + (i >> 2)) * ROW + ((half * F + f) ^ ((i >> 2) + 4 * (q & 1))) * 32 + (i & 3) * 8;
         } else {
-#pragma unroll
-            for (int i = 0; i < COPIES; ++i) part[i] = (uint32_t)(row_of(wave * (F / 2), 0) + row_of(i / 2, i % 2 * 8)) * ld;
+            // (the halves of two fragments in turn, the first ones first: rows 0, 4, 16, 20 and so on)
+            wave_part = (uint32_t)row_of(wave * (F / 2), 0) * ld;
+            step[0] = 4 * ld;
+            step[1] = 12 * ld;
             const int r = lane >> 3, piece = (lane & 7) ^ r;
             voff[0] = (uint32_t)row_of(0, r) * ld + (uint32_t)piece * 16u;
             // pieces behind the end of a row, in the last stage: out of the buffer, which gives zeros
@@ -180,7 +184,7 @@ template <bool ACROSS, int F, int PLACES> struct Operand {
             bytes = ((left < TILE ? left : TILE) - 1) * ld + n * 2;
         }
         now = v4i{(int)(uint32_t)from, (int)(uint32_t)(from >> 32), (int)(uint32_t)bytes, 0x00020000};
-        off = (uint32_t)k0 * stride;
+        off = (uint32_t)k0 * stride + wave_part;
     }
     __device__ inline void nothing()
     {
@@ -188,14 +192,19 @@ template <bool ACROSS, int F, int PLACES> struct Operand {
         off = 0;
         stride = 0;
     }
-    __device__ inline void last_stage(bool is) { if constexpr (!ACROSS) tail = is && tail_lane ? 0x70000000u : voff[0]; }
-    template <int I> __device__ inline void set_m0() const { copy_to<I * 1024>(to); }
-    template <int I> __device__ inline void issue() const
+    __device__ inline void begin_stage(bool last)
+    {
+        at_copy = off;
+        if constexpr (!ACROSS) tail = last && tail_lane ? 0x70000000u : voff[0];
+    }
+    template <int I> __device__ inline void set_m0() const { copy_to<(ACROSS ? I : I / 4 * 4 + I % 2 * 2 + I / 2 % 2) * 1024>(to); }
+    template <int I> __device__ inline void issue()
     {
         if constexpr (ACROSS)
-            copy(voff[F == 8 ? I % 2 + 2 * (I / 4) : I / 2], now, off + part[I]);
+            copy(voff[F == 8 ? I % 2 + 2 * (I / 4) : I / 2], now, at_copy);
         else
-            copy(tail, now, off + part[I]);
+            copy(tail, now, at_copy);
+        at_copy += step[I % 2];
     }
     __device__ inline void issued()
     {
@@ -239,7 +248,7 @@ template <bool ACROSS, int F, int PLACES, bool IS_A> struct Stream : Operand<ACR
             stage = -(1 << 30);
         }
     }
-    __device__ inline void begin(const Args& g) { this->last_stage(stage == g.KT - 1); }
+    __device__ inline void begin(const Args& g) { this->begin_stage(stage == g.KT - 1); }
     __device__ inline void end(const Args& g)
     {
         this->issued();
@@ -248,18 +257,24 @@ template <bool ACROSS, int F, int PLACES, bool IS_A> struct Stream : Operand<ACR
     }
 };
 
-__device__ inline float over_quarters_max(float v)
+// over the four lanes l, l ^ 16, l ^ 32, l ^ 48
+template <class F> __device__ inline float over_quarters(float v, F&& f)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ inline float over_quarters_sum(float v)
-{
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-template <int TYPE, int DTYPE> __device__ inline void put(const Args& g, float alpha, int64_t row, int64_t col, const float* v)
+// vmcnt(N), by the builtin: the compiler then knows what loads of its own are there
+template <int N> __device__ inline void wait_vmcnt_known()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xf70);
+    asm volatile("" ::: "memory");
+}
+
+template <int DTYPE, bool STREAM> __device__ inline void put(const Args& g, float alpha, int64_t row, int64_t col, const float* v)
 {
     typedef typename Elem<DTYPE>::Bits Bits;
     if (row >= g.m || col >= g.p) return;
@@ -274,7 +289,15 @@ template <int TYPE, int DTYPE> __device__ inline void put(const Args& g, float a
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = from_float<DTYPE>(alpha * v[e]);
     }
-    store_row<DTYPE, 8>(out, left, x);
+    if (STREAM && left >= 8) {
+        typedef v4i Anywhere __attribute__((aligned(2)));
+        v4i y[sizeof(x) / 16];
+        __builtin_memcpy(y, x, sizeof(x));
+#pragma unroll
+        for (int h = 0; h < (int)(sizeof(x) / 16); ++h) __builtin_nontemporal_store(y[h], (Anywhere*)out + h);
+    } else {
+        store_row<DTYPE, 8>(out, left, x);
+    }
 }
 
 // A workgroup of four waves, 128 x 128 sums each in 256 registers a lane, one wave a SIMD, takes one item after the other.  A stage is 64
@@ -301,6 +324,37 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
     StreamB b(g);
     a.set(g.lda, lds, wave, wm, lane, g.n);
     b.set(g.ldb, lds + A_PLACES * StreamA::BYTES, wave, wn, lane, g.n);
+    // Of the rows that a lane has of an item: targets as columns of the wave's (none of them: TILE_B; SLOPE: also NO_TARGET, BAD_TARGET), and
+    // log2(e) lse.  They come an item ahead, so that no wait for them is one for the copies.
+    struct Rows {
+        int target[FA];
+        float lse2[FA];
+    };
+    constexpr bool BY_ROW = KIND == lmk::LOSS || KIND == lmk::SLOPE;
+    auto look_at = [&](int tm, int tp, Rows& o) __attribute__((always_inline)) {
+        const int first = tm * TILE_A + wm * (TILE_A / 2) + row_of(0, lane & 15), col0 = tp * TILE_B + wn * (TILE_B / 2) + g.column0;
+        static_for<0, FA>([&](auto I) __attribute__((always_inline)) {
+            constexpr int i = decltype(I)::value;
+            const int row = first + row_of(i, 0);
+            if constexpr (KIND == lmk::LOSS) {
+                // (rows behind the last one: its target, for nothing)
+                const int64_t y = g.targets.y[min(row, (int)g.m - 1) * g.targets.stride], c = y - col0;
+                o.target[i] = y != g.targets.ignore && (uint64_t)c < TILE_B / 2 ? (int)c : TILE_B;
+            } else {
+                const int target = g.known[row], c = target - col0;
+                o.target[i] = target < 0 ? target : ((uint32_t)c < TILE_B / 2 ? c : TILE_B);
+                o.lse2[i] = g.lse2[row];
+            }
+        });
+    };
+    Order order(g);
+    int tm = 0, tp = 0, split = 0, k0 = 0, k1 = 0;
+    bool any = order.take(tm, tp, split, k0, k1);
+    Rows coming;
+    if constexpr (BY_ROW) {
+        look_at(tm, tp, coming);
+        wait_vmcnt_known<0>();
+    }
     a.look_up(g);
     b.look_up(g);
     auto whole_stage = [&](auto& o) __attribute__((always_inline)) {
@@ -312,12 +366,11 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
         });
         o.end(g);
     };
-    whole_stage(a);
-    whole_stage(b);
-    whole_stage(b);
-    whole_stage(a);
-    if constexpr (A_PLACES == 3) whole_stage(a);
-    whole_stage(b);
+#pragma clang loop unroll(disable)
+    for (int place = 0; place < B_PLACES; ++place) {
+        whole_stage(b);
+        if (place < A_PLACES) whole_stage(a);
+    }
     constexpr int ON_THE_WAY = (A_PLACES - 2) * FA + FB;  // copies of a wave that need not be there yet when the next stage is looked at
 
     v4f acc[FA][FB];
@@ -328,7 +381,8 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
     static_for<0, FA>([&](auto F) __attribute__((always_inline)) { fa[0][decltype(F)::value] = a.template fetch<decltype(F)::value, 0>(); });
     static_for<0, FB>([&](auto F) __attribute__((always_inline)) { fb[0][decltype(F)::value] = b.template fetch<decltype(F)::value, 0>(); });
 
-    auto half = [&](auto H) __attribute__((always_inline)) {
+    // FIRST: of an item, whose sums begin here
+    auto half = [&](auto H, auto FIRST, auto&& wait) __attribute__((always_inline)) {
         constexpr int h = decltype(H)::value, READS = FA + FB, EVERY = M / READS;
         if constexpr (h == 1) {
             a.begin(g);
@@ -351,12 +405,17 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
                 if constexpr (x % EVERY == 0 && c >= FA && c < READS) b.template set_m0<c - FA>();
                 if constexpr (x % EVERY == 1 && c >= FA && c < READS) b.template issue<c - FA>();
             }
-            acc[i][j] = mfma<TYPE>(fb[h][j], fa[h][i], acc[i][j]);
+            if constexpr (decltype(FIRST)::value) {
+                acc[i][j] = mfma<TYPE>(fb[h][j], fa[h][i], v4f{0, 0, 0, 0});
+                asm volatile("" : "+a"(acc[i][j]));  // (in its accumulation registers from here on)
+            } else {
+                acc[i][j] = mfma<TYPE>(fb[h][j], fa[h][i], acc[i][j]);
+            }
             __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (h == 0) {
             // all of this stage is read, and the next one is there
-            wait_vmcnt<ON_THE_WAY>();
+            wait();
             wait_lds();
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
@@ -369,20 +428,35 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
     };
 
     const float alpha = KIND == lmk::WEIGHTS ? g.alpha * *g.alpha_at : g.alpha;
-    Order order(g);
-    int tm, tp, split, k0, k1;
-    while (order.take(tm, tp, split, k0, k1)) {
-#pragma unroll
-        for (int i = 0; i < FA; ++i)
-#pragma unroll
-            for (int j = 0; j < FB; ++j) {
-                acc[i][j] = v4f{0, 0, 0, 0};
-                asm volatile("" : "+a"(acc[i][j]));  // (in its accumulation registers from here on)
-            }
+    typedef std::integral_constant<int, 0> N0;
+    typedef std::integral_constant<int, 1> N1;
+    const auto usual = [] { wait_vmcnt<ON_THE_WAY>(); };
+    // The stores of an item stand behind the copies that its successor's first stage waits for, and need not be over then.  SLOPE: nor before them
+    // the loads of `coming`.
+    constexpr int STORES = KIND == lmk::STATES ? FA * FB : FA * FB / 2, LATER = ON_THE_WAY + STORES < 63 ? ON_THE_WAY + STORES : 63;
+    bool stored = false;  // that many of them, by the last item
+    while (any) {
+        if constexpr (KIND == lmk::SLOPE)
+            half(N0{}, std::true_type{}, [&]() __attribute__((always_inline)) {
+                if (stored)
+                    wait_vmcnt_known<STORES>();
+                else
+                    wait_vmcnt_known<0>();
+            });
+        else if constexpr (KIND == lmk::LOSS)
+            half(N0{}, std::true_type{}, [] { wait_vmcnt_known<0>(); });
+        else
+            half(N0{}, std::true_type{}, [&]() __attribute__((always_inline)) {
+                if (stored)
+                    wait_vmcnt<LATER>();
+                else
+                    wait_vmcnt<ON_THE_WAY>();
+            });
+        half(N1{}, std::false_type{}, usual);
 #pragma clang loop unroll(disable)
-        for (int k = k0; k < k1; ++k) {
-            half(std::integral_constant<int, 0>{});
-            half(std::integral_constant<int, 1>{});
+        for (int k = k0 + 1; k < k1; ++k) {
+            half(N0{}, std::false_type{}, usual);
+            half(N1{}, std::false_type{}, usual);
         }
 
         // (read by asm statements, or the register allocator parks sums in scratch memory; the wait states behind the last matrix instruction are
@@ -406,87 +480,88 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
-        if constexpr (KIND == lmk::LOSS || KIND == lmk::SLOPE) {
-            // the targets of the lane's rows, as columns of this wave's 128
-            int target[FA];
-            bool any = false;
-            static_for<0, FA>([&](auto I) {
-                constexpr int i = decltype(I)::value;
-                const int64_t row = row0 + row_of(i, 0);
-                if constexpr (KIND == lmk::LOSS)
-                    target[i] = row < g.m ? g.targets[row] : lmk::NO_TARGET;
-                else
-                    target[i] = g.known[row];
-                const int c = target[i] - g.column0 - (int)col0;
-                target[i] = target[i] < 0 ? target[i] : (c >= 0 && c < TILE_B / 2 ? c : TILE_B);
-                any |= target[i] >= 0 && target[i] < TILE_B;
-            });
-            const bool found = __any(any), edge = col0 + TILE_B / 2 > g.p;
+        // the item at hand, and the next one
+        const int this_split = split;
+        const bool whole = (int64_t)(tm + 1) * TILE_A <= g.m && (int64_t)(tp + 1) * TILE_B <= g.p && g.beta == 0.0f;
+        const Rows mine = coming;
+        any = order.take(tm, tp, split, k0, k1);
+        if constexpr (BY_ROW) {
+            look_at(tm, tp, coming);
+            uint32_t least = TILE_B;
+#pragma unroll
+            for (int i = 0; i < FA; ++i) least = min(least, (uint32_t)mine.target[i]);
+            const bool found = __any(least < TILE_B / 2), edge = col0 + TILE_B / 2 > g.p;
             const int cols = (int)(g.p - col0 < TILE_B / 2 ? g.p - col0 : TILE_B / 2);
+            // f(e, column - this lane's column e), one after the other.  (The column is made opaque each time, and nothing moves between them: their
+            // comparisons, kept for all rows or made side by side, would take all scalar registers.)
+            auto compared = [&](int column, auto&& f) __attribute__((always_inline)) {
+                column -= lc * 8;
+                asm volatile("" : "+v"(column));
+                static_for<0, N>([&](auto E) __attribute__((always_inline)) {
+                    constexpr int e = decltype(E)::value;
+                    f(e, column - (e / 8 * 32 + e % 8));
+                    if constexpr (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                });
+            };
             if constexpr (KIND == lmk::LOSS) {
                 if (col0 < g.p)
                     rows([&](auto I, auto RI, float* v) __attribute__((always_inline)) {
                         constexpr int i = decltype(I)::value, ri = decltype(RI)::value;
+                        const int target = mine.target[i];
                         const float none = -__builtin_inff();
-                        if (edge)
-#pragma unroll
-                            for (int e = 0; e < N; ++e) v[e] = e / 8 * 32 + lc * 8 + e % 8 < cols ? v[e] : none;
+                        if (edge) compared(cols, [&](int e, int c) { v[e] = c > 0 ? v[e] : none; });
                         if (found) {
-#pragma unroll
-                            for (int e = 0; e < N; ++e)
-                                if (target[i] == e / 8 * 32 + lc * 8 + e % 8) {
-                                    g.at_target[row0 + ri] = v[e];
-                                    v[e] = none;
-                                }
+                            float z = 0.0f;
+                            compared(target, [&](int e, int c) {
+                                z = c == 0 ? v[e] : z;
+                                v[e] = c == 0 ? none : v[e];
+                            });
+                            if ((uint32_t)target < TILE_B / 2 && (target >> 3 & 3) == lc) g.at_target[row0 + ri] = z;
                         }
                         float m = none;
 #pragma unroll
                         for (int e = 0; e < N; ++e) m = fmaxf(m, v[e]);
-                        m = over_quarters_max(m) * LOG2E;
+                        m = over_quarters(m, [](float p, float q) { return fmaxf(p, q); }) * LOG2E;
                         const float m2 = m == none ? 0.0f : m;
-                        float s = 0.0f;
+                        float s[4] = {0, 0, 0, 0};
 #pragma unroll
-                        for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], LOG2E, -m2));
-                        s = over_quarters_sum(s);
-                        if (lc == 0) g.parts[col0 / (TILE_B / 2) * g.parts_ld + row0 + ri] = make_float2(m, s);
+                        for (int e = 0; e < N; ++e) s[e % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], LOG2E, -m2));
+                        const float sum = over_quarters((s[0] + s[1]) + (s[2] + s[3]), [](float p, float q) { return p + q; });
+                        if (lc == 0) g.parts[col0 / (TILE_B / 2) * g.parts_ld + row0 + ri] = make_float2(m, sum);
                     });
             } else {
-                float lse2[FA];
-#pragma unroll
-                for (int i = 0; i < FA; ++i) lse2[i] = g.lse2[row0 + row_of(i, 0)];
                 typedef typename Elem<TYPE>::Bits Bits;
                 rows([&](auto I, auto RI, float* v) __attribute__((always_inline)) {
                     constexpr int i = decltype(I)::value, ri = decltype(RI)::value;
                     constexpr float SCALE = TYPE == F16 ? lmk::SLOPE_SCALE_F16 : 1.0f;
-                    float target_slope = 0.0f;
+                    const int target = mine.target[i];
+                    const float lse2 = mine.lse2[i];
+                    float own = 0.0f;
                     if (found) {
-#pragma unroll
-                        for (int e = 0; e < N; ++e)
-                            if (target[i] == e / 8 * 32 + lc * 8 + e % 8) target_slope = expm1f((v[e] * LOG2E - lse2[i]) * 0.693147180559945309f);
+                        float z = 0.0f;
+                        compared(target, [&](int e, int c) { z = c == 0 ? v[e] : z; });
+                        own = expm1f((z * LOG2E - lse2) * 0.693147180559945309f);
                     }
-                    const uint32_t keep = target[i] == lmk::NO_TARGET ? 0u : 0xffffffffu;
+                    const uint32_t keep = target == lmk::NO_TARGET ? 0u : 0xffffffffu;
                     Bits* const out = (Bits*)g.D + (row0 + ri) * g.ldd + col0 + lc * 8;
 #pragma unroll
+                    for (int e = 0; e < N; ++e) v[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], LOG2E, -lse2));
+                    if (edge) compared(cols, [&](int e, int c) { v[e] = c > 0 ? v[e] : 0.0f; });
+                    if (found) compared(target, [&](int e, int c) { v[e] = c == 0 ? own : v[e]; });
+#pragma unroll
                     for (int jj = 0; jj < FB / 2; ++jj) {
-                        Bits x[8];
-                        uint32_t w[4];
+                        v4i w;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float d = __builtin_amdgcn_exp2f(__builtin_fmaf(v[8 * jj + e], LOG2E, -lse2[i]));
-                            if (edge) d = jj * 32 + lc * 8 + e < cols ? d : 0.0f;
-                            if (found) d = target[i] == jj * 32 + lc * 8 + e ? target_slope : d;
-                            x[e] = from_float<TYPE>(SCALE * d);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = ((uint32_t)x[2 * e] | (uint32_t)x[2 * e + 1] << 16) & keep;
-                        __builtin_memcpy(out + jj * 32, w, 16);
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = (int)(((uint32_t)from_float<TYPE>(SCALE * v[8 * jj + 2 * e]) | (uint32_t)from_float<TYPE>(SCALE * v[8 * jj + 2 * e + 1]) << 16) & keep);
+                        *(v4i*)(out + jj * 32) = w;
                     }
                 });
             }
         } else if constexpr (KIND == lmk::STATES) {
             rows([&](auto, auto RI, float* v) __attribute__((always_inline)) {
                 constexpr int ri = decltype(RI)::value;
-                float* const out = (float*)g.D + split * g.split_stride + (row0 + ri) * g.ldd + col0 + lc * 4;
+                float* const out = (float*)g.D + this_split * g.split_stride + (row0 + ri) * g.ldd + col0 + lc * 4;
                 if (g.beta != 0.0f) {
                     v4f old[FB];
 #pragma unroll
@@ -513,12 +588,13 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
                 const int eight = B_ACROSS ? (lc & 1) * 16 + (lc >> 1) * 8 : lc * 8;  // of 32 columns
 #pragma unroll
                 for (int jj = 0; jj < FB / 2; ++jj) {
-                    if (g.dtype == F32) put<TYPE, F32>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
-                    if (g.dtype == BF16) put<TYPE, BF16>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
-                    if (g.dtype == F16) put<TYPE, F16>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
+                    if (g.dtype == F32) put<F32, KIND == lmk::WEIGHTS>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
+                    if (g.dtype == BF16) put<BF16, KIND == lmk::WEIGHTS>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
+                    if (g.dtype == F16) put<F16, KIND == lmk::WEIGHTS>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
                 }
             });
         }
+        stored = KIND == lmk::STATES || KIND == lmk::SLOPE || whole;
     }
     wait_vmcnt<0>();  // no copy may still be writing LDS when the workgroup retires
 }
