@@ -274,29 +274,24 @@ template <int N> __device__ inline void wait_vmcnt_known()
     asm volatile("" ::: "memory");
 }
 
-template <int DTYPE, bool STREAM> __device__ inline void put(const Args& g, float alpha, int64_t row, int64_t col, const float* v)
+// Eight neighbouring sums into D.  EDGE: of which not all need lie in D.
+template <int DTYPE, bool BETA, bool EDGE>
+__device__ inline void put(const Args& g, float alpha, int64_t row, int64_t col, const float* v)
 {
     typedef typename Elem<DTYPE>::Bits Bits;
-    if (row >= g.m || col >= g.p) return;
     Bits* const out = (Bits*)g.D + row * g.ldd + col;
-    const int64_t left = g.p - col;
     Bits x[8];
-    if (g.beta != 0.0f) {
-        load_row<DTYPE, 8>(out, left, x);
+    if constexpr (EDGE) {
+        if (row >= g.m) return;
+        const int left = (int)(g.p - col);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = from_float<DTYPE>(alpha * v[e] + g.beta * to_float<DTYPE>(x[e]));
+        for (int e = 0; e < 8; ++e)
+            if (e < left) out[e] = from_float<DTYPE>(BETA ? alpha * v[e] + g.beta * to_float<DTYPE>(out[e]) : alpha * v[e]);
     } else {
+        if constexpr (BETA) __builtin_memcpy(x, out, sizeof(x));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = from_float<DTYPE>(alpha * v[e]);
-    }
-    if (STREAM && left >= 8) {
-        typedef v4i Anywhere __attribute__((aligned(2)));
-        v4i y[sizeof(x) / 16];
-        __builtin_memcpy(y, x, sizeof(x));
-#pragma unroll
-        for (int h = 0; h < (int)(sizeof(x) / 16); ++h) __builtin_nontemporal_store(y[h], (Anywhere*)out + h);
-    } else {
-        store_row<DTYPE, 8>(out, left, x);
+        for (int e = 0; e < 8; ++e) x[e] = from_float<DTYPE>(BETA ? alpha * v[e] + g.beta * to_float<DTYPE>(x[e]) : alpha * v[e]);
+        __builtin_memcpy(out, x, sizeof(x));
     }
 }
 
@@ -482,7 +477,7 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
         };
         // the item at hand, and the next one
         const int this_split = split;
-        const bool whole = (int64_t)(tm + 1) * TILE_A <= g.m && (int64_t)(tp + 1) * TILE_B <= g.p && g.beta == 0.0f;
+        const bool inside = (int64_t)(tm + 1) * TILE_A <= g.m && (int64_t)(tp + 1) * TILE_B <= g.p, whole = inside && g.beta == 0.0f;
         const Rows mine = coming;
         any = order.take(tm, tp, split, k0, k1);
         if constexpr (BY_ROW) {
@@ -573,26 +568,40 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
                 for (int j = 0; j < FB; ++j) *(v4f*)(out + 16 * j) = v4f{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
             });
         } else {
-            rows([&](auto, auto RI, float* v) __attribute__((always_inline)) {
-                constexpr int ri = decltype(RI)::value;
-                if constexpr (B_ACROSS) {
-                    // two fragments' fours into eights: the odd sixteens of lanes give theirs of the first for the even ones' of the second
+            // (each type and case a piece of code of its own, taken as a whole: woven into each other they do not fit the instruction cache, and a
+            // gradient of weights of 256 x 256 sums took 25 us to write, so 14)
+            auto write = [&](auto DTYPE, auto BETA, auto EDGE) __attribute__((always_inline)) {
+                rows([&](auto, auto RI, float* v) __attribute__((always_inline)) {
+                    constexpr int ri = decltype(RI)::value;
+                    if constexpr (B_ACROSS) {
+                        // two fragments' fours into eights: the odd sixteens of lanes give theirs of the first for the even ones' of the second
 #pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (e / 4 % 2 == 0) {
-                            const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[e]), __float_as_uint(v[e + 4]), false, false);
-                            v[e] = __uint_as_float(x[0]);
-                            v[e + 4] = __uint_as_float(x[1]);
-                        }
-                }
-                const int eight = B_ACROSS ? (lc & 1) * 16 + (lc >> 1) * 8 : lc * 8;  // of 32 columns
+                        for (int e = 0; e < N; ++e)
+                            if (e / 4 % 2 == 0) {
+                                const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[e]), __float_as_uint(v[e + 4]), false, false);
+                                v[e] = __uint_as_float(x[0]);
+                                v[e + 4] = __uint_as_float(x[1]);
+                            }
+                    }
+                    const int eight = B_ACROSS ? (lc & 1) * 16 + (lc >> 1) * 8 : lc * 8;  // of 32 columns
 #pragma unroll
-                for (int jj = 0; jj < FB / 2; ++jj) {
-                    if (g.dtype == F32) put<F32, KIND == lmk::WEIGHTS>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
-                    if (g.dtype == BF16) put<BF16, KIND == lmk::WEIGHTS>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
-                    if (g.dtype == F16) put<F16, KIND == lmk::WEIGHTS>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
-                }
-            });
+                    for (int jj = 0; jj < FB / 2; ++jj)
+                        put<decltype(DTYPE)::value, decltype(BETA)::value, decltype(EDGE)::value>(g, alpha, row0 + ri, col0 + jj * 32 + eight, v + 8 * jj);
+                });
+            };
+            auto write_as = [&](auto DTYPE) __attribute__((always_inline)) {
+                if (whole)
+                    write(DTYPE, std::false_type{}, std::false_type{});
+                else if (inside)
+                    write(DTYPE, std::true_type{}, std::false_type{});
+                else if (g.beta == 0.0f)
+                    write(DTYPE, std::false_type{}, std::true_type{});
+                else
+                    write(DTYPE, std::true_type{}, std::true_type{});
+            };
+            if (g.dtype == F32) write_as(std::integral_constant<int, F32>{});
+            if (g.dtype == BF16) write_as(std::integral_constant<int, BF16>{});
+            if (g.dtype == F16) write_as(std::integral_constant<int, F16>{});
         }
         stored = KIND == lmk::STATES || KIND == lmk::SLOPE || whole;
     }
