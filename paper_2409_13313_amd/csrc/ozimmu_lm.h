@@ -126,6 +126,25 @@ hipError_t launch_tile(const Tile& t, hipStream_t st);
 hipError_t launch_tile_1(const Tile& t, hipStream_t st);  // BF16
 hipError_t launch_tile_2(const Tile& t, hipStream_t st);  // F16
 
+// ---- the loss without tiles (ozimmu_lm_few.hip) ----
+
+struct FewLoss {
+    int64_t m, n, p;
+    const void* X;
+    int64_t ldx;
+    const void* W;
+    int64_t ldw;
+    Targets targets;
+    float* at_target;
+    float2* parts;   // [columns of the plan][row], rows of whole workgroups
+    int64_t parts_ld;
+};
+// tokens (16, 32, 64) and words (16, 64) a workgroup; rows == 0: by tiles
+struct FewPlan {
+    int rows, columns;
+};
+hipError_t launch_few_loss(int type, const FewLoss& g, const FewPlan& plan, hipStream_t st);
+
 // ---- what stands around them in the loss (ozimmu_lm_loss.hip) ----
 
 constexpr float SLOPE_SCALE_F16 = 32768.0f;     // slopes in FP16 are held times this: most of them are far below 2^-14

@@ -246,17 +246,28 @@ int64_t laid_out_rows(int64_t width, int64_t p)
     return rows < round_to(p, 256) ? rows : round_to(p, 256);
 }
 
+// How a loss is taken: straight from memory (rows of the plan > 0) for few tokens, more of them where W would have to be laid out for the tiles, and where
+// there is little to do.  (us, straight and by tiles: 1 x 4096 x 32768 59 and 72, rows that begin anywhere 96 and 185;  32 rows 75 and 75;  64 rows 92
+// and 75, anywhere 158 and 194;  133 x 1001 x 5003 20 and 27;  256 x 1024 x 8192 25 and 18;  16 x 512 x 2048 7.7 and 13.)
+lmk::FewPlan few_plan(int64_t m, int64_t n, int64_t p, bool aligned)
+{
+    if (m > (aligned ? 32 : 64) && (double)m * (double)n * (double)p >= 1e9) return {0, 0};
+    const int rows = m <= 16 ? 16 : m <= 32 ? 32 : 64;
+    return {rows, m > 4 && (m + rows - 1) / rows * ((p + 63) / 64) >= 128 ? 64 : 16};
+}
+
 struct LossPlan {
+    lmk::FewPlan few;
     int64_t width, tokens, words;   // of a row laid out; tokens at a time; rows of W laid out at a time
     float* at_target;
     float2* parts;
     uint16_t *X, *W;
     size_t bytes;
-    LossPlan(int64_t m, int64_t n, int64_t p, void* workspace)
+    LossPlan(int64_t m, int64_t n, int64_t p, lmk::FewPlan few_, void* workspace) : few(few_)
     {
         Room room{(uint8_t*)workspace};
         width = round_to(n, 64);
-        const int64_t blocks = (p + 63) / 64;
+        const int64_t blocks = few.rows ? (p + few.columns - 1) / few.columns : (p + 63) / 64;
         // tokens at a time: parts of at most 256 MB
         tokens = ((int64_t)1 << 25) / blocks / 256 * 256;
         if (tokens < 256) tokens = 256;
@@ -264,8 +275,8 @@ struct LossPlan {
         words = laid_out_rows(width, p);
         at_target = room.take<float>(tokens);
         parts = room.take<float2>(blocks * tokens);
-        X = room.take<uint16_t>(tokens * width);
-        W = room.take<uint16_t>(words * width);
+        X = room.take<uint16_t>(few.rows ? 0 : tokens * width);
+        W = room.take<uint16_t>(few.rows ? 0 : words * width);
         bytes = room.used;
     }
 };
@@ -399,7 +410,10 @@ int ozimmu_lm_linear_way(int way, int64_t m, int64_t n, int64_t p, float alpha, 
 
 size_t ozimmu_lm_cross_entropy_workspace_bytes(int64_t m, int64_t n, int64_t p)
 {
-    return loss_sizes_ok(m, n, p) && m > 0 ? LossPlan(m, n, p, nullptr).bytes : 0;
+    if (!loss_sizes_ok(m, n, p) || m == 0) return 0;
+    // (for rows that begin anywhere too)
+    const size_t a = LossPlan(m, n, p, few_plan(m, n, p, true), nullptr).bytes, b = LossPlan(m, n, p, few_plan(m, n, p, false), nullptr).bytes;
+    return a > b ? a : b;
 }
 
 int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* y,
@@ -414,7 +428,7 @@ int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const voi
     CHECK(vector_status(lse, m, 1, 4));
     CHECK(workspace_status(workspace, workspace_bytes, ozimmu_lm_cross_entropy_workspace_bytes(m, n, p)));
     if (m == 0) return OZIMMU_OK;
-    const LossPlan plan(m, n, p, workspace);
+    const LossPlan plan(m, n, p, few_plan(m, n, p, as_it_is(X, n, ldx) && as_it_is(W, n, ldw)), workspace);
     const hipStream_t st = (hipStream_t)stream;
     // (one that is laid out has zeros up to `width`; where that is beyond n the other may not be read so far, so both are)
     const bool x_as_it_is = as_it_is(X, n, ldx) && (n == plan.width || as_it_is(W, n, ldw));
@@ -422,6 +436,13 @@ int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const voi
     for (int64_t t0 = 0; t0 < m; t0 += plan.tokens) {
         const int64_t rows = m - t0 < plan.tokens ? m - t0 : plan.tokens, step = w_as_it_is ? p : plan.words;
         const lmk::Targets targets{y + t0 * y_stride, y_stride, ignore, p};
+        if (plan.few.rows) {
+            const lmk::FewLoss few{rows, n, p, (const uint16_t*)X + t0 * ldx, ldx, W, ldw, targets, plan.at_target, plan.parts, plan.tokens};
+            CHECK(launched(lmk::launch_few_loss(type, few, plan.few, st)));
+            CHECK(launched(lmk::launch_join(rows, (p + plan.few.columns - 1) / plan.few.columns, plan.parts, plan.tokens, targets, plan.at_target, loss + t0,
+                                            lse + t0, st)));
+            continue;
+        }
         const lmk::LayOut x{rows, n, (const uint16_t*)X + t0 * ldx, ldx, plan.X, plan.width};
         Tile t{lmk::LOSS, type};
         t.m = rows;
