@@ -91,13 +91,13 @@ template <int LANES, class T, class F> __device__ inline T over_lanes(T v, F&& f
 // ---- quantisation ----
 
 // x / D, rounded once: with r the FP32 number nearest to 1 / D, q = x r and what q is short of, x - D q, exactly, q + (x - D q) r is the nearest
-// number to the quotient (Markstein 1990).  Below 2^-100, where x - D q may not be a normal number, by a division.
+// number to the quotient (Markstein 1990).  Below 2^-100, where x - D q may not be a normal number, and for what is no number, by a division.
 template <int D> __device__ inline float over(float x)
 {
     constexpr float r = 1.0f / D;
     const float q = x * r;
     float y = __builtin_fmaf(__builtin_fmaf(-(float)D, q, x), r, q);
-    if (__any(x < 0x1p-100f && x != 0.0f)) {
+    if (__any((x < 0x1p-100f && x != 0.0f) || !(x < __builtin_inff()))) {
         asm volatile("");  // (a branch, and not both)
         y = x / (float)D;
     }
@@ -147,7 +147,7 @@ __device__ inline void quantize_eight(const Shape& s, int stype, const typename 
     }
     const float scale = scale_float(stype, bits);
     const bool some = scale > 0.0f;
-    // (it overflows, and more, for the smallest scales in BF16)
+    // (it overflows for the smallest scales in BF16, and is none of the hardware's numbers for the largest)
     const float inverse = some ? __builtin_amdgcn_rcpf(scale) : 0.0f;
     const auto short_of = [&](float v, float rounded) { return __builtin_fmaf(v, inverse, -rounded); };
     float zero = 8.0f, near = 0.0f;
@@ -162,7 +162,7 @@ __device__ inline void quantize_eight(const Shape& s, int stype, const typename 
         q[e] = __builtin_fmaf(x[e], inverse, base);
         near = fmaxf(near, fabsf(short_of(x[e], q[e] - base)));
     }
-    const bool close = !(near < NEAR), by_division = !finite || (some && scale < 0x1p-120f) || (TYPE == F32 && close);
+    const bool close = !(near < NEAR), by_division = !finite || (some && !(scale > 0x1p-120f && scale < 0x1p+120f)) || (TYPE == F32 && close);
     if (__any(by_division)) {
         if constexpr (ZEROS) zero = some ? rintf(-lo / scale) : 0.0f;
         zero = __builtin_amdgcn_fmed3f(zero, 0.0f, 15.0f);
