@@ -62,6 +62,9 @@ def build(verbose: bool = False) -> str:
             if src in LOOKED_AT:
                 text, = (open(f).read() for f in glob.glob(os.path.join(tmp, "*gfx950*.s")))
                 codegen.check_mx(text)
+            if src == "ozimmu_lm_tile.hip":
+                text, = (open(f).read() for f in glob.glob(os.path.join(tmp, "*gfx950*.s")))
+                codegen.check_lm(text, int(defs[0].split("=")[1]))
             if src == "ozimmu_resident.hip":
                 text, = (open(f).read() for f in glob.glob(os.path.join(tmp, "*gfx950*.s")))
                 seen = codegen.check_resident(text, int(defs[0].split("=")[1]))

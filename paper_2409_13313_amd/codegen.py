@@ -272,3 +272,67 @@ def check_mx(text: str) -> dict:
         seen[kind] += 1
     _require(seen == {"k_mx_tile": 3, "k_mx_half": 3}, "kernels in the assembly", seen)
     return seen
+
+
+# ---- products of 16-bit matrices in tiles (csrc/ozimmu_lm_tile.hip) ----
+#
+# k_lm_tile rests on asm statements as the tiles above do: copies into LDS counted by hand, M0 set before each of them, sums read out of their
+# accumulation registers.
+LM_KERNEL = re.compile(r"^(_ZN12_GLOBAL__N_1\d+k_lm_tileILi(\d)ELi(\d)ELi(\d)ELi(\d)EEEv\w+):(.*?)^\.Lfunc_end", re.S | re.M)
+LM_KINDS, LM_SHAPES = range(5), ((8, 8), (4, 8), (4, 4))
+
+
+def check_lm_body(body: str, a: int, b: int, what: tuple) -> None:
+    code, by_hand, hand = [], set(), False
+    for line in body.split("\n"):
+        if "#ASMSTART" in line or "#ASMEND" in line:
+            hand = "#ASMSTART" in line
+            continue
+        c = line.split(";")[0].strip()
+        if not c or (c.startswith(".") and not c.startswith(".LBB")):
+            continue
+        if hand:
+            by_hand.add(len(code))
+        code.append(c)
+    mfma = [i for i, c in enumerate(code) if c.startswith("v_mfma_f32_16x16x32_")]
+    stage = 2 * a * b                       # (a first stage of an item, and the loop over the others)
+    _require(len(mfma) == 2 * stage, what, "matrix instructions", len(mfma))
+    loop = mfma[stage:]
+    for i in loop:
+        d, _, _, c = re.findall(r"[va]\[\d+:\d+\]", code[i])[:4]
+        _require(d == c, what, code[i])
+    for i, c in enumerate(code):
+        if re.search(r"\bm0\b", c):
+            _require(i in by_hand and re.match(r"s_add_u32 m0, s\d+, \w+$", c) and not code[i + 1].endswith(" lds"), what, c)
+        if c.endswith(" lds"):
+            _require(i in by_hand, what, c)
+        _require(not c.startswith("scratch_"), what, c)
+    begin = max(i for i, c in enumerate(code) if c.startswith(".LBB") and i < loop[0])
+    end = min(i for i, c in enumerate(code) if i > loop[-1] and re.match(r"s_cbranch\w+ ", c))
+    _require(begin > mfma[stage - 1], what, "stages that are not a loop of their own")
+    waits = [i for i in range(begin, end + 1) if "vmcnt" in code[i]]
+    _require(len(waits) == 1 and waits[0] in by_hand, what, "waits for copies", [code[i] for i in waits])
+    _require(sum(c.startswith("s_barrier") for c in code[begin:end + 1]) == 1, what, "barriers in the loop")
+    _require(sum(c.endswith(" lds") for c in code[begin:end + 1]) == a + b, what, "copies in the loop")
+    for i in range(begin, end + 1):
+        _require(i in by_hand or not re.match(r"(buffer|global|flat)_|v_accvgpr", code[i]), what, code[i])
+    reads = [i for i, c in enumerate(code) if c.startswith("v_accvgpr_read") and i in by_hand]
+    nops = [i for i in range(end, reads[0]) if code[i] == "s_nop 15" and i in by_hand]
+    _require(reads[0] > end and len(nops) == 2, what, "no wait states between the products and the reads of their sums")
+    check_mx_scalars(code, by_hand, what)
+
+
+def check_lm(text: str, kind: int) -> dict:
+    """Looks at every tile kernel in the assembly of ozimmu_lm_tile.hip for one element type; raises Wrong, also where one is missing."""
+    seen = {(k, a, b): 0 for k in LM_KINDS for a, b in LM_SHAPES}
+    for m in LM_KERNEL.finditer(text):
+        name, of, k, a, b = m.group(1), *map(int, m.group(2, 3, 4, 5))
+        _require(of == kind, name)
+        check_lm_body(m.group(6), a, b, (k, a, b))
+        at = text.index(".name:           " + name)
+        about = text[text.rindex("- .agpr_count", 0, at):text.find("- .agpr_count", at)]
+        for key in ("private_segment_fixed_size", "vgpr_spill_count"):
+            _require(re.search(r"\.%s:\s+(\d+)" % key, about).group(1) == "0", (k, a, b), key)
+        seen[k, a, b] += 1
+    _require(all(count == 1 for count in seen.values()), "kernels in the assembly", seen)
+    return seen

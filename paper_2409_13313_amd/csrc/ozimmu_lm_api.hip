@@ -39,9 +39,6 @@ static int64_t tiles_of(int shape, int64_t m, int64_t p)
 
 int tile_shape(int64_t m, int64_t n, int64_t p, int splits)
 {
-#ifdef VAR_SHAPE
-    return VAR_SHAPE;
-#endif
     int best = TILE_256;
     for (int s : {TILE_128_256, TILE_128})
         if (estimate_us(s, tiles_of(s, m, p) * splits, (double)((n + 63) / 64) / splits) <
