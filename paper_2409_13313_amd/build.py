@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libozimmu.so")
 SOURCES = ["ozimmu_api.hip", "ozimmu_split.hip", "ozimmu_gemm.hip", "ozimmu_mx_api.hip", "ozimmu_mx_quantize.hip", "ozimmu_mx_gemm.hip",
-           "ozimmu_lm_api.hip", "ozimmu_lm_weights.hip", "ozimmu_lm_few.hip", "ozimmu_lm_loss.hip"]
+           "ozimmu_lm_api.hip", "ozimmu_lm_weights.hip", "ozimmu_lm_few.hip", "ozimmu_lm_loss.hip", "ozimmu_lm_tile.hip"]
 # ozimmu_resident.hip holds kernels specialised for a slice count: one compilation per count, all of them linked into
 # the object of the chunk GEMM (whoever links that object gets every way to run the schedule)
 RESIDENT_KS = range(3, 17)
@@ -40,9 +40,10 @@ def build(verbose: bool = False) -> str:
     objs = [os.path.join(CSRC, src.replace(".hip", ".o")) for src in SOURCES]
     core = os.path.join(CSRC, "ozimmu_gemm_core.o")
     resident = [os.path.join(CSRC, f"ozimmu_resident_k{k}.o") for k in RESIDENT_KS]
-    jobs = [(src, [], core if obj.endswith("ozimmu_gemm.o") else obj) for src, obj in zip(SOURCES, objs)]
-    tiles = [os.path.join(CSRC, f"ozimmu_lm_tile_{t}.o") for t in LM_TYPES]
-    jobs += [("ozimmu_lm_tile.hip", [f"-DLM_TYPE={t}"], obj) for t, obj in zip(LM_TYPES, tiles)]
+    tile = os.path.join(CSRC, "ozimmu_lm_tile.o")
+    tiles = [os.path.join(CSRC, f"ozimmu_lm_tile_{t}.o") for t in LM_TYPES] if tile in objs else []
+    jobs = [("ozimmu_lm_tile.hip", [f"-DLM_TYPE={t}"], obj) for t, obj in zip(LM_TYPES, tiles)]   # (the longest first)
+    jobs += [(src, [], core if obj.endswith("ozimmu_gemm.o") else obj) for src, obj in zip(SOURCES, objs) if obj != tile]
     jobs += [("ozimmu_resident.hip", [f"-DOZ_RES_K={k}"], obj) for k, obj in zip(RESIDENT_KS, resident)]
 
     def compile_one(job):
@@ -75,7 +76,9 @@ def build(verbose: bool = False) -> str:
     with ThreadPoolExecutor(max_workers=8) as pool:
         list(pool.map(compile_one, jobs))
     subprocess.run(["ld", "-r", "-o", os.path.join(CSRC, "ozimmu_gemm.o"), core, *resident], check=True)
-    cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs, *tiles]
+    if tiles:
+        subprocess.run(["ld", "-r", "-o", tile, *tiles], check=True)
+    cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     subprocess.run(cmd, check=True)
     return LIB
 
