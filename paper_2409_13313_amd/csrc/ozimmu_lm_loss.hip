@@ -38,6 +38,13 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_prepare(Prepare p)
     __shared__ float of_wave[4];
     const int t = threadIdx.x;
     const bool first = blockIdx.x == 0;
+    const int64_t begin = (int64_t)blockIdx.x * 256 + t, step = (int64_t)gridDim.x * 256;
+    // (W first, which needs no |g|, from the last workgroups on, which have less of X)
+    const int64_t of_w = p.w.Y ? p.w.rows * (p.w.width / 8) : 0;
+    for (int64_t at = step - 1 - begin; at < of_w; at += step) {
+        uint16_t x[8];
+        lay_out<TYPE>(p.w, at, x);
+    }
     float most = 0.0f;
     for (int64_t r = t; r < p.padded; r += 256) {
         const int target = r < p.rows ? p.targets[r] : NO_TARGET;
@@ -52,13 +59,9 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_prepare(Prepare p)
     __syncthreads();
     most = fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
     if (first && t == 0) *p.largest = most;
-    const int64_t of_x = p.x.Y || p.scaled ? p.x.rows * (p.x.width / 8) : 0, all = of_x + (p.w.Y ? p.w.rows * (p.w.width / 8) : 0);
-    for (int64_t at = (int64_t)blockIdx.x * 256 + t; at < all; at += (int64_t)gridDim.x * 256) {
+    const int64_t of_x = p.x.Y || p.scaled ? p.x.rows * (p.x.width / 8) : 0;
+    for (int64_t at = begin; at < of_x; at += step) {
         uint16_t x[8];
-        if (at >= of_x) {
-            lay_out<TYPE>(p.w, at - of_x, x);
-            continue;
-        }
         const int64_t row = lay_out<TYPE>(p.x, at, x);
         if (!p.scaled) continue;
         const float own = p.targets[row] == NO_TARGET ? 0.0f : p.g[row * p.g_stride], ratio = own == 0.0f ? 0.0f : own / most;
@@ -85,17 +88,18 @@ __global__ __launch_bounds__(1024) void k_join(int64_t rows, int64_t blocks, con
     const int64_t row = (int64_t)blockIdx.x * 16 + (lane & 15);  // (parts have rows of whole tiles)
     float2 sum = make_float2(-__builtin_inff(), 0.0f);
     // (eight loads on their way at a time: one after the other, they are what one token's join takes)
-    for (int64_t b = t >> 4; b < blocks; b += 64 * 8) {
-        float2 part[8];
+    constexpr int AT_A_TIME = 8;
+    for (int64_t b = t >> 4; b < blocks; b += 64 * AT_A_TIME) {
+        float2 part[AT_A_TIME];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) part[u] = b + 64 * u < blocks ? parts[(b + 64 * u) * parts_ld + row] : make_float2(-__builtin_inff(), 0.0f);
+        for (int u = 0; u < AT_A_TIME; ++u) part[u] = b + 64 * u < blocks ? parts[(b + 64 * u) * parts_ld + row] : make_float2(-__builtin_inff(), 0.0f);
         float most = sum.x;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) most = fmaxf(most, part[u].x);
+        for (int u = 0; u < AT_A_TIME; ++u) most = fmaxf(most, part[u].x);
         const float base = most == -__builtin_inff() ? 0.0f : most;
         float s = sum.y * exp2f(sum.x - base);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) s += part[u].y * exp2f(part[u].x - base);
+        for (int u = 0; u < AT_A_TIME; ++u) s += part[u].y * exp2f(part[u].x - base);
         sum = make_float2(most, s);
     }
     for (int far = 16; far < 64; far *= 2) {

@@ -328,7 +328,15 @@ template <int XTYPE> __device__ inline v4i numbers(uint32_t w, float zero)
 }
 
 // FOUR: at most four rows, row i at place 4 i of the fragment, so that a lane's first sum is the one that counts
-template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR>
+//
+// Bound by memory: what it takes is reading the codes once.  16 x 8192 x 16384 (70 MB) 18 us, 1 x 4096 x 131072 (302 MB) 57 us, 5.2 TB/s; 1 x 4096 x 4096
+// (8.7 MB) 4.7 us and 4.3 from the caches, of which 2 are a launch's start and end.  A second block on its way beside the one that is multiplied gives
+// nothing (20.8 and 20.7 us, 69 and 65: fewer waves); X in LDS is worth its barriers from more rows on (k_lm_shared).
+//
+// STREAM: codes past the caches, of weights that do not fit into the 256 MB of the memory-side cache (302 MB, one row: 57 us, else 61).  Smaller ones may
+// stay there from one token to the next, and then it costs (8.7 MB, one row: 5.0 and 4.3 us; 70 MB, 16 rows, three such matrices in turn: 18.9 and 18.2; ten
+// of them 19.1 and 20.7).
+template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
 {
     static_assert(!FOUR || MF == 1, "four rows are one fragment");
@@ -374,7 +382,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
     auto load = [&](int kb, Stored (&o)[PF], v4i (&x)[MF][4]) __attribute__((always_inline)) {
 #pragma unroll
         for (int f = 0; f < PF; ++f) {
-            o[f].code = *(const v4i*)(code_at[f] + (int64_t)kb * BLOCK_BYTES);
+            const v4i* const from = (const v4i*)(code_at[f] + (int64_t)kb * BLOCK_BYTES);
+            o[f].code = STREAM ? __builtin_nontemporal_load(from) : *from;
             o[f].record.load(record_at[f] + (int64_t)kb * (ROWS * record));
         }
 #pragma unroll
@@ -717,26 +726,27 @@ template <int XTYPE> void shared(const Shared& a, const lmk::SharedPlan& plan, h
     if (a.w.shape.group == 128) shared<XTYPE, 128>(a, plan, st);
 }
 
-template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR> void direct(const Linear& g, const Weights& w, hipStream_t st)
+template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR, bool STREAM = false> void direct(const Linear& g, const Weights& w, hipStream_t st)
 {
     const dim3 grid((unsigned)((w.shape.row_blocks() + PF - 1) / PF), (unsigned)((g.m + 16 * MF - 1) / (16 * MF)));
-    k_lm_direct<XTYPE, GROUP, MF, PF, WAVES, FOUR><<<grid, dim3(64 * WAVES), 0, st>>>(g, w);
+    k_lm_direct<XTYPE, GROUP, MF, PF, WAVES, FOUR, STREAM><<<grid, dim3(64 * WAVES), 0, st>>>(g, w);
 }
 
 template <int XTYPE, int GROUP> void direct(const Linear& g, const Weights& w, hipStream_t st)
 {
     const int64_t units = w.shape.row_blocks();
+    const bool stream = w.shape.bytes() >= (int64_t)1 << 28;
     if (g.m <= 4) {
         if (units <= COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 1, 16, true>(g, w, st);
         if (units <= 4 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 2, 16, true>(g, w, st);
         if (units <= 16 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 2, 8, true>(g, w, st);
-        return direct<XTYPE, GROUP, 1, 4, 4, true>(g, w, st);
+        return stream ? direct<XTYPE, GROUP, 1, 4, 4, true, true>(g, w, st) : direct<XTYPE, GROUP, 1, 4, 4, true>(g, w, st);
     }
     if (g.m <= 16) {
         if (units <= COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 1, 8, false>(g, w, st);
         if (units < 4 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 2, 8, false>(g, w, st);
-        if (units <= 16 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 1, 4, 8, false>(g, w, st);
-        return direct<XTYPE, GROUP, 1, 4, 4, false>(g, w, st);
+        if (units <= 16 * COMPUTE_UNITS) return stream ? direct<XTYPE, GROUP, 1, 4, 8, false, true>(g, w, st) : direct<XTYPE, GROUP, 1, 4, 8, false>(g, w, st);
+        return stream ? direct<XTYPE, GROUP, 1, 4, 4, false, true>(g, w, st) : direct<XTYPE, GROUP, 1, 4, 4, false>(g, w, st);
     }
     if (g.m <= 32) {
         if (units < 2 * COMPUTE_UNITS) return direct<XTYPE, GROUP, 2, 1, 8, false>(g, w, st);

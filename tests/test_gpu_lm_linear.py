@@ -166,3 +166,18 @@ def test_pieces_of_weights_read_back(lm, kind):
     off = (got.double() - want).norm() / want.norm()
     assert off <= 1.5 * HALF[kind]
     assert torch.equal(got[:, 8192:], lm.linear(X, lm.quantize(W0[8192:]), way="tile"))
+
+
+# few rows through weights of many rows, in each way they are shared out, and of more than 256 MB, which are read past the caches
+@pytest.mark.parametrize("m,n,p", [(2, 264, 40000), (3, 136, 70001), (9, 264, 9000), (9, 136, 20000), (13, 264, 70001), (1, 4100, 131101), (11, 4100, 131101),
+                                   (16, 33100, 16373)])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_few_rows_of_wide_layers(lm, m, n, p, kind):
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    for group, zeros, scale in FORMS[:3] if n * p < 1 << 26 else FORMS[2:3]:
+        P = lm.quantize(torch.randn((p, n), device="cuda", generator=gen) * 0.02, group=group, zeros=zeros, scale_type=TYPES[scale])
+        W = lm.dequantize(P, torch.float32).double()   # (exact: a scale of 11 bits times at most 15)
+        S = lm.unpack(P)[1].double().repeat_interleave(group, dim=1)[:, :n]
+        X = rows(m, n, kind, n, 1)
+        got = lm.linear(X, P, D=torch.empty((m, p), device="cuda", dtype=torch.float32))
+        check(got, X.double() @ W.t(), bound(X, W, S, kind, "direct", group), "f32", (m, n, p, group))
