@@ -136,7 +136,7 @@ struct FewLoss {
     int64_t ldw;
     Targets targets;
     float* at_target;
-    float2* parts;   // [columns of the plan][row], rows of whole workgroups
+    float2* parts;   // [row][columns of the plan], rows of whole workgroups
     int64_t parts_ld;
 };
 // tokens (16, 32, 64) and words (16, 64) a workgroup; rows == 0: by tiles
@@ -158,6 +158,8 @@ struct LayOut {
     int64_t width;
 };
 hipError_t launch_lay_out(int type, const LayOut& a, const LayOut& b, hipStream_t st);  // both, of one type
+hipError_t launch_join_rows(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const Targets& targets, const float* at_target,
+                            float* loss, float* lse, hipStream_t st);
 hipError_t launch_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const Targets& targets, const float* at_target, float* loss,
                        float* lse, hipStream_t st);
 // What the gradient begins with: targets and log2(e) lse (NaN where the target is bad) per row, `padded` of them, the largest |g| of rows with a

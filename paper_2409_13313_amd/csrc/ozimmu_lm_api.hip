@@ -434,10 +434,10 @@ int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const voi
         const int64_t rows = m - t0 < plan.tokens ? m - t0 : plan.tokens, step = w_as_it_is ? p : plan.words;
         const lmk::Targets targets{y + t0 * y_stride, y_stride, ignore, p};
         if (plan.few.rows) {
-            const lmk::FewLoss few{rows, n, p, (const uint16_t*)X + t0 * ldx, ldx, W, ldw, targets, plan.at_target, plan.parts, plan.tokens};
+            const int64_t blocks = (p + plan.few.columns - 1) / plan.few.columns;
+            const lmk::FewLoss few{rows, n, p, (const uint16_t*)X + t0 * ldx, ldx, W, ldw, targets, plan.at_target, plan.parts, blocks};
             CHECK(launched(lmk::launch_few_loss(type, few, plan.few, st)));
-            CHECK(launched(lmk::launch_join(rows, (p + plan.few.columns - 1) / plan.few.columns, plan.parts, plan.tokens, targets, plan.at_target, loss + t0,
-                                            lse + t0, st)));
+            CHECK(launched(lmk::launch_join_rows(rows, blocks, plan.parts, blocks, targets, plan.at_target, loss + t0, lse + t0, st)));
             continue;
         }
         const lmk::LayOut x{rows, n, (const uint16_t*)X + t0 * ldx, ldx, plan.X, plan.width};

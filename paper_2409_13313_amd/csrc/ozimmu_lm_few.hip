@@ -150,7 +150,7 @@ template <int TYPE, int MF, int PF, int WAVES> __global__ __launch_bounds__(64 *
 #pragma unroll
         for (int f = 0; f < PF; ++f) s += __builtin_amdgcn_exp2f(__builtin_fmaf(z[f], LOG2E, -base));
         s = over_sixteen(s, [](float p, float q) { return p + q; });
-        if ((t & 15) == 0) g.parts[blockIdx.x * g.parts_ld + row] = make_float2(m, s);
+        if ((t & 15) == 0) g.parts[row * g.parts_ld + blockIdx.x] = make_float2(m, s);
     }
 }
 

@@ -78,39 +78,10 @@ __device__ inline float2 join(float2 a, float2 b)
     return make_float2(m, a.y * exp2f(a.x - m0) + b.y * exp2f(b.x - m0));
 }
 
-// 16 rows a workgroup, their parts shared by 64 threads each, joined in a fixed order.  The parts leave out the target's own exponential, so that
-// loss = log(1 + others / own) keeps its digits where the target has nearly all of the row.
-__global__ __launch_bounds__(1024) void k_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, Targets targets, const float* at_target,
-                                               float* loss, float* lse)
+// A row's loss and lse from its parts' sum, which leaves out the target's own exponential, so that loss = log(1 + others / own) keeps its digits where
+// the target has nearly all of the row.
+__device__ inline void finish(int64_t row, float2 sum, const Targets& targets, const float* at_target, float* loss, float* lse)
 {
-    __shared__ float2 of_wave[16][16];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int64_t row = (int64_t)blockIdx.x * 16 + (lane & 15);  // (parts have rows of whole tiles)
-    float2 sum = make_float2(-__builtin_inff(), 0.0f);
-    // (eight loads on their way at a time: one after the other, they are what one token's join takes)
-    constexpr int AT_A_TIME = 8;
-    for (int64_t b = t >> 4; b < blocks; b += 64 * AT_A_TIME) {
-        float2 part[AT_A_TIME];
-#pragma unroll
-        for (int u = 0; u < AT_A_TIME; ++u) part[u] = b + 64 * u < blocks ? parts[(b + 64 * u) * parts_ld + row] : make_float2(-__builtin_inff(), 0.0f);
-        float most = sum.x;
-#pragma unroll
-        for (int u = 0; u < AT_A_TIME; ++u) most = fmaxf(most, part[u].x);
-        const float base = most == -__builtin_inff() ? 0.0f : most;
-        float s = sum.y * exp2f(sum.x - base);
-#pragma unroll
-        for (int u = 0; u < AT_A_TIME; ++u) s += part[u].y * exp2f(part[u].x - base);
-        sum = make_float2(most, s);
-    }
-    for (int far = 16; far < 64; far *= 2) {
-        const float2 other = make_float2(__shfl_xor(sum.x, far), __shfl_xor(sum.y, far));
-        sum = lane & far ? join(other, sum) : join(sum, other);
-    }
-    if (lane < 16) of_wave[wave][lane] = sum;
-    __syncthreads();
-    if (t >= 16 || row >= rows) return;
-    sum = of_wave[0][t];
-    for (int w = 1; w < 16; ++w) sum = join(sum, of_wave[w][t]);
     const int target = targets[row];
     if (target >= 0) {
         const float own = at_target[row];
@@ -122,6 +93,64 @@ __global__ __launch_bounds__(1024) void k_join(int64_t rows, int64_t blocks, con
         loss[row] = target == BAD_TARGET ? __builtin_nanf("") : 0.0f;
         lse[row] = LN2 * (sum.x + log2f(sum.y));
     }
+}
+
+// The sum of parts first, first + STEP, ..., `stride` between neighbours, eight loads on their way at a time
+template <int STEP> __device__ inline float2 joined(const float2* parts, int64_t stride, int64_t first, int64_t blocks)
+{
+    float2 sum = make_float2(-__builtin_inff(), 0.0f);
+    for (int64_t b = first; b < blocks; b += STEP * 8) {
+        float2 part[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) part[u] = b + STEP * u < blocks ? parts[(b + STEP * u) * stride] : make_float2(-__builtin_inff(), 0.0f);
+        float most = sum.x;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) most = fmaxf(most, part[u].x);
+        const float base = most == -__builtin_inff() ? 0.0f : most;
+        float s = sum.y * exp2f(sum.x - base);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += part[u].y * exp2f(part[u].x - base);
+        sum = make_float2(most, s);
+    }
+    return sum;
+}
+template <int FROM> __device__ inline float2 over_wave(float2 sum, int lane)
+{
+    for (int far = FROM; far < 64; far *= 2) {
+        const float2 other = make_float2(__shfl_xor(sum.x, far), __shfl_xor(sum.y, far));
+        sum = lane & far ? join(other, sum) : join(sum, other);
+    }
+    return sum;
+}
+
+// Parts [column block][row]: 16 rows a workgroup, shared by 64 threads each, joined in a fixed order.  Reading the parts is what it takes: of 4096 rows and
+// 131072 words 67 MB, 10.6 us.
+__global__ __launch_bounds__(1024) void k_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, Targets targets, const float* at_target,
+                                               float* loss, float* lse)
+{
+    __shared__ float2 of_wave[16][16];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int64_t row = (int64_t)blockIdx.x * 16 + (lane & 15);  // (parts have rows of whole tiles)
+    float2 sum = over_wave<16>(joined<64>(parts + row, parts_ld, t >> 4, blocks), lane);
+    if (lane < 16) of_wave[wave][lane] = sum;
+    __syncthreads();
+    if (t >= 16 || row >= rows) return;
+    sum = of_wave[0][t];
+    for (int w = 1; w < 16; ++w) sum = join(sum, of_wave[w][t]);
+    finish(row, sum, targets, at_target, loss, lse);
+}
+
+// Parts [row][column block], of few tokens: a row by a workgroup.
+__global__ __launch_bounds__(256) void k_join_rows(int64_t blocks, const float2* parts, int64_t parts_ld, Targets targets, const float* at_target, float* loss,
+                                                   float* lse)
+{
+    __shared__ float2 of_wave[4];
+    const int t = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const float2 sum = over_wave<1>(joined<256>(parts + row * parts_ld, 1, t, blocks), t & 63);
+    if ((t & 63) == 0) of_wave[t >> 6] = sum;
+    __syncthreads();
+    if (t == 0) finish(row, join(join(of_wave[0], of_wave[1]), join(of_wave[2], of_wave[3])), targets, at_target, loss, lse);
 }
 
 template <int TYPE>
@@ -184,6 +213,13 @@ hipError_t launch_prepare(int type, const Prepare& p, hipStream_t st)
     const dim3 grid(rounds_of((p.x.Y || p.scaled ? p.x.rows * (p.x.width / 8) : 0) + (p.w.Y ? p.w.rows * (p.w.width / 8) : 0)));
     if (type == BF16) k_prepare<BF16><<<grid, dim3(256), 0, st>>>(p);
     if (type == F16) k_prepare<F16><<<grid, dim3(256), 0, st>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_join_rows(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const Targets& targets, const float* at_target,
+                            float* loss, float* lse, hipStream_t st)
+{
+    k_join_rows<<<dim3((unsigned)rows), dim3(256), 0, st>>>(blocks, parts, parts_ld, targets, at_target, loss, lse);
     return hipGetLastError();
 }
 
