@@ -61,9 +61,10 @@ int ozimmu_lm_unpack(int64_t p, int64_t n, int group, const void *packed, uint8_
 
 /* D <- alpha X W^T + beta D: X (device, m x n, of type xtype: BF16 or F16), W packed p x n, D (device, m x p, of type dtype).
  * Sums in FP32, alpha and beta applied in FP32, D rounded once; beta == 0: the old D is not read.  Up to a number of rows (by the library's
- * choice) the codes are multiplied as they are and nothing else is rounded; beyond it the weights are read back in the type of X, each rounded once, a
- * piece at a time.  In BF16 the first of the two forms sums x (128 + q): a row of X that holds an infinity gives NaN.
- * Workspace: 0 bytes where the library takes the first form (workspace may be NULL then). */
+ * choice: about a thousand through 4096 x 4096) the codes are multiplied as they are and nothing else is rounded; beyond it the weights are read back in
+ * the type of X, each rounded once (in FP16 infinite where they are beyond its range), a piece at a time.  In BF16 the first of the two forms sums
+ * x (128 + q): a row of X that holds an infinity, or numbers of 2^113 and more, may give NaN.
+ * Workspace: 0 bytes (workspace may be NULL then) up to 16 rows, and for more of them where the codes are multiplied without splitting the sums. */
 size_t ozimmu_lm_linear_workspace_bytes(int64_t m, int64_t n, int64_t p);
 int ozimmu_lm_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void *X, int64_t ldx, int group, int zeros, int scale_type,
                      const void *W, float beta, int dtype, void *D, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);

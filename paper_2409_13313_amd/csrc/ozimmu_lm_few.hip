@@ -35,6 +35,9 @@ template <class F> __device__ inline float over_sixteen(float v, F&& f)
 // A workgroup has 16 MF tokens and 16 PF words.  Its waves share the inner dimension, 64 elements (a whole line of a row) at a time, one piece on its way
 // while the other is multiplied; operands come from memory into registers as the matrix instruction wants them, from rows that begin
 // anywhere.  The waves' sums meet in LDS in a fixed order, and 16 lanes make a row's part of them.
+//
+// Bound by reading W: 1 x 4096 x 32768 43 us, 268 MB at 6.2 TB/s, what a kernel that only reads reaches; of rows that begin at odd elements 100 us, as every
+// 16 bytes then lie in two requests.
 template <int TYPE, int MF, int PF, int WAVES> __global__ __launch_bounds__(64 * WAVES) void k_few_loss(FewLoss g)
 {
     typedef typename Elem<TYPE>::Bits Bits;
