@@ -331,11 +331,11 @@ template <int XTYPE> __device__ inline v4i numbers(uint32_t w, float zero)
 
 // FOUR: at most four rows, row i at place 4 i of the fragment, so that a lane's first sum is the one that counts
 //
-// Bound by memory: what it takes is reading the codes once.  16 x 8192 x 16384 (70 MB) 18 us, 1 x 4096 x 131072 (302 MB) 57 us, 5.2 TB/s; 1 x 4096 x 4096
+// Bound by memory: what it takes is reading the codes once.  16 x 8192 x 16384 (70 MB) 18 us, 1 x 4096 x 131072 (293 MB) 57 us, 5.2 TB/s; 1 x 4096 x 4096
 // (8.7 MB) 4.7 us and 4.3 from the caches, of which 2 are a launch's start and end.  A second block on its way beside the one that is multiplied gives
 // nothing (20.8 and 20.7 us, 69 and 65: fewer waves); X in LDS is worth its barriers from more rows on (k_lm_shared).
 //
-// STREAM: codes past the caches, of weights that do not fit into the 256 MB of the memory-side cache (302 MB, one row: 57 us, else 61).  Smaller ones may
+// STREAM: codes past the caches, of weights that do not fit into the 256 MB of the memory-side cache (293 MB, one row: 57 us, else 61).  Smaller ones may
 // stay there from one token to the next, and then it costs (8.7 MB, one row: 5.0 and 4.3 us; 70 MB, 16 rows, three such matrices in turn: 18.9 and 18.2; ten
 // of them 19.1 and 20.7).
 template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR, bool STREAM>
