@@ -44,8 +44,9 @@ struct Weights {
 };
 
 hipError_t launch_quantize(int type, const void* W, int64_t ldw, const lml::Shape& s, int stype, void* packed, hipStream_t st);
-// rows row0 .. row0 + rows - 1 into X (of `type`); columns n .. cols - 1 (no more than whole blocks have) become zeros; stream: past the caches
-hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, bool stream, hipStream_t st);
+// rows row0 .. row0 + rows - 1 into X (of `type`); columns n .. cols - 1 (no more than whole blocks have) become zeros; through: for
+// a reader right behind it (k_lm_dequantize)
+hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, bool through, hipStream_t st);
 hipError_t launch_pack(const lml::Shape& s, const uint8_t* codes, int64_t ldc, const void* scales, int64_t lds, const uint8_t* zeros, int64_t ldz,
                        void* packed, hipStream_t st);
 hipError_t launch_unpack(const lml::Shape& s, const void* packed, uint8_t* codes, int64_t ldc, void* scales, int64_t lds, uint8_t* zeros,

@@ -220,7 +220,7 @@ int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const v
     const int64_t size = dtype == OZIMMU_LM_F32 ? 4 : 2;
     for (int64_t at = 0; at < p; at += plan.rows) {
         t.p = t.b_rows = p - at < plan.rows ? p - at : plan.rows;
-        CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, false, st)));
+        CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, true, st)));
         t.D = (uint8_t*)D + at * size;
         t.shape = lmk::tile_shape(t.m, t.n, t.p, t.splits);
         CHECK(launched(lmk::launch_tile(t, st)));
@@ -336,7 +336,7 @@ int ozimmu_lm_dequantize(int type, int64_t p, int64_t n, int group, int zeros, i
     CHECK(packed_status(packed, p, n, group, scale_type));
     if (p == 0 || n == 0) return OZIMMU_OK;
     const lmk::Weights w{Shape{p, n, group, zeros != 0}, scale_type, (const uint8_t*)packed};
-    return launched(lmk::launch_dequantize(type, w, 0, p, n, W, ldw, true, (hipStream_t)stream));
+    return launched(lmk::launch_dequantize(type, w, 0, p, n, W, ldw, false, (hipStream_t)stream));
 }
 
 static int plain_status(int64_t p, int64_t n, int group, const void* codes, int64_t ldc, const void* scales, int64_t lds, const void* zeros, int64_t ldz,
