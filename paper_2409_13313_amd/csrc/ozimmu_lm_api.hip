@@ -244,12 +244,12 @@ int64_t laid_out_rows(int64_t width, int64_t p)
 }
 
 // How a loss is taken: straight from memory (rows of the plan > 0) for few tokens, more of them where W would have to be laid out for the tiles, and where
-// there is little to do.  (us, straight and by tiles: 1 x 4096 x 32768 56 and 71, rows that begin anywhere 113 and 181;  32 rows 77 and 75, anywhere 156 and
-// 190;  48 rows anywhere 188 and 192;  64 rows anywhere 205 and 193;  24 x 8192 x 16384 anywhere 147 and 219;  64 x 1001 x 10007 20.5 and 29.3;  133 x 1001 x
-// 5003 18.8 and 27;  16 x 512 x 2048 7.0 and 13.8.)
+// there is little to do.  (us, straight and by tiles: 1 x 4096 x 32768 56 and 71, rows at odd elements 73 and 181;  32 rows 74 and 73;  40 rows 82 and 75;
+// 64 rows at odd elements 123 and 194;  96 rows 201 and 196;  133 x 1001 x 5003 19 and 27, at odd elements 21 and 27;  64 x 1001 x 10007 at odd elements 23 and
+// 29;  128 rows 38 and 30;  16 x 512 x 2048 7.0 and 13.8.)
 lmk::FewPlan few_plan(int64_t m, int64_t n, int64_t p, bool aligned)
 {
-    if (m > (aligned ? 32 : 48) && (double)m * (double)n * (double)p >= 1e9) return {0, 0};
+    if (m > (aligned ? 32 : 64) && (double)m * (double)n * (double)p >= 1e9) return {0, 0};
     const int rows = m <= 16 ? 16 : m <= 32 ? 32 : 64;
     return {rows, m > 4 && (m + rows - 1) / rows * ((p + 63) / 64) >= 128 ? 64 : 16};
 }

@@ -36,9 +36,12 @@ template <class F> __device__ inline float over_sixteen(float v, F&& f)
 // while the other is multiplied; operands come from memory into registers as the matrix instruction wants them, from rows that begin
 // anywhere.  The waves' sums meet in LDS in a fixed order, and 16 lanes make a row's part of them.
 //
-// Bound by reading W: 1 x 4096 x 32768 43 us, 268 MB at 6.2 TB/s, what a kernel that only reads reaches; of rows that begin at odd elements 100 us, as every
-// 16 bytes then lie in two requests.
-template <int TYPE, int MF, int PF, int WAVES> __global__ __launch_bounds__(64 * WAVES) void k_few_loss(FewLoss g)
+// Bound by reading W: 1 x 4096 x 32768 43 us, 268 MB at 6.2 TB/s, what a kernel that only reads reaches.
+//
+// ODD: rows may begin at odd elements.  A load of 16 bytes takes twice as long where it does not begin at a whole word, so whole words are loaded, one more
+// where the elements begin in the middle of one, and shifted when they are multiplied (1 x 4096 x 32768, rows 4097 apart: 73 us, else 113; 4098 apart 68).  (A word that is loaded holds an element of the row: what lies
+// beside it in that word, also before the first row or behind the last, is shifted out.)
+template <int TYPE, int MF, int PF, int WAVES, bool ODD> __global__ __launch_bounds__(64 * WAVES) void k_few_loss(FewLoss g)
 {
     typedef typename Elem<TYPE>::Bits Bits;
     constexpr int PIECE = 64, COLUMNS = 16 * PF, PITCH = COLUMNS + 4;
@@ -53,6 +56,18 @@ template <int TYPE, int MF, int PF, int WAVES> __global__ __launch_bounds__(64 *
     for (int i = 0; i < MF; ++i) x_at[i] = (const Bits*)g.X + min(row0 + 16 * i + (lane & 15), g.m - 1) * g.ldx + (lane >> 4) * 8;
 #pragma unroll
     for (int f = 0; f < PF; ++f) w_at[f] = (const Bits*)g.W + min(col0 + 16 * f + (lane & 15), g.p - 1) * g.ldw + (lane >> 4) * 8;
+    // ODD: to the word that the row begins in, and the bits in front of it there
+    uint32_t x_shift[MF], w_shift[PF];
+    if constexpr (ODD) {
+        auto to_word = [](const Bits*& p, uint32_t& shift) {
+            shift = (uint32_t)(uintptr_t)p % 4 * 8;
+            p -= shift / 16;
+        };
+#pragma unroll
+        for (int i = 0; i < MF; ++i) to_word(x_at[i], x_shift[i]);
+#pragma unroll
+        for (int f = 0; f < PF; ++f) to_word(w_at[f], w_shift[f]);
+    }
     const int n = (int)g.n, left = n - (lane >> 4) * 8, pieces = (n + PIECE - 1) / PIECE;
 
     v4f acc[MF][PF];
@@ -62,6 +77,19 @@ template <int TYPE, int MF, int PF, int WAVES> __global__ __launch_bounds__(64 *
         for (int f = 0; f < PF; ++f) acc[i][f] = v4f{0, 0, 0, 0};
     struct Piece {
         v4i x[MF][2], w[PF][2];
+        uint32_t x_last[MF][2], w_last[PF][2];  // ODD
+    };
+    // (no further word where the eight end with the fourth)
+    auto last_word = [](const Bits* p, uint32_t shift) {
+        uint32_t last;
+        __builtin_memcpy(&last, p + (shift ? 8 : 6), 4);
+        return last;
+    };
+    auto shifted = [](v4i v, uint32_t last, uint32_t shift) {
+        if constexpr (!ODD) return v;
+        const uint32_t a = (uint32_t)v[0], b = (uint32_t)v[1], c = (uint32_t)v[2], d = (uint32_t)v[3];
+        return v4i{(int)__builtin_amdgcn_alignbit(b, a, shift), (int)__builtin_amdgcn_alignbit(c, b, shift), (int)__builtin_amdgcn_alignbit(d, c, shift),
+                   (int)__builtin_amdgcn_alignbit(last, d, shift)};
     };
     auto load = [&](int piece, Piece& o) __attribute__((always_inline)) {
 #pragma unroll
@@ -71,22 +99,36 @@ template <int TYPE, int MF, int PF, int WAVES> __global__ __launch_bounds__(64 *
 #pragma unroll
             for (int f = 0; f < PF; ++f) {
                 o.w[f][h] = v4i{0, 0, 0, 0};
-                if (there) __builtin_memcpy(&o.w[f][h], w_at[f] + k, 16);
+                if constexpr (ODD) o.w_last[f][h] = 0;
+                if (there) {
+                    __builtin_memcpy(&o.w[f][h], w_at[f] + k, 16);
+                    if constexpr (ODD) o.w_last[f][h] = last_word(w_at[f] + k, w_shift[f]);
+                }
             }
 #pragma unroll
             for (int i = 0; i < MF; ++i) {
                 o.x[i][h] = v4i{0, 0, 0, 0};
-                if (there) __builtin_memcpy(&o.x[i][h], x_at[i] + k, 16);
+                if constexpr (ODD) o.x_last[i][h] = 0;
+                if (there) {
+                    __builtin_memcpy(&o.x[i][h], x_at[i] + k, 16);
+                    if constexpr (ODD) o.x_last[i][h] = last_word(x_at[i] + k, x_shift[i]);
+                }
             }
         }
     };
     auto multiply = [&](const Piece& o) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
+            v4i w[PF];
 #pragma unroll
-            for (int i = 0; i < MF; ++i)
+            for (int f = 0; f < PF; ++f) w[f] = shifted(o.w[f][h], o.w_last[f][h], w_shift[f]);
 #pragma unroll
-                for (int f = 0; f < PF; ++f) acc[i][f] = mfma<TYPE>(o.x[i][h], o.w[f][h], acc[i][f]);
+            for (int i = 0; i < MF; ++i) {
+                const v4i x = shifted(o.x[i][h], o.x_last[i][h], x_shift[i]);
+#pragma unroll
+                for (int f = 0; f < PF; ++f) acc[i][f] = mfma<TYPE>(x, w[f], acc[i][f]);
+            }
+        }
     };
     Piece o[2];
     if (wave < pieces) load(wave, o[0]);
@@ -100,6 +142,16 @@ template <int TYPE, int MF, int PF, int WAVES> __global__ __launch_bounds__(64 *
     }
     // the eight elements that a row ends in, where they are not whole: zeros for the others
     if (n % 8 != 0 && wave == (pieces - 1) % WAVES) {
+        if constexpr (ODD) {  // (one by one, and nothing to shift)
+            auto to_row = [](const Bits*& p, uint32_t& shift) {
+                p += shift / 16;
+                shift = 0;
+            };
+#pragma unroll
+            for (int i = 0; i < MF; ++i) to_row(x_at[i], x_shift[i]);
+#pragma unroll
+            for (int f = 0; f < PF; ++f) to_row(w_at[f], w_shift[f]);
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int k = (pieces - 1) * PIECE + 32 * h, here = left - k;
@@ -160,7 +212,8 @@ template <int TYPE, int MF, int PF, int WAVES> __global__ __launch_bounds__(64 *
 template <int TYPE, int MF, int PF, int WAVES> void run(const FewLoss& g, hipStream_t st)
 {
     const dim3 grid((unsigned)((g.p + 16 * PF - 1) / (16 * PF)), (unsigned)((g.m + 16 * MF - 1) / (16 * MF)));
-    k_few_loss<TYPE, MF, PF, WAVES><<<grid, dim3(64 * WAVES), 0, st>>>(g);
+    const bool odd = (((uintptr_t)g.X | (uintptr_t)g.W) % 4 | (g.ldx | g.ldw) % 2) != 0;
+    odd ? k_few_loss<TYPE, MF, PF, WAVES, true><<<grid, dim3(64 * WAVES), 0, st>>>(g) : k_few_loss<TYPE, MF, PF, WAVES, false><<<grid, dim3(64 * WAVES), 0, st>>>(g);
 }
 template <int TYPE> void run(const FewLoss& g, const lmk::FewPlan& plan, hipStream_t st)
 {

@@ -277,3 +277,24 @@ def test_a_workspace_of_the_users_and_one_too_small(lm):
             assert (room[need:] == 255).all()
             with pytest.raises(OzimmuError):
                 call()
+
+
+@pytest.mark.parametrize("m,n,p", [(1, 8, 16), (1, 96, 300), (3, 1001, 70), (20, 130, 500), (33, 64, 200), (48, 515, 1000)])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_rows_that_begin_at_odd_elements_beside_nan(lm, m, n, p, kind):
+    """The same numbers wherever their rows begin, in memory that is full of NaN elsewhere."""
+    X, W, y = layer(m, n, p, kind, m + n + p)
+
+    def placed(t, begin, ld):
+        room = torch.full((begin + len(t) * ld,), float("nan"), device="cuda", dtype=t.dtype)
+        at = room.as_strided((len(t), n), (ld, 1), begin)
+        at.copy_(t)
+        return at
+    even = n + n % 2 + 2                                        # (neither of whole 16 bytes where it matters which plan is taken, nor odd)
+    even += 2 * (even % 8 == 0)
+    want = lm.cross_entropy(placed(X, 2, even), placed(W, 2, even), y)
+    loss, lse, size = exact(X, W, y)
+    assert ((want[0].double() - loss).abs() <= 2 * size + 40 * 2.0 ** -24 * (1 + lse.abs())).all()
+    for x, w in (((1, even), (1, even)), ((1, even + 1), (2, even)), ((2, even), (2, even + 1)), ((1, n + 1 - n % 2), (1, n + 1 - n % 2))):
+        got = lm.cross_entropy(placed(X, *x), placed(W, *w), y)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (x, w)
