@@ -39,8 +39,8 @@ template <class F> __device__ inline float over_sixteen(float v, F&& f)
 // Bound by reading W: 1 x 4096 x 32768 43 us, 268 MB at 6.2 TB/s, what a kernel that only reads reaches.
 //
 // ODD: rows may begin at odd elements.  A load of 16 bytes takes twice as long where it does not begin at a whole word, so whole words are loaded, one more
-// where the elements begin in the middle of one, and shifted when they are multiplied (1 x 4096 x 32768, rows 4097 apart: 73 us, else 113; 4098 apart 68).  (A word that is loaded holds an element of the row: what lies
-// beside it in that word, also before the first row or behind the last, is shifted out.)
+// where the elements begin in the middle of one, and shifted when they are multiplied (1 x 4096 x 32768, rows 4097 apart: 73 us, else 113; 4098 apart 68).
+// (A word that is loaded holds an element of the row: what lies beside it in that word, also before the first row or behind the last, is shifted out.)
 template <int TYPE, int MF, int PF, int WAVES, bool ODD> __global__ __launch_bounds__(64 * WAVES) void k_few_loss(FewLoss g)
 {
     typedef typename Elem<TYPE>::Bits Bits;

@@ -356,7 +356,12 @@ template <int XTYPE> __device__ inline v4i numbers(uint32_t w, float zero)
 // STREAM: codes past the caches, of weights that do not fit into the 256 MB of the memory-side cache (293 MB, one row: 57 us, else 61).  Smaller ones may
 // stay there from one token to the next, and then it costs (8.7 MB, one row: 5.0 and 4.3 us; 70 MB, 16 rows, three such matrices in turn: 18.9 and 18.2; ten
 // of them 19.1 and 20.7).
-template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR, bool STREAM>
+//
+// ODD, for more than four rows: rows of X may begin at odd elements.  A load of 16 bytes takes twice as long where it does not begin at a whole word, and
+// each of X is made by every workgroup; so whole words are loaded, one more where the elements begin in the middle of one, and shifted when they are
+// multiplied (16 x 4099 x 4096, rows 4099 apart: 8.7 us, else 13.7; 4100 apart 6.8;  37 x 2051 x 1283: 11.3, else 14.1; 9.2).  (A word that is loaded holds an
+// element of the row: what lies beside it in that word is shifted out.)
+template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR, bool STREAM, bool ODD>
 __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
 {
     static_assert(!FOUR || MF == 1, "four rows are one fragment");
@@ -385,6 +390,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
         const int64_t row = row0 + 16 * i + (FOUR ? (lane & 15) >> 2 : lane & 15);
         x_at[i] = (const Bits*)g.X + (row < g.m ? row : g.m - 1) * g.ldx + (lane >> 4) * 8;
     }
+    // ODD: to the word that the row begins in, and the bits in front of it there
+    uint32_t shift[MF];
+    if constexpr (ODD)
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            shift[i] = (uint32_t)(uintptr_t)x_at[i] % 4 * 8;
+            x_at[i] -= shift[i] / 16;
+        }
     const int left = (int)s.n - (lane >> 4) * 8;  // elements of a row from this lane's first on
 
     float acc[MF][PF][R];
@@ -399,7 +412,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
         v4i code;
         Record<GROUP> record;
     };
-    auto load = [&](int kb, Stored (&o)[PF], v4i (&x)[MF][4]) __attribute__((always_inline)) {
+    struct Rows {
+        v4i x[MF][4];
+        uint32_t last[MF][4];  // ODD: the words behind them
+    };
+    auto load = [&](int kb, Stored (&o)[PF], Rows& rows) __attribute__((always_inline)) {
 #pragma unroll
         for (int f = 0; f < PF; ++f) {
             const v4i* const from = (const v4i*)(code_at[f] + (int64_t)kb * BLOCK_BYTES);
@@ -410,12 +427,27 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
         for (int i = 0; i < MF; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                x[i][j] = v4i{0, 0, 0, 0};
-                if (left - kb * INNER - 32 * j >= 8) __builtin_memcpy(&x[i][j], x_at[i] + kb * INNER + 32 * j, 16);
+                const Bits* const from = x_at[i] + kb * INNER + 32 * j;
+                rows.x[i][j] = v4i{0, 0, 0, 0};
+                if constexpr (ODD) rows.last[i][j] = 0;
+                if (left - kb * INNER - 32 * j >= 8) {
+                    __builtin_memcpy(&rows.x[i][j], from, 16);
+                    // (none where the eight end with the fourth)
+                    if constexpr (ODD) __builtin_memcpy(&rows.last[i][j], from + (shift[i] ? 8 : 6), 4);
+                }
             }
     };
     const v4i ones = {0x3f803f80, 0x3f803f80, 0x3f803f80, 0x3f803f80};
-    auto multiply = [&](const Stored (&o)[PF], const v4i (&x)[MF][4]) __attribute__((always_inline)) {
+    auto multiply = [&](const Stored (&o)[PF], Rows& rows) __attribute__((always_inline)) {
+        v4i(&x)[MF][4] = rows.x;
+        if constexpr (ODD)
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[i][j][e] = (int)__builtin_amdgcn_alignbit(e < 3 ? (uint32_t)x[i][j][e + 1 & 3] : rows.last[i][j], (uint32_t)x[i][j][e], shift[i]);
         static_for<0, GROUPS>([&](auto Q) __attribute__((always_inline)) {
             constexpr int q = decltype(Q)::value;
             v4f xs[MF];
@@ -451,7 +483,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
 
     // one block on its way while the other is multiplied
     Stored o[2][PF];
-    v4i x[2][MF][4];
+    Rows x[2];
     if (wave < KB) load(wave, o[0], x[0]);
     for (int kb = wave; kb < KB; kb += 2 * WAVES) {
         if (kb + WAVES < KB) load(kb + WAVES, o[1], x[1]);
@@ -464,6 +496,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
     // the eight elements that a row ends in, where they are not whole: zeros for the others
     if (s.n % 8 != 0 && wave == (KB - 1) % WAVES) {
         load(KB - 1, o[0], x[0]);
+        if constexpr (ODD)  // (one by one, and nothing to shift)
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                x_at[i] += shift[i] / 16;
+                shift[i] = 0;
+            }
 #pragma unroll
         for (int i = 0; i < MF; ++i)
 #pragma unroll
@@ -472,7 +510,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
                 Bits e[8];
 #pragma unroll
                 for (int n = 0; n < 8; ++n) e[n] = here < 8 && n < here ? x_at[i][(KB - 1) * INNER + 32 * j + n] : 0;
-                __builtin_memcpy(&x[0][i][j], e, 16);
+                __builtin_memcpy(&x[0].x[i][j], e, 16);
             }
         multiply(o[0], x[0]);
     }
@@ -752,7 +790,12 @@ template <int XTYPE> void shared(const Shared& a, const lmk::SharedPlan& plan, h
 template <int XTYPE, int GROUP, int MF, int PF, int WAVES, bool FOUR, bool STREAM = false> void direct(const Linear& g, const Weights& w, hipStream_t st)
 {
     const dim3 grid((unsigned)((w.shape.row_blocks() + PF - 1) / PF), (unsigned)((g.m + 16 * MF - 1) / (16 * MF)));
-    k_lm_direct<XTYPE, GROUP, MF, PF, WAVES, FOUR, STREAM><<<grid, dim3(64 * WAVES), 0, st>>>(g, w);
+    if constexpr (!FOUR)
+        if ((uintptr_t)g.X % 4 != 0 || g.ldx % 2 != 0) {
+            k_lm_direct<XTYPE, GROUP, MF, PF, WAVES, FOUR, STREAM, true><<<grid, dim3(64 * WAVES), 0, st>>>(g, w);
+            return;
+        }
+    k_lm_direct<XTYPE, GROUP, MF, PF, WAVES, FOUR, STREAM, false><<<grid, dim3(64 * WAVES), 0, st>>>(g, w);
 }
 
 template <int XTYPE, int GROUP> void direct(const Linear& g, const Weights& w, hipStream_t st)

@@ -181,3 +181,23 @@ def test_few_rows_of_wide_layers(lm, m, n, p, kind):
         X = rows(m, n, kind, n, 1)
         got = lm.linear(X, P, D=torch.empty((m, p), device="cuda", dtype=torch.float32))
         check(got, X.double() @ W.t(), bound(X, W, S, kind, "direct", group), "f32", (m, n, p, group))
+
+
+@pytest.mark.parametrize("m,n,p", [(5, 8, 40), (9, 96, 300), (16, 1001, 4100), (16, 257, 17000), (13, 1030, 17000), (31, 515, 1000), (32, 129, 9000), (60, 333, 2000),
+                                   (60, 264, 9000), (70, 130, 20000)])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_rows_that_begin_at_odd_elements_beside_nan(lm, m, n, p, kind):
+    """The same numbers wherever the rows of X begin, in memory that is full of NaN elsewhere."""
+    P, W, S = weights(lm, p, n, 64, True, "f16", m + n + p)
+    X = rows(m, n, kind, n)
+
+    def placed(begin, ld):
+        room = torch.full((begin + m * ld,), float("nan"), device="cuda", dtype=X.dtype)
+        at = room.as_strided((m, n), (ld, 1), begin)
+        at.copy_(X)
+        return at
+    for way in ("direct", "shared"):
+        want = lm.linear(placed(0, n + n % 2 + 2), P, dtype=torch.float32, way=way)
+        check(want, X.double() @ W.t(), bound(X, W, S, kind, way, 64), "f32", (m, n, p, way))
+        for begin, ld in ((1, n + n % 2 + 2), (0, n + 1 - n % 2), (1, n + 1 - n % 2), (1, n + 3 - n % 2)):
+            assert torch.equal(lm.linear(placed(begin, ld), P, dtype=torch.float32, way=way), want), (way, begin, ld)
