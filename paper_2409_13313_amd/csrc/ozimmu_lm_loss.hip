@@ -170,10 +170,23 @@ __global__ __launch_bounds__(256) void k_states(int64_t rows, int64_t cols, cons
         for (int e = 0; e < 8; ++e) x[e] = 0;
     } else {
         const float* const p = parts + row * ld + col;
-        v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 4);
-        for (int s = 1; s < splits; ++s) {
-            lo += *(const v4f*)(p + s * split_stride);
-            hi += *(const v4f*)(p + s * split_stride + 4);
+        v4f lo = {0, 0, 0, 0}, hi = lo;
+        // (eight splits on their way at a time: 18 tokens x 253 in 235 splits 24 us, one after the other 72)
+        for (int s = 0; s < splits; s += 8) {
+            v4f part[8][2];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                part[u][0] = part[u][1] = v4f{0, 0, 0, 0};
+                if (s + u < splits) {
+                    part[u][0] = *(const v4f*)(p + (s + u) * split_stride);
+                    part[u][1] = *(const v4f*)(p + (s + u) * split_stride + 4);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                lo += part[u][0];
+                hi += part[u][1];
+            }
         }
         const float f = g[row * g_stride] * scale;
 #pragma unroll
