@@ -18,7 +18,9 @@
  * A row whose target is `ignore` has loss 0, a row of zeros in dX and no part in dW, whatever X and g hold there.  A target that is neither `ignore` nor
  * one of 0 .. p - 1 has a NaN as its loss, in its row of dX and in all of dW.  z is never stored: the loss takes it a tile at a time, the gradient
  * computes it again, a piece of the vocabulary at a time.  X and W are of one 16-bit type.  Products are summed in FP32; the slopes
- * exp(z - lse) - [v = y] are rounded to 16 bits (FP16: times 2^15) before they are multiplied, as gradients of 16-bit logits are.
+ * exp(z - lse) - [v = y] are rounded to 16 bits (FP16: times 2^15) before they are multiplied, as gradients of 16-bit logits are.  For dW, X g / max|g| is
+ * rounded to 16 bits too: in BF16 to 8 digits; in FP16 to 11, or to 2^-21 of the largest |x| of its row where that is more, whatever g is (tokens whose |x g| is
+ * far below the largest are added in FP32, to a dW that is rounded twice then).
  *
  * Conventions are those of ozimmu_mx.h: row-major matrices with leading dimensions counted in elements, device pointers owned by the caller, no
  * allocation, all work enqueued on `stream`, OZIMMU_OK or a negative status, nothing enqueued when a check fails; rows may begin at any element of

@@ -163,8 +163,12 @@ hipError_t launch_join_rows(int64_t rows, int64_t blocks, const float2* parts, i
                             float* loss, float* lse, hipStream_t st);
 hipError_t launch_join(int64_t rows, int64_t blocks, const float2* parts, int64_t parts_ld, const Targets& targets, const float* at_target, float* loss,
                        float* lse, hipStream_t st);
+// FP16: the largest finite magnitude of each row of X
+hipError_t launch_row_peaks(int64_t rows, int64_t cols, const void* X, int64_t ldx, float* peaks, hipStream_t st);
 // What the gradient begins with: targets and log2(e) lse (NaN where the target is bad) per row, `padded` of them, the largest |g| of rows with a
-// target, X laid out (as x says) and, in `scaled` (nullptr: not wanted), X times each row's share of that |g|, zeros in rows without a target; and W laid out
+// target, X laid out (as x says) and, in `scaled` (nullptr: not wanted), X times each row's share of that |g|, zeros in rows without a target; and W laid out.
+// FP16 with `scaled`: that times a power of two, which `largest` is divided by; zeros also in rows too small for it, whose numbers are in `far` (as many as
+// the gradient has tokens at the most)
 struct Prepare {
     int64_t rows, padded;
     Targets targets;
@@ -173,6 +177,8 @@ struct Prepare {
     const float* lse;
     int* known;
     float *lse2, *largest;
+    const float* peaks;   // FP16 with `scaled`: of launch_row_peaks
+    int *far, *far_count;
     LayOut x;
     void* scaled;
     LayOut w;
@@ -181,6 +187,9 @@ hipError_t launch_prepare(int type, const Prepare& p, hipStream_t st);
 // dX <- g (the sum of the splits) / scale, zeros in rows without a target
 hipError_t launch_states(int type, int64_t rows, int64_t cols, const float* parts, int64_t ld, int splits, int64_t split_stride, const float* g,
                          int64_t g_stride, const int* targets, float scale, void* dX, int64_t ldx, hipStream_t st);
+// FP16: dW (of `type`) += what the rows in `far` give, from slopes (times SLOPE_SCALE_F16), X and g
+hipError_t launch_far(int type, int64_t words, int64_t cols, const uint16_t* slopes, int64_t lds, const void* X, int64_t ldx, const float* g, int64_t g_stride,
+                      const int* far, const int* far_count, void* dW, int64_t ldw, hipStream_t st);
 // X <- beta X (beta == 0: zeros)
 hipError_t launch_scale(int type, int64_t rows, int64_t cols, float beta, void* X, int64_t ldx, hipStream_t st);
 

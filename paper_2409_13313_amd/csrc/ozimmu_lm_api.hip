@@ -282,8 +282,8 @@ struct LossPlan {
 struct GradientPlan {
     int64_t padded, width, states_ld, words;   // rows and columns of whole tiles; words at a time
     int splits;
-    int* known;
-    float *lse2, *largest, *states;
+    int *known, *far, *far_count;
+    float *lse2, *largest, *peaks, *states;
     uint16_t *slopes, *X, *scaled, *W;
     size_t bytes;
     GradientPlan(int64_t m, int64_t n, int64_t p, void* workspace)
@@ -302,6 +302,9 @@ struct GradientPlan {
         known = room.take<int>(padded);
         lse2 = room.take<float>(padded);
         largest = room.take<float>(1);
+        peaks = room.take<float>(m);
+        far = room.take<int>(m);
+        far_count = room.take<int>(1);
         slopes = room.take<uint16_t>(padded * words);
         states = room.take<float>(splits * padded * states_ld);
         X = room.take<uint16_t>(m * width);
@@ -507,8 +510,9 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
         const int64_t ldw_at = lay_out ? plan.width : ldw;
         if (v0 == 0) {
             const lmk::LayOut x{m, n, X, ldx, lay_out ? plan.X : nullptr, plan.width};
-            CHECK(launched(lmk::launch_prepare(type, {m, plan.padded, {y, y_stride, ignore, p}, g, g_stride, lse, plan.known, plan.lse2, plan.largest, x,
-                                                      dW ? plan.scaled : nullptr, w}, st)));
+            if (dW && type == lmk::F16) CHECK(launched(lmk::launch_row_peaks(m, n, X, ldx, plan.peaks, st)));
+            CHECK(launched(lmk::launch_prepare(type, {m, plan.padded, {y, y_stride, ignore, p}, g, g_stride, lse, plan.known, plan.lse2, plan.largest, plan.peaks,
+                                                      plan.far, plan.far_count, x, dW ? plan.scaled : nullptr, w}, st)));
         } else if (lay_out) {
             CHECK(launched(lmk::launch_lay_out(type, w, {}, st)));
         }
@@ -566,6 +570,8 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
             if (!lmk::tile_fits(s)) return OZIMMU_ERR_DIM;
             s.shape = lmk::tile_shape(s.m, s.n, s.p, s.splits);
             CHECK(launched(lmk::launch_tile(s, st)));
+            if (type == lmk::F16)
+                CHECK(launched(lmk::launch_far(dw_type, words, n, plan.slopes, whole, X, ldx, g, g_stride, plan.far, plan.far_count, s.D, lddw, st)));
         }
     }
     if (dX)

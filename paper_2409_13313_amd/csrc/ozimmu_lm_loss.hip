@@ -32,14 +32,51 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_lay_out(LayOut a, L
     }
 }
 
+// The largest finite |x| of each row in FP16: a wave a row.  Memory: 4096 x 4096 in FP16, 34 MB, 9 to 10 us.
+__global__ __launch_bounds__(256) void k_row_peaks(int64_t rows, int64_t cols, const uint16_t* X, int64_t ldx, float* peaks)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    int most = 0;
+    for (int64_t col = lane * 8; col < cols; col += 64 * 8) {
+        uint16_t x[8];
+        load_row<F16, 8>(X + row * ldx + col, cols - col, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int magnitude = x[e] & 0x7fff;
+            most = max(most, magnitude < 0x7c00 ? magnitude : 0);
+        }
+    }
+    for (int far = 1; far < 64; far *= 2) most = max(most, __shfl_xor(most, far));
+    if (lane == 0) peaks[row] = to_float<F16>((uint16_t)most);
+}
+
+// dW in FP16.  A row of X times its share of the largest |g| may lie anywhere below the numbers of FP16, so what is held is X times the share times 2^up: the
+// largest of all lies in 2^14 .. 2^15 then, and 2^-up times the largest |g| stands in front of the sums.  (No more than leaves 2^-15 times that, which is what
+// the sums are multiplied by, a normal number.)
+__device__ inline int share_exponent(float most, float peak)
+{
+    if (!(most > 0.0f && most < __builtin_inff())) return 0;
+    // (a peak that is none of FP32's normal numbers says nothing; without it nothing can overflow)
+    const int up = peak >= 0x1p-100f && peak < __builtin_inff() ? 15 - __builtin_amdgcn_frexp_expf(peak / most) : 0;
+    return min(up, 110 + __builtin_amdgcn_frexp_expf(most));
+}
+// Rows whose largest element lies 2^18 or more below that are not held so: what FP16 cuts off there, 2^-25, is more than 2^-21 of it.  They are added to dW in
+// FP32 (k_far).  A row that is not made smaller than X itself loses nothing that X has.
+__device__ inline bool is_far(float own, float share, float peak)
+{
+    return own != 0.0f && peak > 0.0f && fabsf(share) < 1.0f && fabsf(share) * peak < 0x1p-4f;
+}
+
 // Every workgroup finds the largest |g| for itself, so that one launch does.  (With it in front, the slopes and each row's share of it lie in -1 .. 1, and
 // a g that is the same for all rows costs no rounding.)  4096 x 4096 states scaled: 40 us, 777 x 1001 states and 10007 words laid out 13; of a step's
 // 12 ms and 147 us.
 template <int TYPE> __global__ __launch_bounds__(256) void k_prepare(Prepare p)
 {
-    __shared__ float of_wave[4];
+    __shared__ float of_wave[4], of_wave_peak[4];
     const int t = threadIdx.x;
-    const bool first = blockIdx.x == 0;
+    const bool first = blockIdx.x == 0, raised = TYPE == F16 && p.scaled;
     const int64_t begin = (int64_t)blockIdx.x * 256 + t, step = (int64_t)gridDim.x * 256;
     // (W first, which needs no |g|, from the last workgroups on, which have less of X)
     const int64_t of_w = p.w.Y ? p.w.rows * (p.w.width / 8) : 0;
@@ -47,29 +84,106 @@ template <int TYPE> __global__ __launch_bounds__(256) void k_prepare(Prepare p)
         uint16_t x[8];
         lay_out<TYPE>(p.w, at, x);
     }
-    float most = 0.0f;
+    float most = 0.0f, peak = 0.0f;
     for (int64_t r = t; r < p.padded; r += 256) {
         const int target = r < p.rows ? p.targets[r] : NO_TARGET;
-        if (target != NO_TARGET) most = fmaxf(most, fabsf(p.g[r * p.g_stride]));
+        if (target != NO_TARGET) {
+            const float own = fabsf(p.g[r * p.g_stride]);
+            most = fmaxf(most, own);
+            if (raised) peak = fmaxf(peak, own * p.peaks[r]);
+        }
         if (first) {
             p.known[r] = target;
             p.lse2[r] = target == BAD_TARGET ? __builtin_nanf("") : (target == NO_TARGET ? 0.0f : p.lse[r] * LOG2E);
         }
     }
-    for (int far = 1; far < 64; far *= 2) most = fmaxf(most, __shfl_xor(most, far));
-    if ((t & 63) == 0) of_wave[t >> 6] = most;
+    for (int far = 1; far < 64; far *= 2) {
+        most = fmaxf(most, __shfl_xor(most, far));
+        if (raised) peak = fmaxf(peak, __shfl_xor(peak, far));
+    }
+    if ((t & 63) == 0) {
+        of_wave[t >> 6] = most;
+        of_wave_peak[t >> 6] = peak;
+    }
     __syncthreads();
     most = fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
-    if (first && t == 0) *p.largest = most;
+    peak = fmaxf(fmaxf(of_wave_peak[0], of_wave_peak[1]), fmaxf(of_wave_peak[2], of_wave_peak[3]));
+    const int up = raised ? share_exponent(most, peak) : 0;
+    if (first && t == 0) *p.largest = ldexpf(most, -up);
+    // g, times 2^up over the largest |g|
+    auto share_of = [&](float own) { return own == 0.0f ? 0.0f : ldexpf(own / most, up); };
+    if (first && raised) {
+        // the rows that are added in FP32, in their order
+        __shared__ int of_wave_far[4];
+        int count = 0;
+        for (int64_t base = 0; base < p.rows; base += 256) {
+            const int64_t r = base + t;
+            bool far = false;
+            if (r < p.rows && p.targets[r] != NO_TARGET) {
+                const float own = p.g[r * p.g_stride];
+                far = is_far(own, share_of(own), p.peaks[r]);
+            }
+            const uint64_t all = __ballot(far);
+            if ((t & 63) == 0) of_wave_far[t >> 6] = __popcll(all);
+            __syncthreads();
+            int at = count + __popcll(all & (((uint64_t)1 << (t & 63)) - 1));
+            for (int w = 0; w < 4; ++w) {
+                if (w < t >> 6) at += of_wave_far[w];
+                count += of_wave_far[w];
+            }
+            if (far) p.far[at] = (int)r;
+            __syncthreads();
+        }
+        if (t == 0) *p.far_count = count;
+    }
     const int64_t of_x = p.x.Y || p.scaled ? p.x.rows * (p.x.width / 8) : 0;
     for (int64_t at = begin; at < of_x; at += step) {
         uint16_t x[8];
         const int64_t row = lay_out<TYPE>(p.x, at, x);
         if (!p.scaled) continue;
-        const float own = p.targets[row] == NO_TARGET ? 0.0f : p.g[row * p.g_stride], ratio = own == 0.0f ? 0.0f : own / most;
+        const float own = p.targets[row] == NO_TARGET ? 0.0f : p.g[row * p.g_stride];
+        float share = share_of(own);
+        if (raised && is_far(own, share, p.peaks[row])) share = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = ratio == 0.0f ? 0 : from_float<TYPE>(ratio * to_float<TYPE>(x[e]));
+        for (int e = 0; e < 8; ++e) x[e] = share == 0.0f ? 0 : from_float<TYPE>(share * to_float<TYPE>(x[e]));
         __builtin_memcpy((uint16_t*)p.scaled + at * 8, x, 16);
+    }
+}
+
+// What the rows in `far` give to a piece of dW, added to it in FP32 and rounded once more.  Slopes are held times SLOPE_SCALE_F16, their rows whole tiles; a thread
+// has eight words and eight columns.  Mostly there are no such rows, and all it takes is a launch, 4.6 us; 100 of 4096 tokens, 16384 words x 4096: 610 us.
+template <int DTYPE>
+__global__ __launch_bounds__(256) void k_far(int64_t words, int64_t cols, const uint16_t* slopes, int64_t lds, const uint16_t* X, int64_t ldx, const float* g,
+                                             int64_t g_stride, const int* far, const int* far_count, typename Elem<DTYPE>::Bits* dW, int64_t ldw)
+{
+    const int count = *far_count;
+    if (count == 0) return;
+    const int64_t eights = (cols + 7) / 8, all = (words + 7) / 8 * eights;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
+        const int64_t word = at / eights * 8, col = at % eights * 8;
+        float sum[8][8] = {};
+        for (int i = 0; i < count; ++i) {
+            const int64_t row = far[i];
+            const float own = g[row * g_stride];
+            uint16_t slope[8], x[8];
+            __builtin_memcpy(slope, slopes + row * lds + word, 16);
+            load_row<F16, 8>(X + row * ldx + col, cols - col, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float of_x = own * to_float<F16>(x[e]);
+#pragma unroll
+                for (int w = 0; w < 8; ++w) sum[w][e] = __builtin_fmaf(to_float<F16>(slope[w]), of_x, sum[w][e]);
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            if (word + w >= words) break;
+            typename Elem<DTYPE>::Bits y[8];
+            load_row<DTYPE, 8>(dW + (word + w) * ldw + col, cols - col, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = from_float<DTYPE>(__builtin_fmaf(sum[w][e], 1.0f / lmk::SLOPE_SCALE_F16, to_float<DTYPE>(y[e])));
+            store_row<DTYPE, 8>(dW + (word + w) * ldw + col, cols - col, y);
+        }
     }
 }
 
@@ -229,6 +343,25 @@ hipError_t launch_prepare(int type, const Prepare& p, hipStream_t st)
     const dim3 grid(rounds_of((p.x.Y || p.scaled ? p.x.rows * (p.x.width / 8) : 0) + (p.w.Y ? p.w.rows * (p.w.width / 8) : 0)));
     if (type == BF16) k_prepare<BF16><<<grid, dim3(256), 0, st>>>(p);
     if (type == F16) k_prepare<F16><<<grid, dim3(256), 0, st>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_row_peaks(int64_t rows, int64_t cols, const void* X, int64_t ldx, float* peaks, hipStream_t st)
+{
+    k_row_peaks<<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st>>>(rows, cols, (const uint16_t*)X, ldx, peaks);
+    return hipGetLastError();
+}
+
+hipError_t launch_far(int type, int64_t words, int64_t cols, const uint16_t* slopes, int64_t lds, const void* X, int64_t ldx, const float* g, int64_t g_stride,
+                      const int* far, const int* far_count, void* dW, int64_t ldw, hipStream_t st)
+{
+    // (few workgroups: mostly all that they do is to begin and end)
+    const unsigned blocks = rounds_of((words + 7) / 8 * ((cols + 7) / 8));
+    const dim3 grid(blocks < 512 ? blocks : 512);
+    const auto* const x = (const uint16_t*)X;
+    if (type == F32) k_far<F32><<<grid, dim3(256), 0, st>>>(words, cols, slopes, lds, x, ldx, g, g_stride, far, far_count, (uint32_t*)dW, ldw);
+    if (type == BF16) k_far<BF16><<<grid, dim3(256), 0, st>>>(words, cols, slopes, lds, x, ldx, g, g_stride, far, far_count, (uint16_t*)dW, ldw);
+    if (type == F16) k_far<F16><<<grid, dim3(256), 0, st>>>(words, cols, slopes, lds, x, ldx, g, g_stride, far, far_count, (uint16_t*)dW, ldw);
     return hipGetLastError();
 }
 
