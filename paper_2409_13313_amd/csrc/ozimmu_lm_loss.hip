@@ -195,19 +195,21 @@ __device__ inline float2 join(float2 a, float2 b)
 }
 
 // A row's loss and lse from its parts' sum, which leaves out the target's own exponential, so that loss = log(1 + others / own) keeps its digits where
-// the target has nearly all of the row.
+// the target has nearly all of the row.  lse is made from the larger of the two, not as own + loss: a target far below the others (a word that may not be
+// taken, at -1e9 or at -infinity) would leave it the digits of its own magnitude, and the gradient takes exponentials of what is off.
 __device__ inline void finish(int64_t row, float2 sum, const Targets& targets, const float* at_target, float* loss, float* lse)
 {
     const int target = targets[row];
+    const float others = LN2 * (sum.x + log2f(sum.y));
     if (target >= 0) {
         const float own = at_target[row];
         const float x = LN2 * ((sum.x - own * LOG2E) + log2f(sum.y));  // log(others / own)
-        const float l = x > 0.0f ? x + log1pf(expf(-x)) : log1pf(expf(x));
-        loss[row] = l;
-        lse[row] = own + l;
+        const float rest = log1pf(expf(-fabsf(x)));
+        loss[row] = x > 0.0f ? x + rest : rest;
+        lse[row] = (x > 0.0f ? others : own) + rest;
     } else {
         loss[row] = target == BAD_TARGET ? __builtin_nanf("") : 0.0f;
-        lse[row] = LN2 * (sum.x + log2f(sum.y));
+        lse[row] = others;
     }
 }
 
