@@ -204,7 +204,8 @@ __device__ inline void finish(int64_t row, float2 sum, const Targets& targets, c
     if (target >= 0) {
         const float own = at_target[row];
         const float x = LN2 * ((sum.x - own * LOG2E) + log2f(sum.y));  // log(others / own)
-        const float rest = log1pf(expf(-fabsf(x)));
+        // (a logit of infinity has no share: infinity less infinity, as among the others)
+        const float rest = own == __builtin_inff() ? __builtin_nanf("") : log1pf(expf(-fabsf(x)));
         loss[row] = x > 0.0f ? x + rest : rest;
         lse[row] = (x > 0.0f ? others : own) + rest;
     } else {

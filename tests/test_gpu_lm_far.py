@@ -53,3 +53,18 @@ def test_targets_far_below_the_other_words(lm, m, n, p, pad, kind, bias):  # noq
     w[::5, 0] = w[::5, 0].clamp(min=-1e30)
     first = 1 if bias == float("-inf") else 0                         # (no slope times an infinity is a number)
     check_gradient(dX[:, first:], d, w[:, first:], g.double(), size, kind, "f32", False, "dX")
+
+
+@pytest.mark.parametrize("m,n,p,pad", SIZES)
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_a_logit_that_is_infinite(lm, m, n, p, pad, kind):  # noqa: F811
+    """Its row has neither a logarithm of a sum nor a loss that are numbers (infinity less infinity), whether it is the target's logit or not."""
+    X, W, y = masked(m, n, p, kind, pad, m + n, -100.0)
+    X[2, :] = 0
+    X[2, 0] = 1                                                       # (a row in which no other element meets the infinity)
+    for word in (int(y[2]), int(y[2]) + 1):
+        V = W.clone()
+        V[word, 0] = float("inf")
+        loss, lse = lm.cross_entropy(X, V, y)
+        learnt = y != IGNORE
+        assert torch.isnan(loss[learnt]).all() and torch.isnan(lse).all() and (loss[~learnt] == 0).all(), word
