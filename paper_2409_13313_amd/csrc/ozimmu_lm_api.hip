@@ -266,10 +266,11 @@ struct LossPlan {
         Room room{(uint8_t*)workspace};
         width = round_to(n, 64);
         const int64_t blocks = few.rows ? (p + few.columns - 1) / few.columns : (p + 63) / 64;
-        // tokens at a time: parts of at most 256 MB
-        tokens = ((int64_t)1 << 25) / blocks / 256 * 256;
-        if (tokens < 256) tokens = 256;
-        if (tokens > round_to(m, 256)) tokens = round_to(m, 256);
+        // tokens at a time, whole workgroups of them: parts of at most 256 MB (by tiles for 2^22 words, the most there are, 512 tokens)
+        const int64_t unit = few.rows ? few.rows : 256;
+        tokens = ((int64_t)1 << 25) / blocks / unit * unit;
+        if (tokens < unit) tokens = unit;
+        if (tokens > round_to(m, unit)) tokens = round_to(m, unit);
         words = laid_out_rows(width, p);
         at_target = room.take<float>(tokens);
         parts = room.take<float2>(blocks * tokens);
