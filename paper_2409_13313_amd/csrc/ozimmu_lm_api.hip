@@ -287,15 +287,17 @@ struct GradientPlan {
     float *lse2, *largest, *peaks, *states;
     uint16_t *slopes, *X, *scaled, *W;
     size_t bytes;
-    GradientPlan(int64_t m, int64_t n, int64_t p, void* workspace)
+    // lay_out: X and W are laid out anew
+    GradientPlan(int64_t m, int64_t n, int64_t p, bool lay_out, void* workspace)
     {
         Room room{(uint8_t*)workspace};
         padded = round_to(m, 256);
         width = round_to(n, 64);
         states_ld = round_to(n, 256);
-        // slopes of at most 128 MB, which stay in the memory-side cache for the two products that read them, and pieces of W of at most 1 GB
+        // slopes of at most 128 MB, which stay in the memory-side cache for the two products that read them (of 256 words at the least: from 262144 tokens on
+        // they take more), and pieces of W of at most 1 GB where it is, 256 MB where it is laid out
         words = ((int64_t)1 << 26) / padded / 256 * 256;
-        const int64_t most = ((int64_t)1 << 29) / width / 256 * 256;
+        const int64_t most = lay_out ? laid_out_rows(width, p) : ((int64_t)1 << 29) / width / 256 * 256;
         if (words > most) words = most;
         if (words < 256) words = 256;
         if (words > round_to(p, 256)) words = round_to(p, 256);
@@ -308,9 +310,9 @@ struct GradientPlan {
         far_count = room.take<int>(1);
         slopes = room.take<uint16_t>(padded * words);
         states = room.take<float>(splits * padded * states_ld);
-        X = room.take<uint16_t>(m * width);
         scaled = room.take<uint16_t>(m * width);
-        W = room.take<uint16_t>(words * width);
+        X = room.take<uint16_t>(lay_out ? m * width : 0);
+        W = room.take<uint16_t>(lay_out ? words * width : 0);
         bytes = room.used;
     }
 };
@@ -475,7 +477,10 @@ int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const voi
 
 size_t ozimmu_lm_cross_entropy_backward_workspace_bytes(int64_t m, int64_t n, int64_t p)
 {
-    return loss_sizes_ok(m, n, p) && m > 0 ? GradientPlan(m, n, p, nullptr).bytes : 0;
+    if (!loss_sizes_ok(m, n, p) || m == 0) return 0;
+    // (for rows that begin anywhere too)
+    const size_t a = GradientPlan(m, n, p, false, nullptr).bytes, b = GradientPlan(m, n, p, true, nullptr).bytes;
+    return a > b ? a : b;
 }
 
 int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, const float* g, int64_t g_stride, const void* X, int64_t ldx, const void* W,
@@ -499,9 +504,10 @@ int ozimmu_lm_cross_entropy_backward(int type, int64_t m, int64_t n, int64_t p, 
         if (dW && beta != 1.0f) return launched(lmk::launch_scale(dw_type, p, n, beta, dW, lddw, st));
         return OZIMMU_OK;
     }
-    const GradientPlan plan(m, n, p, workspace);
     // (W is read along its rows and across them, a piece of `words` rows at a time)
-    const bool lay_out = !as_it_is(X, n, ldx) || !as_it_is(W, n, ldw) || plan.words * ldw * 2 >= ((int64_t)1 << 32) - (1 << 20);
+    const bool lay_out = !as_it_is(X, n, ldx) || !as_it_is(W, n, ldw) ||
+                         GradientPlan(m, n, p, false, nullptr).words * ldw * 2 >= ((int64_t)1 << 32) - (1 << 20);
+    const GradientPlan plan(m, n, p, lay_out, workspace);
     const float unscale = type == OZIMMU_LM_F16 ? 1.0f / lmk::SLOPE_SCALE_F16 : 1.0f;
     int splits = 0;
     for (int64_t v0 = 0; v0 < p; v0 += plan.words) {
