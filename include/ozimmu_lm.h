@@ -62,10 +62,14 @@ int ozimmu_lm_unpack(int64_t p, int64_t n, int group, const void *packed, uint8_
                      uint8_t *zeros, int64_t ldz, void *stream);
 
 /* D <- alpha X W^T + beta D: X (device, m x n, of type xtype: BF16 or F16), W packed p x n, D (device, m x p, of type dtype).
- * Sums in FP32, alpha and beta applied in FP32, D rounded once; beta == 0: the old D is not read.  Up to a number of rows (by the library's
- * choice: about a thousand through 4096 x 4096) the codes are multiplied as they are and nothing else is rounded; beyond it the weights are read back in
- * the type of X, each rounded once (in FP16 infinite where they are beyond its range), a piece at a time.  In BF16 the first of the two forms sums
- * x (128 + q): a row of X that holds an infinity, or numbers of 2^113 and more, may give NaN.
+ * Sums in FP32, alpha and beta applied in FP32, D rounded once; beta == 0: the old D is not read.  There are two forms.  In the first, always taken up to 16
+ * rows, the codes are multiplied as they are and nothing else is rounded.  In BF16 it sums x (128 + q) and takes (128 + zero) times the sum of x off again: what
+ * passes through the FP32 sums is up to ten times larger than the values, and a row of X that holds an infinity, or numbers of 2^113 and more, may give NaN.
+ * In the second the weights are read back in the type of X, a piece at a time, each rounded once (in FP16 infinite beyond 65504, and to a multiple of 2^-24
+ * below 2^-14).  Between them the library chooses by estimated times, and a few hundred rows more may change the choice back: through 4096 x 4096 the codes
+ * are taken up to 960 rows, from 1025 to 1472 and from 2049 to 2368 (ozimmu_lm_linear_choose tells).  Results whose roundings may not depend on the
+ * number of rows are had from ozimmu_lm_linear_way.
+ * n is 1 at the least (nothing is stored of n = 0).
  * Workspace: 0 bytes (workspace may be NULL then) up to 16 rows, and for more of them where the codes are multiplied without splitting the sums. */
 size_t ozimmu_lm_linear_workspace_bytes(int64_t m, int64_t n, int64_t p);
 int ozimmu_lm_linear(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void *X, int64_t ldx, int group, int zeros, int scale_type,
@@ -83,8 +87,9 @@ int ozimmu_lm_linear_way(int way, int64_t m, int64_t n, int64_t p, float alpha, 
 size_t ozimmu_lm_linear_way_workspace_bytes(int way, int64_t m, int64_t n, int64_t p);
 int ozimmu_lm_linear_choose(int64_t m, int64_t n, int64_t p);
 
-/* loss and lse (device, FP32, m each) of X (m x n), W (p x n) of type `type` and targets (device, m, y_stride elements apart).  m n below
- * 2^31 - 2^20.  Workspace bytes: 0 for sizes out of range. */
+/* loss and lse (device, FP32, m each) of X (m x n), W (p x n) of type `type` and targets (device, m, y_stride elements apart).  n and p are 1 at the
+ * least, and m times n, each rounded up to a multiple of 256, is below 2^31 - 2^20.  A row with a logit of +infinity has a NaN as its lse (and, unless it is
+ * ignored, as its loss).  Workspace bytes: 0 for sizes out of range. */
 size_t ozimmu_lm_cross_entropy_workspace_bytes(int64_t m, int64_t n, int64_t p);
 int ozimmu_lm_cross_entropy(int type, int64_t m, int64_t n, int64_t p, const void *X, int64_t ldx, const void *W, int64_t ldw, const int64_t *y,
                             int64_t y_stride, int64_t ignore, float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream);
