@@ -66,9 +66,8 @@ int ozimmu_lm_unpack(int64_t p, int64_t n, int group, const void *packed, uint8_
  * rows, the codes are multiplied as they are and nothing else is rounded.  In BF16 it sums x (128 + q) and takes (128 + zero) times the sum of x off again: what
  * passes through the FP32 sums is up to ten times larger than the values, and a row of X that holds an infinity, or numbers of 2^113 and more, may give NaN.
  * In the second the weights are read back in the type of X, a piece at a time, each rounded once (in FP16 infinite beyond 65504, and to a multiple of 2^-24
- * below 2^-14).  Between them the library chooses by estimated times, and a few hundred rows more may change the choice back: through 4096 x 4096 the codes
- * are taken up to 960 rows, from 1025 to 1472 and from 2049 to 2368 (ozimmu_lm_linear_choose tells).  Results whose roundings may not depend on the
- * number of rows are had from ozimmu_lm_linear_way.
+ * below 2^-14).  The library takes the first up to 512 rows, or up to m p = 2^21 where that is more of them, and the second beyond (ozimmu_lm_linear_choose
+ * tells); results whose roundings may not depend on the number of rows are had from ozimmu_lm_linear_way.
  * n is 1 at the least (nothing is stored of n = 0).
  * Workspace: 0 bytes (workspace may be NULL then) up to 16 rows, and for more of them where the codes are multiplied without splitting the sums. */
 size_t ozimmu_lm_linear_workspace_bytes(int64_t m, int64_t n, int64_t p);

@@ -120,7 +120,6 @@ struct Tile {
 };
 bool tile_fits(const Tile& t);
 int tile_shape(int64_t m, int64_t n, int64_t p, int splits);   // the one that takes the least time, by an estimate
-double tile_us(int64_t m, int64_t n, int64_t p);                // that estimate
 int tile_splits(int64_t m, int64_t n, int64_t p);             // STATES: the number of splits that does
 inline int part_columns(int shape) { return shape == TILE_128 ? 64 : 128; }  // LOSS: columns of a part
 hipError_t launch_tile(const Tile& t, hipStream_t st);

@@ -47,12 +47,6 @@ int tile_shape(int64_t m, int64_t n, int64_t p, int splits)
     return best;
 }
 
-double tile_us(int64_t m, int64_t n, int64_t p)
-{
-    const int shape = tile_shape(m, n, p, 1);
-    return estimate_us(shape, tiles_of(shape, m, p), (double)((n + 63) / 64));
-}
-
 // The number of splits of n, four stages each at the least, that takes the least time; the sums of each are written and read again in FP32
 int tile_splits(int64_t m, int64_t n, int64_t p)
 {
@@ -184,16 +178,17 @@ size_t shared_bytes(int64_t m, int64_t n, int64_t p)
 }
 
 // Up to 16 rows from the codes in one launch, in any case (callers need not ask for a workspace then), and more of them where there is little to do (128
-// rows through 512 x 512: 5.6 us, with X in LDS 6.9; 37 rows through 2051 x 1283: 9.4, 11.1; 32 rows through 4096 x 4096: 11.5 and 11.4; 256 rows: 38 and 25).  Beyond, estimates
-// fitted to (rows x n x p: X in LDS, weights read back)  256 x 1024 x 16384: 22, 38;  512 x 4096 x 4096: 34, 52;  1024 x 4096 x 4096: 53, 53;  2048 x 4096 x
-// 4096: 90, 75;  4096 x 4096 x 16384: 630, 460.
-constexpr int64_t DIRECT_ROWS = 16;
+// rows through 512 x 512: 5.6 us, with X in LDS 6.9; 37 rows through 2051 x 1283: 9.4, 11.1; 32 rows through 4096 x 4096: 10.6 and 12.1; 256 rows: 38 and 24).
+// Beyond, weights are read back from one number of rows on, so that what is rounded does not change back and forth with them: behind 512, or where the outputs
+// come to more than 128 tiles of 128 x 128, whichever is later.  (us, n x p, rows: X in LDS, weights read back)  4096 x 4096, 512: 36, 48;  640: 53, 48;  1024: 55,
+// 48;  1200: 69, 62;  2048: 88, 68;  2100: 144, 87;  4096 x 16384, 384: 75, 80;  640: 146, 117;  8192 x 8192, 512: 99, 96;  640: 127, 119;  4096 x 1024, 1024: 26, 40;
+// 2048: 38, 41;  2100: 54, 41;  2048 x 2048, 960: 24, 29;  1100: 31, 29;  2048 x 256, 6000: 24, 28;  8192: 26, 24.  It is the slower one right behind 512 rows where the
+// inner dimension is short: 1024 x 4096, 1100: 25, 30;  512 x 8192, 640: 18, 21 (1100: 40, 32).
+constexpr int64_t DIRECT_ROWS = 16, CODES_ROWS = 512, CODES_OUTPUTS = (int64_t)1 << 21;
 int choose(int64_t m, int64_t n, int64_t p)
 {
-    const double weights = (double)p * (double)n;
-    if (m <= DIRECT_ROWS || (m <= 128 && (double)m * weights < 1 << 27)) return OZIMMU_LM_WAY_DIRECT;
-    const double shared = 8 + 2.4e-6 * (double)round_to(m, 64) * weights * 1e-3, tile = 3 + weights / 1.8e6 + lmk::tile_us(m, n, p);
-    return shared <= tile ? OZIMMU_LM_WAY_SHARED : OZIMMU_LM_WAY_TILE;
+    if (m <= DIRECT_ROWS || (m <= 128 && (double)m * (double)p * (double)n < 1 << 27)) return OZIMMU_LM_WAY_DIRECT;
+    return m <= CODES_ROWS || m * p <= CODES_OUTPUTS ? OZIMMU_LM_WAY_SHARED : OZIMMU_LM_WAY_TILE;
 }
 
 int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const void* X, int64_t ldx, const lmk::Weights& w, float beta, int dtype, void* D,

@@ -17,12 +17,14 @@ def lib():
     return lm._lib
 
 
-def test_rows_of_which_the_codes_are_taken_as_they_are(lib):
+@pytest.mark.parametrize("n,p", [(4096, 4096), (512, 1024), (4096, 1000), (2048, 300), (64, 4097), (8192, 32768), (1, 1)])
+def test_weights_are_read_back_from_one_number_of_rows_on(lib, n, p):
     text = re.sub(r"\s*\n \* ", " ", open(os.path.join(ROOT, "include", "ozimmu_lm.h")).read())
-    first, *others = re.search(r"through 4096 x 4096 the codes are taken up to (\d+) rows, from (\d+) to (\d+) and from (\d+) to (\d+)", text).groups()
-    stated = [range(1, int(first) + 1), range(int(others[0]), int(others[1]) + 1), range(int(others[2]), int(others[3]) + 1)]
-    for m in range(1, 6000):
-        assert (lib.ozimmu_lm_linear_choose(m, 4096, 4096) != TILE) == any(m in r for r in stated), m
+    rows, power = map(int, re.search(r"takes the first up to (\d+) rows, or up to m p = 2\^(\d+) where that is more", text).groups())
+    last = max(rows, 2 ** power // p)
+    for m in [*range(1, 4500), last - 1, last, last + 1, 2 * last]:
+        if m < 2 ** 22 - 255:
+            assert (lib.ozimmu_lm_linear_choose(m, n, p) == TILE) == (m > last), m
 
 
 def test_sizes_of_a_loss(lib):
