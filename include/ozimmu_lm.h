@@ -65,8 +65,9 @@ int ozimmu_lm_unpack(int64_t p, int64_t n, int group, const void *packed, uint8_
  * Sums in FP32, alpha and beta applied in FP32, D rounded once; beta == 0: the old D is not read.  There are two forms.  In the first, always taken up to 16
  * rows, the codes are multiplied as they are and nothing else is rounded.  In BF16 it sums x (128 + q) and takes (128 + zero) times the sum of x off again: what
  * passes through the FP32 sums is up to ten times larger than the values, and a row of X that holds an infinity, or numbers of 2^113 and more, may give NaN.
- * In the second the weights are read back in the type of X, a piece at a time, each rounded once (in FP16 infinite beyond 65504, and to a multiple of 2^-24
- * below 2^-14).  The library takes the first up to 512 rows, or up to m p = 2^21 where that is more of them, and the second beyond (ozimmu_lm_linear_choose
+ * In the second the weights are read back in the type of X, a piece at a time, each rounded once.  In FP16 with scales in BF16 they are held times a power of
+ * two, so that no scale is out of its range (those below 2^-28 of the piece's largest lose digits); with scales in FP16 weights beyond 65504 become infinite.
+ * The library takes the first up to 512 rows, or up to m p = 2^21 where that is more of them, and the second beyond (ozimmu_lm_linear_choose
  * tells); results whose roundings may not depend on the number of rows are had from ozimmu_lm_linear_way.
  * n is 1 at the least (nothing is stored of n = 0).
  * Workspace: 0 bytes (workspace may be NULL then) up to 16 rows, and for more of them where the codes are multiplied without splitting the sums. */

@@ -45,8 +45,11 @@ struct Weights {
 
 hipError_t launch_quantize(int type, const void* W, int64_t ldw, const lml::Shape& s, int stype, void* packed, hipStream_t st);
 // rows row0 .. row0 + rows - 1 into X (of `type`); columns n .. cols - 1 (no more than whole blocks have) become zeros; through: for
-// a reader right behind it (k_lm_dequantize)
-hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, bool through, hipStream_t st);
+// a reader right behind it (k_lm_dequantize).  peaks (nullptr: without; else FP16 from scales in BF16, `through`, X's rows 16-byte aligned): room for
+// SCALE_PEAKS + 1 numbers; X is held times a power of two then, and the last of them is what the products have to be multiplied by
+constexpr int SCALE_PEAKS = 256;
+hipError_t launch_dequantize(int type, const Weights& w, int64_t row0, int64_t rows, int64_t cols, void* X, int64_t ldx, bool through, float* peaks,
+                             hipStream_t st);
 hipError_t launch_pack(const lml::Shape& s, const uint8_t* codes, int64_t ldc, const void* scales, int64_t lds, const uint8_t* zeros, int64_t ldz,
                        void* packed, hipStream_t st);
 hipError_t launch_unpack(const lml::Shape& s, const void* packed, uint8_t* codes, int64_t ldc, void* scales, int64_t lds, uint8_t* zeros,
@@ -107,7 +110,7 @@ struct Tile {
     int64_t ldd = 0;
     int dtype = 0;
     float alpha = 1, beta = 0;
-    const float* alpha_at = nullptr;   // WEIGHTS: alpha is multiplied by this
+    const float* alpha_at = nullptr;   // WEIGHTS, and LINEAR of FP16 where it is given: alpha is multiplied by this
     int splits = 1;                    // STATES: of the inner dimension
     int64_t split_stride = 0;          // STATES: elements between the D of splits
     Targets targets{};                 // LOSS

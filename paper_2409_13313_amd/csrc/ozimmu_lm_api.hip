@@ -206,6 +206,20 @@ int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const v
         t.A = plan.X;
         t.lda = plan.width;
     }
+    int64_t rows = plan.rows;
+    float* peaks = nullptr;
+    if (xtype == lmk::F16 && w.stype == lmk::BF16) {
+        // room for the scales' peaks: where X would be laid out, or the last 16 rows of W's (2 KB at the least), which pieces leave free then
+        constexpr int64_t ROOM = 16 * 64 * 2;
+        static_assert((lmk::SCALE_PEAKS + 1) * sizeof(float) <= ROOM, "they fit");
+        if (t.A == X && m * plan.width * 2 >= ROOM) {
+            peaks = (float*)plan.X;
+        } else {
+            rows -= 16;
+            peaks = (float*)(plan.W + rows * plan.width);
+        }
+        t.alpha_at = peaks + lmk::SCALE_PEAKS;
+    }
     t.B = plan.W;
     t.ldb = plan.width;
     t.ldd = ldd;
@@ -213,9 +227,9 @@ int linear_tile(int64_t m, int64_t n, int64_t p, float alpha, int xtype, const v
     t.alpha = alpha;
     t.beta = beta;
     const int64_t size = dtype == OZIMMU_LM_F32 ? 4 : 2;
-    for (int64_t at = 0; at < p; at += plan.rows) {
-        t.p = t.b_rows = p - at < plan.rows ? p - at : plan.rows;
-        CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, true, st)));
+    for (int64_t at = 0; at < p; at += rows) {
+        t.p = t.b_rows = p - at < rows ? p - at : rows;
+        CHECK(launched(lmk::launch_dequantize(xtype, w, at, t.p, plan.width, plan.W, plan.width, true, peaks, st)));
         t.D = (uint8_t*)D + at * size;
         t.shape = lmk::tile_shape(t.m, t.n, t.p, t.splits);
         CHECK(launched(lmk::launch_tile(t, st)));
@@ -337,7 +351,7 @@ int ozimmu_lm_dequantize(int type, int64_t p, int64_t n, int group, int zeros, i
     CHECK(packed_status(packed, p, n, group, scale_type));
     if (p == 0 || n == 0) return OZIMMU_OK;
     const lmk::Weights w{Shape{p, n, group, zeros != 0}, scale_type, (const uint8_t*)packed};
-    return launched(lmk::launch_dequantize(type, w, 0, p, n, W, ldw, false, (hipStream_t)stream));
+    return launched(lmk::launch_dequantize(type, w, 0, p, n, W, ldw, false, nullptr, (hipStream_t)stream));
 }
 
 static int plain_status(int64_t p, int64_t n, int group, const void* codes, int64_t ldc, const void* scales, int64_t lds, const void* zeros, int64_t ldz,

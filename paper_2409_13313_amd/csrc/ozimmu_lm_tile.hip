@@ -426,7 +426,7 @@ template <int TYPE, int KIND, int FA, int FB> __global__ __launch_bounds__(256, 
         }
     };
 
-    const float alpha = KIND == lmk::WEIGHTS ? g.alpha * *g.alpha_at : g.alpha;
+    const float alpha = KIND == lmk::WEIGHTS || (KIND == lmk::LINEAR && TYPE == F16 && g.alpha_at) ? g.alpha * *g.alpha_at : g.alpha;
     typedef std::integral_constant<int, 0> N0;
     typedef std::integral_constant<int, 1> N1;
     const auto usual = [] { wait_vmcnt<ON_THE_WAY>(); };
