@@ -63,3 +63,27 @@ def test_groups_without_a_number_and_rows_behind_the_last(lm):  # noqa: F811
     for Q in (made, dirty):
         got = lm.linear(X, Q, dtype=torch.float32, way="tile")
         assert torch.isnan(got[:, 7]).all() and not torch.isfinite(got[:, 50]).any() and torch.equal(got[:, keep], want[:, keep])
+
+
+def test_a_captured_layer_whose_weights_change(lm):  # noqa: F811
+    """Replayed with weights of other magnitudes in the same place: what they are scaled by is found at each replay."""
+    sets = [stored(lm, 300, 200, 64, True, low, high, 3)[0] for low, high in ((-3, 0), (-30, -28), (40, 41))]
+    X = rows(700, 200, "f16", 1)
+    P = lm.Packed(sets[0].data.clone(), 300, 200, 64, True, torch.bfloat16)
+    D = torch.empty((700, 300), device="cuda")
+    room = torch.empty(lm.linear_workspace_bytes(700, 200, 300, "tile"), dtype=torch.uint8, device="cuda")
+    run = lambda: lm.linear(X, P, D=D, workspace=room, way="tile")  # noqa: E731
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(6):
+        Q = sets[(i + 1) % 3]
+        P.data.copy_(Q.data)
+        room.fill_(255)
+        graph.replay()
+        want = lm.linear(X, Q, dtype=torch.float32, way="tile")      # (eager work between replays)
+        assert torch.equal(D, want) and torch.isfinite(D).all(), i
+        if i % 3 == 0:
+            torch.cuda.synchronize()

@@ -107,3 +107,48 @@ def test_a_vocabulary_in_pieces(lm):  # noqa: F811
     dX, dW = lm.cross_entropy_backward(g, X, W, y, lse, dw_type=torch.float32)
     want, _ = check_rows(dW, X, d, g.double(), size, "f16", "f32", "pieces")
     assert (dW[words].double() - want[words]).norm() <= 4 * HALF["f16"] * want[words].norm()
+
+
+def test_a_captured_gradient_with_other_tokens_far(lm):  # noqa: F811
+    """Captured where no token's g is far below the others', replayed where many are, and back: which they are is found at each replay."""
+    X, W, y, g, _ = parted(90, 136, 500, "f16", 0, 3, (1.0, 1e-7, 1e-30))
+    even = torch.sign(g)
+    _, lse = lm.cross_entropy(X, W, y)
+    held = even.clone()
+    room = torch.empty(lm.cross_entropy_workspace_bytes(90, 136, 500, True), dtype=torch.uint8, device="cuda")
+    dX, dW = torch.empty_like(X), torch.empty((500, 136), device="cuda")
+    run = lambda: lm.cross_entropy_backward(held, X, W, y, lse, dX=dX, dW=dW, workspace=room)  # noqa: E731
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(5):
+        now = g if i % 2 == 0 else even
+        held.copy_(now)
+        room.fill_(255)
+        graph.replay()
+        want = lm.cross_entropy_backward(now, X, W, y, lse, dw_type=torch.float32)      # (eager work between replays)
+        assert torch.equal(dX, want[0]) and torch.equal(dW, want[1]), i
+        if i % 3 == 0:
+            torch.cuda.synchronize()
+
+
+def test_gradients_that_are_not_finite(lm):  # noqa: F811
+    """A g that is a NaN or an infinity, or a row of X that holds one: what comes of it is no number in the rows and words that it reaches, and those are
+    dX's row of that token and all of dW."""
+    X, W, y, g, _ = parted(30, 64, 60, "f16", 0, 4, (1.0, 1e-9))
+    _, lse = lm.cross_entropy(X, W, y)
+    want = lm.cross_entropy_backward(g, X, W, y, lse)[0]
+    for row in (0, 1):                                                # (of either magnitude)
+        for bad in (float("nan"), float("inf")):
+            h = g.clone()
+            h[row] = bad
+            dX, dW = lm.cross_entropy_backward(h, X, W, y, lse, dw_type=torch.float32)
+            rest = torch.arange(30, device="cuda") != row
+            assert torch.equal(dX[rest], want[rest]) and not torch.isfinite(dX[row]).any() and not torch.isfinite(dW[y[row]]).any()
+            V = X.clone()
+            V[row, 5] = bad
+            _, other = lm.cross_entropy(V, W, y)
+            dX, dW = lm.cross_entropy_backward(g, V, W, y, other, dw_type=torch.float32)
+            assert torch.equal(dX[rest], want[rest]) and not torch.isfinite(dW).any()
