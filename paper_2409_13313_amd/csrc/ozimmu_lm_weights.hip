@@ -198,8 +198,8 @@ __device__ inline void quantize_eight(const Shape& s, int stype, const typename 
     }
 }
 
-// A thread takes eight elements of each of two rows, whose loads are on their way together.  16384 x 8192 in BF16, groups of 128: 86 to 90 us, 337 MB at
-// 3.8 TB/s (a copy 4.7), where vector instructions and memory take as long as each other: with a division for each element it was 118.
+// A thread takes eight elements of each of two rows, whose loads are on their way together.  16384 x 8192 in BF16, groups of 128: 83 us, 337 MB at
+// 4.1 TB/s (a copy 4.7), where vector instructions and memory take as long as each other: with a division for each element it was 118.
 template <int TYPE, int GROUP, bool ZEROS>
 __global__ __launch_bounds__(256) void k_lm_quantize(Shape s, int stype, const typename Elem<TYPE>::Bits* W, int64_t ldw, uint8_t* out)
 {
@@ -248,7 +248,8 @@ __global__ __launch_bounds__(256) void k_scale_peaks(Weights w, int64_t row0, in
 }
 
 // ---- reading back ----
-// A thread takes eight elements of each of two rows.  Bound by its stores: 16384 x 8192 into BF16 55 us, 340 MB at 6.1 TB/s (a copy 4.7, stores alone 6.9).
+// A thread takes eight elements of each of two rows.  Bound by its stores: 16384 x 8192 into BF16 48 us, 268 MB at 5.6 TB/s beside 70 MB of codes from the
+// memory-side cache (a copy 4.7, stores alone 6.9).
 // Where rows begin at multiples of 16 bytes they go PAST the caches (with one row a thread 58 us, else 98), or, where a product reads them next, THROUGH L2, which has nothing left to
 // write back then when the kernel ends (4096 x 4096 with the product of 2048 rows: 2.5 of 68 us less).
 //
@@ -310,7 +311,8 @@ __global__ __launch_bounds__(256) void k_lm_dequantize(Weights w, int64_t row0, 
     }
 }
 
-// ---- the plain layout: a word of eight codes a thread, changed over between the two orders; both ways once for a model that is loaded or stored ----
+// ---- the plain layout: a word of eight codes a thread, changed over between the two orders; both ways once for a model that is loaded or stored.
+// pack and unpack, us:  4096 x 4096 9.1, 9.2 (1.9 TB/s);  16384 x 8192 53, 52 (2.6);  131072 x 4096, groups of 64 with zero points, 333, 349 (1.7) ----
 __global__ __launch_bounds__(256) void k_lm_pack(Shape s, const uint8_t* codes, int64_t ldc, const uint16_t* scales, int64_t lds, const uint8_t* zeros,
                                                  int64_t ldz, uint8_t* out)
 {
@@ -601,7 +603,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_lm_direct(Linear g, Weights w)
 // dimension is split over workgroups, whose sums meet in a second launch.
 //
 // Bound by vector instructions (seven for eight codes, beside the matrix instruction they feed) and, where there are few rows, by the start and end of two
-// launches.  4096 x 4096, groups of 128, BF16: 32 rows 11.4 us, 128 18.2, 512 34 (0.5 PFLOP/s), 1024 53; from there on weights read back are quicker (choose).
+// launches.  4096 x 4096, groups of 128, BF16: 32 rows 12.1 us, 128 17.7, 512 34 (0.5 PFLOP/s); beyond, weights are read back (choose).
 struct Shared {
     Linear g;
     Weights w;
